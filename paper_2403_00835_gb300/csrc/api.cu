@@ -57,6 +57,19 @@ bool make_map(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, 
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// rank-dimensional tensor of 16-bit values (strides[i]: bytes between steps of
+// dimension i + 1), 64-element innermost boxes with the 128-byte swizzle.
+bool make_map_nd(CUtensorMap* m, bool bf16, const void* base, int rank, const cuuint64_t* dims,
+                 const cuuint64_t* strides, const cuuint32_t* box) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return false;
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return enc(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank,
+             const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Split of one stand-alone GEMM over the SMs.  T <= 256: one N-tile holding every
 // token and the (tile, k-chunk) space cut into equal contiguous ranges; the
 // cut depends on the weight shape and the SM count only.  T > 256: whole
@@ -253,7 +266,7 @@ struct cllm_ctx {
   int rec_count = 0;
 };
 
-namespace {
+namespace cllm {
 
 thread_local char g_last_cuda_error[160] = "none";
 
@@ -278,6 +291,10 @@ cudaError_t lib_malloc(void** p, size_t bytes) {
   if (alloc_injected_failure()) return cudaErrorMemoryAllocation;
   return cudaMalloc(p, bytes);
 }
+
+}  // namespace cllm
+
+namespace {
 
 template <typename T>
 bool dev_alloc(cllm_ctx* c, T** p, size_t bytes) {

@@ -295,6 +295,11 @@ constexpr int kGroupShift = 2;
 Part plan_group(int mtiles, int K, int T, int sms);  // the engine's launches of up to 256 tokens
 // bf16 [outer][inner] tensor map: 64-column x box_outer-row tiles, 128-byte swizzle.
 bool make_map(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint32_t box_outer);
+bool make_map_nd(CUtensorMap* m, bool bf16, const void* base, int rank, const cuuint64_t* dims,
+                 const cuuint64_t* strides, const cuuint32_t* box);
+// Record a failed CUDA call (cllm_last_cuda_error) and return CLLM_ECUDA.
+int cuda_fail(cudaError_t e, const char* where);
+cudaError_t lib_malloc(void** p, size_t bytes);  // cudaMalloc under the failure-injection hook
 
 // up to 256 tokens, plan_group's split (gemm_pair.cu); the activation map's box has
 // pair_box_rows(bn) rows

@@ -1,0 +1,61 @@
+// Internal declarations of the paged cache (include/cllm_paged.h).
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/cllm_paged.h"
+
+namespace cllm {
+
+// Arguments of an attention launch (device pointers; strides in elements).
+struct PagedAttnArgs {
+  const void* q;
+  void* out;
+  float* lse;
+  long long q_row, q_head, out_row, out_head;
+  const int* row_start;
+  const int* seq_len;
+  const int* table;
+  int table_width, batch, rows;
+  int H, Hkv, group;       // group = H / Hkv query heads share a key/value head
+  float scale_log2;        // scale * log2(e)
+  int window;
+  const uint32_t* mask;
+  int mask_words;
+  // this layer's pools
+  const void* k;
+  const void* v;
+  long long s_page, s_head, s_pos;
+  int layer, n_pages, page_shift;
+  // work that is cut over several CTAs: two partial tiles per CTA and an
+  // arrival counter per CTA (zero between launches)
+  float* part_o;
+  float2* part_ml;
+  int* tickets;
+  int* err;
+};
+
+// Partials: CTA c's slot 2c is a tile that began in an earlier CTA, slot 2c + 1
+// one that it begins and does not end.
+constexpr int kPagedPartRows = 256;  // most rows of a tile
+
+cudaError_t launch_page_plan(const cllm_page_tables& in, const cllm_page_tables& out, const cllm_page_rows& rows,
+                             int B, const int* ctx, const int* new_rows, cudaStream_t s);
+
+struct PagedAppendArgs {
+  const void *k, *v, *q;
+  void *kp, *vp, *q_out;  // this layer's pools
+  long long k_row, v_row, q_row, qo_row, s_page, s_head, s_pos;
+  const long long* slots;
+  const float2* rope;
+  const int* positions;
+  int max_pos, T, H, Hkv, hd, n_pages, page_shift;  // H = 0: no queries
+  int* err;
+};
+cudaError_t launch_paged_append(const PagedAppendArgs& a, int dtype, cudaStream_t s);
+
+cudaError_t launch_paged_attention_simt(const PagedAttnArgs& a, int dtype, int hd, int grid, cudaStream_t s);
+cudaError_t paged_attention_simt_set_attributes();
+
+}  // namespace cllm

@@ -1,0 +1,214 @@
+// Host side of include/cllm_paged.h: argument checks, the cache's tensor maps and
+// scratch, and the launches.
+#include <math.h>
+
+#include <new>
+
+#include "internal.cuh"
+#include "paged.cuh"
+
+using namespace cllm;
+
+struct cllm_paged {
+  cllm_paged_desc d;
+  int dev = 0, sms = 0, page_shift = 0, es = 0;
+  float* part_o = nullptr;
+  float2* part_ml = nullptr;
+  int* tickets = nullptr;  // one per CTA, then the status word
+  int* err = nullptr;
+};
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
+int log2i(int x) {
+  int s = 0;
+  while ((1 << s) < x) ++s;
+  return s;
+}
+
+bool tables_ok(const cllm_page_tables* t) {
+  return t && t->table && t->held && t->ring && t->state && aligned(t->table, 4) && aligned(t->held, 4) &&
+         aligned(t->ring, 4) && aligned(t->state, 4) && t->max_batch >= 1 && t->max_batch <= 4096 && t->width >= 1 &&
+         t->n_pages >= 1 && pow2(t->page_size) &&
+         static_cast<int64_t>(t->width) * t->page_size <= 0x7fffffff &&
+         static_cast<int64_t>(t->max_batch) * t->width <= 0x7fffffff;
+}
+
+}  // namespace
+
+extern "C" int cllm_page_plan(const cllm_page_tables* in, const cllm_page_tables* out, const cllm_page_rows* rows,
+                              int B, const int32_t* ctx, const int32_t* new_rows, void* cuda_stream) {
+  if (!tables_ok(in) || !tables_ok(out) || !rows || !rows->row_start || !rows->seq_len || !rows->granted ||
+      !rows->slots || !rows->positions || rows->max_rows < 1 || !aligned(rows->slots, 8) ||
+      !aligned(rows->row_start, 4) || !aligned(rows->seq_len, 4) || !aligned(rows->granted, 4) ||
+      !aligned(rows->positions, 4) || B < 0 || B > in->max_batch || in->max_batch != out->max_batch ||
+      in->width != out->width || in->n_pages != out->n_pages || in->page_size != out->page_size ||
+      in->ring != out->ring)
+    return CLLM_EINVAL;
+  if (B > 0 && (!ctx || !new_rows || !aligned(ctx, 4) || !aligned(new_rows, 4))) return CLLM_EINVAL;
+  const cudaError_t e = launch_page_plan(*in, *out, *rows, B, ctx, new_rows, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? CLLM_OK : cuda_fail(e, "page_plan");
+}
+
+extern "C" void cllm_paged_destroy(cllm_paged* c) {
+  if (!c) return;
+  int dev = 0;
+  const bool back = cudaGetDevice(&dev) == cudaSuccess && dev != c->dev;
+  cudaSetDevice(c->dev);
+  cudaDeviceSynchronize();
+  cudaFree(c->part_o);
+  cudaFree(c->part_ml);
+  cudaFree(c->tickets);
+  if (back) cudaSetDevice(dev);
+  delete c;
+}
+
+extern "C" int cllm_paged_create(const cllm_paged_desc* desc, cllm_paged** out) {
+  if (!desc || !out) return CLLM_EINVAL;
+  *out = nullptr;
+  const cllm_paged_desc& d = *desc;
+  if (!d.k || !d.v || (d.dtype != CLLM_F32 && d.dtype != CLLM_BF16 && d.dtype != CLLM_F16) || d.layers < 1 ||
+      d.n_pages < 1 || d.page_size < 1 || d.n_kv_heads < 1 || d.head_dim < 1 || d.n_heads < 1)
+    return CLLM_EINVAL;
+  if ((d.head_dim != 64 && d.head_dim != 128) || !pow2(d.page_size) || d.page_size < 8 || d.page_size > 256 ||
+      d.n_heads % d.n_kv_heads || d.n_heads / d.n_kv_heads > 64)
+    return CLLM_EUNSUPPORTED;
+  const int es = d.dtype == CLLM_F32 ? 4 : 2;
+  const int64_t strides[4] = {d.stride_layer, d.stride_page, d.stride_head, d.stride_pos};
+  const int64_t counts[4] = {d.layers, d.n_pages, d.n_kv_heads, d.page_size};
+  for (int i = 0; i < 4; ++i)
+    if (counts[i] > 1 && (strides[i] < d.head_dim || strides[i] * es % 16 || strides[i] > (int64_t(1) << 38)))
+      return CLLM_EINVAL;
+  if (!aligned(d.k, 16) || !aligned(d.v, 16)) return CLLM_EINVAL;
+
+  int dev = 0, major = 0, minor = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return cuda_fail(e, "paged_create");
+  if (major != 10 || minor != 3) return CLLM_EUNSUPPORTED;
+
+  cllm_paged* c = new (std::nothrow) cllm_paged;
+  if (!c) return CLLM_ENOMEM;
+  c->d = d;
+  // a dimension of one needs no stride
+  if (d.layers == 1) c->d.stride_layer = d.head_dim;
+  if (d.n_pages == 1) c->d.stride_page = d.head_dim;
+  if (d.n_kv_heads == 1) c->d.stride_head = d.head_dim;
+  c->dev = dev;
+  c->sms = sms;
+  c->es = es;
+  c->page_shift = log2i(d.page_size);
+  int rc = CLLM_OK;
+  do {
+    e = paged_attention_simt_set_attributes();
+    if (e != cudaSuccess) {
+      rc = cuda_fail(e, "paged_create");
+      break;
+    }
+    const size_t slots = 2 * static_cast<size_t>(sms);
+    if (lib_malloc(reinterpret_cast<void**>(&c->part_o), slots * kPagedPartRows * d.head_dim * 4) != cudaSuccess ||
+        lib_malloc(reinterpret_cast<void**>(&c->part_ml), slots * kPagedPartRows * 8) != cudaSuccess ||
+        lib_malloc(reinterpret_cast<void**>(&c->tickets), (sms + 1) * 4) != cudaSuccess) {
+      rc = CLLM_ENOMEM;
+      break;
+    }
+    c->err = c->tickets + sms;
+    // (the default stream orders the clearing before any later work)
+    e = cudaMemset(c->tickets, 0, (sms + 1) * 4);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) rc = cuda_fail(e, "paged_create");
+  } while (false);
+  if (rc != CLLM_OK) {
+    cllm_paged_destroy(c);
+    return rc;
+  }
+  *out = c;
+  return CLLM_OK;
+}
+
+extern "C" int cllm_paged_status(cllm_paged* c, void* cuda_stream) {
+  if (!c) return CLLM_EINVAL;
+  const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  int err = 0;
+  cudaError_t e = cudaMemcpyAsync(&err, c->err, 4, cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e == cudaSuccess && err != 0) {
+    // (a timed-out launch may leave arrival counters behind)
+    e = cudaMemsetAsync(c->tickets, 0, (c->sms + 1) * 4, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  }
+  if (e != cudaSuccess) return cuda_fail(e, "paged_status");
+  return err == 0 ? CLLM_OK : err & DERR_TIMEOUT ? CLLM_ETIMEOUT : CLLM_EDEVICE;
+}
+
+extern "C" int cllm_paged_append(cllm_paged* c, int layer, int T, const void* k, int64_t k_stride, const void* v,
+                                 int64_t v_stride, const int64_t* slots, const void* q, int64_t q_stride, void* q_out,
+                                 int64_t q_out_stride, const float* rope, int max_pos, const int32_t* positions,
+                                 void* cuda_stream) {
+  if (!c || layer < 0 || layer >= c->d.layers || T < 0) return CLLM_EINVAL;
+  if (T == 0) return CLLM_OK;
+  const cllm_paged_desc& d = c->d;
+  auto rows_ok = [&](const void* p, int64_t stride, int heads) {
+    return p && aligned(p, 16) &&
+           (T == 1 || (stride * c->es % 16 == 0 && stride >= static_cast<int64_t>(heads) * d.head_dim));
+  };
+  if (!rows_ok(k, k_stride, d.n_kv_heads) || !rows_ok(v, v_stride, d.n_kv_heads) || !slots || !aligned(slots, 8))
+    return CLLM_EINVAL;
+  if (rope && (!aligned(rope, 16) || max_pos < 1 || !positions || !aligned(positions, 4))) return CLLM_EINVAL;
+  if (q && (!rope || !rows_ok(q, q_stride, d.n_heads) || !rows_ok(q_out, q_out_stride, d.n_heads))) return CLLM_EINVAL;
+  PagedAppendArgs a{};
+  const int64_t at = layer * d.stride_layer * c->es;
+  a.k = k, a.v = v, a.q = q, a.q_out = q_out;
+  a.kp = static_cast<char*>(d.k) + at, a.vp = static_cast<char*>(d.v) + at;
+  a.k_row = k_stride, a.v_row = v_stride, a.q_row = q_stride, a.qo_row = q_out_stride;
+  a.s_page = d.stride_page, a.s_head = d.stride_head, a.s_pos = d.stride_pos;
+  a.slots = reinterpret_cast<const long long*>(slots);
+  a.rope = reinterpret_cast<const float2*>(rope);
+  a.positions = positions;
+  a.max_pos = max_pos, a.T = T, a.H = q ? d.n_heads : 0, a.Hkv = d.n_kv_heads, a.hd = d.head_dim;
+  a.n_pages = d.n_pages, a.page_shift = c->page_shift;
+  a.err = c->err;
+  const cudaError_t e = launch_paged_append(a, d.dtype, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? CLLM_OK : cuda_fail(e, "paged_append");
+}
+
+extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, void* cuda_stream) {
+  if (!c || !p || p->layer < 0 || p->layer >= c->d.layers || p->batch < 0 || p->rows < 0) return CLLM_EINVAL;
+  if (p->batch == 0 || p->rows == 0) return CLLM_OK;
+  const cllm_paged_desc& d = c->d;
+  auto strides_ok = [&](const void* x, int64_t row, int64_t head) {
+    auto ok = [&](int64_t stride) { return stride >= d.head_dim && stride * c->es % 16 == 0 && stride < (int64_t(1) << 37); };
+    return x && aligned(x, 16) && (p->rows == 1 || ok(row)) && (d.n_heads == 1 || ok(head));
+  };
+  if (!strides_ok(p->q, p->q_stride, p->q_head_stride) || !strides_ok(p->out, p->out_stride, p->out_head_stride) ||
+      !p->row_start || !p->seq_len || !p->table || !aligned(p->row_start, 4) || !aligned(p->seq_len, 4) ||
+      !aligned(p->table, 4) || !aligned(p->lse, 4) || p->table_width < 1 || p->window < 0 ||
+      !(p->scale > 0.f) || !isfinite(p->scale * kLog2e) ||
+      static_cast<int64_t>(p->table_width) * d.page_size > 0x7fffffff ||
+      (p->mask && (p->mask_words < 1 || !aligned(p->mask, 4))))
+    return CLLM_EINVAL;
+  PagedAttnArgs a{};
+  const int64_t at = p->layer * d.stride_layer * c->es;
+  a.q = p->q, a.out = p->out, a.lse = p->lse;
+  // (one row, or one head, needs no stride)
+  a.q_row = p->rows == 1 ? d.head_dim : p->q_stride, a.q_head = d.n_heads == 1 ? d.head_dim : p->q_head_stride;
+  a.out_row = p->rows == 1 ? d.head_dim : p->out_stride, a.out_head = d.n_heads == 1 ? d.head_dim : p->out_head_stride;
+  a.row_start = p->row_start, a.seq_len = p->seq_len, a.table = p->table;
+  a.table_width = p->table_width, a.batch = p->batch, a.rows = p->rows;
+  a.H = d.n_heads, a.Hkv = d.n_kv_heads, a.group = d.n_heads / d.n_kv_heads;
+  a.scale_log2 = p->scale * kLog2e;
+  a.window = p->window, a.mask = p->mask, a.mask_words = p->mask_words;
+  a.k = static_cast<const char*>(d.k) + at, a.v = static_cast<const char*>(d.v) + at;
+  a.s_page = d.stride_page, a.s_head = d.stride_head, a.s_pos = d.stride_pos;
+  a.layer = p->layer, a.n_pages = d.n_pages, a.page_shift = c->page_shift;
+  a.part_o = c->part_o, a.part_ml = c->part_ml, a.tickets = c->tickets, a.err = c->err;
+  const cudaError_t e =
+      launch_paged_attention_simt(a, d.dtype, d.head_dim, c->sms, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? CLLM_OK : cuda_fail(e, "paged_attention");
+}

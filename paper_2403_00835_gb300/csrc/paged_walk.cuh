@@ -1,0 +1,285 @@
+// The work of a paged attention launch and its division among CTAs, and what
+// both attention kernels share at a row's end.
+//
+// A tile is a run of tokens of one request times the query heads of one key/value
+// head; its units are the chunks of keys that any of its rows may see (one unit,
+// if there are none: its rows are written as zeros).  Lengths live on the device, so
+// the division is made there: all units in order (request, head, tile, chunk)
+// are cut into equal runs, one per CTA.  A run's ends may cut a tile; the pieces
+// leave partial results, and the CTA that finishes a tile last merges them in
+// order of their CTAs, so sums do not depend on who that is.
+#pragma once
+#include "act.cuh"
+#include "internal.cuh"
+#include "paged.cuh"
+
+namespace cllm {
+
+struct PagedGeom {
+  int tile_tok;   // tokens of a tile
+  int chunk;      // keys of a unit
+  int min_units;  // fewest units of a CTA's run
+};
+
+// Request b's rows and length as the device has them.  Rows outside the arrays
+// or a length past the block table make it a request without rows, or without keys.
+struct Request {
+  int row0, n, len;
+};
+__device__ __forceinline__ Request request(const PagedAttnArgs& a, int b) {
+  Request r{__ldg(a.row_start + b), __ldg(a.row_start + b + 1), __ldg(a.seq_len + b)};
+  r.n -= r.row0;
+  const bool rows = r.row0 >= 0 && r.n >= 0 && r.row0 <= a.rows && r.n <= a.rows - r.row0;
+  const bool fits = r.len <= static_cast<long long>(a.table_width) << a.page_shift;
+  if (!rows) r.n = 0;
+  if (!fits) r.len = 0;
+  if (!rows || !fits) atomicOr(a.err, DERR_CAPACITY);
+  return r;
+}
+
+struct TileKeys {
+  int lo, hi;  // keys [lo, hi) that some row sees (hi <= lo: none)
+};
+// Keys seen by tokens [t0, t1) of a request of n new tokens and `len` in all.
+__device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, int n, int len, int t0, int t1) {
+  TileKeys k;
+  const int ctx = len - n;
+  k.hi = ctx < 0 ? 0 : (a.mask != nullptr ? len : ctx + t1);
+  k.lo = a.window > 0 ? max(0, ctx + t0 - a.window + 1) : 0;
+  return k;
+}
+__device__ __forceinline__ int tile_units(const PagedGeom& g, const TileKeys& k) {
+  return k.hi > k.lo ? (k.hi + g.chunk - 1) / g.chunk - k.lo / g.chunk : 1;
+}
+// Units of one head of a request.
+__device__ __forceinline__ long long head_units(const PagedAttnArgs& a, const PagedGeom& g, int n, int len) {
+  long long u = 0;
+  for (int t0 = 0; t0 < n; t0 += g.tile_tok) u += tile_units(g, tile_keys(a, n, len, t0, min(n, t0 + g.tile_tok)));
+  return u;
+}
+
+// Where a CTA's run begins (shared memory, made once by all threads).
+struct RunStart {
+  long long u0, u1, per;  // the run, and the units of every run
+  long long begin;        // first unit of request b
+  int b;
+};
+
+// A piece: the chunks [ca, cb) of a tile that belong to this CTA's run.
+struct Piece {
+  int b, h, t0, nt;        // request, key/value head, first token and tokens of the tile
+  int n, len, row0;        // the request's new tokens, all tokens, first row
+  int lo, hi;              // keys of the tile
+  int ca, cb;              // this piece's chunks
+  int tca, tcb;            // the tile's
+  long long tile_u;        // the tile's first unit
+  __device__ bool whole() const { return ca == tca && cb == tcb; }
+  __device__ bool empty() const { return tca == tcb; }
+};
+
+// All threads of the block (a multiple of 32, at most 1024): the block's run.
+// `sm` holds 33 values.
+__device__ inline void run_start(const PagedAttnArgs& a, const PagedGeom& g, RunStart* rs, long long* sm) {
+  const int tid = threadIdx.x, nthr = blockDim.x, lane = tid & 31, warp = tid >> 5;
+  const int per_t = (a.batch + nthr - 1) / nthr, b0 = min(tid * per_t, a.batch), b1 = min(b0 + per_t, a.batch);
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Request q = request(a, b);
+    mine += a.Hkv * head_units(a, g, q.n, q.len);
+  }
+  long long v = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long o = __shfl_up_sync(0xffffffffu, v, d);
+    if (lane >= d) v += o;
+  }
+  if (lane == 31) sm[warp] = v;
+  __syncthreads();
+  long long total = 0, before = 0;
+  for (int w = 0; w < nthr / 32; ++w) {
+    if (w < warp) before += sm[w];
+    total += sm[w];
+  }
+  v += before - mine;  // units before this thread's requests
+  long long per = (total + gridDim.x - 1) / gridDim.x;
+  if (per < g.min_units) per = g.min_units;
+  const long long u0 = blockIdx.x * per, u1 = min(u0 + per, total);
+  if (tid == 0) {
+    rs->u0 = u0;
+    rs->u1 = max(u0, u1);
+    rs->per = per;
+  }
+  if (u0 < total && u0 >= v && u0 < v + mine) {  // one thread at most
+    int b = b0;
+    for (;; ++b) {
+      const Request q = request(a, b);
+      const long long u = a.Hkv * head_units(a, g, q.n, q.len);
+      if (u0 < v + u || b + 1 >= b1) break;
+      v += u;
+    }
+    rs->b = b;
+    rs->begin = v;
+  }
+  __syncthreads();
+}
+
+// The pieces of the block's run, in order.  Every warp that works on them walks
+// for itself; the whole warp calls.
+struct PagedWalk {
+  long long u, u1, per, tu;  // next unit, end of the run, units of a run, first unit of the tile
+  int b, h, t0, n, len, row0;
+
+  __device__ void load(const PagedAttnArgs& a) {
+    const Request q = request(a, b);
+    row0 = q.row0, n = q.n, len = q.len;
+    t0 = 0;
+    h = 0;
+  }
+  __device__ void begin(const PagedAttnArgs& a, const PagedGeom& g, const RunStart& rs) {
+    u = rs.u0;
+    u1 = rs.u1;
+    per = rs.per;
+    if (u >= u1) return;
+    b = rs.b;
+    load(a);
+    const long long hu = head_units(a, g, n, len), rest = u - rs.begin;
+    h = static_cast<int>(rest / hu);
+    tu = rs.begin + h * hu;
+  }
+  __device__ bool next(const PagedAttnArgs& a, const PagedGeom& g, Piece& p) {
+    if (u >= u1) return false;
+    for (;;) {
+      const int t1 = min(n, t0 + g.tile_tok);
+      const TileKeys k = tile_keys(a, n, len, t0, t1);
+      const int units = tile_units(g, k);
+      if (u < tu + units) {
+        p.b = b, p.h = h, p.t0 = t0, p.nt = t1 - t0, p.n = n, p.len = len, p.row0 = row0;
+        p.lo = k.lo, p.hi = k.hi;
+        p.tile_u = tu;
+        p.tca = k.lo / g.chunk;
+        p.tcb = k.hi > k.lo ? p.tca + units : p.tca;
+        p.ca = p.tca + static_cast<int>(u - tu);
+        const long long e = min(u1, tu + units);
+        p.cb = min(p.tcb, p.tca + static_cast<int>(e - tu));
+        if (p.tcb == p.tca) p.ca = p.tca;
+        u = e;
+        return true;
+      }
+      tu += units;
+      t0 = t1;
+      if (t0 < n) continue;
+      t0 = 0;
+      if (++h < a.Hkv) continue;
+      // the next request with rows, 32 at a time
+      const int lane = threadIdx.x & 31;
+      for (;;) {
+        const int c = b + 1 + lane;
+        const bool some = c < a.batch && request(a, c).n > 0;
+        const unsigned any = __ballot_sync(0xffffffffu, some);
+        if (any) {
+          b += __ffs(any);
+          break;
+        }
+        b += 32;
+        if (b + 1 >= a.batch) return false;  // (the lengths changed under the launch)
+      }
+      load(a);
+    }
+  }
+  // contributors of a cut tile: CTAs [first, last]; CTA c's partial slot
+  __device__ int first_cta(const Piece& p) const { return static_cast<int>(p.tile_u / per); }
+  __device__ int last_cta(const Piece& p) const { return static_cast<int>((p.tile_u + (p.tcb - p.tca) - 1) / per); }
+  __device__ int slot(const Piece& p, int c) const { return 2 * c + (c * per < p.tile_u ? 1 : 0); }
+};
+
+// ---- a row's keys ------------------------------------------------------------------
+
+// Keys [lo, hi) that token i of a request may see; with a mask, those from ctx on
+// only where their bit is set.
+struct RowKeys {
+  int lo, hi, ctx;
+  const uint32_t* bits;  // the row's mask words, or null
+  int words;
+};
+__device__ __forceinline__ RowKeys row_keys(const PagedAttnArgs& a, int n, int len, int row0, int i) {
+  RowKeys r;
+  r.ctx = len - n;
+  const int idx = r.ctx + i;
+  r.hi = r.ctx < 0 ? 0 : (a.mask != nullptr ? len : idx + 1);
+  r.lo = a.window > 0 ? max(0, idx - a.window + 1) : 0;
+  r.bits = a.mask != nullptr ? a.mask + static_cast<size_t>(row0 + i) * a.mask_words : nullptr;
+  r.words = a.mask_words;
+  return r;
+}
+// Bit j: whether the row sees key kb + j, j < 32.
+__device__ __forceinline__ uint32_t key_bits(const RowKeys& r, int kb) {
+  const int below = r.lo - kb, above = r.hi - kb;
+  uint32_t m = below <= 0 ? ~0u : below >= 32 ? 0u : ~0u << below;
+  m &= above >= 32 ? ~0u : above <= 0 ? 0u : ~(~0u << above);
+  if (r.bits != nullptr && m != 0) {
+    const int j = kb - r.ctx;  // new token of bit 0
+    if (j >= 0) {
+      const int w = j >> 5;
+      const uint32_t w0 = w < r.words ? __ldg(r.bits + w) : 0u, w1 = w + 1 < r.words ? __ldg(r.bits + w + 1) : 0u;
+      m &= __funnelshift_r(w0, w1, j & 31);
+    } else if (j > -32) {
+      m &= (__ldg(r.bits) << -j) | ~(~0u << -j);
+    }
+  }
+  return m;
+}
+
+// Address of (page of position pos) in a pool; null when the table's entry is
+// outside the pool (noted in the status word).
+template <class T>
+__device__ __forceinline__ const T* pool_row(const PagedAttnArgs& a, const void* pool, int b, int h, int pos) {
+  const int j = pos >> a.page_shift;
+  const int page = j < a.table_width ? __ldg(a.table + static_cast<size_t>(b) * a.table_width + j) : -1;
+  if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
+    atomicOr(a.err, DERR_CAPACITY);
+    return nullptr;
+  }
+  return static_cast<const T*>(pool) + page * a.s_page + h * a.s_head + (pos & ((1 << a.page_shift) - 1)) * a.s_pos;
+}
+
+// One row from the definition, by a warp: a key that the row does not see is not
+// touched.  Called where a row's tile gave something other than a finite number,
+// which a value of a key that only other rows see can cause (0 * inf).
+template <class T, int HD>
+__device__ __noinline__ void exact_row(const PagedAttnArgs& a, const Piece& p, int tok, int head) {
+  const int lane = threadIdx.x & 31;
+  constexpr int E = HD / 32;
+  const RowKeys r = row_keys(a, p.n, p.len, p.row0, tok);
+  const size_t row = static_cast<size_t>(p.row0 + tok);
+  const T* q = static_cast<const T*>(a.q) + row * a.q_row + head * a.q_head;
+  float qv[E], o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) qv[e] = ld_act(q, lane * E + e), o[e] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  for (int kb = r.lo & ~31; kb < r.hi; kb += 32) {
+    for (uint32_t bits = key_bits(r, kb); bits; bits &= bits - 1) {
+      const int k = kb + __ffs(bits) - 1;
+      const T* kp = pool_row<T>(a, a.k, p.b, p.h, k);
+      const T* vp = pool_row<T>(a, a.v, p.b, p.h, k);
+      float s = 0.f;
+      if (kp != nullptr) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) s = fmaf(qv[e], ld_act(kp, lane * E + e), s);
+      }
+      s = warp_sum(s) * a.scale_log2;
+      const float nm = s > m ? s : m;
+      const float f = m == -INFINITY ? 0.f : exp2f(m - nm), w = s == -INFINITY ? 0.f : exp2f(s - nm);
+      m = nm;
+      l = l * f + w;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = o[e] * f + (vp != nullptr ? w * ld_act(vp, lane * E + e) : 0.f);
+    }
+  }
+  const bool any = l != 0.f;  // (NaN counts)
+  T* out = static_cast<T*>(a.out) + row * a.out_row + head * a.out_head;
+#pragma unroll
+  for (int e = 0; e < E; ++e) st_act(out, lane * E + e, any ? o[e] / l : 0.f);
+  if (lane == 0 && a.lse != nullptr) a.lse[row * a.H + head] = any ? (m + log2f(l)) * 0.69314718055994530942f : -INFINITY;
+}
+
+}  // namespace cllm

@@ -1,0 +1,288 @@
+"""Python binding of the paged key/value cache in include/cllm_paged.h (argument
+marshalling only).
+
+A step of a serving loop over requests that come and go::
+
+    tables = PageTables.empty(n_pages, page_size, max_batch, width)
+    rows = PageRows.empty(max_batch, max_rows)
+    cache = PagedCache(k_pool, v_pool, n_heads)   # pools [layer][page][head][position][hd]
+
+    plan(tables, rows, ctx, new_rows)             # pages, slots, positions of the step
+    for layer in ...:
+        cache.append(layer, k, v, rows.slots, q=q, q_out=q, rope=rope, positions=rows.positions)
+        cache.attention(layer, q, rows, tables, out=o)
+
+Calls queue their work on ``stream`` (a torch stream; None: the current one) and
+return; tensors are the caller's and are not copied.  Arguments of the wrong
+type, device or shape raise ValueError, what the library refuses CllmError;
+``PagedCache.check`` waits and raises for what only the device could see.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from . import cllm as _c
+
+CLLM_F16 = 2
+DTYPES = {torch.float32: _c.CLLM_F32, torch.bfloat16: _c.CLLM_BF16, torch.float16: CLLM_F16}
+
+# Every function declared in include/cllm_paged.h.
+EXPORTS = ("cllm_page_plan", "cllm_paged_create", "cllm_paged_destroy", "cllm_paged_status", "cllm_paged_append",
+           "cllm_paged_attention")
+
+
+class _Tables(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("held", ctypes.c_void_p), ("ring", ctypes.c_void_p),
+                ("state", ctypes.c_void_p), ("max_batch", ctypes.c_int), ("width", ctypes.c_int),
+                ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("row_start", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("granted", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("max_rows", ctypes.c_int)]
+
+
+class _Desc(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int), ("layers", ctypes.c_int),
+                ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("n_heads", ctypes.c_int), ("stride_layer", ctypes.c_int64),
+                ("stride_page", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_pos", ctypes.c_int64)]
+
+
+class _Attn(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_int), ("batch", ctypes.c_int), ("rows", ctypes.c_int), ("q", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("out_head_stride", ctypes.c_int64), ("row_start", ctypes.c_void_p), ("seq_len", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("table_width", ctypes.c_int), ("scale", ctypes.c_float),
+                ("window", ctypes.c_int), ("mask", ctypes.c_void_p), ("mask_words", ctypes.c_int)]
+
+
+_lib = None
+
+
+def load():
+    """The library with this header's signatures."""
+    global _lib
+    if _lib is None:
+        lib = _c.load()
+        vp, i, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+        lib.cllm_page_plan.argtypes = [vp, vp, vp, i, vp, vp, vp]
+        lib.cllm_paged_create.argtypes = [ctypes.POINTER(_Desc), ctypes.POINTER(vp)]
+        lib.cllm_paged_destroy.argtypes = [vp]
+        lib.cllm_paged_destroy.restype = None
+        lib.cllm_paged_status.argtypes = [vp, vp]
+        lib.cllm_paged_append.argtypes = [vp, i, i, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i, vp, vp]
+        lib.cllm_paged_attention.argtypes = [vp, vp, vp]
+        for name in EXPORTS:
+            if name != "cllm_paged_destroy":
+                getattr(lib, name).restype = ctypes.c_int
+        _lib = lib
+    return _lib
+
+
+def _tensor(t, what: str, dtype, shape=None, device=None):
+    """A contiguous CUDA tensor's address."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        raise ValueError(f"{what}: need a contiguous {dtype} CUDA tensor")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: need shape {tuple(shape)}, got {tuple(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{what}: on {t.device}, the others on {device}")
+    return t.data_ptr()
+
+
+def _stream(stream, device) -> int:
+    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+
+
+class PageTables:
+    """Block tables of up to max_batch requests and the ring of free pages
+    (``cllm_page_tables``): int32 tensors table [max_batch][width], held
+    [max_batch], ring [n_pages], state [4] = (first free, free, 0, 0).
+    With the table alone the object serves ``PagedCache.attention`` only."""
+
+    def __init__(self, table, held=None, ring=None, state=None, page_size: int = 16):
+        if not (isinstance(table, torch.Tensor) and table.dim() == 2):
+            raise ValueError("table: need a [max_batch][width] tensor")
+        i32, dev = torch.int32, table.device
+        s = _Tables(_tensor(table, "table", i32))
+        s.max_batch, s.width = table.shape
+        s.page_size = page_size
+        if held is not None:
+            s.held = _tensor(held, "held", i32, (s.max_batch,), dev)
+            s.ring = _tensor(ring, "ring", i32, None, dev)
+            s.state = _tensor(state, "state", i32, (4,), dev)
+            s.n_pages = ring.numel()
+        self.table, self.held, self.ring, self.state, self.page_size = table, held, ring, state, page_size
+        self._s, self._p = s, ctypes.addressof(s)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, max_batch: int, width: int, device="cuda"):
+        """All pages free, in order."""
+        z = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((max_batch, width), -1, **z), torch.zeros(max_batch, **z), torch.arange(n_pages, **z),
+                   torch.tensor([0, n_pages, 0, 0], **z), page_size)
+
+
+class PageRows:
+    """What a plan says about the step's rows (``cllm_page_rows``): row_start
+    [max_batch + 1], seq_len [max_batch], granted [max_batch], positions [max_rows]
+    int32 and slots [max_rows] int64.  row_start and seq_len alone serve
+    ``PagedCache.attention``.  ``batch``: the requests of the last plan."""
+
+    def __init__(self, row_start, seq_len, granted=None, slots=None, positions=None):
+        i32 = torch.int32
+        s = _Rows(_tensor(row_start, "row_start", i32))
+        dev, n = row_start.device, row_start.numel() - 1
+        s.seq_len = _tensor(seq_len, "seq_len", i32, (n,), dev)
+        if granted is not None:
+            s.granted = _tensor(granted, "granted", i32, (n,), dev)
+            s.slots = _tensor(slots, "slots", torch.int64, (slots.numel(),), dev)
+            s.positions = _tensor(positions, "positions", i32, (slots.numel(),), dev)
+            s.max_rows = slots.numel()
+        self.row_start, self.seq_len, self.granted, self.slots, self.positions = row_start, seq_len, granted, slots, positions
+        self.batch = n
+        self._s, self._p = s, ctypes.addressof(s)
+
+    @classmethod
+    def empty(cls, max_batch: int, max_rows: int, device="cuda"):
+        z = dict(dtype=torch.int32, device=device)
+        return cls(torch.zeros(max_batch + 1, **z), torch.zeros(max_batch, **z), torch.zeros(max_batch, **z),
+                   torch.full((max_rows,), -1, dtype=torch.int64, device=device), torch.zeros(max_rows, **z))
+
+
+def plan(tables: PageTables, rows: PageRows, ctx, new_rows, out: Optional[PageTables] = None, stream=None):
+    """Pages for requests of ctx cached and new_rows new tokens (int32 [B]) and
+    the slots of the new rows (``cllm_page_plan``).  Updates ``tables`` in place, or
+    leaves them and fills ``out`` (over the same ring)."""
+    out = tables if out is None else out
+    if tables.held is None or out.held is None or rows.slots is None:
+        raise ValueError("plan needs whole tables and rows")
+    dev, b = tables.table.device, ctx.numel()
+    c = _tensor(ctx, "ctx", torch.int32, None, dev)
+    n = _tensor(new_rows, "new_rows", torch.int32, ctx.shape, dev)
+    if rows.row_start.device != dev or rows.seq_len.numel() < b:
+        raise ValueError("rows: on another device, or too small for the batch")
+    rc = load().cllm_page_plan(tables._p, out._p, rows._p, b, c, n, _stream(stream, dev))
+    if rc:
+        _c._check(rc, "cllm_page_plan")
+    rows.batch = b
+
+
+class PagedCache:
+    """K and V pools [layer][page][kv_head][position][head_dim] of one dtype and
+    equal strides, the innermost contiguous (a permuted view gives pages that
+    hold one position's heads together), and the scratch of their attention."""
+
+    def __init__(self, k, v, n_heads: int):
+        lib = load()
+        for t, what in ((k, "k"), (v, "v")):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 5 and t.dtype in DTYPES):
+                raise ValueError(f"{what}: need a [layer][page][head][position][head_dim] CUDA tensor of "
+                                 "float32, bfloat16 or float16")
+        if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device or k.stride(4) != 1:
+            raise ValueError("k and v: need the same shape, strides, type and device, head_dim contiguous")
+        self.k, self.v, self.n_heads = k, v, n_heads
+        self.layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.dtype, self.device = k.dtype, k.device
+        d = _Desc(k.data_ptr(), v.data_ptr(), DTYPES[k.dtype], self.layers, self.n_pages, self.page_size,
+                  self.n_kv_heads, self.head_dim, n_heads, *k.stride()[:4])
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            _c._check(lib.cllm_paged_create(ctypes.byref(d), ctypes.byref(h)), "cllm_paged_create")
+        self._h, self._lib = h, lib
+        self._a = _Attn()
+        self._ap = ctypes.addressof(self._a)
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            self._lib.cllm_paged_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _heads(self, t, what: str, heads: int):
+        """Rows of heads side by side: (address, row stride)."""
+        if not (isinstance(t, torch.Tensor) and t.dtype == self.dtype and t.device == self.device and t.dim() == 3
+                and t.shape[1] == heads and t.shape[2] == self.head_dim and t.stride(2) == 1
+                and (heads == 1 or t.stride(1) == self.head_dim)):
+            raise ValueError(f"{what}: need [rows][{heads}][{self.head_dim}] {self.dtype} on {self.device}, heads side by side")
+        return t.data_ptr(), t.stride(0)
+
+    def append(self, layer: int, k, v, slots, q=None, q_out=None, rope=None, positions=None, stream=None):
+        """Write rows k, v [T][kv_heads][hd] into slots (int64 [T]; -1: none).  With
+        rope (float32 [max_pos][hd/2][2]: cos, sin) K is rotated by positions
+        (int32 [T]), and q [T][n_heads][hd] into q_out (None: in place)."""
+        kp, ks = self._heads(k, "k", self.n_kv_heads)
+        vp, vs = self._heads(v, "v", self.n_kv_heads)
+        t = k.shape[0]
+        if v.shape[0] != t or slots.numel() < t:
+            raise ValueError("k, v and slots: different numbers of rows")
+        qp = qs = op = os = rp = pp = None
+        max_pos = 0
+        if rope is not None:
+            max_pos = rope.shape[0]
+            rp = _tensor(rope, "rope", torch.float32, (max_pos, self.head_dim // 2, 2), self.device)
+            pp = _tensor(positions, "positions", torch.int32, None, self.device)
+            if positions.numel() < t:
+                raise ValueError("positions: fewer than rows")
+            if q is not None:
+                qp, qs = self._heads(q, "q", self.n_heads)
+                op, os = (qp, qs) if q_out is None else self._heads(q_out, "q_out", self.n_heads)
+                if q.shape[0] != t or (q_out is not None and q_out.shape[0] != t):
+                    raise ValueError("q, q_out and k: different numbers of rows")
+        elif q is not None:
+            raise ValueError("q is only rotated: pass rope")
+        rc = self._lib.cllm_paged_append(self._h, layer, t, kp, ks, vp, vs, _tensor(slots, "slots", torch.int64, None, self.device),
+                                         qp, qs or 0, op, os or 0, rp, max_pos, pp, _stream(stream, self.device))
+        if rc:
+            _c._check(rc, "cllm_paged_append")
+
+    def attention(self, layer: int, q, rows: PageRows, tables: PageTables, out=None, lse=None,
+                  scale: Optional[float] = None, window: int = 0, block_mask=None, stream=None):
+        """Attention of the step's rows q [T][n_heads][hd] (any row and head stride)
+        over their requests' pages; returns out.  lse: float32 [T][n_heads] to fill.
+        scale: default head_dim ** -0.5.  window: keys nearer than that (0: all).
+        block_mask: int32 [T][words], bit j of word w: the row sees new token 32 w + j of
+        its request (None: causal)."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        shape = (q.shape[0], self.n_heads, self.head_dim)
+        for t, what in ((q, "q"), (out, "out")):
+            if not (t.shape == shape and t.dtype == self.dtype and t.device == self.device and t.stride(2) == 1):
+                raise ValueError(f"{what}: need [rows][{self.n_heads}][{self.head_dim}] {self.dtype} on {self.device}")
+        if tables.page_size != self.page_size or rows.batch > tables._s.max_batch or tables.table.device != self.device \
+                or rows.row_start.device != self.device:
+            raise ValueError("rows and tables: another page size or device, or more requests than tables")
+        a = self._a
+        a.layer, a.batch, a.rows = layer, rows.batch, shape[0]
+        a.q, a.out = q.data_ptr(), out.data_ptr()
+        a.q_stride, a.q_head_stride, _ = q.stride()
+        a.out_stride, a.out_head_stride, _ = out.stride()
+        a.lse = None if lse is None else _tensor(lse, "lse", torch.float32, shape[:2], self.device)
+        a.row_start, a.seq_len = rows._s.row_start, rows._s.seq_len
+        a.table, a.table_width = tables._s.table, tables._s.width
+        a.scale = self.head_dim ** -0.5 if scale is None else scale
+        a.window = window
+        if block_mask is None:
+            a.mask, a.mask_words = None, 0
+        else:
+            a.mask = _tensor(block_mask, "block_mask", torch.int32, (shape[0], block_mask.shape[1]), self.device)
+            a.mask_words = block_mask.shape[1]
+        rc = self._lib.cllm_paged_attention(self._h, self._ap, _stream(stream, self.device))
+        if rc:
+            _c._check(rc, "cllm_paged_attention")
+        return out
+
+    def check(self, stream=None):
+        """Wait for the stream; raise CllmError if a call found a page, slot or
+        position outside its pool or table, or a wait ran out (and forget it)."""
+        _c._check(self._lib.cllm_paged_status(self._h, _stream(stream, self.device)), "cllm_paged_status")
