@@ -8,6 +8,8 @@
 
 #include <stdint.h>
 
+#include "cllm_paged.h"
+
 #ifdef __cplusplus
 extern "C" {
 #endif
@@ -102,6 +104,16 @@ int cllm_test_hold_attention(cllm_ctx *ctx, int chunk);
  * ctx or chunk < -1.
  */
 int cllm_test_hold_gemm(cllm_ctx *ctx, int chunk);
+
+/*
+ * The same for the paged attention of 16-bit pools: the thread that issues a
+ * CTA's tensor-core work stops at chunk `chunk` >= 0 of a piece of its work (pieces
+ * with fewer are not affected).  The other roles' waits run out (2 s), the CTA lets
+ * its loads and MMAs in flight end and returns; cllm_paged_status then returns
+ * CLLM_ETIMEOUT and the cache stays usable.  -1 disarms.  EINVAL on a null cache or
+ * chunk < -1.
+ */
+int cllm_test_hold_paged(cllm_paged *cache, int chunk);
 
 /*
  * The same for the split-K waits of launches of up to 256 rows: every weight

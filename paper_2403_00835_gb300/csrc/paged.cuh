@@ -55,7 +55,14 @@ struct PagedAppendArgs {
 };
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int dtype, cudaStream_t s);
 
-cudaError_t launch_paged_attention_simt(const PagedAttnArgs& a, int dtype, int hd, int grid, cudaStream_t s);
-cudaError_t paged_attention_simt_set_attributes();
+// fp32 pools (paged_attn.cu)
+cudaError_t launch_paged_attention_f32(const PagedAttnArgs& a, int hd, int grid, cudaStream_t s);
+cudaError_t paged_attention_f32_set_attributes();
+// 16-bit pools (paged_attn_tc.cu); k, v: the pools' maps; hold: test hook, 1 + the chunk
+// of a piece at which the MMA issuer gives up (0: none)
+cudaError_t launch_paged_attention_tc(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
+                                      int hold, int grid, cudaStream_t s);
+cudaError_t paged_attention_tc_set_attributes();
+bool paged_pool_map(CUtensorMap* m, const void* pool, const cllm_paged_desc& d);
 
 }  // namespace cllm

@@ -4,6 +4,7 @@
 
 #include <new>
 
+#include "../../include/cllm_testing.h"
 #include "internal.cuh"
 #include "paged.cuh"
 
@@ -16,6 +17,8 @@ struct cllm_paged {
   float2* part_ml = nullptr;
   int* tickets = nullptr;  // one per CTA, then the status word
   int* err = nullptr;
+  CUtensorMap mk, mv;      // the pools (16-bit types)
+  int hold = 0;            // test hook
 };
 
 namespace {
@@ -106,9 +109,13 @@ extern "C" int cllm_paged_create(const cllm_paged_desc* desc, cllm_paged** out) 
   c->page_shift = log2i(d.page_size);
   int rc = CLLM_OK;
   do {
-    e = paged_attention_simt_set_attributes();
+    e = es == 4 ? paged_attention_f32_set_attributes() : paged_attention_tc_set_attributes();
     if (e != cudaSuccess) {
       rc = cuda_fail(e, "paged_create");
+      break;
+    }
+    if (es == 2 && (!paged_pool_map(&c->mk, d.k, c->d) || !paged_pool_map(&c->mv, d.v, c->d))) {
+      rc = CLLM_EINVAL;
       break;
     }
     const size_t slots = 2 * static_cast<size_t>(sms);
@@ -208,7 +215,14 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
   a.s_page = d.stride_page, a.s_head = d.stride_head, a.s_pos = d.stride_pos;
   a.layer = p->layer, a.n_pages = d.n_pages, a.page_shift = c->page_shift;
   a.part_o = c->part_o, a.part_ml = c->part_ml, a.tickets = c->tickets, a.err = c->err;
-  const cudaError_t e =
-      launch_paged_attention_simt(a, d.dtype, d.head_dim, c->sms, static_cast<cudaStream_t>(cuda_stream));
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = c->es == 4 ? launch_paged_attention_f32(a, d.head_dim, c->sms, st)
+                                   : launch_paged_attention_tc(a, c->mk, c->mv, d.dtype, d.head_dim, c->hold, c->sms, st);
   return e == cudaSuccess ? CLLM_OK : cuda_fail(e, "paged_attention");
+}
+
+extern "C" int cllm_test_hold_paged(cllm_paged* c, int chunk) {
+  if (!c || chunk < -1) return CLLM_EINVAL;
+  c->hold = chunk + 1;
+  return CLLM_OK;
 }

@@ -48,7 +48,7 @@ __device__ __forceinline__ bool finite4(float4 v) {
 }
 
 template <class T, int HD, int BM>
-__global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const PagedAttnArgs a, const PagedGeom g) {
+__global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_constant__ PagedAttnArgs a, const PagedGeom g) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   PagedSmem<HD, BM>& s = *reinterpret_cast<PagedSmem<HD, BM>*>(smem_raw);
   constexpr int R = BM / 16, C = HD / 64;
@@ -233,42 +233,28 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const PagedAtt
   }
 }
 
-template <class T, int HD, int BM>
+template <int HD, int BM>
 cudaError_t launch(const PagedAttnArgs& a, int grid, cudaStream_t s) {
   const PagedGeom g{BM / a.group, kPChunk, 1};
-  paged_attn_kernel<T, HD, BM><<<grid, kPThreads, sizeof(PagedSmem<HD, BM>), s>>>(a, g);
+  paged_attn_kernel<float, HD, BM><<<grid, kPThreads, sizeof(PagedSmem<HD, BM>), s>>>(a, g);
   return cudaGetLastError();
-}
-template <class T>
-cudaError_t launch_t(const PagedAttnArgs& a, int hd, int grid, cudaStream_t s) {
-  // rows of one key/value head in an average request
-  const long long rows = (static_cast<long long>(a.rows) + a.batch - 1) / a.batch * a.group;
-  if (rows <= 16 && a.group <= 16) return hd == 64 ? launch<T, 64, 16>(a, grid, s) : launch<T, 128, 16>(a, grid, s);
-  return hd == 64 ? launch<T, 64, 64>(a, grid, s) : launch<T, 128, 64>(a, grid, s);
-}
-
-template <class T>
-cudaError_t attrs() {
-  cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<T, 64, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 16>));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<T, 128, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 16>));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<T, 64, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 64>));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<T, 128, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 64>));
-  return e;
 }
 
 }  // namespace
 
-cudaError_t paged_attention_simt_set_attributes() {
-  cudaError_t e = attrs<float>();
-  if (e == cudaSuccess) e = attrs<__half>();
-  if (e == cudaSuccess) e = attrs<__nv_bfloat16>();
+cudaError_t paged_attention_f32_set_attributes() {
+  cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<float, 64, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 16>));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<float, 128, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 16>));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<float, 64, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 64>));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<float, 128, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 64>));
   return e;
 }
 
-cudaError_t launch_paged_attention_simt(const PagedAttnArgs& a, int dtype, int hd, int grid, cudaStream_t s) {
-  if (dtype == CLLM_F32) return launch_t<float>(a, hd, grid, s);
-  if (dtype == CLLM_BF16) return launch_t<__nv_bfloat16>(a, hd, grid, s);
-  return launch_t<__half>(a, hd, grid, s);
+cudaError_t launch_paged_attention_f32(const PagedAttnArgs& a, int hd, int grid, cudaStream_t s) {
+  // rows of one key/value head in an average request
+  const long long rows = (static_cast<long long>(a.rows) + a.batch - 1) / a.batch * a.group;
+  if (rows <= 16 && a.group <= 16) return hd == 64 ? launch<64, 16>(a, grid, s) : launch<128, 16>(a, grid, s);
+  return hd == 64 ? launch<64, 64>(a, grid, s) : launch<128, 64>(a, grid, s);
 }
 
 }  // namespace cllm

@@ -2,6 +2,7 @@
 against a model on Python lists): types, head layouts, page sizes and orders, lengths
 0, 1 and around tile edges, windows, masks that leave a row nothing, pages of NaN
 around every request, refusals, streams and graphs."""
+import ctypes
 import math
 
 import numpy as np
@@ -404,6 +405,29 @@ def test_allocation_failure():
         assert e.value.status == -2
     lib.cllm_test_fail_alloc(-1)
     paged.PagedCache(step.k, step.v, 4).close()
+
+
+@pytest.mark.parametrize("chunk", [0, 2])
+@pytest.mark.parametrize("new", [3, 200])
+def test_a_wait_that_runs_out_is_reported(chunk, new):
+    """The MMA issuer gives up in every piece of more than `chunk` chunks: the call
+    ends, the status says so, and the cache goes on working."""
+    lib = cllm.load()
+    step = Step([60000], [new], 2, 2, 128, 256, "bf16", seed=9)  # pieces of 7 chunks or so
+    cache = paged.PagedCache(step.k, step.v, 2)
+    rows, tables = paged.PageRows(step.row_start, step.seq_len), paged.PageTables(step.table, page_size=256)
+    want = cache.attention(0, step.q, rows, tables)
+    cache.check()
+    lib.cllm_test_hold_paged.argtypes = [ctypes.c_void_p, ctypes.c_int]
+    assert lib.cllm_test_hold_paged(cache._h, chunk) == 0
+    cache.attention(0, step.q, rows, tables)
+    with pytest.raises(cllm.CllmError) as e:
+        cache.check()
+    assert e.value.status == -5
+    assert lib.cllm_test_hold_paged(cache._h, -1) == 0
+    assert torch.equal(cache.attention(0, step.q, rows, tables), want)
+    cache.check()
+    assert lib.cllm_test_hold_paged(None, 0) == -1 and lib.cllm_test_hold_paged(cache._h, -2) == -1
 
 
 # ---- together --------------------------------------------------------------------------
