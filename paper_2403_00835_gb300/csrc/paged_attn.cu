@@ -28,16 +28,6 @@ struct PagedSmem {
 };
 
 __device__ __forceinline__ float4 ld4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 ld4(const __half* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&u.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&u.y));
-  return make_float4(a.x, a.y, b.x, b.y);
-}
-__device__ __forceinline__ float4 ld4(const __nv_bfloat16* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xffff0000u));
-}
 template <class T>
 __device__ __forceinline__ void st4(T* p, float4 v) {
   st_act(p, 0, v.x), st_act(p, 1, v.y), st_act(p, 2, v.z), st_act(p, 3, v.w);
@@ -55,7 +45,7 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   run_start(a, g, &s.run, s.scan);
   PagedWalk w;
-  w.begin(a, g, s.run);
+  w.begin(s.run);
   Piece p;
   while (w.next(a, g, p)) {
     const int rows = p.nt * a.group;
@@ -229,13 +219,13 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
     __syncthreads();
     if (done)
       for (int r = tid >> 5; r < rows; r += kPThreads / 32)
-        if (s.bad[r >> 5] >> (r & 31) & 1) exact_row<T, HD>(a, p, p.t0 + r / a.group, p.h * a.group + r % a.group);
+        if (s.bad[r >> 5] >> (r & 31) & 1) exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + r / a.group, p.h * a.group + r % a.group);
   }
 }
 
 template <int HD, int BM>
 cudaError_t launch(const PagedAttnArgs& a, int grid, cudaStream_t s) {
-  const PagedGeom g{BM / a.group, kPChunk, 1};
+  const PagedGeom g{BM / a.group, BM / a.group, kPChunk, 1};
   paged_attn_kernel<float, HD, BM><<<grid, kPThreads, sizeof(PagedSmem<HD, BM>), s>>>(a, g);
   return cudaGetLastError();
 }

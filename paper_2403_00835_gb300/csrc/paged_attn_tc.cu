@@ -30,13 +30,36 @@ namespace cllm {
 
 namespace {
 
-constexpr int kTcThreads = 384;  // warps 0-3, 4-7: the slots' rows; 8 MMAs; 9 loads; 10, 11 idle
-constexpr int kTcRegsLow = 72, kTcRegsRow = 216;
+// Warps 0-3, 4-7: the slots' rows; 8 MMAs; 9 loads (10, 11 idle).  Of the launch's
+// 384 x 168 registers the last warpgroup keeps 88 a thread, the rows' warps take 208.
+constexpr int kTcThreads = 384;
+constexpr int kTcRegsLow = 88, kTcRegsRow = 208;
 static_assert(128 * kTcRegsLow + 256 * kTcRegsRow <= kTcThreads * 168, "register split");
 constexpr int kTcRows = 128, kTcChunk = 128;
 // A row's running maximum follows only growth of more than this (in log2): P may
 // then reach 2^8, and O in tensor memory is rarely rescaled.
 constexpr float kTcSlack = 8.f;
+
+// The chunks of a piece that a slot works on: first, first + step, .. < end
+// (relative to the piece).
+struct SlotChunks {
+  int first, end, step;
+  __device__ bool any() const { return first < end; }
+  __device__ bool has(int i) const { return i >= first && i < end && (step == 1 || ((i - first) & 1) == 0); }
+  __device__ int last() const { return step == 1 ? end - 1 : first + ((end - 1 - first) & ~1); }
+};
+
+// A piece as the loading warp hands it to the others.
+struct TcPiece {
+  int b, h, t0, nt, n, len, row0, lo, hi;  // as in Piece
+  int ca, chunks;                          // first chunk and number of chunks (0: no keys)
+  int two, whole;                          // 128 rows in each slot; the whole tile
+  int slot, cta0, cta1, first_slot;        // of a cut tile: this part's slot, the CTAs of its parts, the first's slot
+  SlotChunks c[2];
+  int end;                                 // no piece: the run is over
+  __device__ int part(int cta) const { return cta == cta0 ? first_slot : 2 * cta; }
+};
+constexpr int kTcPieces = 4;
 
 template <int HD>
 struct TcSmem {
@@ -46,6 +69,8 @@ struct TcSmem {
   alignas(1024) uint8_t ring[kRing][kTile];
   float2 ml[2][kTcRows];  // also the scratch of run_start
   uint64_t full[kRing], empty[kRing], qfull, qempty, sfull[2], pready[2], ofull[2], ofree, drain;
+  uint64_t pfull[kTcPieces], pempty[kTcPieces], pfree[kTcPieces];  // a piece is there; the rows, the issuer are done with it
+  TcPiece piece[kTcPieces];
   RunStart run;
   unsigned bad[8];  // rows whose result is not finite
   uint32_t tmem;
@@ -77,24 +102,26 @@ __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile
   return true;
 }
 
-// The chunks of a piece that a slot works on: indices first, first + step, .. < end
-// (relative to the piece).
-struct SlotChunks {
-  int first, end, step;
-  __device__ bool any() const { return first < end; }
-  __device__ bool has(int i) const { return i >= first && i < end && (i - first) % step == 0; }
-  __device__ int last() const { return first + (end - 1 - first) / step * step; }
-};
-__device__ __forceinline__ SlotChunks slot_chunks(const PagedAttnArgs& a, const Piece& p, int tt, int t) {
-  const int n = p.cb - p.ca;
-  if (p.nt <= tt) return {t, n, 2};
-  const int t0 = p.t0 + t * tt, t1 = min(p.t0 + p.nt, t0 + tt);
-  const TileKeys k = tile_keys(a, p.n, p.len, t0, t1);
-  return {max(0, k.lo / kTcChunk - p.ca), min(n, (k.hi + kTcChunk - 1) / kTcChunk - p.ca), 1};
+// A row warp's wait for its next piece.  The loading warp always brings one (an end,
+// after a wait of its own has run out), and the 8 row warps have to agree on it: they take no
+// notice of the other roles' failures here, and the limit is past all of theirs.
+__device__ __forceinline__ bool piece_wait(uint64_t* bar, uint32_t parity) {
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t it = 0; !mbar_try_wait(bar, parity); ++it)
+    if ((it & 63u) == 63u && globaltimer_ns() - t0 > 8 * kWaitBudgetNs) return false;
+  return true;
 }
 
-// Ring position of a piece's loads (K0 K1 V0 K2 V1 .. V(n-1)), relative to its first.
-__device__ __forceinline__ int ring_k(int i) { return i == 0 ? 0 : 2 * i - 1; }
+// A position of a ring and the phase of its barriers.
+template <int N>
+struct RingAt {
+  uint32_t i = 0, phase = 0;
+  __device__ void operator++() {
+    if (++i == N) i = 0, phase ^= 1;
+  }
+};
+
+// Ring position of a piece's V tiles (loaded as K0 K1 V0 K2 V1 .. V(n-1)), relative to K0.
 __device__ __forceinline__ int ring_v(int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; }
 
 template <class T> struct TcType;
@@ -107,26 +134,67 @@ template <> struct TcType<__nv_bfloat16> {
   static constexpr uint32_t idesc(int n, bool mn) { return idesc_bf16_f32(kTcRows, n, mn); }
 };
 
-template <class T, int HD>
+// Walk the CTA's run, hand each piece to the other warps, and load its queries, keys and
+// values.
+template <int HD>
 __device__ __forceinline__ void issue_loads(TcSmem<HD>& s, const PagedAttnArgs& a, const PagedGeom& g, const TcMaps& m) {
   constexpr int NH = HD / 64, NR = TcSmem<HD>::kRing;
-  const int lane = threadIdx.x & 31, tt = g.tile_tok / 2, P = 1 << a.page_shift;
+  const int lane = threadIdx.x & 31, tt = g.slot_tok, P = 1 << a.page_shift;
   const int box = min(P, kTcChunk), boxes = kTcChunk / box;
-  uint32_t r = 0, pieces = 0;  // loads so far, pieces with keys so far
+  RingAt<NR> at;
+  RingAt<kTcPieces> pat;
+  uint32_t r = 0, pieces = 0, with_keys = 0;  // loads, pieces, pieces with keys so far
   bool ok = true;
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    ok = ok && tc_wait(bar, parity, &s.abort, &s.busy);
+    ok = __all_sync(0xffffffffu, ok);
+  };
   PagedWalk w;
-  w.begin(a, g, s.run);
-  Piece p;
-  while (ok && w.next(a, g, p)) {
+  w.begin(s.run);
+  for (;;) {
+    Piece p;
+    const bool more = w.next(a, g, p);
+    if (pieces >= kTcPieces) {
+      wait(&s.pempty[pat.i], pat.phase ^ 1);
+      wait(&s.pfree[pat.i], pat.phase ^ 1);
+    }
+    if (!ok) break;
+    ++pieces;
+    if (lane == 0) {
+      TcPiece& o = s.piece[pat.i];
+      o.end = !more;
+      if (more) {
+        o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0, o.lo = p.lo, o.hi = p.hi;
+        o.ca = p.ca, o.chunks = p.cb - p.ca;
+        o.two = p.nt > tt, o.whole = p.whole();
+        if (!p.whole()) {
+          o.slot = w.slot(p, blockIdx.x);
+          o.cta0 = w.first_cta(p), o.cta1 = w.last_cta(p);
+          o.first_slot = w.slot(p, o.cta0);
+        }
+        for (int t = 0; t < 2; ++t) {
+          if (!o.two) {
+            o.c[t] = {t, o.chunks, 2};
+          } else {
+            const int t0 = p.t0 + t * tt;
+            const TileKeys k = tile_keys(a, p.n, p.len, t0, min(p.t0 + p.nt, t0 + tt));
+            o.c[t] = {max(0, k.lo / kTcChunk - p.ca), min(o.chunks, (k.hi + kTcChunk - 1) / kTcChunk - p.ca), 1};
+          }
+        }
+      }
+      mbar_arrive(&s.pfull[pat.i]);
+    }
+    __syncwarp();
+    ++pat;
+    if (!more) break;
     if (p.empty()) continue;
     const int n = p.cb - p.ca;
     auto tile = [&](const CUtensorMap* map, int c) {  // 128 keys from chunk c: those pages that hold keys of the tile
-      const int kb = c * kTcChunk, slot = r % NR;
-      if (r >= NR) ok = tc_wait(&s.empty[slot], (r / NR - 1) & 1, &s.abort, &s.busy);
-      ok = __all_sync(0xffffffffu, ok);
+      const int kb = c * kTcChunk;
+      if (r >= NR) wait(&s.empty[at.i], at.phase ^ 1);
       if (!ok) return;
       const int b0 = max(p.lo - kb, 0) / box, b1 = (min(p.hi - kb, kTcChunk) + box - 1) / box;
-      if (lane == 0) mbar_arrive_expect_tx(&s.full[slot], (b1 - b0) * box * HD * 2);
+      if (lane == 0) mbar_arrive_expect_tx(&s.full[at.i], (b1 - b0) * box * HD * 2);
       __syncwarp();
       const int j = lane / NH, half = lane % NH;  // (boxes * NH <= 32)
       if (j >= b0 && j < b1 && j < boxes) {
@@ -136,13 +204,13 @@ __device__ __forceinline__ void issue_loads(TcSmem<HD>& s, const PagedAttnArgs& 
           atomicOr(a.err, DERR_CAPACITY);
           page = a.n_pages;  // outside the map: reads as zeros
         }
-        tma_load_5d(s.ring[slot] + half * kTcChunk * 128 + j * box * 128, map, &s.full[slot], half * 64, pos & (P - 1), p.h,
+        tma_load_5d(s.ring[at.i] + half * kTcChunk * 128 + j * box * 128, map, &s.full[at.i], half * 64, pos & (P - 1), p.h,
                     page, a.layer);
       }
       ++r;
+      ++at;
     };
-    if (pieces > 0) ok = tc_wait(&s.qempty, (pieces - 1) & 1, &s.abort, &s.busy);
-    ok = __all_sync(0xffffffffu, ok);
+    if (with_keys > 0) wait(&s.qempty, (with_keys - 1) & 1);
     if (!ok) break;
     const int slots = p.nt > tt ? 2 : 1;
     if (lane == 0) mbar_arrive_expect_tx(&s.qfull, slots * NH * tt * a.group * 128);
@@ -150,117 +218,145 @@ __device__ __forceinline__ void issue_loads(TcSmem<HD>& s, const PagedAttnArgs& 
     if (lane < slots * NH)
       tma_load_3d(s.q[lane / NH] + lane % NH * kTcRows * 128, &m.q, &s.qfull, lane % NH * 64, p.h * a.group,
                   p.row0 + p.t0 + lane / NH * tt);
-    ++pieces;
+    ++with_keys;
     tile(&m.k, p.ca);
     for (int i = 0; ok && i < n; ++i) {
       if (i + 1 < n) tile(&m.k, p.ca + i + 1);
       if (ok) tile(&m.v, p.ca + i);
     }
+    if (!ok) break;
   }
-  if (!ok && lane == 0) {  // loads in flight land before the CTA leaves
+  if (!ok && lane == 0) {
+    // the rows get their end (they go on past every wait now), and loads in flight land
+    // before the CTA leaves
+    *const_cast<volatile int*>(&s.abort) = 1;
+    if (pieces >= kTcPieces) mbar_wait(&s.pempty[pat.i], pat.phase ^ 1, nullptr);
+    s.piece[pat.i].end = 1;
+    mbar_arrive(&s.pfull[pat.i]);
     for (uint32_t i = r > NR ? r - NR : 0; i < r; ++i) mbar_wait(&s.full[i % NR], (i / NR) & 1, nullptr);
-    if (pieces > 0) mbar_wait(&s.qfull, (pieces - 1) & 1, nullptr);
+    if (with_keys > 0) mbar_wait(&s.qfull, (with_keys - 1) & 1, nullptr);
   }
 }
 
+// The MMAs of the CTA, all by one thread, whose instructions are what its chunks cost
+// beside the tensor cores' own time: descriptors are made once and moved by an add.
+// (Made anew for every MMA they held the thread up for 8800 cycles per chunk of 256
+// rows, against 2048 of tensor-core time.)
 template <class T, int HD>
-__device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, const PagedAttnArgs& a, const PagedGeom& g, uint32_t tmem, int hold) {
+__device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, uint32_t tmem, int hold) {
   constexpr int NR = TcSmem<HD>::kRing;
   constexpr uint32_t id_s = TcType<T>::idesc(kTcChunk, false), id_o = TcType<T>::idesc(HD, true);
-  const int lane = threadIdx.x & 31, tt = g.tile_tok / 2;
-  uint32_t r = 0, pieces = 0, np[2] = {0, 0};  // loads of the pieces before, pieces, P tiles taken
+  // low words of the descriptors of the first tile (the address field, in 16 bytes, never carries out of them)
+  const uint64_t dq = sdesc_kmajor_sw128(smem_u32(s.q[0])), dk = sdesc_kmajor_sw128(smem_u32(s.ring[0])),
+                 dv = sdesc_mnmajor_sw128(smem_u32(s.ring[0]), kTcChunk * 128);
+  const uint32_t q_lo = static_cast<uint32_t>(dq), k_lo = static_cast<uint32_t>(dk), v_lo = static_cast<uint32_t>(dv);
+  const uint32_t q_hi = static_cast<uint32_t>(dq >> 32), k_hi = static_cast<uint32_t>(dk >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
+  auto desc = [](uint32_t lo, uint32_t hi) { return static_cast<uint64_t>(hi) << 32 | lo; };
+  RingAt<NR> at;
+  RingAt<kTcPieces> pat;
+  uint32_t pieces = 0, np0 = 0, np1 = 0;  // pieces so far, P tiles taken of each slot
   bool ok = true;
-  PagedWalk w;
-  w.begin(a, g, s.run);
-  Piece p;
-  while (ok && w.next(a, g, p)) {
-    if (p.empty()) continue;
-    const int n = p.cb - p.ca;
-    const bool two = p.nt > tt;  // 128 rows in each slot
-    const SlotChunks sc[2] = {slot_chunks(a, p, tt, 0), slot_chunks(a, p, tt, 1)};
-    if (lane == 0) {
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        ok = ok && tc_wait(bar, parity, &s.abort, &s.busy);
-        tc_fence_after();
+  if ((threadIdx.x & 31) == 0) {
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && tc_wait(bar, parity, &s.abort, &s.busy);
+      tc_fence_after();
+    };
+    for (;; ++pat) {
+      wait(&s.pfull[pat.i], pat.phase);
+      if (!ok) break;
+      const TcPiece& p = s.piece[pat.i];
+      if (p.end) break;
+      const int n = p.chunks;
+      const bool two = p.two;
+      const SlotChunks c0 = p.c[0], c1 = p.c[1];
+      mbar_arrive(&s.pfree[pat.i]);
+      if (n == 0) continue;
+      auto next_tile = [&] {  // the next tile of the ring, landed
+        const uint32_t slot = at.i;
+        wait(&s.full[slot], at.phase);
+        ++at;
+        return slot;
       };
-      auto landed = [&](int at) { wait(&s.full[(r + at) % NR], ((r + at) / NR) & 1); };
-      auto release = [&](int at) {
-        if (ok) tc_commit(&s.empty[(r + at) % NR]);
+      auto release = [&](uint32_t slot) {
+        if (ok) tc_commit(&s.empty[slot]);
       };
-      auto mma_s = [&](int t, int i) {  // S of slot t over chunk i
+      auto mma_s = [&](int t, uint32_t slot) {  // S of slot t over the keys of a tile
         if (!ok) return;
-        const uint32_t qa = smem_u32(s.q[two ? t : 0]), ka = smem_u32(s.ring[(r + ring_k(i)) % NR]);
+        const uint32_t qa = q_lo + (two && t ? sizeof(s.q[0]) >> 4 : 0), ka = k_lo + slot * (TcSmem<HD>::kTile >> 4);
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * kTcRows * 128 + (kk & 3) * 32;
-          tc_mma_f16(tmem + t * 256, sdesc_kmajor_sw128(qa + off), sdesc_kmajor_sw128(ka + off), id_s, kk > 0);
+          const uint32_t off = ((kk >> 2) * kTcRows * 128 + (kk & 3) * 32) >> 4;
+          tc_mma_f16(tmem + t * 256, desc(qa + off, q_hi), desc(ka + off, k_hi), id_s, kk > 0);
         }
         tc_commit(&s.sfull[t]);
       };
-      auto mma_o = [&](int t, int i) {  // O of slot t += P V of chunk i
+      auto mma_o = [&](int t, uint32_t slot, int i, const SlotChunks& c) {  // O of slot t += P V of chunk i
         if (hold > 0 && i + 1 >= hold) ok = false;  // test hook: as if this thread's wait had run out
-        wait(&s.pready[t], np[t] & 1);
-        ++np[t];
+        uint32_t& np = t ? np1 : np0;
+        wait(&s.pready[t], np & 1);
+        ++np;
         if (!ok) return;
-        const uint32_t va = smem_u32(s.ring[(r + ring_v(i, n)) % NR]);
+        const uint32_t va = v_lo + slot * (TcSmem<HD>::kTile >> 4), first = i > c.first;
 #pragma unroll
         for (int kk = 0; kk < kTcChunk / 16; ++kk)
-          tc_mma_f16_ts(tmem + t * 256 + 128, tmem + t * 256 + kk * 8, sdesc_mnmajor_sw128(va + kk * 16 * 128, kTcChunk * 128),
-                        id_o, i > sc[t].first || kk > 0);
-        if (i == sc[t].last()) tc_commit(&s.ofull[t]);
+          tc_mma_f16_ts(tmem + t * 256 + 128, tmem + t * 256 + kk * 8, desc(va + (kk * 16 * 128 >> 4), v_hi), id_o,
+                        kk > 0 ? 1u : first);
+        if (i == c.last()) tc_commit(&s.ofull[t]);
       };
       wait(&s.qfull, pieces & 1);
-      landed(0);
+      const uint32_t k0 = next_tile();
       if (two) {
-        for (int t = 0; t < 2; ++t)
-          if (sc[t].has(0)) mma_s(t, 0);
-        release(0);
+        if (c0.has(0)) mma_s(0, k0);
+        if (c1.has(0)) mma_s(1, k0);
+        release(k0);
         if (n == 1 && ok) tc_commit(&s.qempty);
         for (int i = 0; ok && i < n; ++i) {
-          landed(ring_v(i, n));
-          if (i + 1 < n) landed(ring_k(i + 1));
+          const bool more = i + 1 < n;
+          const uint32_t k = more ? next_tile() : 0, v = next_tile();
           if (i == 0 && pieces > 0) wait(&s.ofree, (pieces - 1) & 1);
-          for (int t = 0; t < 2; ++t) {
-            if (sc[t].has(i)) mma_o(t, i);
-            if (i + 1 < n && sc[t].has(i + 1)) mma_s(t, i + 1);
-          }
-          release(ring_v(i, n));
-          if (i + 1 < n) release(ring_k(i + 1));
+          if (c0.has(i)) mma_o(0, v, i, c0);
+          if (more && c0.has(i + 1)) mma_s(0, k);
+          if (c1.has(i)) mma_o(1, v, i, c1);
+          if (more && c1.has(i + 1)) mma_s(1, k);
+          release(v);
+          if (more) release(k);
           if (i + 2 == n && ok) tc_commit(&s.qempty);
         }
       } else {
-        mma_s(0, 0);
-        release(0);
+        mma_s(0, k0);
+        release(k0);
+        uint32_t k = 0;
         if (n > 1) {
-          landed(ring_k(1));
-          mma_s(1, 1);
-          release(ring_k(1));
+          k = next_tile();
+          mma_s(1, k);
+          release(k);
         }
         if (n <= 2 && ok) tc_commit(&s.qempty);
-        for (int i = 0; ok && i < n; ++i) {
-          landed(ring_v(i, n));
+        auto step = [&](int t, int i, const SlotChunks& c) {
+          const uint32_t v = next_tile();
           if (i == 0 && pieces > 0) wait(&s.ofree, (pieces - 1) & 1);
-          mma_o(i & 1, i);
-          release(ring_v(i, n));
+          mma_o(t, v, i, c);
+          release(v);
           if (i + 2 < n) {
-            landed(ring_k(i + 2));
-            mma_s(i & 1, i + 2);
-            release(ring_k(i + 2));
+            k = next_tile();
+            mma_s(t, k);
+            release(k);
             if (i + 3 == n && ok) tc_commit(&s.qempty);
           }
+        };
+        for (int i = 0; ok && i < n; i += 2) {
+          step(0, i, c0);
+          if (ok && i + 1 < n) step(1, i + 1, c1);
         }
       }
-      if (!ok) {
-        s.abort = 1;
-        tc_commit(&s.drain);  // MMAs in flight end before the CTA leaves
-        mbar_wait(&s.drain, 0, nullptr);
-      }
+      if (!ok) break;
+      ++pieces;
     }
-    ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-    r += 2 * n;
-    ++pieces;
-    np[0] = __shfl_sync(0xffffffffu, np[0], 0);
-    np[1] = __shfl_sync(0xffffffffu, np[1], 0);
+    if (!ok) {
+      *const_cast<volatile int*>(&s.abort) = 1;
+      tc_commit(&s.drain);  // MMAs in flight end before the CTA leaves
+      mbar_wait(&s.drain, 0, nullptr);
+    }
   }
 }
 
@@ -270,7 +366,7 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, const PagedAttnArgs& a
 template <class T, int HD>
 __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, const PagedGeom& g, uint32_t tmem) {
   constexpr int NR = TcSmem<HD>::kRing;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t = warp >> 2, tt = g.tile_tok / 2;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t = warp >> 2, tt = g.slot_tok;
   const int row = (warp & 3) * 32 + lane;
   const uint32_t ts = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);  // this warp's lanes, slot 0
   const uint32_t mine = ts + t * 256;
@@ -281,29 +377,31 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
   };
   auto all_rows = [&] { named_bar_sync(1, 256); };
   uint32_t r = 0, ns = 0, no[2] = {0, 0};  // loads of the pieces before, S tiles of this slot, outputs of both
-  PagedWalk w;
-  w.begin(a, g, s.run);
-  Piece p;
-  while (w.next(a, g, p)) {
-    const int n = p.cb - p.ca;
-    const bool two = p.nt > tt;
-    const int tok0 = two ? t * tt : 0, ntok = two ? min(tt, p.nt - tok0) : p.nt;
-    const int rows = ntok * a.group, tok = p.t0 + tok0 + min(row, rows - 1) / a.group;
-    const int head = p.h * a.group + row % a.group;
-    const RowKeys rk = row_keys(a, p.n, p.len, p.row0, tok);
-    const SlotChunks sc[2] = {slot_chunks(a, p, tt, 0), slot_chunks(a, p, tt, 1)};
+  RingAt<kTcPieces> pat;
+  for (;; ++pat) {
+    if (!piece_wait(&s.pfull[pat.i], pat.phase)) break;
+    const TcPiece& p = s.piece[pat.i];
+    if (p.end) break;
+    const int n = p.chunks;
+    const bool two = p.two;
+    const int tok0 = two ? t * tt : 0;
+    const int rows = (two ? min(tt, p.nt - tok0) : p.nt) * a.group;  // live rows of this slot
+    const int tok = p.t0 + tok0 + min(row, rows - 1) / a.group;
     const bool band = (warp & 3) * 32 < rows;  // some row of the warp is live
     float m = -INFINITY, l = 0.f;
-    if (!p.empty()) {
-      for (int i = t == 0 ? sc[0].first : sc[1].first; i < sc[t].end; i += sc[t].step) {
+    if (n > 0) {
+      const int first = p.c[t].first, end = p.c[t].end, step = p.c[t].step, lo = p.lo, hi = p.hi;
+      RowKeys rk = row_keys(a, p.n, p.len, p.row0, tok);
+      const int all_to = rk.bits != nullptr ? rk.ctx : rk.hi;  // every key from rk.lo to here is seen
+      for (int i = first; i < end; i += step) {
         const int kb = (p.ca + i) * kTcChunk;
         warp_wait(&s.sfull[t], ns++ & 1);
-        if (p.lo > kb || p.hi < kb + kTcChunk) {
+        if (lo > kb || hi < kb + kTcChunk) {
           // keys of the chunk that no row of the tile sees (not loaded, or what the
           // page held before): p is 0 there, and so is V
           const int v = r + ring_v(i, n);
           warp_wait(&s.full[v % NR], (v / NR) & 1);
-          if (kb + row < p.lo || kb + row >= p.hi) {
+          if (kb + row < lo || kb + row >= hi) {
 #pragma unroll
             for (int c = 0; c < HD / 8; ++c)
               *reinterpret_cast<uint4*>(s.ring[v % NR] + (c >> 3) * kTcChunk * 128 + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
@@ -314,8 +412,8 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
           float x0[64], x1[64];
           tmem_ld64(mine, x0);
           tmem_ld64(mine + 64, x1);
-          const bool sees_all = rk.lo <= kb && kb + kTcChunk <= (rk.bits != nullptr ? rk.ctx : rk.hi);
-          if (__any_sync(0xffffffffu, !sees_all)) {
+          if (__any_sync(0xffffffffu, rk.lo > kb || kb + kTcChunk > all_to)) {
+            rk = row_keys(a, p.n, p.len, p.row0, tok);
             const uint32_t b0 = key_bits(rk, kb), b1 = key_bits(rk, kb + 32), b2 = key_bits(rk, kb + 64), b3 = key_bits(rk, kb + 96);
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
@@ -331,7 +429,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
 #pragma unroll
             for (int u = 0; u < 4; ++u) m4[u] = fmaxf(m4[u], fmaxf(x0[j + u], x1[j + u]));
           const float cm = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2;
-          if (i == sc[t].first) {
+          if (i == first) {
             m = cm;
           } else {
             const bool grow = cm > m + kTcSlack || (m == -INFINITY && cm > m);
@@ -379,10 +477,10 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
         if (lane == 0) mbar_arrive(&s.pready[t]);
       }
     }
-    const bool whole = p.whole();
-    const int cta0 = whole ? 0 : w.first_cta(p), cta1 = whole ? 0 : w.last_cta(p);
-    const size_t slot_row = whole ? 0 : static_cast<size_t>(w.slot(p, blockIdx.x)) * kPagedPartRows;
-    // `count` columns of a row from column d: a result, or a partial one
+    const bool whole = p.whole;
+    const size_t slot_row = static_cast<size_t>(p.slot) * kPagedPartRows;
+    const int head = p.h * a.group + row % a.group;
+    // 16 columns of a row from column d: a result, or a partial one
     auto store16 = [&](const float (&o)[16], int rr, int d, float scale, bool live) {
       if (!live) return false;
       if (!whole) {
@@ -413,12 +511,12 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
     auto redo = [&](int rr) {  // (the whole warp)
       __syncwarp();
       if (lane == 0) atomicAdd(&s.busy, 1);
-      exact_row<T, HD>(a, p, p.t0 + (two ? rr / kTcRows * tt : 0) + (rr % kTcRows) / a.group, p.h * a.group + (rr % kTcRows) % a.group);
+      exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + (two ? rr / kTcRows * tt : 0) + (rr % kTcRows) / a.group, p.h * a.group + (rr % kTcRows) % a.group);
       if (lane == 0) atomicAdd(&s.busy, -1);
     };
     bool shared_rows = false;  // rows whose columns several warps have written
     if (two) {
-      const bool has = sc[t].any() && !p.empty();
+      const bool has = p.c[t].any();
       if (has) warp_wait(&s.ofull[t], no[t] & 1);
       const bool live = row < rows;
       const float scale = l != 0.f ? 1.f / l : 0.f;
@@ -449,7 +547,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       const float2 ml0 = s.ml[0][row], ml1 = s.ml[1][row];
       bool has[2];
       for (int u = 0; u < 2; ++u) {
-        has[u] = sc[u].any() && !p.empty();
+        has[u] = p.c[u].any();
         if (has[u]) warp_wait(&s.ofull[u], no[u] & 1);
       }
       const bool use0 = has[0] && ml0.x != -INFINITY, use1 = has[1] && ml1.x != -INFINITY;
@@ -477,14 +575,15 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       if (bad) atomicOr(&s.bad[row >> 5], 1u << (row & 31));
       shared_rows = whole;
     }
-    if (!p.empty()) {  // the accumulators may be overwritten
+    if (n > 0) {  // the accumulators may be overwritten
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&s.ofree);
       r += 2 * n;
-      for (int u = 0; u < 2; ++u) no[u] += sc[u].any();
+      for (int u = 0; u < 2; ++u) no[u] += p.c[u].any();
     }
     if (!whole) {
+      const int cta0 = p.cta0, cta1 = p.cta1;
       __threadfence();
       all_rows();
       if (tid == 0) {
@@ -494,33 +593,61 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       }
       all_rows();
       if (s.last) {
-        // merge the parts of the tile in order, 4 columns of a row per thread
-        const int items = p.nt * a.group * (HD / 4);
-        for (int i = tid; i < items; i += 256) {
-          const int k = i / (HD / 4), d = i % (HD / 4) * 4, kt = k / a.group, hh = p.h * a.group + k % a.group;
-          const int rr = two && kt >= tt ? kTcRows + (kt - tt) * a.group + k % a.group : k;
+        // Merge the parts of the tile, in order.  First the rows' maxima and sums, a
+        // thread per row; then 4 columns of a row per thread, several loads in
+        // flight (one SM takes the parts in at 64 bytes a cycle at best).
+        const int live = p.nt * a.group;
+        if (tid < live) {
+          const int kt = tid / a.group, rr = two && kt >= tt ? kTcRows + tid - tt * a.group : tid;
           float mm = -INFINITY, ll = 0.f;
-          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
+          for (int c = cta0; c <= cta1; ++c) mm = fmaxf(mm, __ldcg(a.part_ml + static_cast<size_t>(p.part(c)) * kPagedPartRows + rr).x);
+#pragma unroll 8
           for (int c = cta0; c <= cta1; ++c) {
-            const size_t at = static_cast<size_t>(w.slot(p, c)) * kPagedPartRows + rr;
-            const float2 ml = __ldcg(a.part_ml + at);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * HD + d));
-            const bool use = ml.x != -INFINITY;
-            const float nm = fmaxf(mm, ml.x), f = mm == -INFINITY ? 0.f : ex2_ftz(mm - nm), u = use ? ex2_ftz(ml.x - nm) : 0.f;
-            mm = nm;
-            ll = ll * f + (use ? ml.y * u : 0.f);
-            x.x = x.x * f + (use ? y.x * u : 0.f);
-            x.y = x.y * f + (use ? y.y * u : 0.f);
-            x.z = x.z * f + (use ? y.z * u : 0.f);
-            x.w = x.w * f + (use ? y.w * u : 0.f);
+            const float2 ml = __ldcg(a.part_ml + static_cast<size_t>(p.part(c)) * kPagedPartRows + rr);
+            ll += ml.x != -INFINITY ? ml.y * ex2_ftz(ml.x - mm) : 0.f;
           }
-          const float scale = ll != 0.f ? 1.f / ll : 0.f;
-          x = ll != 0.f ? make_float4(x.x * scale, x.y * scale, x.z * scale, x.w * scale) : make_float4(0.f, 0.f, 0.f, 0.f);
-          if (!isfinite(x.x) || !isfinite(x.y) || !isfinite(x.z) || !isfinite(x.w)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
-          *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + kt) * a.out_row + hh * a.out_head + d) =
-              make_uint2(TcType<T>::pack(x.x, x.y), TcType<T>::pack(x.z, x.w));
-          if (d == 0) store_lse(p.t0 + kt, hh, mm, ll);
+          (&s.ml[0][0])[tid] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
+          store_lse(p.t0 + kt, p.h * a.group + tid % a.group, mm, ll);
+        }
+        all_rows();
+        constexpr int kItems = 4;  // rows of a thread at a time, 256 / (HD / 4) apart
+        constexpr int kStep = 256 / (HD / 4);
+        const int d = tid % (HD / 4) * 4;
+        for (int k0 = tid / (HD / 4); k0 < live; k0 += kItems * kStep) {
+          float4 x[kItems];
+          float2 mi[kItems];
+          int rr[kItems];
+#pragma unroll
+          for (int e = 0; e < kItems; ++e) {
+            const int k = min(k0 + e * kStep, live - 1);
+            rr[e] = two && k >= tt * a.group ? kTcRows + k - tt * a.group : k;
+            mi[e] = (&s.ml[0][0])[k];
+            x[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+#pragma unroll 2
+          for (int c = cta0; c <= cta1; ++c) {
+            const size_t at = static_cast<size_t>(p.part(c)) * kPagedPartRows;
+#pragma unroll
+            for (int e = 0; e < kItems; ++e) {
+              const float m1 = __ldcg(a.part_ml + at + rr[e]).x;
+              const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part_o + (at + rr[e]) * HD + d));
+              const float u = ex2_ftz(m1 - mi[e].x);
+              if (m1 != -INFINITY) x[e].x = fmaf(y.x, u, x[e].x), x[e].y = fmaf(y.y, u, x[e].y), x[e].z = fmaf(y.z, u, x[e].z), x[e].w = fmaf(y.w, u, x[e].w);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < kItems; ++e) {
+            const int k = k0 + e * kStep;
+            if (k >= live) break;
+            const float f = mi[e].y;
+            float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (f != 0.f) z = make_float4(x[e].x * f, x[e].y * f, x[e].z * f, x[e].w * f);
+            if (!isfinite(z.x) || !isfinite(z.y) || !isfinite(z.z) || !isfinite(z.w)) atomicOr(&s.bad[rr[e] >> 5], 1u << (rr[e] & 31));
+            *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + k / a.group) * a.out_row +
+                                      (p.h * a.group + k % a.group) * a.out_head + d) =
+                make_uint2(TcType<T>::pack(z.x, z.y), TcType<T>::pack(z.z, z.w));
+          }
         }
         shared_rows = true;
       }
@@ -537,6 +664,8 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
         all_rows();
       }
     }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&s.pempty[pat.i]);
   }
 }
 
@@ -563,6 +692,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       mbar_init(&s.pready[t], 4);
       mbar_init(&s.ofull[t], 1);
     }
+    for (int i = 0; i < kTcPieces; ++i) {
+      mbar_init(&s.pfull[i], 1);
+      mbar_init(&s.pempty[i], 8);
+      mbar_init(&s.pfree[i], 1);
+    }
     mbar_init(&s.ofree, 8);
     mbar_init(&s.drain, 1);
     s.abort = s.busy = 0;
@@ -580,8 +714,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const uint32_t tmem = s.tmem;
   if (warp >= 8) {
     setmaxnreg_dec<kTcRegsLow>();
-    if (warp == 8) issue_mmas<T, HD>(s, a, g, tmem, hold);
-    else if (warp == 9) issue_loads<T, HD>(s, a, g, m);
+    if (warp == 8) issue_mmas<T, HD>(s, tmem, hold);
+    else if (warp == 9) issue_loads<HD>(s, a, g, m);
   } else {
     setmaxnreg_inc<kTcRegsRow>();
     run_rows<T, HD>(s, a, g, tmem);
@@ -598,7 +732,12 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 
 template <class T, int HD>
 cudaError_t launch_tc(const TcMaps& m, const PagedAttnArgs& a, int hold, int grid, cudaStream_t s) {
-  const PagedGeom g{2 * (kTcRows / a.group), kTcChunk, 2};
+  const int tt = kTcRows / a.group;
+  // Tiles of 256 rows read K and V once for twice the rows; with fewer of them than CTAs
+  // their keys would have to be cut and their rows merged, so they are halved instead.
+  const long long per_request = (static_cast<long long>(a.rows) + a.batch - 1) / a.batch;
+  const bool two = per_request > tt && (per_request + 2 * tt - 1) / (2 * tt) * a.batch * a.Hkv >= grid;
+  const PagedGeom g{two ? 2 * tt : tt, tt, kTcChunk, 2};
   paged_attn_tc_kernel<T, HD><<<grid, kTcThreads, sizeof(TcSmem<HD>), s>>>(m, a, g, hold);
   return cudaGetLastError();
 }

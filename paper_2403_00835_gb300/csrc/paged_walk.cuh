@@ -17,6 +17,7 @@ namespace cllm {
 
 struct PagedGeom {
   int tile_tok;   // tokens of a tile
+  int slot_tok;   // tokens of 128 rows (tensor-core kernel: a tile has one or two times that)
   int chunk;      // keys of a unit
   int min_units;  // fewest units of a CTA's run
 };
@@ -51,18 +52,36 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, int n, int
 __device__ __forceinline__ int tile_units(const PagedGeom& g, const TileKeys& k) {
   return k.hi > k.lo ? (k.hi + g.chunk - 1) / g.chunk - k.lo / g.chunk : 1;
 }
-// Units of one head of a request.
+// Units of one head of each lane's request (the whole warp calls; n = 0: none).  A
+// request of many tiles is summed by all lanes.
 __device__ __forceinline__ long long head_units(const PagedAttnArgs& a, const PagedGeom& g, int n, int len) {
   long long u = 0;
-  for (int t0 = 0; t0 < n; t0 += g.tile_tok) u += tile_units(g, tile_keys(a, n, len, t0, min(n, t0 + g.tile_tok)));
+  const bool many = n > 2 * g.tile_tok;
+  if (!many)
+    for (int t0 = 0; t0 < n; t0 += g.tile_tok) u += tile_units(g, tile_keys(a, n, len, t0, min(n, t0 + g.tile_tok)));
+  for (unsigned rest = __ballot_sync(0xffffffffu, many); rest; rest &= rest - 1) {
+    const int src = __ffs(rest) - 1, lane = threadIdx.x & 31;
+    const int bn = __shfl_sync(0xffffffffu, n, src), bl = __shfl_sync(0xffffffffu, len, src);
+    long long v = 0;
+    for (int t0 = lane * g.tile_tok; t0 < bn; t0 += 32 * g.tile_tok)
+      v += tile_units(g, tile_keys(a, bn, bl, t0, min(bn, t0 + g.tile_tok)));
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if (lane == src) u = v;
+  }
   return u;
+}
+
+// x / y of values that almost always have 32 bits
+__device__ __forceinline__ long long div_units(long long x, long long y) {
+  return (x | y) >> 32 ? x / y : static_cast<unsigned>(x) / static_cast<unsigned>(y);
 }
 
 // Where a CTA's run begins (shared memory, made once by all threads).
 struct RunStart {
   long long u0, u1, per;  // the run, and the units of every run
-  long long begin;        // first unit of request b
-  int b;
+  long long begin, head;  // first unit of request b, and the units of one of its heads
+  int b, row0, n, len;
 };
 
 // A piece: the chunks [ca, cb) of a tile that belong to this CTA's run.
@@ -78,53 +97,57 @@ struct Piece {
 };
 
 // All threads of the block (a multiple of 32, at most 1024): the block's run.
-// `sm` holds 33 values.
-__device__ inline void run_start(const PagedAttnArgs& a, const PagedGeom& g, RunStart* rs, long long* sm) {
+// `sm` holds 32 values.
+__device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeom& g, RunStart* rs, long long* sm) {
   const int tid = threadIdx.x, nthr = blockDim.x, lane = tid & 31, warp = tid >> 5;
-  const int per_t = (a.batch + nthr - 1) / nthr, b0 = min(tid * per_t, a.batch), b1 = min(b0 + per_t, a.batch);
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    const Request q = request(a, b);
-    mine += a.Hkv * head_units(a, g, q.n, q.len);
-  }
-  long long v = mine;
+  long long total = 0, head = 0, units = 0, before = 0;
+  Request r{0, 0, 0};
+  // a thread per request and round: this round's units before the thread's request
+  auto round = [&](int b0) {
+    r = b0 + tid < a.batch ? request(a, b0 + tid) : Request{0, 0, 0};
+    head = head_units(a, g, r.n, r.len);
+    units = head * a.Hkv;
+    long long v = units;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long o = __shfl_up_sync(0xffffffffu, v, d);
-    if (lane >= d) v += o;
-  }
-  if (lane == 31) sm[warp] = v;
-  __syncthreads();
-  long long total = 0, before = 0;
-  for (int w = 0; w < nthr / 32; ++w) {
-    if (w < warp) before += sm[w];
-    total += sm[w];
-  }
-  v += before - mine;  // units before this thread's requests
-  long long per = (total + gridDim.x - 1) / gridDim.x;
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) v += o;
+    }
+    if (b0 > 0) __syncthreads();
+    if (lane == 31) sm[warp] = v;
+    __syncthreads();
+    long long sum = 0;
+    before = v - units;
+    for (int w = 0; w < nthr / 32; ++w) {
+      if (w < warp) before += sm[w];
+      sum += sm[w];
+    }
+    return sum;
+  };
+  for (int b0 = 0; b0 < a.batch; b0 += nthr) total += round(b0);
+  long long per = div_units(total + gridDim.x - 1, gridDim.x);
   if (per < g.min_units) per = g.min_units;
-  const long long u0 = blockIdx.x * per, u1 = min(u0 + per, total);
+  const long long u0 = blockIdx.x * per;
   if (tid == 0) {
     rs->u0 = u0;
-    rs->u1 = max(u0, u1);
+    rs->u1 = max(u0, min(u0 + per, total));
     rs->per = per;
   }
-  if (u0 < total && u0 >= v && u0 < v + mine) {  // one thread at most
-    int b = b0;
-    for (;; ++b) {
-      const Request q = request(a, b);
-      const long long u = a.Hkv * head_units(a, g, q.n, q.len);
-      if (u0 < v + u || b + 1 >= b1) break;
-      v += u;
+  long long base = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += nthr) {
+    const long long sum = a.batch <= nthr ? total : round(b0);
+    if (u0 >= base + before && u0 < base + before + units) {  // one thread at most
+      rs->b = b0 + tid;
+      rs->begin = base + before;
+      rs->head = head;
+      rs->row0 = r.row0, rs->n = r.n, rs->len = r.len;
     }
-    rs->b = b;
-    rs->begin = v;
+    base += sum;
   }
   __syncthreads();
 }
 
-// The pieces of the block's run, in order.  Every warp that works on them walks
-// for itself; the whole warp calls.
+// The pieces of the block's run, in order (the whole warp calls).
 struct PagedWalk {
   long long u, u1, per, tu;  // next unit, end of the run, units of a run, first unit of the tile
   int b, h, t0, n, len, row0;
@@ -135,16 +158,15 @@ struct PagedWalk {
     t0 = 0;
     h = 0;
   }
-  __device__ void begin(const PagedAttnArgs& a, const PagedGeom& g, const RunStart& rs) {
+  __device__ void begin(const RunStart& rs) {
     u = rs.u0;
     u1 = rs.u1;
     per = rs.per;
     if (u >= u1) return;
-    b = rs.b;
-    load(a);
-    const long long hu = head_units(a, g, n, len), rest = u - rs.begin;
-    h = static_cast<int>(rest / hu);
-    tu = rs.begin + h * hu;
+    b = rs.b, row0 = rs.row0, n = rs.n, len = rs.len;
+    t0 = 0;
+    h = static_cast<int>(div_units(u - rs.begin, rs.head));
+    tu = rs.begin + h * rs.head;
   }
   __device__ bool next(const PagedAttnArgs& a, const PagedGeom& g, Piece& p) {
     if (u >= u1) return false;
@@ -187,8 +209,8 @@ struct PagedWalk {
     }
   }
   // contributors of a cut tile: CTAs [first, last]; CTA c's partial slot
-  __device__ int first_cta(const Piece& p) const { return static_cast<int>(p.tile_u / per); }
-  __device__ int last_cta(const Piece& p) const { return static_cast<int>((p.tile_u + (p.tcb - p.tca) - 1) / per); }
+  __device__ int first_cta(const Piece& p) const { return static_cast<int>(div_units(p.tile_u, per)); }
+  __device__ int last_cta(const Piece& p) const { return static_cast<int>(div_units(p.tile_u + (p.tcb - p.tca) - 1, per)); }
   __device__ int slot(const Piece& p, int c) const { return 2 * c + (c * per < p.tile_u ? 1 : 0); }
 };
 
@@ -242,15 +264,15 @@ __device__ __forceinline__ const T* pool_row(const PagedAttnArgs& a, const void*
   return static_cast<const T*>(pool) + page * a.s_page + h * a.s_head + (pos & ((1 << a.page_shift) - 1)) * a.s_pos;
 }
 
-// One row from the definition, by a warp: a key that the row does not see is not
-// touched.  Called where a row's tile gave something other than a finite number,
+// One row (token tok of a request, query head `head` of key/value head h) from the
+// definition, by a warp: a key that the row does not see is not touched.  Called where a row's tile gave something other than a finite number,
 // which a value of a key that only other rows see can cause (0 * inf).
 template <class T, int HD>
-__device__ __noinline__ void exact_row(const PagedAttnArgs& a, const Piece& p, int tok, int head) {
+__device__ __noinline__ void exact_row(const PagedAttnArgs& a, int b, int h, int n, int len, int row0, int tok, int head) {
   const int lane = threadIdx.x & 31;
   constexpr int E = HD / 32;
-  const RowKeys r = row_keys(a, p.n, p.len, p.row0, tok);
-  const size_t row = static_cast<size_t>(p.row0 + tok);
+  const RowKeys r = row_keys(a, n, len, row0, tok);
+  const size_t row = static_cast<size_t>(row0 + tok);
   const T* q = static_cast<const T*>(a.q) + row * a.q_row + head * a.q_head;
   float qv[E], o[E];
 #pragma unroll
@@ -259,8 +281,8 @@ __device__ __noinline__ void exact_row(const PagedAttnArgs& a, const Piece& p, i
   for (int kb = r.lo & ~31; kb < r.hi; kb += 32) {
     for (uint32_t bits = key_bits(r, kb); bits; bits &= bits - 1) {
       const int k = kb + __ffs(bits) - 1;
-      const T* kp = pool_row<T>(a, a.k, p.b, p.h, k);
-      const T* vp = pool_row<T>(a, a.v, p.b, p.h, k);
+      const T* kp = pool_row<T>(a, a.k, b, h, k);
+      const T* vp = pool_row<T>(a, a.v, b, h, k);
       float s = 0.f;
       if (kp != nullptr) {
 #pragma unroll
