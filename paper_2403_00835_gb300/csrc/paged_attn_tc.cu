@@ -30,11 +30,7 @@ namespace cllm {
 
 namespace {
 
-// Warps 0-3, 4-7: the slots' rows; 8 MMAs; 9 loads (10, 11 idle).  Of the launch's
-// 384 x 168 registers the last warpgroup keeps 88 a thread, the rows' warps take 208.
-constexpr int kTcThreads = 384;
-constexpr int kTcRegsLow = 88, kTcRegsRow = 208;
-static_assert(128 * kTcRegsLow + 256 * kTcRegsRow <= kTcThreads * 168, "register split");
+constexpr int kTcThreads = 320;  // warps 0-3, 4-7: the slots' rows; 8 MMAs; 9 loads
 constexpr int kTcRows = 128, kTcChunk = 128;
 // A row's running maximum follows only growth of more than this (in log2): P may
 // then reach 2^8, and O in tensor memory is rarely rescaled.
@@ -84,8 +80,7 @@ struct TcMaps {
 
 // mbar_wait, but time in which a warp redoes rows (busy) does not count, and once
 // a wait has run out the others end at once.
-__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile int* abort, volatile int* busy) {
-  if (mbar_try_wait(bar, parity)) return true;
+__device__ __noinline__ bool tc_wait_on(uint64_t* bar, uint32_t parity, volatile int* abort, volatile int* busy) {
   if (*abort) return false;
   uint64_t t0 = globaltimer_ns();
   uint32_t it = 0;
@@ -100,6 +95,9 @@ __device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile
     }
   }
   return true;
+}
+__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile int* abort, volatile int* busy) {
+  return mbar_try_wait(bar, parity) || tc_wait_on(bar, parity, abort, busy);
 }
 
 // A row warp's wait for its next piece.  The loading warp always brings one (an end,
@@ -409,26 +407,44 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
           fence_proxy_async_smem();
         }
         if (band) {
-          float x0[64], x1[64];
-          tmem_ld64(mine, x0);
-          tmem_ld64(mine + 64, x1);
+          // (32 columns at a time, their load under way while the 32 before are worked
+          // on; the loops are kept small: a call of a few microseconds runs its code cold)
+          uint32_t x[2][32];
           if (__any_sync(0xffffffffu, rk.lo > kb || kb + kTcChunk > all_to)) {
+            // some row does not see every key: what it does not see becomes -inf
             rk = row_keys(a, p.n, p.len, p.row0, tok);
-            const uint32_t b0 = key_bits(rk, kb), b1 = key_bits(rk, kb + 32), b2 = key_bits(rk, kb + 64), b3 = key_bits(rk, kb + 96);
+#pragma unroll 1
+            for (int c = 0; c < kTcChunk; c += 32) {
+              tmem_ld32_start(mine + c, x[0]);
+              const uint32_t see = key_bits(rk, kb + c);
+              tmem_wait32(x[0]);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              if (!(b0 >> j & 1)) x0[j] = -INFINITY;
-              if (!(b1 >> j & 1)) x0[32 + j] = -INFINITY;
-              if (!(b2 >> j & 1)) x1[j] = -INFINITY;
-              if (!(b3 >> j & 1)) x1[32 + j] = -INFINITY;
+              for (int j = 0; j < 32; ++j)
+                if (!(see >> j & 1)) x[0][j] = 0xff800000u;
+              tmem_st32(mine + c, x[0]);
             }
+            tmem_st_wait();
           }
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float m2[2] = {-INFINITY, -INFINITY};
+          tmem_ld32_start(mine, x[0]);
+#pragma unroll 1
+          for (int c = 0; c < kTcChunk; c += 64) {
+            tmem_wait32(x[0]);
+            tmem_ld32_start(mine + c + 32, x[1]);
 #pragma unroll
-          for (int j = 0; j < 64; j += 4)
+            for (int j = 0; j < 32; j += 4)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) m4[u] = fmaxf(m4[u], fmaxf(x0[j + u], x1[j + u]));
-          const float cm = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2;
+              for (int u = 0; u < 2; ++u)
+                m2[u] = fmaxf(m2[u], fmaxf(__uint_as_float(x[0][j + 2 * u]), __uint_as_float(x[0][j + 2 * u + 1])));
+            tmem_wait32(x[1]);
+            tmem_ld32_start(mine + (c + 64 & 127), x[0]);  // (at the end: the first columns again, for the next loop)
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+#pragma unroll
+              for (int u = 0; u < 2; ++u)
+                m2[u] = fmaxf(m2[u], fmaxf(__uint_as_float(x[1][j + 2 * u]), __uint_as_float(x[1][j + 2 * u + 1])));
+          }
+          const float cm = fmaxf(m2[0], m2[1]) * a.scale_log2;
           if (i == first) {
             m = cm;
           } else {
@@ -439,37 +455,40 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
               l *= f;
               m = nm;
 #pragma unroll 1
-              for (int d = 0; d < HD; d += 64) {
-                float o[64];
-                tmem_ld64(mine + 128 + d, o);
-                uint32_t u[32];
+              for (int d = 0; d < HD; d += 32) {
+                tmem_ld32_start(mine + 128 + d, x[1]);
+                tmem_wait32(x[1]);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) u[j] = __float_as_uint(o[j] * f);
-                tmem_st32(mine + 128 + d, u);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) u[j] = __float_as_uint(o[32 + j] * f);
-                tmem_st32(mine + 128 + d + 32, u);
+                for (int j = 0; j < 32; ++j) x[1][j] = __float_as_uint(__uint_as_float(x[1][j]) * f);
+                tmem_st32(mine + 128 + d, x[1]);
               }
             }
           }
           const float nm = m == -INFINITY ? 0.f : -m;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          uint32_t pk[32];
+          const float2 base = make_float2(nm, nm), scale = make_float2(a.scale_log2, a.scale_log2);
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          auto probabilities = [&](uint32_t (&v)[32], int c) {  // columns c .. c + 31 into columns c / 2 ..
+            uint32_t pk[16];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float p0 = ex2_ftz(fmaf(x0[2 * j], a.scale_log2, nm)), p1 = ex2_ftz(fmaf(x0[2 * j + 1], a.scale_log2, nm));
-            sum[j & 3] += p0 + p1;
-            pk[j] = TcType<T>::pack(p0, p1);
+            for (int j = 0; j < 16; ++j) {
+              float2 e = fma2(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale, base);
+              e.x = ex2_ftz(e.x);
+              e.y = ex2_ftz(e.y);
+              sum[j & 1] = add2(sum[j & 1], e);
+              pk[j] = TcType<T>::pack(e.x, e.y);
+            }
+            tmem_st16(mine + c / 2, pk);
+          };
+#pragma unroll 1
+          for (int c = 0; c < kTcChunk; c += 64) {
+            tmem_wait32(x[0]);
+            tmem_ld32_start(mine + c + 32, x[1]);
+            probabilities(x[0], c);
+            tmem_wait32(x[1]);
+            if (c == 0) tmem_ld32_start(mine + 64, x[0]);
+            probabilities(x[1], c + 32);
           }
-          tmem_st32(mine, pk);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float p0 = ex2_ftz(fmaf(x1[2 * j], a.scale_log2, nm)), p1 = ex2_ftz(fmaf(x1[2 * j + 1], a.scale_log2, nm));
-            sum[j & 3] += p0 + p1;
-            pk[j] = TcType<T>::pack(p0, p1);
-          }
-          tmem_st32(mine + 32, pk);
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
           tmem_st_wait();
         }
         tc_fence_before();
@@ -478,18 +497,12 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       }
     }
     const bool whole = p.whole;
-    const size_t slot_row = static_cast<size_t>(p.slot) * kPagedPartRows;
+    // a part: [HD / 4][rows][4], so that the rows' threads write and read side by side
+    const int part_rows = two ? kPagedPartRows : (rows + 31) & ~31;
+    float4* part = reinterpret_cast<float4*>(a.part_o) + static_cast<size_t>(p.slot) * (kPagedPartRows * HD / 4);
+    float2* part_ml = a.part_ml + static_cast<size_t>(p.slot) * kPagedPartRows;
     const int head = p.h * a.group + row % a.group;
-    // 16 columns of a row from column d: a result, or a partial one
-    auto store16 = [&](const float (&o)[16], int rr, int d, float scale, bool live) {
-      if (!live) return false;
-      if (!whole) {
-        float4* po = reinterpret_cast<float4*>(a.part_o + (slot_row + rr) * HD + d);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) po[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-        return false;
-      }
-      T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + tok) * a.out_row + head * a.out_head + d;
+    auto write16 = [](T* out, const float (&o)[16], float scale) {  // 16 columns of a result; whether one is not finite
       bool bad = false;
 #pragma unroll
       for (int j = 0; j < 16; j += 8) {
@@ -503,6 +516,16 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
         *reinterpret_cast<uint4*>(out + j) = make_uint4(u[0], u[1], u[2], u[3]);
       }
       return bad;
+    };
+    // 16 columns of a row from column d: a result, or a part of one
+    auto store16 = [&](const float (&o)[16], int rr, int d, float scale, bool live) {
+      if (!live) return false;
+      if (!whole) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part[(d / 4 + j) * part_rows + rr] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+        return false;
+      }
+      return write16(static_cast<T*>(a.out) + static_cast<long long>(p.row0 + tok) * a.out_row + head * a.out_head + d, o, scale);
     };
     auto store_lse = [&](int row_tok, int hh, float mm, float ll) {
       if (a.lse != nullptr)
@@ -534,7 +557,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       }
       if (live) {
         if (whole) store_lse(tok, head, m, l);
-        else a.part_ml[slot_row + t * kTcRows + row] = make_float2(m, l);
+        else part_ml[t * kTcRows + row] = make_float2(m, l);
       }
       if (whole)
         for (unsigned redo_rows = __ballot_sync(0xffffffffu, bad); redo_rows; redo_rows &= redo_rows - 1)
@@ -570,7 +593,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       }
       if (live && t == 0) {
         if (whole) store_lse(tok, head, mm, ll);
-        else a.part_ml[slot_row + row] = make_float2(mm, ll);
+        else part_ml[row] = make_float2(mm, ll);
       }
       if (bad) atomicOr(&s.bad[row >> 5], 1u << (row & 31));
       shared_rows = whole;
@@ -594,60 +617,50 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       all_rows();
       if (s.last) {
         // Merge the parts of the tile, in order.  First the rows' maxima and sums, a
-        // thread per row; then 4 columns of a row per thread, several loads in
-        // flight (one SM takes the parts in at 64 bytes a cycle at best).
+        // thread per row; then 16 columns of a row per thread, with the loads of
+        // several parts in flight (an SM takes them in at 64 bytes a cycle at best).
         const int live = p.nt * a.group;
+        auto row_of = [&](int k) { return two && k >= tt * a.group ? kTcRows + k - tt * a.group : k; };
         if (tid < live) {
-          const int kt = tid / a.group, rr = two && kt >= tt ? kTcRows + tid - tt * a.group : tid;
+          const int rr = row_of(tid);
           float mm = -INFINITY, ll = 0.f;
-#pragma unroll 8
+#pragma unroll 4
           for (int c = cta0; c <= cta1; ++c) mm = fmaxf(mm, __ldcg(a.part_ml + static_cast<size_t>(p.part(c)) * kPagedPartRows + rr).x);
-#pragma unroll 8
+#pragma unroll 4
           for (int c = cta0; c <= cta1; ++c) {
             const float2 ml = __ldcg(a.part_ml + static_cast<size_t>(p.part(c)) * kPagedPartRows + rr);
             ll += ml.x != -INFINITY ? ml.y * ex2_ftz(ml.x - mm) : 0.f;
           }
           (&s.ml[0][0])[tid] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
-          store_lse(p.t0 + kt, p.h * a.group + tid % a.group, mm, ll);
+          store_lse(p.t0 + tid / a.group, p.h * a.group + tid % a.group, mm, ll);
         }
         all_rows();
-        constexpr int kItems = 4;  // rows of a thread at a time, 256 / (HD / 4) apart
-        constexpr int kStep = 256 / (HD / 4);
-        const int d = tid % (HD / 4) * 4;
-        for (int k0 = tid / (HD / 4); k0 < live; k0 += kItems * kStep) {
-          float4 x[kItems];
-          float2 mi[kItems];
-          int rr[kItems];
+#pragma unroll 1
+        for (int i = tid; i < live * (HD / 16); i += 256) {
+          const int k = i % live, d = i / live * 16, rr = row_of(k);
+          const float2 mi = (&s.ml[0][0])[k];
+          float o[16];
 #pragma unroll
-          for (int e = 0; e < kItems; ++e) {
-            const int k = min(k0 + e * kStep, live - 1);
-            rr[e] = two && k >= tt * a.group ? kTcRows + k - tt * a.group : k;
-            mi[e] = (&s.ml[0][0])[k];
-            x[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-          }
-#pragma unroll 2
+          for (int j = 0; j < 16; ++j) o[j] = 0.f;
+#pragma unroll 4
           for (int c = cta0; c <= cta1; ++c) {
-            const size_t at = static_cast<size_t>(p.part(c)) * kPagedPartRows;
+            const float m1 = __ldcg(a.part_ml + static_cast<size_t>(p.part(c)) * kPagedPartRows + rr).x;
+            const float4* from = reinterpret_cast<const float4*>(a.part_o) + static_cast<size_t>(p.part(c)) * (kPagedPartRows * HD / 4) + d / 4 * part_rows + rr;
+            const float u = m1 != -INFINITY ? ex2_ftz(m1 - mi.x) : 0.f;
 #pragma unroll
-            for (int e = 0; e < kItems; ++e) {
-              const float m1 = __ldcg(a.part_ml + at + rr[e]).x;
-              const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part_o + (at + rr[e]) * HD + d));
-              const float u = ex2_ftz(m1 - mi[e].x);
-              if (m1 != -INFINITY) x[e].x = fmaf(y.x, u, x[e].x), x[e].y = fmaf(y.y, u, x[e].y), x[e].z = fmaf(y.z, u, x[e].z), x[e].w = fmaf(y.w, u, x[e].w);
+            for (int j = 0; j < 4; ++j) {
+              const float4 y = __ldcg(from + j * part_rows);
+              if (u != 0.f) {
+                o[4 * j] = fmaf(y.x, u, o[4 * j]);
+                o[4 * j + 1] = fmaf(y.y, u, o[4 * j + 1]);
+                o[4 * j + 2] = fmaf(y.z, u, o[4 * j + 2]);
+                o[4 * j + 3] = fmaf(y.w, u, o[4 * j + 3]);
+              }
             }
           }
-#pragma unroll
-          for (int e = 0; e < kItems; ++e) {
-            const int k = k0 + e * kStep;
-            if (k >= live) break;
-            const float f = mi[e].y;
-            float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (f != 0.f) z = make_float4(x[e].x * f, x[e].y * f, x[e].z * f, x[e].w * f);
-            if (!isfinite(z.x) || !isfinite(z.y) || !isfinite(z.z) || !isfinite(z.w)) atomicOr(&s.bad[rr[e] >> 5], 1u << (rr[e] & 31));
-            *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + k / a.group) * a.out_row +
-                                      (p.h * a.group + k % a.group) * a.out_head + d) =
-                make_uint2(TcType<T>::pack(z.x, z.y), TcType<T>::pack(z.z, z.w));
-          }
+          T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + k / a.group) * a.out_row +
+                   static_cast<long long>(p.h * a.group + k % a.group) * a.out_head + d;
+          if (write16(out, o, mi.y)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
         }
         shared_rows = true;
       }
@@ -712,14 +725,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s.tmem;
-  if (warp >= 8) {
-    setmaxnreg_dec<kTcRegsLow>();
-    if (warp == 8) issue_mmas<T, HD>(s, tmem, hold);
-    else if (warp == 9) issue_loads<HD>(s, a, g, m);
-  } else {
-    setmaxnreg_inc<kTcRegsRow>();
-    run_rows<T, HD>(s, a, g, tmem);
-  }
+  if (warp == 8) issue_mmas<T, HD>(s, tmem, hold);
+  else if (warp == 9) issue_loads<HD>(s, a, g, m);
+  else run_rows<T, HD>(s, a, g, tmem);
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && s.abort) atomicOr(a.err, DERR_TIMEOUT);

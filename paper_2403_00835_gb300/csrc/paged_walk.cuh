@@ -102,9 +102,11 @@ __device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeo
   const int tid = threadIdx.x, nthr = blockDim.x, lane = tid & 31, warp = tid >> 5;
   long long total = 0, head = 0, units = 0, before = 0;
   Request r{0, 0, 0};
-  // a thread per request and round: this round's units before the thread's request
-  auto round = [&](int b0) {
-    r = b0 + tid < a.batch ? request(a, b0 + tid) : Request{0, 0, 0};
+  // a thread per request and round: this round's units, those before the thread's request
+  // (up to 32 requests: every warp works it out for itself)
+  const bool few = a.batch <= 32;
+  auto round = [&](int b) {
+    r = b < a.batch ? request(a, b) : Request{0, 0, 0};
     head = head_units(a, g, r.n, r.len);
     units = head * a.Hkv;
     long long v = units;
@@ -113,18 +115,21 @@ __device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeo
       const long long o = __shfl_up_sync(0xffffffffu, v, d);
       if (lane >= d) v += o;
     }
-    if (b0 > 0) __syncthreads();
+    before = v - units;
+    if (few) return __shfl_sync(0xffffffffu, v, 31);
+    __syncthreads();
     if (lane == 31) sm[warp] = v;
     __syncthreads();
     long long sum = 0;
-    before = v - units;
     for (int w = 0; w < nthr / 32; ++w) {
       if (w < warp) before += sm[w];
       sum += sm[w];
     }
     return sum;
   };
-  for (int b0 = 0; b0 < a.batch; b0 += nthr) total += round(b0);
+  if (few) total = round(lane);
+  else
+    for (int b0 = 0; b0 < a.batch; b0 += nthr) total += round(b0 + tid);
   long long per = div_units(total + gridDim.x - 1, gridDim.x);
   if (per < g.min_units) per = g.min_units;
   const long long u0 = blockIdx.x * per;
@@ -135,8 +140,8 @@ __device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeo
   }
   long long base = 0;
   for (int b0 = 0; b0 < a.batch; b0 += nthr) {
-    const long long sum = a.batch <= nthr ? total : round(b0);
-    if (u0 >= base + before && u0 < base + before + units) {  // one thread at most
+    const long long sum = a.batch <= nthr ? total : round(b0 + tid);
+    if ((tid < 32 || !few) && u0 >= base + before && u0 < base + before + units) {  // one thread at most
       rs->b = b0 + tid;
       rs->begin = base + before;
       rs->head = head;
