@@ -10,7 +10,7 @@
 // hold a row of S per thread, so maximum and sum need no exchange, and write P over S.
 //
 // The two slots (S/P and O in 256 tensor-memory columns each) hide each other's
-// latency.  A tile of more than 128 rows has 128 rows in each, which share K and V; a tile
+// latency; P V starts on the first 64 keys of a chunk while the rows work on the others.  A tile of more than 128 rows has 128 rows in each, which share K and V; a tile
 // of up to 128 rows (a block of a few tokens, greedy decoding) has all its rows in
 // both, slot t taking every other chunk of keys, and the halves are merged at the end.
 // Rows are tokens times the query heads of a key/value head, so grouped heads
@@ -31,7 +31,7 @@ namespace cllm {
 namespace {
 
 constexpr int kTcThreads = 320;  // warps 0-3, 4-7: the slots' rows; 8 MMAs; 9 loads
-constexpr int kTcRows = 128, kTcChunk = 128;
+constexpr int kTcRows = 128, kTcChunk = 128, kTcHalf = 64;
 // A row's running maximum follows only growth of more than this (in log2): P may
 // then reach 2^8, and O in tensor memory is rarely rescaled.
 constexpr float kTcSlack = 8.f;
@@ -42,7 +42,6 @@ struct SlotChunks {
   int first, end, step;
   __device__ bool any() const { return first < end; }
   __device__ bool has(int i) const { return i >= first && i < end && (step == 1 || ((i - first) & 1) == 0); }
-  __device__ int last() const { return step == 1 ? end - 1 : first + ((end - 1 - first) & ~1); }
 };
 
 // A piece as the loading warp hands it to the others.
@@ -52,7 +51,7 @@ struct TcPiece {
   int two, whole;                          // 128 rows in each slot; the whole tile
   int slot, cta0, cta1, first_slot;        // of a cut tile: this part's slot, the CTAs of its parts, the first's slot
   SlotChunks c[2];
-  int end;                                 // no piece: the run is over
+  int final, end;                          // the run's last piece; no piece: the run is over
   __device__ int part(int cta) const { return cta == cta0 ? first_slot : 2 * cta; }
 };
 constexpr int kTcPieces = 4;
@@ -64,9 +63,10 @@ struct TcSmem {
   alignas(1024) uint8_t q[2][kTcRows * HD * 2];
   alignas(1024) uint8_t ring[kRing][kTile];
   float2 ml[2][kTcRows];  // also the scratch of run_start
-  uint64_t full[kRing], empty[kRing], qfull, qempty, sfull[2], pready[2], ofull[2], ofree, drain;
+  uint64_t full[kRing], empty[kRing], qfull, qempty, ofree, drain;
+  uint64_t sfull[2], pready[2][2], ofull[2];  // of a slot: S is there; P of a half of the keys is; the piece's O is
   uint64_t pfull[kTcPieces], pempty[kTcPieces], pfree[kTcPieces];  // a piece is there; the rows, the issuer are done with it
-  TcPiece piece[kTcPieces];
+  TcPiece piece[kTcPieces], cut;  // (cut: one to be merged after the run)
   RunStart run;
   unsigned bad[8];  // rows whose result is not finite
   uint32_t tmem;
@@ -164,7 +164,7 @@ __device__ __forceinline__ void issue_loads(TcSmem<HD>& s, const PagedAttnArgs& 
       if (more) {
         o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0, o.lo = p.lo, o.hi = p.hi;
         o.ca = p.ca, o.chunks = p.cb - p.ca;
-        o.two = p.nt > tt, o.whole = p.whole();
+        o.two = p.nt > tt, o.whole = p.whole(), o.final = w.done();
         if (!p.whole()) {
           o.slot = w.slot(p, blockIdx.x);
           o.cta0 = w.first_cta(p), o.cta1 = w.last_cta(p);
@@ -236,12 +236,15 @@ __device__ __forceinline__ void issue_loads(TcSmem<HD>& s, const PagedAttnArgs& 
   }
 }
 
-// The MMAs of the CTA, all by one thread, whose instructions are what its chunks cost
-// beside the tensor cores' own time: descriptors are made once and moved by an add.
-// (Made anew for every MMA they held the thread up for 8800 cycles per chunk of 256
-// rows, against 2048 of tensor-core time.)
+// The MMAs of the CTA, by one warp, whose instructions are what its chunks cost beside
+// the tensor cores' own time (it shares its scheduler with two row warps): descriptors
+// are made once and moved by an add, and what decides about them is known to be the
+// same in all lanes.  (Made anew for every MMA they held the warp up for 8800 cycles per
+// chunk of 256 rows, against 2048 of tensor-core time.)
 template <class T, int HD>
 __device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, uint32_t tmem, int hold) {
+  const int lane = threadIdx.x & 31;
+  tmem = __reduce_max_sync(0xffffffffu, tmem);
   constexpr int NR = TcSmem<HD>::kRing;
   constexpr uint32_t id_s = TcType<T>::idesc(kTcChunk, false), id_o = TcType<T>::idesc(HD, true);
   // low words of the descriptors of the first tile (the address field, in 16 bytes, never carries out of them)
@@ -252,22 +255,25 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, uint32_t tmem, int hol
   auto desc = [](uint32_t lo, uint32_t hi) { return static_cast<uint64_t>(hi) << 32 | lo; };
   RingAt<NR> at;
   RingAt<kTcPieces> pat;
-  uint32_t pieces = 0, np0 = 0, np1 = 0;  // pieces so far, P tiles taken of each slot
+  uint32_t pieces = 0, nc0 = 0, nc1 = 0;  // pieces so far, chunks of each slot
   bool ok = true;
-  if ((threadIdx.x & 31) == 0) {
+  {
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      ok = ok && tc_wait(bar, parity, &s.abort, &s.busy);
+      ok = ok && (__all_sync(0xffffffffu, mbar_try_wait(bar, parity)) ||
+                  __all_sync(0xffffffffu, tc_wait_on(bar, parity, &s.abort, &s.busy)));
       tc_fence_after();
     };
+    auto same = [](int x) { return static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(x))); };
     for (;; ++pat) {
       wait(&s.pfull[pat.i], pat.phase);
       if (!ok) break;
       const TcPiece& p = s.piece[pat.i];
-      if (p.end) break;
-      const int n = p.chunks;
-      const bool two = p.two;
-      const SlotChunks c0 = p.c[0], c1 = p.c[1];
-      mbar_arrive(&s.pfree[pat.i]);
+      if (same(p.end)) break;
+      const int n = same(p.chunks);
+      const bool two = same(p.two);
+      const SlotChunks c0{same(p.c[0].first), same(p.c[0].end), two ? 1 : 2}, c1{same(p.c[1].first), same(p.c[1].end), two ? 1 : 2};
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s.pfree[pat.i]);
       if (n == 0) continue;
       auto next_tile = [&] {  // the next tile of the ring, landed
         const uint32_t slot = at.i;
@@ -276,7 +282,7 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, uint32_t tmem, int hol
         return slot;
       };
       auto release = [&](uint32_t slot) {
-        if (ok) tc_commit(&s.empty[slot]);
+        if (ok) tc_commit_warp(&s.empty[slot]);
       };
       auto mma_s = [&](int t, uint32_t slot) {  // S of slot t over the keys of a tile
         if (!ok) return;
@@ -284,22 +290,24 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, uint32_t tmem, int hol
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) {
           const uint32_t off = ((kk >> 2) * kTcRows * 128 + (kk & 3) * 32) >> 4;
-          tc_mma_f16(tmem + t * 256, desc(qa + off, q_hi), desc(ka + off, k_hi), id_s, kk > 0);
+          tc_mma_f16_warp(tmem + t * 256, desc(qa + off, q_hi), desc(ka + off, k_hi), id_s, kk > 0);
         }
-        tc_commit(&s.sfull[t]);
+        tc_commit_warp(&s.sfull[t]);
       };
       auto mma_o = [&](int t, uint32_t slot, int i, const SlotChunks& c) {  // O of slot t += P V of chunk i
         if (hold > 0 && i + 1 >= hold) ok = false;  // test hook: as if this thread's wait had run out
-        uint32_t& np = t ? np1 : np0;
-        wait(&s.pready[t], np & 1);
-        ++np;
-        if (!ok) return;
+        const uint32_t phase = (t ? nc1++ : nc0++) & 1;
         const uint32_t va = v_lo + slot * (TcSmem<HD>::kTile >> 4), first = i > c.first;
 #pragma unroll
-        for (int kk = 0; kk < kTcChunk / 16; ++kk)
-          tc_mma_f16_ts(tmem + t * 256 + 128, tmem + t * 256 + kk * 8, desc(va + (kk * 16 * 128 >> 4), v_hi), id_o,
-                        kk > 0 ? 1u : first);
-        if (i == c.last()) tc_commit(&s.ofull[t]);
+        for (int b = 0; b < 2; ++b) {
+          wait(&s.pready[t][b], phase);
+          if (!ok) return;
+#pragma unroll
+          for (int kk = b * kTcHalf / 16; kk < (b + 1) * kTcHalf / 16; ++kk)
+            tc_mma_f16_ts_warp(tmem + t * 256 + 128, tmem + t * 256 + kk * 8, desc(va + (kk * 16 * 128 >> 4), v_hi), id_o,
+                               kk > 0 ? 1u : first);
+        }
+        if (i + c.step >= c.end) tc_commit_warp(&s.ofull[t]);
       };
       wait(&s.qfull, pieces & 1);
       const uint32_t k0 = next_tile();
@@ -307,7 +315,7 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, uint32_t tmem, int hol
         if (c0.has(0)) mma_s(0, k0);
         if (c1.has(0)) mma_s(1, k0);
         release(k0);
-        if (n == 1 && ok) tc_commit(&s.qempty);
+        if (n == 1 && ok) tc_commit_warp(&s.qempty);
         for (int i = 0; ok && i < n; ++i) {
           const bool more = i + 1 < n;
           const uint32_t k = more ? next_tile() : 0, v = next_tile();
@@ -318,28 +326,27 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, uint32_t tmem, int hol
           if (more && c1.has(i + 1)) mma_s(1, k);
           release(v);
           if (more) release(k);
-          if (i + 2 == n && ok) tc_commit(&s.qempty);
+          if (i + 2 == n && ok) tc_commit_warp(&s.qempty);
         }
       } else {
         mma_s(0, k0);
         release(k0);
-        uint32_t k = 0;
         if (n > 1) {
-          k = next_tile();
+          const uint32_t k = next_tile();
           mma_s(1, k);
           release(k);
         }
-        if (n <= 2 && ok) tc_commit(&s.qempty);
+        if (n <= 2 && ok) tc_commit_warp(&s.qempty);
         auto step = [&](int t, int i, const SlotChunks& c) {
           const uint32_t v = next_tile();
           if (i == 0 && pieces > 0) wait(&s.ofree, (pieces - 1) & 1);
           mma_o(t, v, i, c);
           release(v);
           if (i + 2 < n) {
-            k = next_tile();
+            const uint32_t k = next_tile();
             mma_s(t, k);
             release(k);
-            if (i + 3 == n && ok) tc_commit(&s.qempty);
+            if (i + 3 == n && ok) tc_commit_warp(&s.qempty);
           }
         };
         for (int i = 0; ok && i < n; i += 2) {
@@ -352,7 +359,7 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, uint32_t tmem, int hol
     }
     if (!ok) {
       *const_cast<volatile int*>(&s.abort) = 1;
-      tc_commit(&s.drain);  // MMAs in flight end before the CTA leaves
+      tc_commit_warp(&s.drain);  // MMAs in flight end before the CTA leaves
       mbar_wait(&s.drain, 0, nullptr);
     }
   }
@@ -374,7 +381,119 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
     tc_fence_after();
   };
   auto all_rows = [&] { named_bar_sync(1, 256); };
-  uint32_t r = 0, ns = 0, no[2] = {0, 0};  // loads of the pieces before, S tiles of this slot, outputs of both
+  // -- of a tile, when its keys are done ------------------------------------------------
+  auto write16 = [](T* out, const float (&o)[16], float scale) {  // 16 columns of a result; whether one is not finite
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < 16; j += 8) {
+      uint32_t u[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = scale != 0.f ? o[j + 2 * e] * scale : 0.f, y = scale != 0.f ? o[j + 2 * e + 1] * scale : 0.f;
+        bad |= !isfinite(x) || !isfinite(y);
+        u[e] = TcType<T>::pack(x, y);
+      }
+      *reinterpret_cast<uint4*>(out + j) = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    return bad;
+  };
+  auto store_lse = [&](const TcPiece& p, int tok, int head, float m, float l) {
+    if (a.lse != nullptr)
+      a.lse[static_cast<size_t>(p.row0 + tok) * a.H + head] = l != 0.f ? (m + log2f(l)) * 0.69314718055994530942f : -INFINITY;
+  };
+  auto redo = [&](const TcPiece& p, int rr) {  // row rr of a tile from the definition (the whole warp)
+    __syncwarp();
+    if (lane == 0) atomicAdd(&s.busy, 1);
+    exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + (p.two ? rr / kTcRows * tt : 0) + (rr % kTcRows) / a.group,
+                     p.h * a.group + (rr % kTcRows) % a.group);
+    if (lane == 0) atomicAdd(&s.busy, -1);
+  };
+  // Rows marked in s.bad (marked by any warp, so after a barrier of the 8; the next mark comes after another).
+  auto redo_bad = [&](const TcPiece& p) {
+    unsigned any = 0;
+    for (int i = 0; i < 8; ++i) any |= s.bad[i];
+    if (!any) return;
+    for (int rr = warp; rr < 2 * kTcRows; rr += 8)
+      if (s.bad[rr >> 5] >> (rr & 31) & 1) redo(p, rr);
+    all_rows();
+    if (tid < 8) s.bad[tid] = 0;
+    all_rows();
+  };
+  // A part is [HD / 4][rows][4], so that the rows' threads write and read side by side.
+  auto rows_of_part = [&](const TcPiece& p) { return p.two ? kPagedPartRows : (p.nt * a.group + 31) & ~31; };
+  // Merge the parts of a tile, in order, if the others were there before this CTA's
+  // (`before`: thread 0 has their number).
+  auto merge_if_last = [&](const TcPiece& p, int before) {
+    const int cta0 = p.cta0, cta1 = p.cta1;
+    if (tid == 0) {
+      s.last = before == cta1 - cta0;
+      if (s.last) a.tickets[cta0] = 0;
+      __threadfence();
+    }
+    all_rows();
+    if (!s.last) return;
+    // First the rows' maxima and sums, a thread per row; then 16 columns of a row per
+    // thread, with the loads of several parts in flight (an SM takes them in at 64
+    // bytes a cycle at best).
+    const int live = p.nt * a.group, part_rows = rows_of_part(p);
+    const bool two = p.two;
+    auto row_of = [&](int k) { return two && k >= tt * a.group ? kTcRows + k - tt * a.group : k; };
+    if (tid < live) {
+      const float2* from = a.part_ml + row_of(tid);
+      float mm = -INFINITY, ll = 0.f;
+#pragma unroll 1
+      for (int c = cta0; c <= cta1; c += 8) {
+        float2 ml[8];
+        float nm = mm;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          ml[u] = c + u <= cta1 ? __ldcg(from + static_cast<size_t>(p.part(c + u)) * kPagedPartRows) : make_float2(-INFINITY, 0.f);
+          nm = fmaxf(nm, ml[u].x);
+        }
+        ll = mm != -INFINITY ? ll * ex2_ftz(mm - nm) : 0.f;
+        mm = nm;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) ll += ml[u].x != -INFINITY ? ml[u].y * ex2_ftz(ml[u].x - mm) : 0.f;
+      }
+      (&s.ml[0][0])[tid] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
+      store_lse(p, p.t0 + tid / a.group, p.h * a.group + tid % a.group, mm, ll);
+    }
+    all_rows();
+#pragma unroll 1
+    for (int i = tid; i < live * (HD / 16); i += 256) {
+      const int k = i % live, d = i / live * 16, rr = row_of(k);
+      const float2 mi = (&s.ml[0][0])[k];
+      float o[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[j] = 0.f;
+#pragma unroll 4
+      for (int c = cta0; c <= cta1; ++c) {
+        const size_t part = p.part(c);
+        const float m1 = __ldcg(a.part_ml + part * kPagedPartRows + rr).x;
+        const float4* from = reinterpret_cast<const float4*>(a.part_o) + part * (kPagedPartRows * HD / 4) + d / 4 * part_rows + rr;
+        const float u = m1 != -INFINITY ? ex2_ftz(m1 - mi.x) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float4 y = __ldcg(from + j * part_rows);
+          if (u != 0.f) {
+            o[4 * j] = fmaf(y.x, u, o[4 * j]);
+            o[4 * j + 1] = fmaf(y.y, u, o[4 * j + 1]);
+            o[4 * j + 2] = fmaf(y.z, u, o[4 * j + 2]);
+            o[4 * j + 3] = fmaf(y.w, u, o[4 * j + 3]);
+          }
+        }
+      }
+      T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + k / a.group) * a.out_row +
+               static_cast<long long>(p.h * a.group + k % a.group) * a.out_head + d;
+      if (write16(out, o, mi.y)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
+    }
+    all_rows();
+    redo_bad(p);
+  };
+
+  uint32_t r = 0, ns = 0, no[2] = {0, 0};  // loads of the pieces before, chunks of this slot, pieces of both
+  bool cut = false;        // a part is left to be merged
+  int cut_arrivals = 0;    // thread 0: the parts of it that were there before this CTA's
   RingAt<kTcPieces> pat;
   for (;; ++pat) {
     if (!piece_wait(&s.pfull[pat.i], pat.phase)) break;
@@ -406,10 +525,11 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
           }
           fence_proxy_async_smem();
         }
+        // (32 columns at a time, the next ones under way; the loops are kept small: a
+        // call of a few microseconds runs its code cold)
+        uint32_t x[2][32];
+        float2 base, sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         if (band) {
-          // (32 columns at a time, their load under way while the 32 before are worked
-          // on; the loops are kept small: a call of a few microseconds runs its code cold)
-          uint32_t x[2][32];
           if (__any_sync(0xffffffffu, rk.lo > kb || kb + kTcChunk > all_to)) {
             // some row does not see every key: what it does not see becomes -inf
             rk = row_keys(a, p.n, p.len, p.row0, tok);
@@ -450,6 +570,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
           } else {
             const bool grow = cm > m + kTcSlack || (m == -INFINITY && cm > m);
             if (__any_sync(0xffffffffu, grow)) {
+              // (the P V before is done: this S was issued after it)
               const float nm = grow ? cm : m;
               const float f = grow ? ex2_ftz(m - nm) : 1.f;
               l *= f;
@@ -465,58 +586,45 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
             }
           }
           const float nm = m == -INFINITY ? 0.f : -m;
-          const float2 base = make_float2(nm, nm), scale = make_float2(a.scale_log2, a.scale_log2);
-          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          auto probabilities = [&](uint32_t (&v)[32], int c) {  // columns c .. c + 31 into columns c / 2 ..
-            uint32_t pk[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              float2 e = fma2(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale, base);
-              e.x = ex2_ftz(e.x);
-              e.y = ex2_ftz(e.y);
-              sum[j & 1] = add2(sum[j & 1], e);
-              pk[j] = TcType<T>::pack(e.x, e.y);
-            }
-            tmem_st16(mine + c / 2, pk);
-          };
-#pragma unroll 1
-          for (int c = 0; c < kTcChunk; c += 64) {
-            tmem_wait32(x[0]);
-            tmem_ld32_start(mine + c + 32, x[1]);
-            probabilities(x[0], c);
-            tmem_wait32(x[1]);
-            if (c == 0) tmem_ld32_start(mine + 64, x[0]);
-            probabilities(x[1], c + 32);
-          }
-          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-          tmem_st_wait();
+          base = make_float2(nm, nm);
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s.pready[t]);
+        const float2 scale = make_float2(a.scale_log2, a.scale_log2);
+        auto probabilities = [&](uint32_t (&v)[32], int c) {  // columns c .. c + 31 into columns c / 2 ..
+          uint32_t pk[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            float2 e = fma2(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale, base);
+            e.x = ex2_ftz(e.x);
+            e.y = ex2_ftz(e.y);
+            sum[j & 1] = add2(sum[j & 1], e);
+            pk[j] = TcType<T>::pack(e.x, e.y);
+          }
+          tmem_st16(mine + c / 2, pk);
+        };
+#pragma unroll 1
+        for (int b = 0; b < 2; ++b) {
+          if (band) {
+            tmem_wait32(x[0]);
+            tmem_ld32_start(mine + b * kTcHalf + 32, x[1]);
+            probabilities(x[0], b * kTcHalf);
+            tmem_wait32(x[1]);
+            if (b == 0) tmem_ld32_start(mine + kTcHalf, x[0]);
+            probabilities(x[1], b * kTcHalf + 32);
+            tmem_st_wait();
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s.pready[t][b]);
+        }
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
     }
     const bool whole = p.whole;
     // a part: [HD / 4][rows][4], so that the rows' threads write and read side by side
-    const int part_rows = two ? kPagedPartRows : (rows + 31) & ~31;
+    const int part_rows = rows_of_part(p);
     float4* part = reinterpret_cast<float4*>(a.part_o) + static_cast<size_t>(p.slot) * (kPagedPartRows * HD / 4);
     float2* part_ml = a.part_ml + static_cast<size_t>(p.slot) * kPagedPartRows;
     const int head = p.h * a.group + row % a.group;
-    auto write16 = [](T* out, const float (&o)[16], float scale) {  // 16 columns of a result; whether one is not finite
-      bool bad = false;
-#pragma unroll
-      for (int j = 0; j < 16; j += 8) {
-        uint32_t u[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = scale != 0.f ? o[j + 2 * e] * scale : 0.f, y = scale != 0.f ? o[j + 2 * e + 1] * scale : 0.f;
-          bad |= !isfinite(x) || !isfinite(y);
-          u[e] = TcType<T>::pack(x, y);
-        }
-        *reinterpret_cast<uint4*>(out + j) = make_uint4(u[0], u[1], u[2], u[3]);
-      }
-      return bad;
-    };
     // 16 columns of a row from column d: a result, or a part of one
     auto store16 = [&](const float (&o)[16], int rr, int d, float scale, bool live) {
       if (!live) return false;
@@ -527,17 +635,6 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       }
       return write16(static_cast<T*>(a.out) + static_cast<long long>(p.row0 + tok) * a.out_row + head * a.out_head + d, o, scale);
     };
-    auto store_lse = [&](int row_tok, int hh, float mm, float ll) {
-      if (a.lse != nullptr)
-        a.lse[static_cast<size_t>(p.row0 + row_tok) * a.H + hh] = ll != 0.f ? (mm + log2f(ll)) * 0.69314718055994530942f : -INFINITY;
-    };
-    auto redo = [&](int rr) {  // (the whole warp)
-      __syncwarp();
-      if (lane == 0) atomicAdd(&s.busy, 1);
-      exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + (two ? rr / kTcRows * tt : 0) + (rr % kTcRows) / a.group, p.h * a.group + (rr % kTcRows) % a.group);
-      if (lane == 0) atomicAdd(&s.busy, -1);
-    };
-    bool shared_rows = false;  // rows whose columns several warps have written
     if (two) {
       const bool has = p.c[t].any();
       if (has) warp_wait(&s.ofull[t], no[t] & 1);
@@ -556,12 +653,12 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
         }
       }
       if (live) {
-        if (whole) store_lse(tok, head, m, l);
+        if (whole) store_lse(p, tok, head, m, l);
         else part_ml[t * kTcRows + row] = make_float2(m, l);
       }
       if (whole)
         for (unsigned redo_rows = __ballot_sync(0xffffffffu, bad); redo_rows; redo_rows &= redo_rows - 1)
-          redo(t * kTcRows + (warp & 3) * 32 + __ffs(redo_rows) - 1);
+          redo(p, t * kTcRows + (warp & 3) * 32 + __ffs(redo_rows) - 1);
     } else {
       // both slots hold these rows, each over half of the keys; slot t's warps finish
       // the t-th half of the columns
@@ -592,11 +689,10 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
         }
       }
       if (live && t == 0) {
-        if (whole) store_lse(tok, head, mm, ll);
+        if (whole) store_lse(p, tok, head, mm, ll);
         else part_ml[row] = make_float2(mm, ll);
       }
       if (bad) atomicOr(&s.bad[row >> 5], 1u << (row & 31));
-      shared_rows = whole;
     }
     if (n > 0) {  // the accumulators may be overwritten
       tc_fence_before();
@@ -606,79 +702,31 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       for (int u = 0; u < 2; ++u) no[u] += p.c[u].any();
     }
     if (!whole) {
-      const int cta0 = p.cta0, cta1 = p.cta1;
-      __threadfence();
       all_rows();
+      int before = 0;
       if (tid == 0) {
-        s.last = atomicAdd(a.tickets + cta0, 1) == cta1 - cta0;
-        if (s.last) a.tickets[cta0] = 0;
         __threadfence();
+        before = atomicAdd(a.tickets + p.cta0, 1);
       }
-      all_rows();
-      if (s.last) {
-        // Merge the parts of the tile, in order.  First the rows' maxima and sums, a
-        // thread per row; then 16 columns of a row per thread, with the loads of
-        // several parts in flight (an SM takes them in at 64 bytes a cycle at best).
-        const int live = p.nt * a.group;
-        auto row_of = [&](int k) { return two && k >= tt * a.group ? kTcRows + k - tt * a.group : k; };
-        if (tid < live) {
-          const int rr = row_of(tid);
-          float mm = -INFINITY, ll = 0.f;
-#pragma unroll 4
-          for (int c = cta0; c <= cta1; ++c) mm = fmaxf(mm, __ldcg(a.part_ml + static_cast<size_t>(p.part(c)) * kPagedPartRows + rr).x);
-#pragma unroll 4
-          for (int c = cta0; c <= cta1; ++c) {
-            const float2 ml = __ldcg(a.part_ml + static_cast<size_t>(p.part(c)) * kPagedPartRows + rr);
-            ll += ml.x != -INFINITY ? ml.y * ex2_ftz(ml.x - mm) : 0.f;
-          }
-          (&s.ml[0][0])[tid] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
-          store_lse(p.t0 + tid / a.group, p.h * a.group + tid % a.group, mm, ll);
-        }
-        all_rows();
-#pragma unroll 1
-        for (int i = tid; i < live * (HD / 16); i += 256) {
-          const int k = i % live, d = i / live * 16, rr = row_of(k);
-          const float2 mi = (&s.ml[0][0])[k];
-          float o[16];
-#pragma unroll
-          for (int j = 0; j < 16; ++j) o[j] = 0.f;
-#pragma unroll 4
-          for (int c = cta0; c <= cta1; ++c) {
-            const float m1 = __ldcg(a.part_ml + static_cast<size_t>(p.part(c)) * kPagedPartRows + rr).x;
-            const float4* from = reinterpret_cast<const float4*>(a.part_o) + static_cast<size_t>(p.part(c)) * (kPagedPartRows * HD / 4) + d / 4 * part_rows + rr;
-            const float u = m1 != -INFINITY ? ex2_ftz(m1 - mi.x) : 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float4 y = __ldcg(from + j * part_rows);
-              if (u != 0.f) {
-                o[4 * j] = fmaf(y.x, u, o[4 * j]);
-                o[4 * j + 1] = fmaf(y.y, u, o[4 * j + 1]);
-                o[4 * j + 2] = fmaf(y.z, u, o[4 * j + 2]);
-                o[4 * j + 3] = fmaf(y.w, u, o[4 * j + 3]);
-              }
-            }
-          }
-          T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + k / a.group) * a.out_row +
-                   static_cast<long long>(p.h * a.group + k % a.group) * a.out_head + d;
-          if (write16(out, o, mi.y)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
-        }
-        shared_rows = true;
+      if (p.final) {
+        merge_if_last(p, before);
+      } else {
+        // nothing waits for the counter's answer here: whether this CTA has to merge the
+        // tile is seen to after the run
+        cut = true;
+        cut_arrivals = before;
+        if (tid < sizeof(TcPiece) / 4) reinterpret_cast<int*>(&s.cut)[tid] = reinterpret_cast<const int*>(&p)[tid];
       }
-    }
-    if (!two || !whole) all_rows();  // (rows written by several warps; s.ml is free again)
-    if (shared_rows) {
-      unsigned any = 0;
-      for (int i = 0; i < 8; ++i) any |= s.bad[i];
-      if (any) {
-        for (int rr = warp; rr < 256; rr += 8)
-          if (s.bad[rr >> 5] >> (rr & 31) & 1) redo(rr);
-        all_rows();
-        if (tid < 8) s.bad[tid] = 0;
-        all_rows();
-      }
+    } else if (!two) {
+      all_rows();  // (s.ml is free again)
+      redo_bad(p);
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&s.pempty[pat.i]);
+  }
+  if (cut) {
+    all_rows();
+    merge_if_last(s.cut, cut_arrivals);
   }
 }
 
@@ -702,7 +750,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     mbar_init(&s.qempty, 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(&s.sfull[t], 1);
-      mbar_init(&s.pready[t], 4);
+      mbar_init(&s.pready[t][0], 4);
+      mbar_init(&s.pready[t][1], 4);
       mbar_init(&s.ofull[t], 1);
     }
     for (int i = 0; i < kTcPieces; ++i) {
