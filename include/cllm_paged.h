@@ -122,21 +122,27 @@ void cllm_paged_destroy(cllm_paged *cache);
 int cllm_paged_status(cllm_paged *cache, void *cuda_stream);
 
 /*
- * Write T rows of keys and values into their slots (cllm_page_plan's, or any
+ * Write rows of keys and values into their slots (cllm_page_plan's, or any
  * others; -1 skips a row's K and V, two rows with one slot leave either).
- *   k, v: [T][n_kv_heads][head_dim], q: [T][n_heads][head_dim] with strides
- *   *_stride between rows and heads side by side.
- * rope: fp32 [max_pos][head_dim / 2][2] (cos, sin), or NULL: K as it is, q unused.
- * With it K and, when q is not NULL, q are rotated (pairs i, i + head_dim/2: the
- * engine's convention) by row positions[t] in fp32 and rounded once; q goes to
- * q_out (which may be q).
- * Errors: EINVAL (null or misaligned pointers, strides too small or not multiples of 16
- * bytes, layer outside the pools, T < 0, q without rope), ECUDA.
+ * rope: K as it is when NULL (q unused).  With it K and, when q is not NULL, q are
+ * rotated (pairs i, i + head_dim/2: the engine's convention) by row positions[t] in
+ * fp32 and rounded once; q goes to q_out (which may be q).
  */
-int cllm_paged_append(cllm_paged *cache, int layer, int T, const void *k, int64_t k_stride, const void *v,
-                      int64_t v_stride, const int64_t *slots, const void *q, int64_t q_stride, void *q_out,
-                      int64_t q_out_stride, const float *rope, int max_pos, const int32_t *positions,
-                      void *cuda_stream);
+typedef struct {
+  int layer, rows;
+  const void *k, *v;        /* [rows][n_kv_heads][head_dim], heads side by side */
+  const void *q;            /* [rows][n_heads][head_dim], heads side by side, or NULL */
+  void *q_out;
+  int64_t k_stride, v_stride, q_stride, q_out_stride; /* elements between rows */
+  const int64_t *slots;     /* [rows] */
+  const float *rope;        /* [max_pos][head_dim / 2][2] (cos, sin), or NULL */
+  const int32_t *positions; /* [rows] */
+  int max_pos;
+} cllm_paged_rows;
+
+/* Errors: EINVAL (null or misaligned pointers, strides too small or not multiples of 16
+ * bytes, layer outside the pools, rows < 0, q without rope), ECUDA. */
+int cllm_paged_append(cllm_paged *cache, const cllm_paged_rows *r, void *cuda_stream);
 
 /*
  * Attention of a step.  Request b's rows are row_start[b] .. row_start[b+1]-1 of

@@ -106,8 +106,8 @@ int cllm_test_hold_attention(cllm_ctx *ctx, int chunk);
 int cllm_test_hold_gemm(cllm_ctx *ctx, int chunk);
 
 /*
- * The same for the paged attention of 16-bit pools: the thread that issues a
- * CTA's tensor-core work stops at chunk `chunk` >= 0 of a piece of its work (pieces
+ * The same for the paged attention of 16-bit pools: the warp that issues a CTA's
+ * tensor-core work (with few rows: its loads) stops at chunk `chunk` >= 0 of a piece of its work (pieces
  * with fewer are not affected).  The other roles' waits run out (2 s), the CTA lets
  * its loads and MMAs in flight end and returns; cllm_paged_status then returns
  * CLLM_ETIMEOUT and the cache stays usable.  -1 disarms.  EINVAL on a null cache or

@@ -36,6 +36,23 @@ struct PagedAttnArgs {
   int* err;
 };
 
+// Launch a kernel that may start while the one before it in the stream ends; it
+// waits (griddepcontrol.wait) before it touches memory.
+template <class... P, class... A>
+inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // Partials: CTA c's slot 2c is a tile that began in an earlier CTA, slot 2c + 1
 // one that it begins and does not end.
 constexpr int kPagedPartRows = 256;  // most rows of a tile
@@ -64,5 +81,12 @@ cudaError_t launch_paged_attention_tc(const PagedAttnArgs& a, const CUtensorMap&
                                       int hold, int grid, cudaStream_t s);
 cudaError_t paged_attention_tc_set_attributes();
 bool paged_pool_map(CUtensorMap* m, const void* pool, const cllm_paged_desc& d);
+// queries of a tile of `rows` rows: group heads of rows / group tokens, row = token * group + head
+bool paged_query_map(CUtensorMap* m, const PagedAttnArgs& a, int dtype, int hd, int rows);
+// 16-bit pools, few rows (paged_attn_mma.cu): tiles of 16, 32 or 64 rows (tiles = 1, 2, 4; 16 tiles >= group);
+// hold: 1 + the chunk of a piece at which the loading warp gives up
+cudaError_t launch_paged_attention_mma(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
+                                       int tiles, int hold, int grid, cudaStream_t s);
+cudaError_t paged_attention_mma_set_attributes();
 
 }  // namespace cllm

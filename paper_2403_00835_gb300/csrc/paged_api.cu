@@ -23,6 +23,8 @@ struct cllm_paged {
 
 namespace {
 
+// 16-bit pools: up to this many rows to a key/value head run on warp-level MMAs.
+constexpr int kFewRows = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -110,6 +112,7 @@ extern "C" int cllm_paged_create(const cllm_paged_desc* desc, cllm_paged** out) 
   int rc = CLLM_OK;
   do {
     e = es == 4 ? paged_attention_f32_set_attributes() : paged_attention_tc_set_attributes();
+    if (e == cudaSuccess && es == 2) e = paged_attention_mma_set_attributes();
     if (e != cudaSuccess) {
       rc = cuda_fail(e, "paged_create");
       break;
@@ -154,31 +157,31 @@ extern "C" int cllm_paged_status(cllm_paged* c, void* cuda_stream) {
   return err == 0 ? CLLM_OK : err & DERR_TIMEOUT ? CLLM_ETIMEOUT : CLLM_EDEVICE;
 }
 
-extern "C" int cllm_paged_append(cllm_paged* c, int layer, int T, const void* k, int64_t k_stride, const void* v,
-                                 int64_t v_stride, const int64_t* slots, const void* q, int64_t q_stride, void* q_out,
-                                 int64_t q_out_stride, const float* rope, int max_pos, const int32_t* positions,
-                                 void* cuda_stream) {
-  if (!c || layer < 0 || layer >= c->d.layers || T < 0) return CLLM_EINVAL;
-  if (T == 0) return CLLM_OK;
+extern "C" int cllm_paged_append(cllm_paged* c, const cllm_paged_rows* r, void* cuda_stream) {
+  if (!c || !r || r->layer < 0 || r->layer >= c->d.layers || r->rows < 0) return CLLM_EINVAL;
+  if (r->rows == 0) return CLLM_OK;
   const cllm_paged_desc& d = c->d;
   auto rows_ok = [&](const void* p, int64_t stride, int heads) {
     return p && aligned(p, 16) &&
-           (T == 1 || (stride * c->es % 16 == 0 && stride >= static_cast<int64_t>(heads) * d.head_dim));
+           (r->rows == 1 || (stride * c->es % 16 == 0 && stride >= static_cast<int64_t>(heads) * d.head_dim));
   };
-  if (!rows_ok(k, k_stride, d.n_kv_heads) || !rows_ok(v, v_stride, d.n_kv_heads) || !slots || !aligned(slots, 8))
+  if (!rows_ok(r->k, r->k_stride, d.n_kv_heads) || !rows_ok(r->v, r->v_stride, d.n_kv_heads) || !r->slots ||
+      !aligned(r->slots, 8))
     return CLLM_EINVAL;
-  if (rope && (!aligned(rope, 16) || max_pos < 1 || !positions || !aligned(positions, 4))) return CLLM_EINVAL;
-  if (q && (!rope || !rows_ok(q, q_stride, d.n_heads) || !rows_ok(q_out, q_out_stride, d.n_heads))) return CLLM_EINVAL;
+  if (r->rope && (!aligned(r->rope, 16) || r->max_pos < 1 || !r->positions || !aligned(r->positions, 4)))
+    return CLLM_EINVAL;
+  if (r->q && (!r->rope || !rows_ok(r->q, r->q_stride, d.n_heads) || !rows_ok(r->q_out, r->q_out_stride, d.n_heads)))
+    return CLLM_EINVAL;
   PagedAppendArgs a{};
-  const int64_t at = layer * d.stride_layer * c->es;
-  a.k = k, a.v = v, a.q = q, a.q_out = q_out;
+  const int64_t at = r->layer * d.stride_layer * c->es;
+  a.k = r->k, a.v = r->v, a.q = r->q, a.q_out = r->q_out;
   a.kp = static_cast<char*>(d.k) + at, a.vp = static_cast<char*>(d.v) + at;
-  a.k_row = k_stride, a.v_row = v_stride, a.q_row = q_stride, a.qo_row = q_out_stride;
+  a.k_row = r->k_stride, a.v_row = r->v_stride, a.q_row = r->q_stride, a.qo_row = r->q_out_stride;
   a.s_page = d.stride_page, a.s_head = d.stride_head, a.s_pos = d.stride_pos;
-  a.slots = reinterpret_cast<const long long*>(slots);
-  a.rope = reinterpret_cast<const float2*>(rope);
-  a.positions = positions;
-  a.max_pos = max_pos, a.T = T, a.H = q ? d.n_heads : 0, a.Hkv = d.n_kv_heads, a.hd = d.head_dim;
+  a.slots = reinterpret_cast<const long long*>(r->slots);
+  a.rope = reinterpret_cast<const float2*>(r->rope);
+  a.positions = r->positions;
+  a.max_pos = r->max_pos, a.T = r->rows, a.H = r->q ? d.n_heads : 0, a.Hkv = d.n_kv_heads, a.hd = d.head_dim;
   a.n_pages = d.n_pages, a.page_shift = c->page_shift;
   a.err = c->err;
   const cudaError_t e = launch_paged_append(a, d.dtype, static_cast<cudaStream_t>(cuda_stream));
@@ -216,8 +219,17 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
   a.layer = p->layer, a.n_pages = d.n_pages, a.page_shift = c->page_shift;
   a.part_o = c->part_o, a.part_ml = c->part_ml, a.tickets = c->tickets, a.err = c->err;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = c->es == 4 ? launch_paged_attention_f32(a, d.head_dim, c->sms, st)
-                                   : launch_paged_attention_tc(a, c->mk, c->mv, d.dtype, d.head_dim, c->hold, c->sms, st);
+  // rows of one key/value head in an average request
+  const int64_t rows = (static_cast<int64_t>(p->rows) + p->batch - 1) / p->batch * a.group;
+  cudaError_t e;
+  if (c->es == 4) {
+    e = launch_paged_attention_f32(a, d.head_dim, c->sms, st);
+  } else if (rows <= kFewRows) {
+    const int tiles = rows <= 16 && a.group <= 16 ? 1 : rows <= 32 && a.group <= 32 ? 2 : 4;
+    e = launch_paged_attention_mma(a, c->mk, c->mv, d.dtype, d.head_dim, tiles, c->hold, c->sms, st);
+  } else {
+    e = launch_paged_attention_tc(a, c->mk, c->mv, d.dtype, d.head_dim, c->hold, c->sms, st);
+  }
   return e == cudaSuccess ? CLLM_OK : cuda_fail(e, "paged_attention");
 }
 

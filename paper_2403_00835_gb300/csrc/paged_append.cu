@@ -13,6 +13,7 @@
 #include "act.cuh"
 #include "paged.cuh"
 #include "internal.cuh"
+#include "ptx.cuh"
 
 namespace cllm {
 
@@ -82,6 +83,8 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const Page
   constexpr int kHeads = kAppendThreads / kLanes;   // heads at a time
   const int t = blockIdx.x, d = (threadIdx.x % kLanes) * V::n;
   const int all = a.H + 2 * a.Hkv, step = kHeads * gridDim.y;
+  pdl_launch_dependents();
+  pdl_wait();
   const long long slot = a.slots[t];
   const bool stored = slot >= 0 && (slot >> a.page_shift) < a.n_pages;
   bool rotated = a.rope != nullptr;
@@ -146,9 +149,7 @@ cudaError_t launch_append(const PagedAppendArgs& a, cudaStream_t s) {
   // few rows: a row's heads are spread over as many CTAs as there are groups of heads
   const int groups = (a.H + 2 * a.Hkv + kHeads - 1) / kHeads;
   const dim3 grid(a.T, a.T < 2 * 152 ? groups : 1);
-  if (a.hd == 128) paged_append_kernel<T, 128><<<grid, kAppendThreads, 0, s>>>(a);
-  else paged_append_kernel<T, 64><<<grid, kAppendThreads, 0, s>>>(a);
-  return cudaGetLastError();
+  return launch_after(a.hd == 128 ? paged_append_kernel<T, 128> : paged_append_kernel<T, 64>, grid, kAppendThreads, 0, s, a);
 }
 
 }  // namespace

@@ -7,6 +7,7 @@
 // A thread computes BM/16 rows x 4 scores, and of the output BM/16 rows x HD/16 columns.
 #include "paged.cuh"
 #include "paged_walk.cuh"
+#include "ptx.cuh"
 
 namespace cllm {
 
@@ -43,6 +44,8 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
   PagedSmem<HD, BM>& s = *reinterpret_cast<PagedSmem<HD, BM>*>(smem_raw);
   constexpr int R = BM / 16, C = HD / 64;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  pdl_launch_dependents();
+  pdl_wait();
   run_start(a, g, &s.run, s.scan);
   PagedWalk w;
   w.begin(s.run);
@@ -226,8 +229,7 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
 template <int HD, int BM>
 cudaError_t launch(const PagedAttnArgs& a, int grid, cudaStream_t s) {
   const PagedGeom g{BM / a.group, BM / a.group, kPChunk, 1};
-  paged_attn_kernel<float, HD, BM><<<grid, kPThreads, sizeof(PagedSmem<HD, BM>), s>>>(a, g);
-  return cudaGetLastError();
+  return launch_after(paged_attn_kernel<float, HD, BM>, dim3(grid), kPThreads, sizeof(PagedSmem<HD, BM>), s, a, g);
 }
 
 }  // namespace

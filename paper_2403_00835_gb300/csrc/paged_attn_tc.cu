@@ -22,42 +22,18 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "paged.cuh"
-#include "paged_walk.cuh"
-#include "ptx.cuh"
+#include "paged_pipe.cuh"
 
 namespace cllm {
 
 namespace {
 
 constexpr int kTcThreads = 320;  // warps 0-3, 4-7: the slots' rows; 8 MMAs; 9 loads
-constexpr int kTcRows = 128, kTcChunk = 128, kTcHalf = 64;
-// A row's running maximum follows only growth of more than this (in log2): P may
-// then reach 2^8, and O in tensor memory is rarely rescaled.
-constexpr float kTcSlack = 8.f;
-
-// The chunks of a piece that a slot works on: first, first + step, .. < end
-// (relative to the piece).
-struct SlotChunks {
-  int first, end, step;
-  __device__ bool any() const { return first < end; }
-  __device__ bool has(int i) const { return i >= first && i < end && (step == 1 || ((i - first) & 1) == 0); }
-};
-
-// A piece as the loading warp hands it to the others.
-struct TcPiece {
-  int b, h, t0, nt, n, len, row0, lo, hi;  // as in Piece
-  int ca, chunks;                          // first chunk and number of chunks (0: no keys)
-  int two, whole;                          // 128 rows in each slot; the whole tile
-  int slot, cta0, cta1, first_slot;        // of a cut tile: this part's slot, the CTAs of its parts, the first's slot
-  SlotChunks c[2];
-  int final, end;                          // the run's last piece; no piece: the run is over
-  __device__ int part(int cta) const { return cta == cta0 ? first_slot : 2 * cta; }
-};
-constexpr int kTcPieces = 4;
-
+constexpr int kTcRows = 128, kTcChunk = kPageChunk, kTcHalf = 64;
 template <int HD>
 struct TcSmem {
+  static constexpr int kRows = kTcRows;
+  static constexpr bool kAhead = true, kIssuer = true;
   static constexpr int kRing = HD == 128 ? 5 : 10;
   static constexpr int kTile = kTcChunk * HD * 2;
   alignas(1024) uint8_t q[2][kTcRows * HD * 2];
@@ -65,8 +41,8 @@ struct TcSmem {
   float2 ml[2][kTcRows];  // also the scratch of run_start
   uint64_t full[kRing], empty[kRing], qfull, qempty, ofree, drain;
   uint64_t sfull[2], pready[2][2], ofull[2];  // of a slot: S is there; P of a half of the keys is; the piece's O is
-  uint64_t pfull[kTcPieces], pempty[kTcPieces], pfree[kTcPieces];  // a piece is there; the rows, the issuer are done with it
-  TcPiece piece[kTcPieces], cut;  // (cut: one to be merged after the run)
+  uint64_t pfull[kPagePieces], pempty[kPagePieces], pfree[kPagePieces];  // a piece is there; the rows, the issuer are done with it
+  PagePiece piece[kPagePieces], cut;  // (cut: one to be merged after the run)
   RunStart run;
   unsigned bad[8];  // rows whose result is not finite
   uint32_t tmem;
@@ -74,167 +50,16 @@ struct TcSmem {
 };
 static_assert(sizeof(TcSmem<128>) <= 227 * 1024 && sizeof(TcSmem<64>) <= 227 * 1024, "shared memory");
 
-struct TcMaps {
-  CUtensorMap q, k, v;
+template <class T> struct TcType;
+template <> struct TcType<__half> {
+  static constexpr uint32_t idesc(int n, bool mn) { return idesc_f16_f32(kTcRows, n, mn); }
 };
-
-// mbar_wait, but time in which a warp redoes rows (busy) does not count, and once
-// a wait has run out the others end at once.
-__device__ __noinline__ bool tc_wait_on(uint64_t* bar, uint32_t parity, volatile int* abort, volatile int* busy) {
-  if (*abort) return false;
-  uint64_t t0 = globaltimer_ns();
-  uint32_t it = 0;
-  while (!mbar_try_wait(bar, parity)) {
-    if ((++it & 15u) == 0) {
-      if (*abort) return false;
-      if (*busy) t0 = globaltimer_ns();
-      if (globaltimer_ns() - t0 > kWaitBudgetNs) {
-        *abort = 1;
-        return false;
-      }
-    }
-  }
-  return true;
-}
-__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile int* abort, volatile int* busy) {
-  return mbar_try_wait(bar, parity) || tc_wait_on(bar, parity, abort, busy);
-}
-
-// A row warp's wait for its next piece.  The loading warp always brings one (an end,
-// after a wait of its own has run out), and the 8 row warps have to agree on it: they take no
-// notice of the other roles' failures here, and the limit is past all of theirs.
-__device__ __forceinline__ bool piece_wait(uint64_t* bar, uint32_t parity) {
-  const uint64_t t0 = globaltimer_ns();
-  for (uint32_t it = 0; !mbar_try_wait(bar, parity); ++it)
-    if ((it & 63u) == 63u && globaltimer_ns() - t0 > 8 * kWaitBudgetNs) return false;
-  return true;
-}
-
-// A position of a ring and the phase of its barriers.
-template <int N>
-struct RingAt {
-  uint32_t i = 0, phase = 0;
-  __device__ void operator++() {
-    if (++i == N) i = 0, phase ^= 1;
-  }
+template <> struct TcType<__nv_bfloat16> {
+  static constexpr uint32_t idesc(int n, bool mn) { return idesc_bf16_f32(kTcRows, n, mn); }
 };
 
 // Ring position of a piece's V tiles (loaded as K0 K1 V0 K2 V1 .. V(n-1)), relative to K0.
 __device__ __forceinline__ int ring_v(int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; }
-
-template <class T> struct TcType;
-template <> struct TcType<__half> {
-  static __device__ uint32_t pack(float a, float b) { return pack_f16x2(a, b); }
-  static constexpr uint32_t idesc(int n, bool mn) { return idesc_f16_f32(kTcRows, n, mn); }
-};
-template <> struct TcType<__nv_bfloat16> {
-  static __device__ uint32_t pack(float a, float b) { return pack_bf16x2(a, b); }
-  static constexpr uint32_t idesc(int n, bool mn) { return idesc_bf16_f32(kTcRows, n, mn); }
-};
-
-// Walk the CTA's run, hand each piece to the other warps, and load its queries, keys and
-// values.
-template <int HD>
-__device__ __forceinline__ void issue_loads(TcSmem<HD>& s, const PagedAttnArgs& a, const PagedGeom& g, const TcMaps& m) {
-  constexpr int NH = HD / 64, NR = TcSmem<HD>::kRing;
-  const int lane = threadIdx.x & 31, tt = g.slot_tok, P = 1 << a.page_shift;
-  const int box = min(P, kTcChunk), boxes = kTcChunk / box;
-  RingAt<NR> at;
-  RingAt<kTcPieces> pat;
-  uint32_t r = 0, pieces = 0, with_keys = 0;  // loads, pieces, pieces with keys so far
-  bool ok = true;
-  auto wait = [&](uint64_t* bar, uint32_t parity) {
-    ok = ok && tc_wait(bar, parity, &s.abort, &s.busy);
-    ok = __all_sync(0xffffffffu, ok);
-  };
-  PagedWalk w;
-  w.begin(s.run);
-  for (;;) {
-    Piece p;
-    const bool more = w.next(a, g, p);
-    if (pieces >= kTcPieces) {
-      wait(&s.pempty[pat.i], pat.phase ^ 1);
-      wait(&s.pfree[pat.i], pat.phase ^ 1);
-    }
-    if (!ok) break;
-    ++pieces;
-    if (lane == 0) {
-      TcPiece& o = s.piece[pat.i];
-      o.end = !more;
-      if (more) {
-        o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0, o.lo = p.lo, o.hi = p.hi;
-        o.ca = p.ca, o.chunks = p.cb - p.ca;
-        o.two = p.nt > tt, o.whole = p.whole(), o.final = w.done();
-        if (!p.whole()) {
-          o.slot = w.slot(p, blockIdx.x);
-          o.cta0 = w.first_cta(p), o.cta1 = w.last_cta(p);
-          o.first_slot = w.slot(p, o.cta0);
-        }
-        for (int t = 0; t < 2; ++t) {
-          if (!o.two) {
-            o.c[t] = {t, o.chunks, 2};
-          } else {
-            const int t0 = p.t0 + t * tt;
-            const TileKeys k = tile_keys(a, p.n, p.len, t0, min(p.t0 + p.nt, t0 + tt));
-            o.c[t] = {max(0, k.lo / kTcChunk - p.ca), min(o.chunks, (k.hi + kTcChunk - 1) / kTcChunk - p.ca), 1};
-          }
-        }
-      }
-      mbar_arrive(&s.pfull[pat.i]);
-    }
-    __syncwarp();
-    ++pat;
-    if (!more) break;
-    if (p.empty()) continue;
-    const int n = p.cb - p.ca;
-    auto tile = [&](const CUtensorMap* map, int c) {  // 128 keys from chunk c: those pages that hold keys of the tile
-      const int kb = c * kTcChunk;
-      if (r >= NR) wait(&s.empty[at.i], at.phase ^ 1);
-      if (!ok) return;
-      const int b0 = max(p.lo - kb, 0) / box, b1 = (min(p.hi - kb, kTcChunk) + box - 1) / box;
-      if (lane == 0) mbar_arrive_expect_tx(&s.full[at.i], (b1 - b0) * box * HD * 2);
-      __syncwarp();
-      const int j = lane / NH, half = lane % NH;  // (boxes * NH <= 32)
-      if (j >= b0 && j < b1 && j < boxes) {
-        const int pos = kb + j * box;
-        int page = __ldg(a.table + static_cast<size_t>(p.b) * a.table_width + (pos >> a.page_shift));
-        if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
-          atomicOr(a.err, DERR_CAPACITY);
-          page = a.n_pages;  // outside the map: reads as zeros
-        }
-        tma_load_5d(s.ring[at.i] + half * kTcChunk * 128 + j * box * 128, map, &s.full[at.i], half * 64, pos & (P - 1), p.h,
-                    page, a.layer);
-      }
-      ++r;
-      ++at;
-    };
-    if (with_keys > 0) wait(&s.qempty, (with_keys - 1) & 1);
-    if (!ok) break;
-    const int slots = p.nt > tt ? 2 : 1;
-    if (lane == 0) mbar_arrive_expect_tx(&s.qfull, slots * NH * tt * a.group * 128);
-    __syncwarp();
-    if (lane < slots * NH)
-      tma_load_3d(s.q[lane / NH] + lane % NH * kTcRows * 128, &m.q, &s.qfull, lane % NH * 64, p.h * a.group,
-                  p.row0 + p.t0 + lane / NH * tt);
-    ++with_keys;
-    tile(&m.k, p.ca);
-    for (int i = 0; ok && i < n; ++i) {
-      if (i + 1 < n) tile(&m.k, p.ca + i + 1);
-      if (ok) tile(&m.v, p.ca + i);
-    }
-    if (!ok) break;
-  }
-  if (!ok && lane == 0) {
-    // the rows get their end (they go on past every wait now), and loads in flight land
-    // before the CTA leaves
-    *const_cast<volatile int*>(&s.abort) = 1;
-    if (pieces >= kTcPieces) mbar_wait(&s.pempty[pat.i], pat.phase ^ 1, nullptr);
-    s.piece[pat.i].end = 1;
-    mbar_arrive(&s.pfull[pat.i]);
-    for (uint32_t i = r > NR ? r - NR : 0; i < r; ++i) mbar_wait(&s.full[i % NR], (i / NR) & 1, nullptr);
-    if (with_keys > 0) mbar_wait(&s.qfull, (with_keys - 1) & 1, nullptr);
-  }
-}
 
 // The MMAs of the CTA, by one warp, whose instructions are what its chunks cost beside
 // the tensor cores' own time (it shares its scheduler with two row warps): descriptors
@@ -254,20 +79,20 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD>& s, uint32_t tmem, int hol
   const uint32_t q_hi = static_cast<uint32_t>(dq >> 32), k_hi = static_cast<uint32_t>(dk >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
   auto desc = [](uint32_t lo, uint32_t hi) { return static_cast<uint64_t>(hi) << 32 | lo; };
   RingAt<NR> at;
-  RingAt<kTcPieces> pat;
+  RingAt<kPagePieces> pat;
   uint32_t pieces = 0, nc0 = 0, nc1 = 0;  // pieces so far, chunks of each slot
   bool ok = true;
   {
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = ok && (__all_sync(0xffffffffu, mbar_try_wait(bar, parity)) ||
-                  __all_sync(0xffffffffu, tc_wait_on(bar, parity, &s.abort, &s.busy)));
+                  __all_sync(0xffffffffu, page_wait_on(bar, parity, &s.abort, &s.busy)));
       tc_fence_after();
     };
     auto same = [](int x) { return static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(x))); };
     for (;; ++pat) {
       wait(&s.pfull[pat.i], pat.phase);
       if (!ok) break;
-      const TcPiece& p = s.piece[pat.i];
+      const PagePiece& p = s.piece[pat.i];
       if (same(p.end)) break;
       const int n = same(p.chunks);
       const bool two = same(p.two);
@@ -376,128 +201,17 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
   const uint32_t ts = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);  // this warp's lanes, slot 0
   const uint32_t mine = ts + t * 256;
   auto warp_wait = [&](uint64_t* bar, uint32_t parity) {
-    if (lane == 0) tc_wait(bar, parity, &s.abort, &s.busy);
+    if (lane == 0) page_wait(bar, parity, &s.abort, &s.busy);
     __syncwarp();
     tc_fence_after();
   };
-  auto all_rows = [&] { named_bar_sync(1, 256); };
-  // -- of a tile, when its keys are done ------------------------------------------------
-  auto write16 = [](T* out, const float (&o)[16], float scale) {  // 16 columns of a result; whether one is not finite
-    bool bad = false;
-#pragma unroll
-    for (int j = 0; j < 16; j += 8) {
-      uint32_t u[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = scale != 0.f ? o[j + 2 * e] * scale : 0.f, y = scale != 0.f ? o[j + 2 * e + 1] * scale : 0.f;
-        bad |= !isfinite(x) || !isfinite(y);
-        u[e] = TcType<T>::pack(x, y);
-      }
-      *reinterpret_cast<uint4*>(out + j) = make_uint4(u[0], u[1], u[2], u[3]);
-    }
-    return bad;
-  };
-  auto store_lse = [&](const TcPiece& p, int tok, int head, float m, float l) {
-    if (a.lse != nullptr)
-      a.lse[static_cast<size_t>(p.row0 + tok) * a.H + head] = l != 0.f ? (m + log2f(l)) * 0.69314718055994530942f : -INFINITY;
-  };
-  auto redo = [&](const TcPiece& p, int rr) {  // row rr of a tile from the definition (the whole warp)
-    __syncwarp();
-    if (lane == 0) atomicAdd(&s.busy, 1);
-    exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + (p.two ? rr / kTcRows * tt : 0) + (rr % kTcRows) / a.group,
-                     p.h * a.group + (rr % kTcRows) % a.group);
-    if (lane == 0) atomicAdd(&s.busy, -1);
-  };
-  // Rows marked in s.bad (marked by any warp, so after a barrier of the 8; the next mark comes after another).
-  auto redo_bad = [&](const TcPiece& p) {
-    unsigned any = 0;
-    for (int i = 0; i < 8; ++i) any |= s.bad[i];
-    if (!any) return;
-    for (int rr = warp; rr < 2 * kTcRows; rr += 8)
-      if (s.bad[rr >> 5] >> (rr & 31) & 1) redo(p, rr);
-    all_rows();
-    if (tid < 8) s.bad[tid] = 0;
-    all_rows();
-  };
-  // A part is [HD / 4][rows][4], so that the rows' threads write and read side by side.
-  auto rows_of_part = [&](const TcPiece& p) { return p.two ? kPagedPartRows : (p.nt * a.group + 31) & ~31; };
-  // Merge the parts of a tile, in order, if the others were there before this CTA's
-  // (`before`: thread 0 has their number).
-  auto merge_if_last = [&](const TcPiece& p, int before) {
-    const int cta0 = p.cta0, cta1 = p.cta1;
-    if (tid == 0) {
-      s.last = before == cta1 - cta0;
-      if (s.last) a.tickets[cta0] = 0;
-      __threadfence();
-    }
-    all_rows();
-    if (!s.last) return;
-    // First the rows' maxima and sums, a thread per row; then 16 columns of a row per
-    // thread, with the loads of several parts in flight (an SM takes them in at 64
-    // bytes a cycle at best).
-    const int live = p.nt * a.group, part_rows = rows_of_part(p);
-    const bool two = p.two;
-    auto row_of = [&](int k) { return two && k >= tt * a.group ? kTcRows + k - tt * a.group : k; };
-    if (tid < live) {
-      const float2* from = a.part_ml + row_of(tid);
-      float mm = -INFINITY, ll = 0.f;
-#pragma unroll 1
-      for (int c = cta0; c <= cta1; c += 8) {
-        float2 ml[8];
-        float nm = mm;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          ml[u] = c + u <= cta1 ? __ldcg(from + static_cast<size_t>(p.part(c + u)) * kPagedPartRows) : make_float2(-INFINITY, 0.f);
-          nm = fmaxf(nm, ml[u].x);
-        }
-        ll = mm != -INFINITY ? ll * ex2_ftz(mm - nm) : 0.f;
-        mm = nm;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) ll += ml[u].x != -INFINITY ? ml[u].y * ex2_ftz(ml[u].x - mm) : 0.f;
-      }
-      (&s.ml[0][0])[tid] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
-      store_lse(p, p.t0 + tid / a.group, p.h * a.group + tid % a.group, mm, ll);
-    }
-    all_rows();
-#pragma unroll 1
-    for (int i = tid; i < live * (HD / 16); i += 256) {
-      const int k = i % live, d = i / live * 16, rr = row_of(k);
-      const float2 mi = (&s.ml[0][0])[k];
-      float o[16];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) o[j] = 0.f;
-#pragma unroll 4
-      for (int c = cta0; c <= cta1; ++c) {
-        const size_t part = p.part(c);
-        const float m1 = __ldcg(a.part_ml + part * kPagedPartRows + rr).x;
-        const float4* from = reinterpret_cast<const float4*>(a.part_o) + part * (kPagedPartRows * HD / 4) + d / 4 * part_rows + rr;
-        const float u = m1 != -INFINITY ? ex2_ftz(m1 - mi.x) : 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float4 y = __ldcg(from + j * part_rows);
-          if (u != 0.f) {
-            o[4 * j] = fmaf(y.x, u, o[4 * j]);
-            o[4 * j + 1] = fmaf(y.y, u, o[4 * j + 1]);
-            o[4 * j + 2] = fmaf(y.z, u, o[4 * j + 2]);
-            o[4 * j + 3] = fmaf(y.w, u, o[4 * j + 3]);
-          }
-        }
-      }
-      T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + k / a.group) * a.out_row +
-               static_cast<long long>(p.h * a.group + k % a.group) * a.out_head + d;
-      if (write16(out, o, mi.y)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
-    }
-    all_rows();
-    redo_bad(p);
-  };
-
   uint32_t r = 0, ns = 0, no[2] = {0, 0};  // loads of the pieces before, chunks of this slot, pieces of both
   bool cut = false;        // a part is left to be merged
   int cut_arrivals = 0;    // thread 0: the parts of it that were there before this CTA's
-  RingAt<kTcPieces> pat;
+  RingAt<kPagePieces> pat;
   for (;; ++pat) {
     if (!piece_wait(&s.pfull[pat.i], pat.phase)) break;
-    const TcPiece& p = s.piece[pat.i];
+    const PagePiece& p = s.piece[pat.i];
     if (p.end) break;
     const int n = p.chunks;
     const bool two = p.two;
@@ -518,10 +232,10 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
           // page held before): p is 0 there, and so is V
           const int v = r + ring_v(i, n);
           warp_wait(&s.full[v % NR], (v / NR) & 1);
-          if (kb + row < lo || kb + row >= hi) {
-#pragma unroll
-            for (int c = 0; c < HD / 8; ++c)
-              *reinterpret_cast<uint4*>(s.ring[v % NR] + (c >> 3) * kTcChunk * 128 + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+          const int z0 = max(lo - kb, 0), z1 = min(hi - kb, kTcChunk);  // keys seen: [z0, z1)
+          for (int c = row; c < kTcChunk * HD / 8; c += kTcRows) {       // 16 bytes each, 64 columns of the keys after another
+            const int key = c >> 3 & (kTcChunk - 1);
+            if (key < z0 || key >= z1) *reinterpret_cast<uint4*>(s.ring[v % NR] + c * 16) = make_uint4(0, 0, 0, 0);
           }
           fence_proxy_async_smem();
         }
@@ -568,7 +282,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
           if (i == first) {
             m = cm;
           } else {
-            const bool grow = cm > m + kTcSlack || (m == -INFINITY && cm > m);
+            const bool grow = cm > m + kPageSlack || (m == -INFINITY && cm > m);
             if (__any_sync(0xffffffffu, grow)) {
               // (the P V before is done: this S was issued after it)
               const float nm = grow ? cm : m;
@@ -597,7 +311,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
             e.x = ex2_ftz(e.x);
             e.y = ex2_ftz(e.y);
             sum[j & 1] = add2(sum[j & 1], e);
-            pk[j] = TcType<T>::pack(e.x, e.y);
+            pk[j] = Pack16<T>::pack(e.x, e.y);
           }
           tmem_st16(mine + c / 2, pk);
         };
@@ -621,7 +335,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
     }
     const bool whole = p.whole;
     // a part: [HD / 4][rows][4], so that the rows' threads write and read side by side
-    const int part_rows = rows_of_part(p);
+    const int part_rows = rows_of_part(a, p);
     float4* part = reinterpret_cast<float4*>(a.part_o) + static_cast<size_t>(p.slot) * (kPagedPartRows * HD / 4);
     float2* part_ml = a.part_ml + static_cast<size_t>(p.slot) * kPagedPartRows;
     const int head = p.h * a.group + row % a.group;
@@ -653,12 +367,12 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
         }
       }
       if (live) {
-        if (whole) store_lse(p, tok, head, m, l);
+        if (whole) store_lse(a, p, tok, head, m, l);
         else part_ml[t * kTcRows + row] = make_float2(m, l);
       }
       if (whole)
         for (unsigned redo_rows = __ballot_sync(0xffffffffu, bad); redo_rows; redo_rows &= redo_rows - 1)
-          redo(p, t * kTcRows + (warp & 3) * 32 + __ffs(redo_rows) - 1);
+          redo<T, HD>(s, a, p, tt, t * kTcRows + (warp & 3) * 32 + __ffs(redo_rows) - 1);
     } else {
       // both slots hold these rows, each over half of the keys; slot t's warps finish
       // the t-th half of the columns
@@ -681,15 +395,14 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
 #pragma unroll 1
         for (int d = t * (HD / 2); d < (t + 1) * (HD / 2); d += 16) {
           float o[16], o1[16];
-          if (has[0]) tmem_ld16(ts + 128 + d, o);
-          if (has[1]) tmem_ld16(ts + 256 + 128 + d, o1);
+          tmem_ld16x2(ts + 128 + d, ts + 256 + 128 + d, o, o1);  // (what a slot without keys holds is not used)
 #pragma unroll
           for (int j = 0; j < 16; ++j) o[j] = (use0 ? o[j] * f0 : 0.f) + (use1 ? o1[j] * f1 : 0.f);
           bad |= store16(o, row, d, scale, live);
         }
       }
       if (live && t == 0) {
-        if (whole) store_lse(p, tok, head, mm, ll);
+        if (whole) store_lse(a, p, tok, head, mm, ll);
         else part_ml[row] = make_float2(mm, ll);
       }
       if (bad) atomicOr(&s.bad[row >> 5], 1u << (row & 31));
@@ -709,34 +422,35 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
         before = atomicAdd(a.tickets + p.cta0, 1);
       }
       if (p.final) {
-        merge_if_last(p, before);
+        merge_if_last<T, HD>(s, a, p, tt, before);
       } else {
         // nothing waits for the counter's answer here: whether this CTA has to merge the
         // tile is seen to after the run
         cut = true;
         cut_arrivals = before;
-        if (tid < sizeof(TcPiece) / 4) reinterpret_cast<int*>(&s.cut)[tid] = reinterpret_cast<const int*>(&p)[tid];
+        if (tid < sizeof(PagePiece) / 4) reinterpret_cast<int*>(&s.cut)[tid] = reinterpret_cast<const int*>(&p)[tid];
       }
     } else if (!two) {
       all_rows();  // (s.ml is free again)
-      redo_bad(p);
+      redo_bad<T, HD>(s, a, p, tt);
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&s.pempty[pat.i]);
   }
   if (cut) {
     all_rows();
-    merge_if_last(s.cut, cut_arrivals);
+    merge_if_last<T, HD>(s, a, s.cut, tt, cut_arrivals);
   }
 }
 
 template <class T, int HD>
 __global__ void __launch_bounds__(kTcThreads, 1)
-    paged_attn_tc_kernel(const __grid_constant__ TcMaps m, const __grid_constant__ PagedAttnArgs a, const PagedGeom g,
+    paged_attn_tc_kernel(const __grid_constant__ PagedMaps m, const __grid_constant__ PagedAttnArgs a, const PagedGeom g,
                          const int hold) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   TcSmem<HD>& s = *reinterpret_cast<TcSmem<HD>*>(smem_raw);
   if (smem_u32(smem_raw) & 1023u) {  // (the swizzle's atoms; shared memory starts on one)
+    pdl_wait();
     if (threadIdx.x == 0) atomicOr(a.err, DERR_SHAPE);
     return;
   }
@@ -754,7 +468,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       mbar_init(&s.pready[t][1], 4);
       mbar_init(&s.ofull[t], 1);
     }
-    for (int i = 0; i < kTcPieces; ++i) {
+    for (int i = 0; i < kPagePieces; ++i) {
       mbar_init(&s.pfull[i], 1);
       mbar_init(&s.pempty[i], 8);
       mbar_init(&s.pfree[i], 1);
@@ -769,13 +483,20 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     tmem_alloc(&s.tmem, 512);
     tmem_relinquish();
   }
+  if (threadIdx.x == kTcThreads - 1) {
+    tma_prefetch_desc(&m.q);
+    tma_prefetch_desc(&m.k);
+    tma_prefetch_desc(&m.v);
+  }
+  pdl_launch_dependents();
+  pdl_wait();  // (nothing of the calls before is read above)
   run_start(a, g, &s.run, reinterpret_cast<long long*>(s.ml));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s.tmem;
   if (warp == 8) issue_mmas<T, HD>(s, tmem, hold);
-  else if (warp == 9) issue_loads<HD>(s, a, g, m);
+  else if (warp == 9) issue_loads<HD>(s, a, g, m, 0);
   else run_rows<T, HD>(s, a, g, tmem);
   tc_fence_before();
   __syncthreads();
@@ -788,15 +509,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 }
 
 template <class T, int HD>
-cudaError_t launch_tc(const TcMaps& m, const PagedAttnArgs& a, int hold, int grid, cudaStream_t s) {
+cudaError_t launch_tc(const PagedMaps& m, const PagedAttnArgs& a, int hold, int grid, cudaStream_t s) {
   const int tt = kTcRows / a.group;
   // Tiles of 256 rows read K and V once for twice the rows; with fewer of them than CTAs
   // their keys would have to be cut and their rows merged, so they are halved instead.
   const long long per_request = (static_cast<long long>(a.rows) + a.batch - 1) / a.batch;
   const bool two = per_request > tt && (per_request + 2 * tt - 1) / (2 * tt) * a.batch * a.Hkv >= grid;
   const PagedGeom g{two ? 2 * tt : tt, tt, kTcChunk, 2};
-  paged_attn_tc_kernel<T, HD><<<grid, kTcThreads, sizeof(TcSmem<HD>), s>>>(m, a, g, hold);
-  return cudaGetLastError();
+  return launch_after(paged_attn_tc_kernel<T, HD>, dim3(grid), kTcThreads, sizeof(TcSmem<HD>), s, m, a, g, hold);
 }
 
 }  // namespace
@@ -819,16 +539,19 @@ bool paged_pool_map(CUtensorMap* m, const void* pool, const cllm_paged_desc& d) 
   return make_map_nd(m, d.dtype == CLLM_BF16, pool, 5, dims, strides, box);
 }
 
-cudaError_t launch_paged_attention_tc(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
-                                      int hold, int grid, cudaStream_t s) {
-  TcMaps m;
-  m.k = k;
-  m.v = v;
-  // queries of a tile: group heads of 128 / group tokens, row = token * group + head
+bool paged_query_map(CUtensorMap* m, const PagedAttnArgs& a, int dtype, int hd, int rows) {
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(a.H), static_cast<cuuint64_t>(a.rows)};
   const cuuint64_t strides[2] = {static_cast<cuuint64_t>(a.q_head) * 2, static_cast<cuuint64_t>(a.q_row) * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(a.group), static_cast<cuuint32_t>(kTcRows / a.group)};
-  if (!make_map_nd(&m.q, dtype == CLLM_BF16, a.q, 3, dims, strides, box)) return cudaErrorInvalidValue;
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(a.group), static_cast<cuuint32_t>(rows / a.group)};
+  return make_map_nd(m, dtype == CLLM_BF16, a.q, 3, dims, strides, box);
+}
+
+cudaError_t launch_paged_attention_tc(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
+                                      int hold, int grid, cudaStream_t s) {
+  PagedMaps m;
+  m.k = k;
+  m.v = v;
+  if (!paged_query_map(&m.q, a, dtype, hd, kTcRows)) return cudaErrorInvalidValue;
   if (dtype == CLLM_BF16)
     return hd == 64 ? launch_tc<__nv_bfloat16, 64>(m, a, hold, grid, s) : launch_tc<__nv_bfloat16, 128>(m, a, hold, grid, s);
   return hd == 64 ? launch_tc<__half, 64>(m, a, hold, grid, s) : launch_tc<__half, 128>(m, a, hold, grid, s);

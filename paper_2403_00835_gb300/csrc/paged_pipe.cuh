@@ -1,0 +1,330 @@
+// What the paged attention kernels of 16-bit pools share: the loading warp, which walks the
+// CTA's run of work and streams queries, keys and values by TMA, the bounded waits,
+// and a tile's end: results, parts of cut tiles and their merging.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "paged.cuh"
+#include "paged_walk.cuh"
+#include "ptx.cuh"
+
+namespace cllm {
+
+constexpr int kPageChunk = 128;  // keys of a unit
+// A row's running maximum follows only growth of more than this (in log2): P may
+// then reach 2^8, and O is rarely rescaled.
+constexpr float kPageSlack = 8.f;
+
+// The chunks of a piece that a slot works on: first, first + step, .. < end
+// (relative to the piece).
+struct SlotChunks {
+  int first, end, step;
+  __device__ bool any() const { return first < end; }
+  __device__ bool has(int i) const { return i >= first && i < end && (step == 1 || ((i - first) & 1) == 0); }
+};
+
+// A piece as the loading warp hands it to the others.
+struct PagePiece {
+  int b, h, t0, nt, n, len, row0, lo, hi;  // as in Piece
+  int ca, chunks;                          // first chunk and number of chunks (0: no keys)
+  int two, whole;                          // 128 rows in each slot; the whole tile
+  int slot, cta0, cta1, first_slot;        // of a cut tile: this part's slot, the CTAs of its parts, the first's slot
+  SlotChunks c[2];
+  int final, end;                          // the run's last piece; no piece: the run is over
+  __device__ int part(int cta) const { return cta == cta0 ? first_slot : 2 * cta; }
+};
+constexpr int kPagePieces = 4;
+
+struct PagedMaps {
+  CUtensorMap q, k, v;
+};
+
+// mbar_wait, but time in which a warp redoes rows (busy) does not count, and once
+// a wait has run out the others end at once.
+static __device__ __noinline__ bool page_wait_on(uint64_t* bar, uint32_t parity, volatile int* abort, volatile int* busy) {
+  if (*abort) return false;
+  uint64_t t0 = globaltimer_ns();
+  uint32_t it = 0;
+  while (!mbar_try_wait(bar, parity)) {
+    if ((++it & 15u) == 0) {
+      if (*abort) return false;
+      if (*busy) t0 = globaltimer_ns();
+      if (globaltimer_ns() - t0 > kWaitBudgetNs) {
+        *abort = 1;
+        return false;
+      }
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ bool page_wait(uint64_t* bar, uint32_t parity, volatile int* abort, volatile int* busy) {
+  return mbar_try_wait(bar, parity) || page_wait_on(bar, parity, abort, busy);
+}
+
+// A row warp's wait for its next piece.  The loading warp always brings one (an end,
+// after a wait of its own has run out), and the 8 row warps have to agree on it: they take no
+// notice of the other roles' failures here, and the limit is past all of theirs.
+__device__ __forceinline__ bool piece_wait(uint64_t* bar, uint32_t parity) {
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t it = 0; !mbar_try_wait(bar, parity); ++it)
+    if ((it & 63u) == 63u && globaltimer_ns() - t0 > 8 * kWaitBudgetNs) return false;
+  return true;
+}
+
+// A position of a ring and the phase of its barriers.
+template <int N>
+struct RingAt {
+  uint32_t i = 0, phase = 0;
+  __device__ void operator++() {
+    if (++i == N) i = 0, phase ^= 1;
+  }
+};
+
+template <class T> struct Pack16;  // two fp32 values to 16 bits each
+template <> struct Pack16<__half> {
+  static __device__ uint32_t pack(float a, float b) { return pack_f16x2(a, b); }
+};
+template <> struct Pack16<__nv_bfloat16> {
+  static __device__ uint32_t pack(float a, float b) { return pack_bf16x2(a, b); }
+};
+
+// Walk the CTA's run, hand each piece to the other warps, and load its queries, keys and
+// values.
+// S::kAhead: K one tile ahead of V (K0 K1 V0 K2 V1 ..), else K0 V0 K1 V1 ..; S::kIssuer: a
+// warp beside the row warps takes the pieces too.  hold: test hook, 1 + the chunk of a
+// piece at which this warp gives up (0: none).
+template <int HD, class S>
+__device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const PagedGeom& g, const PagedMaps& m, int hold) {
+  constexpr int NH = HD / 64, NR = S::kRing;
+  const int lane = threadIdx.x & 31, tt = g.slot_tok, P = 1 << a.page_shift;
+  const int box = min(P, kPageChunk), boxes = kPageChunk / box;
+  RingAt<NR> at;
+  RingAt<kPagePieces> pat;
+  uint32_t r = 0, pieces = 0, with_keys = 0;  // loads, pieces, pieces with keys so far
+  bool ok = true;
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    ok = ok && page_wait(bar, parity, &s.abort, &s.busy);
+    ok = __all_sync(0xffffffffu, ok);
+  };
+  PagedWalk w;
+  w.begin(s.run);
+  for (;;) {
+    Piece p;
+    const bool more = w.next(a, g, p);
+    if (pieces >= kPagePieces) {
+      wait(&s.pempty[pat.i], pat.phase ^ 1);
+      if (S::kIssuer) wait(&s.pfree[pat.i], pat.phase ^ 1);
+    }
+    if (!ok) break;
+    ++pieces;
+    if (lane == 0) {
+      PagePiece& o = s.piece[pat.i];
+      o.end = !more;
+      if (more) {
+        o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0, o.lo = p.lo, o.hi = p.hi;
+        o.ca = p.ca, o.chunks = p.cb - p.ca;
+        o.two = p.nt > tt, o.whole = p.whole(), o.final = w.done();
+        if (!p.whole()) {
+          o.slot = w.slot(p, blockIdx.x);
+          o.cta0 = w.first_cta(p), o.cta1 = w.last_cta(p);
+          o.first_slot = w.slot(p, o.cta0);
+        }
+        for (int t = 0; t < 2; ++t) {
+          if (!o.two) {
+            o.c[t] = {t, o.chunks, 2};
+          } else {
+            const int t0 = p.t0 + t * tt;
+            const TileKeys k = tile_keys(a, p.n, p.len, t0, min(p.t0 + p.nt, t0 + tt));
+            o.c[t] = {max(0, k.lo / kPageChunk - p.ca), min(o.chunks, (k.hi + kPageChunk - 1) / kPageChunk - p.ca), 1};
+          }
+        }
+      }
+      mbar_arrive(&s.pfull[pat.i]);
+    }
+    __syncwarp();
+    ++pat;
+    if (!more) break;
+    if (p.empty()) continue;
+    const int n = p.cb - p.ca;
+    auto tile = [&](const CUtensorMap* map, int c) {  // 128 keys from chunk c: those pages that hold keys of the tile
+      const int kb = c * kPageChunk;
+      if (r >= NR) wait(&s.empty[at.i], at.phase ^ 1);
+      if (!ok) return;
+      const int b0 = max(p.lo - kb, 0) / box, b1 = (min(p.hi - kb, kPageChunk) + box - 1) / box;
+      if (lane == 0) mbar_arrive_expect_tx(&s.full[at.i], (b1 - b0) * box * HD * 2);
+      __syncwarp();
+      const int j = lane / NH, half = lane % NH;  // (boxes * NH <= 32)
+      if (j >= b0 && j < b1 && j < boxes) {
+        const int pos = kb + j * box;
+        int page = __ldg(a.table + static_cast<size_t>(p.b) * a.table_width + (pos >> a.page_shift));
+        if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
+          atomicOr(a.err, DERR_CAPACITY);
+          page = a.n_pages;  // outside the map: reads as zeros
+        }
+        tma_load_5d(s.ring[at.i] + half * kPageChunk * 128 + j * box * 128, map, &s.full[at.i], half * 64, pos & (P - 1), p.h,
+                    page, a.layer);
+      }
+      ++r;
+      ++at;
+    };
+    if (with_keys > 0) wait(&s.qempty, (with_keys - 1) & 1);
+    if (!ok) break;
+    const int slots = p.nt > tt ? 2 : 1;
+    if (lane == 0) mbar_arrive_expect_tx(&s.qfull, slots * NH * tt * a.group * 128);
+    __syncwarp();
+    if (lane < slots * NH)
+      tma_load_3d(s.q[lane / NH] + lane % NH * S::kRows * 128, &m.q, &s.qfull, lane % NH * 64, p.h * a.group,
+                  p.row0 + p.t0 + lane / NH * tt);
+    ++with_keys;
+    if (S::kAhead) tile(&m.k, p.ca);
+    for (int i = 0; ok && i < n; ++i) {
+      if (hold > 0 && i + 1 >= hold) ok = false;
+      if (ok && !S::kAhead) tile(&m.k, p.ca + i);
+      if (ok && S::kAhead && i + 1 < n) tile(&m.k, p.ca + i + 1);
+      if (ok) tile(&m.v, p.ca + i);
+    }
+    if (!ok) break;
+  }
+  if (!ok && lane == 0) {
+    // the rows get their end (they go on past every wait now), and loads in flight land
+    // before the CTA leaves
+    *const_cast<volatile int*>(&s.abort) = 1;
+    if (pieces >= kPagePieces) mbar_wait(&s.pempty[pat.i], pat.phase ^ 1, nullptr);
+    s.piece[pat.i].end = 1;
+    mbar_arrive(&s.pfull[pat.i]);
+    for (uint32_t i = r > NR ? r - NR : 0; i < r; ++i) mbar_wait(&s.full[i % NR], (i / NR) & 1, nullptr);
+    if (with_keys > 0) mbar_wait(&s.qfull, (with_keys - 1) & 1, nullptr);
+  }
+}
+
+// ---- a tile's end --------------------------------------------------------------------
+
+__device__ __forceinline__ void all_rows() { named_bar_sync(1, 256); }  // the 8 row warps
+
+// 16 columns of a result; whether one is not finite.
+template <class T>
+__device__ __forceinline__ bool write16(T* out, const float (&o)[16], float scale) {
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < 16; j += 8) {
+    uint32_t u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = scale != 0.f ? o[j + 2 * e] * scale : 0.f, y = scale != 0.f ? o[j + 2 * e + 1] * scale : 0.f;
+      bad |= !isfinite(x) || !isfinite(y);
+      u[e] = Pack16<T>::pack(x, y);
+    }
+    *reinterpret_cast<uint4*>(out + j) = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+  return bad;
+}
+
+__device__ __forceinline__ void store_lse(const PagedAttnArgs& a, const PagePiece& p, int tok, int head, float m, float l) {
+  if (a.lse != nullptr)
+    a.lse[static_cast<size_t>(p.row0 + tok) * a.H + head] = l != 0.f ? (m + log2f(l)) * 0.69314718055994530942f : -INFINITY;
+}
+
+// Row rr of a tile from the definition (the whole warp).
+template <class T, int HD, class S>
+__device__ __forceinline__ void redo(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt, int rr) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+  if (lane == 0) atomicAdd(&s.busy, 1);
+  exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + (p.two ? rr / 128 * tt : 0) + (rr % 128) / a.group,
+                   p.h * a.group + (rr % 128) % a.group);
+  if (lane == 0) atomicAdd(&s.busy, -1);
+}
+
+// Rows marked in s.bad (marked by any warp, so after a barrier of the 8; the next mark comes after another).
+template <class T, int HD, class S>
+__device__ __forceinline__ void redo_bad(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt) {
+  const int tid = threadIdx.x, warp = tid >> 5;
+  unsigned any = 0;
+  for (int i = 0; i < 8; ++i) any |= s.bad[i];
+  if (!any) return;
+  for (int rr = warp; rr < 256; rr += 8)
+    if (s.bad[rr >> 5] >> (rr & 31) & 1) redo<T, HD>(s, a, p, tt, rr);
+  all_rows();
+  if (tid < 8) s.bad[tid] = 0;
+  all_rows();
+}
+
+// A part is [HD / 4][rows][4], so that the rows' threads write and read side by side.
+__device__ __forceinline__ int rows_of_part(const PagedAttnArgs& a, const PagePiece& p) {
+  return p.two ? kPagedPartRows : (p.nt * a.group + 31) & ~31;
+}
+
+// Merge the parts of a tile, in order, if the others were there before this CTA's
+// (`before`: thread 0 has their number).
+template <class T, int HD, class S>
+__device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt, int before) {
+  const int tid = threadIdx.x;
+  const int cta0 = p.cta0, cta1 = p.cta1;
+  if (tid == 0) {
+    s.last = before == cta1 - cta0;
+    if (s.last) a.tickets[cta0] = 0;
+    __threadfence();
+  }
+  all_rows();
+  if (!s.last) return;
+  // First the rows' maxima and sums, a thread per row; then 16 columns of a row per
+  // thread, with the loads of several parts in flight (an SM takes them in at 64
+  // bytes a cycle at best).
+  const int live = p.nt * a.group, part_rows = rows_of_part(a, p);
+  const bool two = p.two;
+  auto row_of = [&](int k) { return two && k >= tt * a.group ? 128 + k - tt * a.group : k; };
+  if (tid < live) {
+    const float2* from = a.part_ml + row_of(tid);
+    float mm = -INFINITY, ll = 0.f;
+#pragma unroll 1
+    for (int c = cta0; c <= cta1; c += 8) {
+      float2 ml[8];
+      float nm = mm;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        ml[u] = c + u <= cta1 ? __ldcg(from + static_cast<size_t>(p.part(c + u)) * kPagedPartRows) : make_float2(-INFINITY, 0.f);
+        nm = fmaxf(nm, ml[u].x);
+      }
+      ll = mm != -INFINITY ? ll * ex2_ftz(mm - nm) : 0.f;
+      mm = nm;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) ll += ml[u].x != -INFINITY ? ml[u].y * ex2_ftz(ml[u].x - mm) : 0.f;
+    }
+    (&s.ml[0][0])[tid] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
+    store_lse(a, p, p.t0 + tid / a.group, p.h * a.group + tid % a.group, mm, ll);
+  }
+  all_rows();
+#pragma unroll 1
+  for (int i = tid; i < live * (HD / 16); i += 256) {
+    const int k = i % live, d = i / live * 16, rr = row_of(k);
+    const float2 mi = (&s.ml[0][0])[k];
+    float o[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[j] = 0.f;
+#pragma unroll 4
+    for (int c = cta0; c <= cta1; ++c) {
+      const size_t part = p.part(c);
+      const float m1 = __ldcg(a.part_ml + part * kPagedPartRows + rr).x;
+      const float4* from = reinterpret_cast<const float4*>(a.part_o) + part * (kPagedPartRows * HD / 4) + d / 4 * part_rows + rr;
+      const float u = m1 != -INFINITY ? ex2_ftz(m1 - mi.x) : 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 y = __ldcg(from + j * part_rows);
+        if (u != 0.f) {
+          o[4 * j] = fmaf(y.x, u, o[4 * j]);
+          o[4 * j + 1] = fmaf(y.y, u, o[4 * j + 1]);
+          o[4 * j + 2] = fmaf(y.z, u, o[4 * j + 2]);
+          o[4 * j + 3] = fmaf(y.w, u, o[4 * j + 3]);
+        }
+      }
+    }
+    T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + k / a.group) * a.out_row +
+             static_cast<long long>(p.h * a.group + k % a.group) * a.out_head + d;
+    if (write16(out, o, mi.y)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
+  }
+  all_rows();
+  redo_bad<T, HD>(s, a, p, tt);
+}
+
+}  // namespace cllm

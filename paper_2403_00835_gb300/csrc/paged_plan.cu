@@ -16,6 +16,7 @@
 // new entries lie behind its live ones, and what every CTA reads (ctx, new_rows,
 // held, state) is only written by the CTA that arrives last, after its scan.
 #include "paged.cuh"
+#include "ptx.cuh"
 
 namespace cllm {
 
@@ -70,6 +71,8 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   int* first = sm_req + 3 * B; // ring index of the first page taken or given back
   int* start = sm_req + 4 * B; // position of the first new row
   if (tid == 0) sm_taken = 0;
+  pdl_launch_dependents();
+  pdl_wait();
 
   // the ring's words are the caller's: whatever they hold, indices stay inside it
   const int head = static_cast<int>(static_cast<unsigned>(__ldcg(a.in.state)) % static_cast<unsigned>(N));
@@ -187,8 +190,7 @@ cudaError_t launch_page_plan(const cllm_page_tables& in, const cllm_page_tables&
     if (e != cudaSuccess) return e;
   }
   const int want = max((rows.max_rows + kPlanThreads - 1) / kPlanThreads, (B + kPlanThreads / 32 - 1) / (kPlanThreads / 32));
-  page_plan_kernel<<<min(max(want, 1), 152), kPlanThreads, smem, s>>>(a);
-  return cudaGetLastError();
+  return launch_after(page_plan_kernel, dim3(min(max(want, 1), 152)), kPlanThreads, smem, s, a);
 }
 
 }  // namespace cllm

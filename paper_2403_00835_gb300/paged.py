@@ -20,6 +20,7 @@ type, device or shape raise ValueError, what the library refuses CllmError;
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional
 
 import torch
@@ -52,14 +53,10 @@ class _Desc(ctypes.Structure):
                 ("stride_page", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_pos", ctypes.c_int64)]
 
 
-class _Attn(ctypes.Structure):
-    _fields_ = [("layer", ctypes.c_int), ("batch", ctypes.c_int), ("rows", ctypes.c_int), ("q", ctypes.c_void_p),
-                ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
-                ("q_head_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
-                ("out_head_stride", ctypes.c_int64), ("row_start", ctypes.c_void_p), ("seq_len", ctypes.c_void_p),
-                ("table", ctypes.c_void_p), ("table_width", ctypes.c_int), ("scale", ctypes.c_float),
-                ("window", ctypes.c_int), ("mask", ctypes.c_void_p), ("mask_words", ctypes.c_int)]
-
+# cllm_paged_rows and cllm_paged_attn as they lie in memory (native alignment): one call
+# fills them, which is a third of what a ctypes structure's fields take.
+_ROWS_IN = struct.Struct("@2i4P4q3Pi")
+_ATTN = struct.Struct("@3i3P4q3PifiPi")
 
 _lib = None
 
@@ -69,13 +66,13 @@ def load():
     global _lib
     if _lib is None:
         lib = _c.load()
-        vp, i, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+        vp, i = ctypes.c_void_p, ctypes.c_int
         lib.cllm_page_plan.argtypes = [vp, vp, vp, i, vp, vp, vp]
         lib.cllm_paged_create.argtypes = [ctypes.POINTER(_Desc), ctypes.POINTER(vp)]
         lib.cllm_paged_destroy.argtypes = [vp]
         lib.cllm_paged_destroy.restype = None
         lib.cllm_paged_status.argtypes = [vp, vp]
-        lib.cllm_paged_append.argtypes = [vp, i, i, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i, vp, vp]
+        lib.cllm_paged_append.argtypes = [vp, vp, vp]
         lib.cllm_paged_attention.argtypes = [vp, vp, vp]
         for name in EXPORTS:
             if name != "cllm_paged_destroy":
@@ -84,19 +81,23 @@ def load():
     return _lib
 
 
-def _tensor(t, what: str, dtype, shape=None, device=None):
+def _tensor(t, what: str, dtype, shape=None, index=None):
     """A contiguous CUDA tensor's address."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()):
         raise ValueError(f"{what}: need a contiguous {dtype} CUDA tensor")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{what}: need shape {tuple(shape)}, got {tuple(t.shape)}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what}: on {t.device}, the others on {device}")
+    if index is not None and t.get_device() != index:
+        raise ValueError(f"{what}: on {t.device}, the others on cuda:{index}")
     return t.data_ptr()
 
 
-def _stream(stream, device) -> int:
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+# the current stream's handle without the Stream object around it (a sixth of a call)
+_current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _stream(stream, index: int) -> int:
+    return _current(index) if stream is None else stream.cuda_stream
 
 
 class PageTables:
@@ -108,7 +109,7 @@ class PageTables:
     def __init__(self, table, held=None, ring=None, state=None, page_size: int = 16):
         if not (isinstance(table, torch.Tensor) and table.dim() == 2):
             raise ValueError("table: need a [max_batch][width] tensor")
-        i32, dev = torch.int32, table.device
+        i32, dev = torch.int32, table.get_device() if table.is_cuda else None
         s = _Tables(_tensor(table, "table", i32))
         s.max_batch, s.width = table.shape
         s.page_size = page_size
@@ -118,7 +119,8 @@ class PageTables:
             s.state = _tensor(state, "state", i32, (4,), dev)
             s.n_pages = ring.numel()
         self.table, self.held, self.ring, self.state, self.page_size = table, held, ring, state, page_size
-        self._s, self._p = s, ctypes.addressof(s)
+        self._s, self._p, self._dev = s, ctypes.addressof(s), dev
+        self._table, self._width, self._batch = s.table, s.width, s.max_batch
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, max_batch: int, width: int, device="cuda"):
@@ -137,7 +139,7 @@ class PageRows:
     def __init__(self, row_start, seq_len, granted=None, slots=None, positions=None):
         i32 = torch.int32
         s = _Rows(_tensor(row_start, "row_start", i32))
-        dev, n = row_start.device, row_start.numel() - 1
+        dev, n = row_start.get_device(), row_start.numel() - 1
         s.seq_len = _tensor(seq_len, "seq_len", i32, (n,), dev)
         if granted is not None:
             s.granted = _tensor(granted, "granted", i32, (n,), dev)
@@ -146,7 +148,8 @@ class PageRows:
             s.max_rows = slots.numel()
         self.row_start, self.seq_len, self.granted, self.slots, self.positions = row_start, seq_len, granted, slots, positions
         self.batch = n
-        self._s, self._p = s, ctypes.addressof(s)
+        self._s, self._p, self._dev = s, ctypes.addressof(s), dev
+        self._start, self._len, self._max = s.row_start, s.seq_len, n
 
     @classmethod
     def empty(cls, max_batch: int, max_rows: int, device="cuda"):
@@ -162,10 +165,10 @@ def plan(tables: PageTables, rows: PageRows, ctx, new_rows, out: Optional[PageTa
     out = tables if out is None else out
     if tables.held is None or out.held is None or rows.slots is None:
         raise ValueError("plan needs whole tables and rows")
-    dev, b = tables.table.device, ctx.numel()
+    dev, b = tables._dev, ctx.numel()
     c = _tensor(ctx, "ctx", torch.int32, None, dev)
     n = _tensor(new_rows, "new_rows", torch.int32, ctx.shape, dev)
-    if rows.row_start.device != dev or rows.seq_len.numel() < b:
+    if rows._dev != dev or rows._max < b:
         raise ValueError("rows: on another device, or too small for the batch")
     rc = load().cllm_page_plan(tables._p, out._p, rows._p, b, c, n, _stream(stream, dev))
     if rc:
@@ -194,9 +197,10 @@ class PagedCache:
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             _c._check(lib.cllm_paged_create(ctypes.byref(d), ctypes.byref(h)), "cllm_paged_create")
-        self._h, self._lib = h, lib
-        self._a = _Attn()
-        self._ap = ctypes.addressof(self._a)
+        self._h, self._lib, self._dev = h, lib, k.get_device()
+        self._args = ctypes.create_string_buffer(max(_ROWS_IN.size, _ATTN.size))
+        self._argp = ctypes.addressof(self._args)
+        self._scale = self.head_dim ** -0.5
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -209,40 +213,39 @@ class PagedCache:
         except Exception:
             pass
 
-    def _heads(self, t, what: str, heads: int):
+    def _heads(self, t, what: str, rows: int, heads: int):
         """Rows of heads side by side: (address, row stride)."""
-        if not (isinstance(t, torch.Tensor) and t.dtype == self.dtype and t.device == self.device and t.dim() == 3
-                and t.shape[1] == heads and t.shape[2] == self.head_dim and t.stride(2) == 1
-                and (heads == 1 or t.stride(1) == self.head_dim)):
-            raise ValueError(f"{what}: need [rows][{heads}][{self.head_dim}] {self.dtype} on {self.device}, heads side by side")
-        return t.data_ptr(), t.stride(0)
+        hd = self.head_dim
+        if isinstance(t, torch.Tensor) and t.dtype is self.dtype and t.get_device() == self._dev and t.shape == (rows, heads, hd):
+            row, head, one = t.stride()
+            if one == 1 and (head == hd or heads == 1):
+                return t.data_ptr(), row
+        raise ValueError(f"{what}: need [{rows}][{heads}][{hd}] {self.dtype} on {self.device}, heads side by side")
 
     def append(self, layer: int, k, v, slots, q=None, q_out=None, rope=None, positions=None, stream=None):
-        """Write rows k, v [T][kv_heads][hd] into slots (int64 [T]; -1: none).  With
-        rope (float32 [max_pos][hd/2][2]: cos, sin) K is rotated by positions
-        (int32 [T]), and q [T][n_heads][hd] into q_out (None: in place)."""
-        kp, ks = self._heads(k, "k", self.n_kv_heads)
-        vp, vs = self._heads(v, "v", self.n_kv_heads)
+        """Write rows k, v [T][kv_heads][hd] into slots (int64 [T] or more; -1: none).
+        With rope (float32 [max_pos][hd/2][2]: cos, sin) K is rotated by positions
+        (int32 [T] or more), and q [T][n_heads][hd] into q_out (None: in place)."""
         t = k.shape[0]
-        if v.shape[0] != t or slots.numel() < t:
-            raise ValueError("k, v and slots: different numbers of rows")
-        qp = qs = op = os = rp = pp = None
-        max_pos = 0
+        kp, ks = self._heads(k, "k", t, self.n_kv_heads)
+        vp, vs = self._heads(v, "v", t, self.n_kv_heads)
+        sp = _tensor(slots, "slots", torch.int64, None, self._dev)
+        if slots.numel() < t:
+            raise ValueError("slots: fewer than rows")
+        qp = qs = op = os = rp = pp = max_pos = 0
         if rope is not None:
             max_pos = rope.shape[0]
-            rp = _tensor(rope, "rope", torch.float32, (max_pos, self.head_dim // 2, 2), self.device)
-            pp = _tensor(positions, "positions", torch.int32, None, self.device)
+            rp = _tensor(rope, "rope", torch.float32, (max_pos, self.head_dim // 2, 2), self._dev)
+            pp = _tensor(positions, "positions", torch.int32, None, self._dev)
             if positions.numel() < t:
                 raise ValueError("positions: fewer than rows")
             if q is not None:
-                qp, qs = self._heads(q, "q", self.n_heads)
-                op, os = (qp, qs) if q_out is None else self._heads(q_out, "q_out", self.n_heads)
-                if q.shape[0] != t or (q_out is not None and q_out.shape[0] != t):
-                    raise ValueError("q, q_out and k: different numbers of rows")
+                qp, qs = self._heads(q, "q", t, self.n_heads)
+                op, os = (qp, qs) if q_out is None else self._heads(q_out, "q_out", t, self.n_heads)
         elif q is not None:
             raise ValueError("q is only rotated: pass rope")
-        rc = self._lib.cllm_paged_append(self._h, layer, t, kp, ks, vp, vs, _tensor(slots, "slots", torch.int64, None, self.device),
-                                         qp, qs or 0, op, os or 0, rp, max_pos, pp, _stream(stream, self.device))
+        _ROWS_IN.pack_into(self._args, 0, layer, t, kp, vp, qp, op, ks, vs, qs, os, sp, rp, pp, max_pos)
+        rc = self._lib.cllm_paged_append(self._h, self._argp, _stream(stream, self._dev))
         if rc:
             _c._check(rc, "cllm_paged_append")
 
@@ -253,31 +256,26 @@ class PagedCache:
         scale: default head_dim ** -0.5.  window: keys nearer than that (0: all).
         block_mask: int32 [T][words], bit j of word w: the row sees new token 32 w + j of
         its request (None: causal)."""
+        dev, dtype = self._dev, self.dtype
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        shape = (q.shape[0], self.n_heads, self.head_dim)
-        for t, what in ((q, "q"), (out, "out")):
-            if not (t.shape == shape and t.dtype == self.dtype and t.device == self.device and t.stride(2) == 1):
-                raise ValueError(f"{what}: need [rows][{self.n_heads}][{self.head_dim}] {self.dtype} on {self.device}")
-        if tables.page_size != self.page_size or rows.batch > tables._s.max_batch or tables.table.device != self.device \
-                or rows.row_start.device != self.device:
+            out = torch.empty(q.shape, dtype=dtype, device=self.device)
+        t = q.shape[0]
+        shape = (t, self.n_heads, self.head_dim)
+        qs, qh, q1 = q.stride() if q.shape == shape else (0, 0, 0)
+        os, oh, o1 = out.stride() if out.shape == shape else (0, 0, 0)
+        if not (q1 == 1 and o1 == 1 and q.dtype is dtype and out.dtype is dtype and q.get_device() == dev
+                and out.get_device() == dev):
+            raise ValueError(f"q and out: need [rows][{self.n_heads}][{self.head_dim}] {dtype} on {self.device}")
+        if tables.page_size != self.page_size or rows.batch > tables._batch or tables._dev != dev or rows._dev != dev:
             raise ValueError("rows and tables: another page size or device, or more requests than tables")
-        a = self._a
-        a.layer, a.batch, a.rows = layer, rows.batch, shape[0]
-        a.q, a.out = q.data_ptr(), out.data_ptr()
-        a.q_stride, a.q_head_stride, _ = q.stride()
-        a.out_stride, a.out_head_stride, _ = out.stride()
-        a.lse = None if lse is None else _tensor(lse, "lse", torch.float32, shape[:2], self.device)
-        a.row_start, a.seq_len = rows._s.row_start, rows._s.seq_len
-        a.table, a.table_width = tables._s.table, tables._s.width
-        a.scale = self.head_dim ** -0.5 if scale is None else scale
-        a.window = window
-        if block_mask is None:
-            a.mask, a.mask_words = None, 0
-        else:
-            a.mask = _tensor(block_mask, "block_mask", torch.int32, (shape[0], block_mask.shape[1]), self.device)
-            a.mask_words = block_mask.shape[1]
-        rc = self._lib.cllm_paged_attention(self._h, self._ap, _stream(stream, self.device))
+        lp = 0 if lse is None else _tensor(lse, "lse", torch.float32, (t, self.n_heads), dev)
+        mp = words = 0
+        if block_mask is not None:
+            words = block_mask.shape[1]
+            mp = _tensor(block_mask, "block_mask", torch.int32, (t, words), dev)
+        _ATTN.pack_into(self._args, 0, layer, rows.batch, t, q.data_ptr(), out.data_ptr(), lp, qs, qh, os, oh, rows._start,
+                        rows._len, tables._table, tables._width, self._scale if scale is None else scale, window, mp, words)
+        rc = self._lib.cllm_paged_attention(self._h, self._argp, _stream(stream, dev))
         if rc:
             _c._check(rc, "cllm_paged_attention")
         return out
@@ -285,4 +283,4 @@ class PagedCache:
     def check(self, stream=None):
         """Wait for the stream; raise CllmError if a call found a page, slot or
         position outside its pool or table, or a wait ran out (and forget it)."""
-        _c._check(self._lib.cllm_paged_status(self._h, _stream(stream, self.device)), "cllm_paged_status")
+        _c._check(self._lib.cllm_paged_status(self._h, _stream(stream, self._dev)), "cllm_paged_status")

@@ -46,9 +46,9 @@ def test_null_caches(lib):
     assert lib.cllm_paged_create(None, None) == EINVAL
     lib.cllm_paged_destroy(None)  # no-op
     assert lib.cllm_paged_status(None, None) == EINVAL
-    assert lib.cllm_paged_append(None, 0, 1, P, 64, P, 64, P, None, 0, None, 0, None, 0, None, None) == EINVAL
-    a = paged._Attn()
-    assert lib.cllm_paged_attention(None, ctypes.addressof(a), None) == EINVAL
+    zeros = ctypes.create_string_buffer(256)
+    assert lib.cllm_paged_append(None, ctypes.addressof(zeros), None) == EINVAL
+    assert lib.cllm_paged_attention(None, ctypes.addressof(zeros), None) == EINVAL
 
 
 def _plan(lib, B=2, ctx=P, new=P, other=None, rows=None, **kw):
