@@ -174,7 +174,9 @@ typedef struct {
 } cllm_paged_attn;
 
 /* Errors: EINVAL (null or misaligned pointers, strides not multiples of 16 bytes,
- * sizes outside their ranges, scale not positive and finite), ECUDA. */
+ * sizes outside their ranges, scale not positive and finite), EUNSUPPORTED (rows x
+ * table_width so large that the work may exceed 2^31 - 1 units of a few rows and 64
+ * keys: cut the step), ECUDA. */
 int cllm_paged_attention(cllm_paged *cache, const cllm_paged_attn *a, void *cuda_stream);
 
 #ifdef __cplusplus

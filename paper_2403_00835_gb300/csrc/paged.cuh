@@ -19,6 +19,7 @@ struct PagedAttnArgs {
   const int* table;
   int table_width, batch, rows;
   int H, Hkv, group;       // group = H / Hkv query heads share a key/value head
+  int group_inv;           // x / group = x * group_inv >> 16 for x < 256 (ceil(2^16 / group), group <= 64)
   float scale_log2;        // scale * log2(e)
   int window;
   const uint32_t* mask;
@@ -54,8 +55,10 @@ inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, si
 }
 
 // Partials: CTA c's slot 2c is a tile that began in an earlier CTA, slot 2c + 1
-// one that it begins and does not end.
-constexpr int kPagedPartRows = 256;  // most rows of a tile
+// one that it begins and does not end.  The tensor-memory kernel has a CTA and slots of
+// 256 rows per SM, the others two CTAs at most and fewer rows.
+constexpr int kPagedPartRows = 256;
+constexpr int kPagedCtas = 2;  // CTAs per SM, at most
 
 cudaError_t launch_page_plan(const cllm_page_tables& in, const cllm_page_tables& out, const cllm_page_rows& rows,
                              int B, const int* ctx, const int* new_rows, cudaStream_t s);
@@ -80,13 +83,16 @@ cudaError_t paged_attention_f32_set_attributes();
 cudaError_t launch_paged_attention_tc(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
                                       int hold, int grid, cudaStream_t s);
 cudaError_t paged_attention_tc_set_attributes();
-bool paged_pool_map(CUtensorMap* m, const void* pool, const cllm_paged_desc& d);
+// a pool in boxes of 64 columns and `keys` positions, or a page's if that is less
+bool paged_pool_map(CUtensorMap* m, const void* pool, const cllm_paged_desc& d, int keys);
 // queries of a tile of `rows` rows: group heads of rows / group tokens, row = token * group + head
 bool paged_query_map(CUtensorMap* m, const PagedAttnArgs& a, int dtype, int hd, int rows);
-// 16-bit pools, few rows (paged_attn_mma.cu): tiles of 16, 32 or 64 rows (tiles = 1, 2, 4; 16 tiles >= group);
-// hold: 1 + the chunk of a piece at which the loading warp gives up
-cudaError_t launch_paged_attention_mma(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
-                                       int tiles, int hold, int grid, cudaStream_t s);
-cudaError_t paged_attention_mma_set_attributes();
+// 16-bit pools, few rows (paged_attn_mma.cu): tiles of 16 rows, group at most 16; k, v:
+// maps of 64 positions; sms: SMs of the device; hold: 1 + the chunk of a piece at which
+// the loading warp gives up
+constexpr int kFewRows = 16, kFewKeys = 64;
+cudaError_t launch_paged_attention_few(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
+                                       int hold, int sms, cudaStream_t s);
+cudaError_t paged_attention_few_set_attributes();
 
 }  // namespace cllm

@@ -15,16 +15,15 @@ struct cllm_paged {
   int dev = 0, sms = 0, page_shift = 0, es = 0;
   float* part_o = nullptr;
   float2* part_ml = nullptr;
-  int* tickets = nullptr;  // one per CTA, then the status word
+  int* tickets = nullptr;  // one per CTA, then the status word (all in part_o's allocation)
+  int n_tickets = 0;
   int* err = nullptr;
-  CUtensorMap mk, mv;      // the pools (16-bit types)
+  CUtensorMap mk, mv, mk_few, mv_few;  // the pools (16-bit types) in boxes of 128 and 64 positions
   int hold = 0;            // test hook
 };
 
 namespace {
 
-// 16-bit pools: up to this many rows to a key/value head run on warp-level MMAs.
-constexpr int kFewRows = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -66,8 +65,6 @@ extern "C" void cllm_paged_destroy(cllm_paged* c) {
   cudaSetDevice(c->dev);
   cudaDeviceSynchronize();
   cudaFree(c->part_o);
-  cudaFree(c->part_ml);
-  cudaFree(c->tickets);
   if (back) cudaSetDevice(dev);
   delete c;
 }
@@ -112,25 +109,33 @@ extern "C" int cllm_paged_create(const cllm_paged_desc* desc, cllm_paged** out) 
   int rc = CLLM_OK;
   do {
     e = es == 4 ? paged_attention_f32_set_attributes() : paged_attention_tc_set_attributes();
-    if (e == cudaSuccess && es == 2) e = paged_attention_mma_set_attributes();
+    if (e == cudaSuccess && es == 2) e = paged_attention_few_set_attributes();
     if (e != cudaSuccess) {
       rc = cuda_fail(e, "paged_create");
       break;
     }
-    if (es == 2 && (!paged_pool_map(&c->mk, d.k, c->d) || !paged_pool_map(&c->mv, d.v, c->d))) {
+    if (es == 2 && (!paged_pool_map(&c->mk, d.k, c->d, 128) || !paged_pool_map(&c->mv, d.v, c->d, 128) ||
+                    !paged_pool_map(&c->mk_few, d.k, c->d, kFewKeys) || !paged_pool_map(&c->mv_few, d.v, c->d, kFewKeys))) {
       rc = CLLM_EINVAL;
       break;
     }
-    const size_t slots = 2 * static_cast<size_t>(sms);
-    if (lib_malloc(reinterpret_cast<void**>(&c->part_o), slots * kPagedPartRows * d.head_dim * 4) != cudaSuccess ||
-        lib_malloc(reinterpret_cast<void**>(&c->part_ml), slots * kPagedPartRows * 8) != cudaSuccess ||
-        lib_malloc(reinterpret_cast<void**>(&c->tickets), (sms + 1) * 4) != cudaSuccess) {
+    // (one allocation: it takes as long as the rest of the call)
+    const size_t rows = 2 * static_cast<size_t>(sms) * kPagedPartRows;
+    const size_t tickets = static_cast<size_t>(sms) * kPagedCtas;
+    const size_t so = rows * d.head_dim * 4, sm = rows * 8;
+    static_assert(kPagedPartRows >= 64 * kPagedCtas, "slots of the kernels with several CTAs per SM");
+    void* base = nullptr;
+    if (lib_malloc(&base, so + sm + (tickets + 1) * 4) != cudaSuccess) {
       rc = CLLM_ENOMEM;
       break;
     }
-    c->err = c->tickets + sms;
+    c->part_o = static_cast<float*>(base);
+    c->part_ml = reinterpret_cast<float2*>(static_cast<char*>(base) + so);
+    c->tickets = reinterpret_cast<int*>(static_cast<char*>(base) + so + sm);
+    c->n_tickets = static_cast<int>(tickets);
+    c->err = c->tickets + tickets;
     // (the default stream orders the clearing before any later work)
-    e = cudaMemset(c->tickets, 0, (sms + 1) * 4);
+    e = cudaMemset(c->tickets, 0, (tickets + 1) * 4);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) rc = cuda_fail(e, "paged_create");
   } while (false);
@@ -150,7 +155,7 @@ extern "C" int cllm_paged_status(cllm_paged* c, void* cuda_stream) {
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e == cudaSuccess && err != 0) {
     // (a timed-out launch may leave arrival counters behind)
-    e = cudaMemsetAsync(c->tickets, 0, (c->sms + 1) * 4, s);
+    e = cudaMemsetAsync(c->tickets, 0, (c->n_tickets + 1) * 4, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   }
   if (e != cudaSuccess) return cuda_fail(e, "paged_status");
@@ -203,6 +208,11 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
       static_cast<int64_t>(p->table_width) * d.page_size > 0x7fffffff ||
       (p->mask && (p->mask_words < 1 || !aligned(p->mask, 4))))
     return CLLM_EINVAL;
+  // the kernels count (tile, 64 or 128 keys) units in 32 bits; tiles have at least 16 / group tokens
+  const int group = d.n_heads / d.n_kv_heads;
+  const int64_t tiles = p->rows / (group < 16 ? 16 / group : 1) + p->batch;
+  const int64_t chunks = (static_cast<int64_t>(p->table_width) * d.page_size >> 6) + 1;
+  if (tiles > 0x7fffffff / (chunks * d.n_kv_heads)) return CLLM_EUNSUPPORTED;
   PagedAttnArgs a{};
   const int64_t at = p->layer * d.stride_layer * c->es;
   a.q = p->q, a.out = p->out, a.lse = p->lse;
@@ -211,8 +221,9 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
   a.out_row = p->rows == 1 ? d.head_dim : p->out_stride, a.out_head = d.n_heads == 1 ? d.head_dim : p->out_head_stride;
   a.row_start = p->row_start, a.seq_len = p->seq_len, a.table = p->table;
   a.table_width = p->table_width, a.batch = p->batch, a.rows = p->rows;
-  a.H = d.n_heads, a.Hkv = d.n_kv_heads, a.group = d.n_heads / d.n_kv_heads;
+  a.H = d.n_heads, a.Hkv = d.n_kv_heads, a.group = group;
   a.scale_log2 = p->scale * kLog2e;
+  a.group_inv = (65536 + group - 1) / group;
   a.window = p->window, a.mask = p->mask, a.mask_words = p->mask_words;
   a.k = static_cast<const char*>(d.k) + at, a.v = static_cast<const char*>(d.v) + at;
   a.s_page = d.stride_page, a.s_head = d.stride_head, a.s_pos = d.stride_pos;
@@ -224,9 +235,8 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
   cudaError_t e;
   if (c->es == 4) {
     e = launch_paged_attention_f32(a, d.head_dim, c->sms, st);
-  } else if (rows <= kFewRows) {
-    const int tiles = rows <= 16 && a.group <= 16 ? 1 : rows <= 32 && a.group <= 32 ? 2 : 4;
-    e = launch_paged_attention_mma(a, c->mk, c->mv, d.dtype, d.head_dim, tiles, c->hold, c->sms, st);
+  } else if (rows <= kFewRows && group <= kFewRows) {
+    e = launch_paged_attention_few(a, c->mk_few, c->mv_few, d.dtype, d.head_dim, c->hold, c->sms, st);
   } else {
     e = launch_paged_attention_tc(a, c->mk, c->mv, d.dtype, d.head_dim, c->hold, c->sms, st);
   }

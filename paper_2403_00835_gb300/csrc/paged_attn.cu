@@ -14,7 +14,7 @@ namespace cllm {
 namespace {
 
 constexpr int kPThreads = 256;
-constexpr int kPChunk = 64;
+constexpr int kPChunk = 64;  // 2^6
 
 template <int HD, int BM>
 struct PagedSmem {
@@ -22,7 +22,7 @@ struct PagedSmem {
   float k[kPChunk][HD + 4];
   float v[kPChunk][HD + 4];
   float p[BM][kPChunk + 4];
-  long long scan[33];
+  unsigned scan[32];
   RunStart run;
   unsigned bad[2];  // rows whose result is not finite
   int last;
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
 
 template <int HD, int BM>
 cudaError_t launch(const PagedAttnArgs& a, int grid, cudaStream_t s) {
-  const PagedGeom g{BM / a.group, BM / a.group, kPChunk, 1};
+  const PagedGeom g{BM / a.group, BM / a.group, 6, 1};
   return launch_after(paged_attn_kernel<float, HD, BM>, dim3(grid), kPThreads, sizeof(PagedSmem<HD, BM>), s, a, g);
 }
 

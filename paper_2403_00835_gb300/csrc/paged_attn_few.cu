@@ -1,17 +1,17 @@
 // Attention of few rows over a paged cache (cllm_paged_attention), fp16 and bf16
-// pools: greedy decoding and blocks of a few tokens.
+// pools: greedy decoding and blocks of a few tokens, up to 16 rows to a key/value head.
 //
 //   S = Q K^T,  p = 2^(scale log2(e) S - m),  O = sum p V,  l = sum p,  out = O / l
 //
-// in one pass over the keys.  With up to 64 rows to a key/value head the keys'
-// bytes bound the work (64 rows x 128 keys are 4.2 MFLOP to 64 KB), and what is left to
-// lose is latency: the tensor-memory kernel hands a chunk from loads to MMAs to rows to
-// MMAs and back, and has one warp of a slot at work on 32 rows.  Here 8 warps
-// take every chunk of 128 keys at once, each 16 rows x 128 / (8 / MT) keys with
-// warp-level MMAs, scores and probabilities in registers, and its own running maximum,
-// sum and output; they meet at the tile's end only, in shared memory.  Warp 8
-// streams K and V through a ring of 128-key tiles.  The same row's keys are dealt to
-// 8 / MT warps in fixed order, so results do not depend on timing.
+// in one pass over the keys.  The keys' bytes bound the work (16 rows x 128 keys are
+// 1 MFLOP to 64 KB), and what there is to lose is latency: the tensor-memory kernel
+// hands a chunk from loads to MMAs to rows to MMAs and back, with one warp of a
+// slot at work on 16 rows.  Here 4 warps take every chunk of 64 keys, each all rows x 16
+// keys, with warp-level MMAs, scores and probabilities in registers, and its own running
+// maximum, sum and output; they meet at the tile's end only, in shared memory.  Warp 4
+// streams K and V through a ring of 64-key tiles.  Two CTAs share an SM, so that one's
+// tile has its beginning or end while the other's streams.  A row's keys are dealt to the
+// warps in fixed order, so results do not depend on timing.
 //
 // Rounding: as in the tensor-memory kernel, P goes to the pools' type.
 #include "paged_pipe.cuh"
@@ -20,19 +20,19 @@ namespace cllm {
 
 namespace {
 
-constexpr int kMmaThreads = 288;  // 8 row warps and the loading one
+constexpr int kFewWarps = 4, kFewThreads = 32 * (kFewWarps + 1);
 
-template <int HD, int MT>
-struct MmaSmem {
-  static constexpr int kRing = HD == 128 ? 4 : 8;
-  static constexpr int kTile = kPageChunk * HD * 2;
-  static constexpr int kRows = 16 * MT;
+template <int HD>
+struct FewSmem {
+  static constexpr int kShift = 6, kRing = HD == 128 ? 4 : 8;
+  static constexpr int kTile = kFewKeys * HD * 2;
+  static constexpr int kRows = kFewRows, kRowWarps = kFewWarps, kPartRows = 32;
   static constexpr bool kAhead = false, kIssuer = false;
   alignas(1024) uint8_t q[1][kRows * HD * 2];
   alignas(1024) uint8_t ring[kRing][kTile];
-  float o[8][16][HD + 4];  // the warps' outputs at a tile's end
-  float2 wml[8][16];
-  float2 ml[2][128];
+  float o[kFewWarps][kFewRows][HD + 4];  // the warps' outputs at a tile's end
+  float2 wml[kFewWarps][kFewRows];
+  float2 ml[1][32];  // also the scratch of run_start
   uint64_t full[kRing], empty[kRing], qfull, qempty;
   uint64_t pfull[kPagePieces], pempty[kPagePieces], pfree[kPagePieces];
   PagePiece piece[kPagePieces], cut;
@@ -40,7 +40,8 @@ struct MmaSmem {
   unsigned bad[8];
   int abort, busy, last;
 };
-static_assert(sizeof(MmaSmem<128, 4>) <= 227 * 1024, "shared memory");
+static_assert(2 * (sizeof(FewSmem<128>) + 1024) <= 228 * 1024, "two CTAs to an SM");
+static_assert(1 << FewSmem<64>::kShift == kFewKeys, "keys of a tile");
 
 template <class T> struct Mma16;
 template <> struct Mma16<__half> {
@@ -55,16 +56,14 @@ __device__ __forceinline__ uint32_t tile_addr(uint32_t base, int rows, int row, 
   return base + (c >> 3) * rows * 128 + row * 128 + (((c & 7) ^ (row & 7)) << 4);
 }
 
-template <class T, int HD, int MT>
-__device__ __forceinline__ void run_few(MmaSmem<HD, MT>& s, const PagedAttnArgs& a, const PagedGeom& g) {
-  using S = MmaSmem<HD, MT>;
-  constexpr int KW = 8 / MT, KEYS = kPageChunk / KW;  // warps that share a row's keys, keys of a warp in a chunk
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, mt = warp % MT, kw = warp / MT;
+template <class T, int HD>
+__device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, const PagedGeom& g) {
+  using S = FewSmem<HD>;
+  constexpr int KW = kFewWarps, KEYS = kFewKeys / KW;  // warps that share a row's keys, keys of a warp in a chunk
+  static_assert(KEYS == 16, "a k step of the second product");
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int quad = lane >> 2, col = (lane & 3) * 2, tt = g.slot_tok;
-  auto warp_wait = [&](uint64_t* bar, uint32_t parity) {
-    if (lane == 0) page_wait(bar, parity, &s.abort, &s.busy);
-    __syncwarp();
-  };
+  auto warp_wait = [&](uint64_t* bar, uint32_t parity) { page_wait(bar, parity, &s.abort, &s.busy); };
   RingAt<S::kRing> at;
   RingAt<kPagePieces> pat;
   uint32_t nq = 0;       // pieces with keys so far
@@ -85,16 +84,16 @@ __device__ __forceinline__ void run_few(MmaSmem<HD, MT>& s, const PagedAttnArgs&
       warp_wait(&s.qfull, nq++ & 1);
       const uint32_t qb = smem_u32(s.q[0]);
 #pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk) ldmatrix_x4_a(q[kk], tile_addr(qb, S::kRows, mt * 16 + (lane & 15), kk * 2 + (lane >> 4)));
+      for (int kk = 0; kk < HD / 16; ++kk) ldmatrix_x4_a(q[kk], tile_addr(qb, S::kRows, lane & 15, kk * 2 + (lane >> 4)));
       __syncwarp();
       if (lane == 0) mbar_arrive(&s.qempty);
       RowKeys rk[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) rk[u] = row_keys(a, p.n, p.len, p.row0, p.t0 + min(mt * 16 + quad + 8 * u, rows - 1) / a.group);
+      for (int u = 0; u < 2; ++u) rk[u] = row_keys(a, p.n, p.len, p.row0, p.t0 + (min(quad + 8 * u, rows - 1) * a.group_inv >> 16));
       const int from = max(rk[0].lo, rk[1].lo), to = min(rk[0].bits != nullptr ? rk[0].ctx : rk[0].hi, rk[1].bits != nullptr ? rk[1].ctx : rk[1].hi);
 #pragma unroll 1
       for (int i = 0; i < n; ++i) {
-        const int kb = (ca + i) * kPageChunk + kw * KEYS;  // this warp's keys: [kb, kb + KEYS)
+        const int kb = (ca + i) * kFewKeys + warp * KEYS;  // this warp's keys: [kb, kb + KEYS)
         const bool some = kb < hi && kb + KEYS > lo;
         const uint32_t kt = at.i, k_phase = at.phase;
         ++at;
@@ -113,7 +112,7 @@ __device__ __forceinline__ void run_few(MmaSmem<HD, MT>& s, const PagedAttnArgs&
 #pragma unroll
             for (int j = 0; j < KEYS / 16; ++j) {
               uint32_t b[4];
-              ldmatrix_x4_a(b, tile_addr(base, kPageChunk, kw * KEYS + j * 16 + (lane >> 4) * 8 + (lane & 7), kk * 2 + (lane >> 3 & 1)));
+              ldmatrix_x4_a(b, tile_addr(base, kFewKeys, warp * KEYS + j * 16 + (lane >> 4) * 8 + (lane & 7), kk * 2 + (lane >> 3 & 1)));
               Mma16<T>::mma(x[2 * j], q[kk], b[0], b[1]);
               Mma16<T>::mma(x[2 * j + 1], q[kk], b[2], b[3]);
             }
@@ -172,7 +171,7 @@ __device__ __forceinline__ void run_few(MmaSmem<HD, MT>& s, const PagedAttnArgs&
             for (int c = lane; c < KEYS * HD / 8; c += 32) {
               const int key = kb + c / (HD / 8);
               if (key < lo || key >= hi)
-                *reinterpret_cast<uint4*>(s.ring[vt] + (c % (HD / 8) >> 3) * kPageChunk * 128 + (kw * KEYS + c / (HD / 8)) * 128 + (c & 7) * 16) =
+                *reinterpret_cast<uint4*>(s.ring[vt] + (c % (HD / 8) >> 3) * kFewKeys * 128 + (warp * KEYS + c / (HD / 8)) * 128 + (c & 7) * 16) =
                     make_uint4(0, 0, 0, 0);
             }
             // (before the tile is loaded anew)
@@ -187,7 +186,7 @@ __device__ __forceinline__ void run_few(MmaSmem<HD, MT>& s, const PagedAttnArgs&
 #pragma unroll
             for (int d = 0; d < HD / 16; ++d) {
               uint32_t b[4];
-              ldmatrix_x4_trans_a(b, tile_addr(base, kPageChunk, kw * KEYS + j * 16 + (lane & 15), d * 2 + (lane >> 4)));
+              ldmatrix_x4_trans_a(b, tile_addr(base, kFewKeys, warp * KEYS + j * 16 + (lane & 15), d * 2 + (lane >> 4)));
               Mma16<T>::mma(o[2 * d], pa, b[0], b[1]);
               Mma16<T>::mma(o[2 * d + 1], pa, b[2], b[3]);
             }
@@ -207,44 +206,55 @@ __device__ __forceinline__ void run_few(MmaSmem<HD, MT>& s, const PagedAttnArgs&
       for (int j = 0; j < HD / 8; ++j)
         *reinterpret_cast<float2*>(&s.o[warp][quad + 8 * u][j * 8 + col]) = make_float2(o[j][2 * u], o[j][2 * u + 1]);
     }
-    all_rows();
+    all_rows<S>();
     const bool whole = p.whole;
-    const int part_rows = rows_of_part(a, p);
-    float4* part = reinterpret_cast<float4*>(a.part_o) + static_cast<size_t>(p.slot) * (kPagedPartRows * HD / 4);
-    float2* part_ml = a.part_ml + static_cast<size_t>(p.slot) * kPagedPartRows;
-    for (int i = tid; i < rows * (HD / 4); i += 256) {
+    const int part_rows = rows_of_part<S>(a, p);
+    float4* part = part_of<S, HD>(a, p.slot);
+    float2* part_ml = part_ml_of<S>(a, p.slot);
+    for (int i = tid; i < rows * (HD / 8); i += 32 * kFewWarps) {
       // (a result's columns side by side, a part's rows)
-      const int r = whole ? i / (HD / 4) : i % rows, d4 = whole ? i % (HD / 4) : i / rows;
+      const int r = whole ? i / (HD / 8) : i % rows, d8 = whole ? i % (HD / 8) : i / rows;
       float mm = -INFINITY, ll = 0.f;
       float2 ml[KW];
 #pragma unroll
       for (int c = 0; c < KW; ++c) {
-        ml[c] = s.wml[r / 16 + MT * c][r % 16];
+        ml[c] = s.wml[c][r];
         mm = fmaxf(mm, ml[c].x);
       }
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
 #pragma unroll
       for (int c = 0; c < KW; ++c) {
         if (ml[c].x == -INFINITY) continue;  // none of its keys is seen
-        const float4 y = *reinterpret_cast<const float4*>(&s.o[r / 16 + MT * c][r % 16][d4 * 4]);
+        const float4* from = reinterpret_cast<const float4*>(&s.o[c][r][d8 * 8]);
+        const float4 u = from[0], w = from[1];
         const float f = ex2_ftz(ml[c].x - mm);
         ll = fmaf(ml[c].y, f, ll);
-        x = make_float4(fmaf(y.x, f, x.x), fmaf(y.y, f, x.y), fmaf(y.z, f, x.z), fmaf(y.w, f, x.w));
+        x = make_float4(fmaf(u.x, f, x.x), fmaf(u.y, f, x.y), fmaf(u.z, f, x.z), fmaf(u.w, f, x.w));
+        y = make_float4(fmaf(w.x, f, y.x), fmaf(w.y, f, y.y), fmaf(w.z, f, y.z), fmaf(w.w, f, y.w));
       }
       if (!whole) {
-        part[d4 * part_rows + r] = x;
-        if (d4 == 0) part_ml[r] = make_float2(mm, ll);
+        part[2 * d8 * part_rows + r] = x;
+        part[(2 * d8 + 1) * part_rows + r] = y;
+        if (d8 == 0) part_ml[r] = make_float2(mm, ll);
         continue;
       }
       const float f = ll != 0.f ? 1.f / ll : 0.f;
-      x = ll != 0.f ? make_float4(x.x * f, x.y * f, x.z * f, x.w * f) : make_float4(0.f, 0.f, 0.f, 0.f);
-      if (!isfinite(x.x) || !isfinite(x.y) || !isfinite(x.z) || !isfinite(x.w)) atomicOr(&s.bad[r >> 5], 1u << (r & 31));
-      const int tok = p.t0 + r / a.group, head = p.h * a.group + r % a.group;
-      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + static_cast<long long>(p.row0 + tok) * a.out_row + head * a.out_head + d4 * 4) =
-          make_uint2(Pack16<T>::pack(x.x, x.y), Pack16<T>::pack(x.z, x.w));
-      if (d4 == 0) store_lse(a, p, tok, head, mm, ll);
+      const float z[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+      uint32_t u[4];
+      float any = 0.f;  // (0 * x is NaN for an infinity or NaN)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v0 = ll != 0.f ? z[2 * e] * f : 0.f, v1 = ll != 0.f ? z[2 * e + 1] * f : 0.f;
+        any = fmaf(v0, 0.f, fmaf(v1, 0.f, any));
+        u[e] = Pack16<T>::pack(v0, v1);
+      }
+      if (any != 0.f) atomicOr(&s.bad[r >> 5], 1u << (r & 31));
+      const int rt = r * a.group_inv >> 16, tok = p.t0 + rt, head = p.h * a.group + r - rt * a.group;
+      *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + static_cast<long long>(p.row0 + tok) * a.out_row + head * a.out_head + d8 * 8) =
+          make_uint4(u[0], u[1], u[2], u[3]);
+      if (d8 == 0) store_lse(a, p, tok, head, mm, ll);
     }
-    all_rows();  // (s.o and s.wml are free again)
+    all_rows<S>();  // (s.o and s.wml are free again)
     if (whole) {
       redo_bad<T, HD>(s, a, p, tt);
     } else {
@@ -267,93 +277,81 @@ __device__ __forceinline__ void run_few(MmaSmem<HD, MT>& s, const PagedAttnArgs&
     if (lane == 0) mbar_arrive(&s.pempty[pat.i]);
   }
   if (cut) {
-    all_rows();
+    all_rows<S>();
     merge_if_last<T, HD>(s, a, s.cut, tt, cut_arrivals);
   }
 }
 
-template <class T, int HD, int MT>
-__global__ void __launch_bounds__(kMmaThreads, 1)
-    paged_attn_mma_kernel(const __grid_constant__ PagedMaps m, const __grid_constant__ PagedAttnArgs a, const PagedGeom g,
+template <class T, int HD>
+__global__ void __launch_bounds__(kFewThreads, 2)
+    paged_attn_few_kernel(const __grid_constant__ PagedMaps m, const __grid_constant__ PagedAttnArgs a, const PagedGeom g,
                           const int hold) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  MmaSmem<HD, MT>& s = *reinterpret_cast<MmaSmem<HD, MT>*>(smem_raw);
+  FewSmem<HD>& s = *reinterpret_cast<FewSmem<HD>*>(smem_raw);
   if (smem_u32(smem_raw) & 1023u) {  // (the swizzle's atoms; shared memory starts on one)
     pdl_wait();
     if (threadIdx.x == 0) atomicOr(a.err, DERR_SHAPE);
     return;
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < MmaSmem<HD, MT>::kRing; ++i) {
+    for (int i = 0; i < FewSmem<HD>::kRing; ++i) {
       mbar_init(&s.full[i], 1);
-      mbar_init(&s.empty[i], 8);
+      mbar_init(&s.empty[i], kFewWarps);
     }
     mbar_init(&s.qfull, 1);
-    mbar_init(&s.qempty, 8);
+    mbar_init(&s.qempty, kFewWarps);
     for (int i = 0; i < kPagePieces; ++i) {
       mbar_init(&s.pfull[i], 1);
-      mbar_init(&s.pempty[i], 8);
+      mbar_init(&s.pempty[i], kFewWarps);
     }
     s.abort = s.busy = 0;
     fence_mbar_init();
   }
   if (threadIdx.x < 8) s.bad[threadIdx.x] = 0;
-  if (threadIdx.x == kMmaThreads - 1) {
+  if (threadIdx.x == kFewThreads - 1) {
     tma_prefetch_desc(&m.q);
     tma_prefetch_desc(&m.k);
     tma_prefetch_desc(&m.v);
   }
   pdl_launch_dependents();
   pdl_wait();  // (nothing of the calls before is read above)
-  run_start(a, g, &s.run, reinterpret_cast<long long*>(s.ml));
-  if (threadIdx.x >= 256) issue_loads<HD>(s, a, g, m, hold);
-  else run_few<T, HD, MT>(s, a, g);
+  run_start(a, g, &s.run, reinterpret_cast<unsigned*>(s.ml));
+  if (threadIdx.x >= 32 * kFewWarps) issue_loads<HD>(s, a, g, m, hold);
+  else run_few<T, HD>(s, a, g);
   __syncthreads();
   if (threadIdx.x == 0 && s.abort) atomicOr(a.err, DERR_TIMEOUT);
 }
 
-template <class T, int HD, int MT>
-cudaError_t launch_mma(const PagedMaps& m, const PagedAttnArgs& a, int hold, int grid, cudaStream_t s) {
-  const int tt = 16 * MT / a.group;
-  return launch_after(paged_attn_mma_kernel<T, HD, MT>, dim3(grid), kMmaThreads, sizeof(MmaSmem<HD, MT>), s, m, a,
-                      PagedGeom{tt, tt, kPageChunk, 1}, hold);
-}
 template <class T, int HD>
-cudaError_t launch_mt(const PagedMaps& m, const PagedAttnArgs& a, int tiles, int hold, int grid, cudaStream_t s) {
-  if (tiles == 1) return launch_mma<T, HD, 1>(m, a, hold, grid, s);
-  if (tiles == 2) return launch_mma<T, HD, 2>(m, a, hold, grid, s);
-  return launch_mma<T, HD, 4>(m, a, hold, grid, s);
+cudaError_t launch_few(const PagedMaps& m, const PagedAttnArgs& a, int hold, int sms, cudaStream_t s) {
+  const int tt = kFewRows / a.group;
+  return launch_after(paged_attn_few_kernel<T, HD>, dim3(2 * sms), kFewThreads, sizeof(FewSmem<HD>), s, m, a,
+                      PagedGeom{tt, tt, FewSmem<HD>::kShift, 2}, hold);
 }
 
-template <class T, int HD, int MT>
-cudaError_t attr() {
-  return cudaFuncSetAttribute(paged_attn_mma_kernel<T, HD, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(MmaSmem<HD, MT>));
-}
 template <class T, int HD>
-cudaError_t attrs() {
-  cudaError_t e = attr<T, HD, 1>();
-  if (e == cudaSuccess) e = attr<T, HD, 2>();
-  return e == cudaSuccess ? attr<T, HD, 4>() : e;
+cudaError_t attr() {
+  return cudaFuncSetAttribute(paged_attn_few_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewSmem<HD>));
 }
 
 }  // namespace
 
-cudaError_t paged_attention_mma_set_attributes() {
-  cudaError_t e = attrs<__half, 64>();
-  if (e == cudaSuccess) e = attrs<__half, 128>();
-  if (e == cudaSuccess) e = attrs<__nv_bfloat16, 64>();
-  return e == cudaSuccess ? attrs<__nv_bfloat16, 128>() : e;
+cudaError_t paged_attention_few_set_attributes() {
+  cudaError_t e = attr<__half, 64>();
+  if (e == cudaSuccess) e = attr<__half, 128>();
+  if (e == cudaSuccess) e = attr<__nv_bfloat16, 64>();
+  return e == cudaSuccess ? attr<__nv_bfloat16, 128>() : e;
 }
 
-cudaError_t launch_paged_attention_mma(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
-                                       int tiles, int hold, int grid, cudaStream_t s) {
+cudaError_t launch_paged_attention_few(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
+                                       int hold, int sms, cudaStream_t s) {
   PagedMaps m;
   m.k = k;
   m.v = v;
-  if (!paged_query_map(&m.q, a, dtype, hd, 16 * tiles)) return cudaErrorInvalidValue;
+  if (!paged_query_map(&m.q, a, dtype, hd, kFewRows)) return cudaErrorInvalidValue;
   if (dtype == CLLM_BF16)
-    return hd == 64 ? launch_mt<__nv_bfloat16, 64>(m, a, tiles, hold, grid, s) : launch_mt<__nv_bfloat16, 128>(m, a, tiles, hold, grid, s);
-  return hd == 64 ? launch_mt<__half, 64>(m, a, tiles, hold, grid, s) : launch_mt<__half, 128>(m, a, tiles, hold, grid, s);
+    return hd == 64 ? launch_few<__nv_bfloat16, 64>(m, a, hold, sms, s) : launch_few<__nv_bfloat16, 128>(m, a, hold, sms, s);
+  return hd == 64 ? launch_few<__half, 64>(m, a, hold, sms, s) : launch_few<__half, 128>(m, a, hold, sms, s);
 }
 
 }  // namespace cllm

@@ -29,10 +29,10 @@ namespace cllm {
 namespace {
 
 constexpr int kTcThreads = 320;  // warps 0-3, 4-7: the slots' rows; 8 MMAs; 9 loads
-constexpr int kTcRows = 128, kTcChunk = kPageChunk, kTcHalf = 64;
+constexpr int kTcRows = 128, kTcShift = 7, kTcChunk = 1 << kTcShift, kTcHalf = 64;
 template <int HD>
 struct TcSmem {
-  static constexpr int kRows = kTcRows;
+  static constexpr int kRows = kTcRows, kRowWarps = 8, kShift = kTcShift, kPartRows = 2 * kTcRows;
   static constexpr bool kAhead = true, kIssuer = true;
   static constexpr int kRing = HD == 128 ? 5 : 10;
   static constexpr int kTile = kTcChunk * HD * 2;
@@ -335,9 +335,9 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
     }
     const bool whole = p.whole;
     // a part: [HD / 4][rows][4], so that the rows' threads write and read side by side
-    const int part_rows = rows_of_part(a, p);
-    float4* part = reinterpret_cast<float4*>(a.part_o) + static_cast<size_t>(p.slot) * (kPagedPartRows * HD / 4);
-    float2* part_ml = a.part_ml + static_cast<size_t>(p.slot) * kPagedPartRows;
+    const int part_rows = rows_of_part<TcSmem<HD>>(a, p);
+    float4* part = part_of<TcSmem<HD>, HD>(a, p.slot);
+    float2* part_ml = part_ml_of<TcSmem<HD>>(a, p.slot);
     const int head = p.h * a.group + row % a.group;
     // 16 columns of a row from column d: a result, or a part of one
     auto store16 = [&](const float (&o)[16], int rr, int d, float scale, bool live) {
@@ -377,7 +377,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       // both slots hold these rows, each over half of the keys; slot t's warps finish
       // the t-th half of the columns
       s.ml[t][row] = make_float2(m, l);
-      all_rows();
+      all_rows<TcSmem<HD>>();
       const float2 ml0 = s.ml[0][row], ml1 = s.ml[1][row];
       bool has[2];
       for (int u = 0; u < 2; ++u) {
@@ -415,7 +415,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       for (int u = 0; u < 2; ++u) no[u] += p.c[u].any();
     }
     if (!whole) {
-      all_rows();
+      all_rows<TcSmem<HD>>();
       int before = 0;
       if (tid == 0) {
         __threadfence();
@@ -431,14 +431,14 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
         if (tid < sizeof(PagePiece) / 4) reinterpret_cast<int*>(&s.cut)[tid] = reinterpret_cast<const int*>(&p)[tid];
       }
     } else if (!two) {
-      all_rows();  // (s.ml is free again)
+      all_rows<TcSmem<HD>>();  // (s.ml is free again)
       redo_bad<T, HD>(s, a, p, tt);
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&s.pempty[pat.i]);
   }
   if (cut) {
-    all_rows();
+    all_rows<TcSmem<HD>>();
     merge_if_last<T, HD>(s, a, s.cut, tt, cut_arrivals);
   }
 }
@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
   pdl_launch_dependents();
   pdl_wait();  // (nothing of the calls before is read above)
-  run_start(a, g, &s.run, reinterpret_cast<long long*>(s.ml));
+  run_start(a, g, &s.run, reinterpret_cast<unsigned*>(s.ml));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -515,7 +515,7 @@ cudaError_t launch_tc(const PagedMaps& m, const PagedAttnArgs& a, int hold, int 
   // their keys would have to be cut and their rows merged, so they are halved instead.
   const long long per_request = (static_cast<long long>(a.rows) + a.batch - 1) / a.batch;
   const bool two = per_request > tt && (per_request + 2 * tt - 1) / (2 * tt) * a.batch * a.Hkv >= grid;
-  const PagedGeom g{two ? 2 * tt : tt, tt, kTcChunk, 2};
+  const PagedGeom g{two ? 2 * tt : tt, tt, kTcShift, 2};
   return launch_after(paged_attn_tc_kernel<T, HD>, dim3(grid), kTcThreads, sizeof(TcSmem<HD>), s, m, a, g, hold);
 }
 
@@ -529,13 +529,13 @@ cudaError_t paged_attention_tc_set_attributes() {
   return e;
 }
 
-bool paged_pool_map(CUtensorMap* m, const void* pool, const cllm_paged_desc& d) {
+bool paged_pool_map(CUtensorMap* m, const void* pool, const cllm_paged_desc& d, int keys) {
   const cuuint64_t dims[5] = {static_cast<cuuint64_t>(d.head_dim), static_cast<cuuint64_t>(d.page_size),
                               static_cast<cuuint64_t>(d.n_kv_heads), static_cast<cuuint64_t>(d.n_pages),
                               static_cast<cuuint64_t>(d.layers)};
   const cuuint64_t strides[4] = {static_cast<cuuint64_t>(d.stride_pos) * 2, static_cast<cuuint64_t>(d.stride_head) * 2,
                                  static_cast<cuuint64_t>(d.stride_page) * 2, static_cast<cuuint64_t>(d.stride_layer) * 2};
-  const cuuint32_t box[5] = {64, static_cast<cuuint32_t>(d.page_size < kTcChunk ? d.page_size : kTcChunk), 1, 1, 1};
+  const cuuint32_t box[5] = {64, static_cast<cuuint32_t>(d.page_size < keys ? d.page_size : keys), 1, 1, 1};
   return make_map_nd(m, d.dtype == CLLM_BF16, pool, 5, dims, strides, box);
 }
 

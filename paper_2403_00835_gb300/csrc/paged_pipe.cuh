@@ -11,7 +11,6 @@
 
 namespace cllm {
 
-constexpr int kPageChunk = 128;  // keys of a unit
 // A row's running maximum follows only growth of more than this (in log2): P may
 // then reach 2^8, and O is rarely rescaled.
 constexpr float kPageSlack = 8.f;
@@ -63,7 +62,7 @@ __device__ __forceinline__ bool page_wait(uint64_t* bar, uint32_t parity, volati
 }
 
 // A row warp's wait for its next piece.  The loading warp always brings one (an end,
-// after a wait of its own has run out), and the 8 row warps have to agree on it: they take no
+// after a wait of its own has run out), and the row warps have to agree on it: they take no
 // notice of the other roles' failures here, and the limit is past all of theirs.
 __device__ __forceinline__ bool piece_wait(uint64_t* bar, uint32_t parity) {
   const uint64_t t0 = globaltimer_ns();
@@ -91,14 +90,15 @@ template <> struct Pack16<__nv_bfloat16> {
 
 // Walk the CTA's run, hand each piece to the other warps, and load its queries, keys and
 // values.
-// S::kAhead: K one tile ahead of V (K0 K1 V0 K2 V1 ..), else K0 V0 K1 V1 ..; S::kIssuer: a
+// S::kShift: log2 of the keys of a tile; S::kAhead: K one tile ahead of V (K0 K1 V0 K2 V1 ..), else K0 V0 K1 V1 ..; S::kIssuer: a
 // warp beside the row warps takes the pieces too.  hold: test hook, 1 + the chunk of a
 // piece at which this warp gives up (0: none).
 template <int HD, class S>
 __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const PagedGeom& g, const PagedMaps& m, int hold) {
-  constexpr int NH = HD / 64, NR = S::kRing;
+  constexpr int NH = HD / 64, NR = S::kRing, kChunk = 1 << S::kShift;
   const int lane = threadIdx.x & 31, tt = g.slot_tok, P = 1 << a.page_shift;
-  const int box = min(P, kPageChunk), boxes = kPageChunk / box;
+  const int box_shift = min(a.page_shift, S::kShift), box = 1 << box_shift;
+  const int j = lane / NH, half = lane % NH;  // this lane's box of a tile and its 64 columns (at most 16 boxes)
   RingAt<NR> at;
   RingAt<kPagePieces> pat;
   uint32_t r = 0, pieces = 0, with_keys = 0;  // loads, pieces, pieces with keys so far
@@ -118,56 +118,64 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
     }
     if (!ok) break;
     ++pieces;
-    if (lane == 0) {
-      PagePiece& o = s.piece[pat.i];
-      o.end = !more;
-      if (more) {
-        o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0, o.lo = p.lo, o.hi = p.hi;
-        o.ca = p.ca, o.chunks = p.cb - p.ca;
-        o.two = p.nt > tt, o.whole = p.whole(), o.final = w.done();
-        if (!p.whole()) {
-          o.slot = w.slot(p, blockIdx.x);
-          o.cta0 = w.first_cta(p), o.cta1 = w.last_cta(p);
-          o.first_slot = w.slot(p, o.cta0);
-        }
-        for (int t = 0; t < 2; ++t) {
-          if (!o.two) {
-            o.c[t] = {t, o.chunks, 2};
-          } else {
-            const int t0 = p.t0 + t * tt;
-            const TileKeys k = tile_keys(a, p.n, p.len, t0, min(p.t0 + p.nt, t0 + tt));
-            o.c[t] = {max(0, k.lo / kPageChunk - p.ca), min(o.chunks, (k.hi + kPageChunk - 1) / kPageChunk - p.ca), 1};
+    auto hand_out = [&] {
+      if (lane == 0) {
+        PagePiece& o = s.piece[pat.i];
+        o.end = !more;
+        if (more) {
+          o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0, o.lo = p.lo, o.hi = p.hi;
+          o.ca = p.ca, o.chunks = p.cb - p.ca;
+          o.two = p.nt > tt, o.whole = p.whole(), o.final = w.done();
+          if (!p.whole()) {
+            o.slot = w.slot(p, blockIdx.x);
+            o.cta0 = w.first_cta(p), o.cta1 = w.last_cta(p);
+            o.first_slot = w.slot(p, o.cta0);
+          }
+          for (int t = 0; t < 2; ++t) {
+            if (!o.two) {
+              o.c[t] = {t, o.chunks, 2};
+            } else {
+              const int t0 = p.t0 + t * tt;
+              const TileKeys k = tile_keys(a, p.n, p.len, t0, min(p.t0 + p.nt, t0 + tt));
+              o.c[t] = {max(0, k.lo / kChunk - p.ca), min(o.chunks, (k.hi + kChunk - 1) / kChunk - p.ca), 1};
+            }
           }
         }
+        mbar_arrive(&s.pfull[pat.i]);
       }
-      mbar_arrive(&s.pfull[pat.i]);
+      __syncwarp();
+      ++pat;
+    };
+    if (!more || p.empty()) {
+      hand_out();
+      if (!more) break;
+      continue;
     }
-    __syncwarp();
-    ++pat;
-    if (!more) break;
-    if (p.empty()) continue;
     const int n = p.cb - p.ca;
-    auto tile = [&](const CUtensorMap* map, int c) {  // 128 keys from chunk c: those pages that hold keys of the tile
-      const int kb = c * kPageChunk;
+    // this lane's page of a chunk (its box's; the pages that hold keys of the tile are loaded)
+    auto page_of = [&](int c) {
+      const int pos = c * kChunk + (j << box_shift);
+      return pos < p.hi ? __ldg(a.table + static_cast<size_t>(p.b) * a.table_width + (pos >> a.page_shift)) : 0;
+    };
+    auto tile = [&](const CUtensorMap* map, int c, int page) {
+      const int kb = c * kChunk;
       if (r >= NR) wait(&s.empty[at.i], at.phase ^ 1);
       if (!ok) return;
-      const int b0 = max(p.lo - kb, 0) / box, b1 = (min(p.hi - kb, kPageChunk) + box - 1) / box;
+      const int b0 = max(p.lo - kb, 0) >> box_shift, b1 = (min(p.hi - kb, kChunk) + box - 1) >> box_shift;
       if (lane == 0) mbar_arrive_expect_tx(&s.full[at.i], (b1 - b0) * box * HD * 2);
       __syncwarp();
-      const int j = lane / NH, half = lane % NH;  // (boxes * NH <= 32)
-      if (j >= b0 && j < b1 && j < boxes) {
-        const int pos = kb + j * box;
-        int page = __ldg(a.table + static_cast<size_t>(p.b) * a.table_width + (pos >> a.page_shift));
+      if (j >= b0 && j < b1) {
         if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
           atomicOr(a.err, DERR_CAPACITY);
           page = a.n_pages;  // outside the map: reads as zeros
         }
-        tma_load_5d(s.ring[at.i] + half * kPageChunk * 128 + j * box * 128, map, &s.full[at.i], half * 64, pos & (P - 1), p.h,
-                    page, a.layer);
+        tma_load_5d(s.ring[at.i] + half * kChunk * 128 + (j << box_shift) * 128, map, &s.full[at.i], half * 64,
+                    (kb + (j << box_shift)) & (P - 1), p.h, page, a.layer);
       }
       ++r;
       ++at;
     };
+    int page = page_of(p.ca);
     if (with_keys > 0) wait(&s.qempty, (with_keys - 1) & 1);
     if (!ok) break;
     const int slots = p.nt > tt ? 2 : 1;
@@ -177,12 +185,15 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
       tma_load_3d(s.q[lane / NH] + lane % NH * S::kRows * 128, &m.q, &s.qfull, lane % NH * 64, p.h * a.group,
                   p.row0 + p.t0 + lane / NH * tt);
     ++with_keys;
-    if (S::kAhead) tile(&m.k, p.ca);
+    tile(&m.k, p.ca, page);
+    hand_out();  // (the first keys are on their way)
     for (int i = 0; ok && i < n; ++i) {
       if (hold > 0 && i + 1 >= hold) ok = false;
-      if (ok && !S::kAhead) tile(&m.k, p.ca + i);
-      if (ok && S::kAhead && i + 1 < n) tile(&m.k, p.ca + i + 1);
-      if (ok) tile(&m.v, p.ca + i);
+      const int next = ok && i + 1 < n ? page_of(p.ca + i + 1) : 0;
+      if (ok && S::kAhead && i + 1 < n) tile(&m.k, p.ca + i + 1, next);
+      if (ok) tile(&m.v, p.ca + i, page);
+      if (ok && !S::kAhead && i + 1 < n) tile(&m.k, p.ca + i + 1, next);
+      page = next;
     }
     if (!ok) break;
   }
@@ -200,7 +211,11 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
 
 // ---- a tile's end --------------------------------------------------------------------
 
-__device__ __forceinline__ void all_rows() { named_bar_sync(1, 256); }  // the 8 row warps
+// The row warps (S::kRowWarps of them).
+template <class S>
+__device__ __forceinline__ void all_rows() {
+  named_bar_sync(1, 32 * S::kRowWarps);
+}
 
 // 16 columns of a result; whether one is not finite.
 template <class T>
@@ -236,23 +251,33 @@ __device__ __forceinline__ void redo(S& s, const PagedAttnArgs& a, const PagePie
   if (lane == 0) atomicAdd(&s.busy, -1);
 }
 
-// Rows marked in s.bad (marked by any warp, so after a barrier of the 8; the next mark comes after another).
+// Rows marked in s.bad (marked by any warp, so after a barrier of all; the next mark comes after another).
 template <class T, int HD, class S>
 __device__ __forceinline__ void redo_bad(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt) {
   const int tid = threadIdx.x, warp = tid >> 5;
   unsigned any = 0;
   for (int i = 0; i < 8; ++i) any |= s.bad[i];
   if (!any) return;
-  for (int rr = warp; rr < 256; rr += 8)
+  for (int rr = warp; rr < 256; rr += S::kRowWarps)
     if (s.bad[rr >> 5] >> (rr & 31) & 1) redo<T, HD>(s, a, p, tt, rr);
-  all_rows();
+  all_rows<S>();
   if (tid < 8) s.bad[tid] = 0;
-  all_rows();
+  all_rows<S>();
 }
 
-// A part is [HD / 4][rows][4], so that the rows' threads write and read side by side.
+// A part of a tile that is cut: [HD / 4][rows][4] floats and a row's (maximum, sum), in
+// slots of S::kPartRows rows; the rows' threads write and read side by side.
+template <class S>
 __device__ __forceinline__ int rows_of_part(const PagedAttnArgs& a, const PagePiece& p) {
-  return p.two ? kPagedPartRows : (p.nt * a.group + 31) & ~31;
+  return p.two ? S::kPartRows : (p.nt * a.group + 31) & ~31;
+}
+template <class S, int HD>
+__device__ __forceinline__ float4* part_of(const PagedAttnArgs& a, int slot) {
+  return reinterpret_cast<float4*>(a.part_o) + static_cast<size_t>(slot) * (S::kPartRows * HD / 4);
+}
+template <class S>
+__device__ __forceinline__ float2* part_ml_of(const PagedAttnArgs& a, int slot) {
+  return a.part_ml + static_cast<size_t>(slot) * S::kPartRows;
 }
 
 // Merge the parts of a tile, in order, if the others were there before this CTA's
@@ -266,16 +291,16 @@ __device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, cons
     if (s.last) a.tickets[cta0] = 0;
     __threadfence();
   }
-  all_rows();
+  all_rows<S>();
   if (!s.last) return;
   // First the rows' maxima and sums, a thread per row; then 16 columns of a row per
   // thread, with the loads of several parts in flight (an SM takes them in at 64
   // bytes a cycle at best).
-  const int live = p.nt * a.group, part_rows = rows_of_part(a, p);
+  const int live = p.nt * a.group, part_rows = rows_of_part<S>(a, p);
   const bool two = p.two;
   auto row_of = [&](int k) { return two && k >= tt * a.group ? 128 + k - tt * a.group : k; };
-  if (tid < live) {
-    const float2* from = a.part_ml + row_of(tid);
+  for (int k = tid; k < live; k += 32 * S::kRowWarps) {
+    const int rr = row_of(k);
     float mm = -INFINITY, ll = 0.f;
 #pragma unroll 1
     for (int c = cta0; c <= cta1; c += 8) {
@@ -283,7 +308,7 @@ __device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, cons
       float nm = mm;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        ml[u] = c + u <= cta1 ? __ldcg(from + static_cast<size_t>(p.part(c + u)) * kPagedPartRows) : make_float2(-INFINITY, 0.f);
+        ml[u] = c + u <= cta1 ? __ldcg(part_ml_of<S>(a, p.part(c + u)) + rr) : make_float2(-INFINITY, 0.f);
         nm = fmaxf(nm, ml[u].x);
       }
       ll = mm != -INFINITY ? ll * ex2_ftz(mm - nm) : 0.f;
@@ -291,12 +316,12 @@ __device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, cons
 #pragma unroll
       for (int u = 0; u < 8; ++u) ll += ml[u].x != -INFINITY ? ml[u].y * ex2_ftz(ml[u].x - mm) : 0.f;
     }
-    (&s.ml[0][0])[tid] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
-    store_lse(a, p, p.t0 + tid / a.group, p.h * a.group + tid % a.group, mm, ll);
+    (&s.ml[0][0])[k] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
+    store_lse(a, p, p.t0 + k / a.group, p.h * a.group + k % a.group, mm, ll);
   }
-  all_rows();
+  all_rows<S>();
 #pragma unroll 1
-  for (int i = tid; i < live * (HD / 16); i += 256) {
+  for (int i = tid; i < live * (HD / 16); i += 32 * S::kRowWarps) {
     const int k = i % live, d = i / live * 16, rr = row_of(k);
     const float2 mi = (&s.ml[0][0])[k];
     float o[16];
@@ -304,9 +329,8 @@ __device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, cons
     for (int j = 0; j < 16; ++j) o[j] = 0.f;
 #pragma unroll 4
     for (int c = cta0; c <= cta1; ++c) {
-      const size_t part = p.part(c);
-      const float m1 = __ldcg(a.part_ml + part * kPagedPartRows + rr).x;
-      const float4* from = reinterpret_cast<const float4*>(a.part_o) + part * (kPagedPartRows * HD / 4) + d / 4 * part_rows + rr;
+      const float m1 = __ldcg(part_ml_of<S>(a, p.part(c)) + rr).x;
+      const float4* from = part_of<S, HD>(a, p.part(c)) + d / 4 * part_rows + rr;
       const float u = m1 != -INFINITY ? ex2_ftz(m1 - mi.x) : 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -323,7 +347,7 @@ __device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, cons
              static_cast<long long>(p.h * a.group + k % a.group) * a.out_head + d;
     if (write16(out, o, mi.y)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
   }
-  all_rows();
+  all_rows<S>();
   redo_bad<T, HD>(s, a, p, tt);
 }
 

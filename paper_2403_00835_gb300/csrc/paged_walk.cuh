@@ -16,11 +16,13 @@
 namespace cllm {
 
 struct PagedGeom {
-  int tile_tok;   // tokens of a tile
-  int slot_tok;   // tokens of 128 rows (tensor-core kernel: a tile has one or two times that)
-  int chunk;      // keys of a unit
-  int min_units;  // fewest units of a CTA's run
+  int tile_tok;     // tokens of a tile
+  int slot_tok;     // tokens of 128 rows (tensor-memory kernel: a tile has one or two times that)
+  int chunk_shift;  // log2 of the keys of a unit
+  int min_units;    // fewest units of a CTA's run
 };
+// (A CTA's first loads wait for what follows, in one thread: units are counted in 32
+// bits, which the host sees to, and nothing is divided that a shift or a compare decides.)
 
 // Request b's rows and length as the device has them.  Rows outside the arrays
 // or a length past the block table make it a request without rows, or without keys.
@@ -50,37 +52,33 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, int n, int
   return k;
 }
 __device__ __forceinline__ int tile_units(const PagedGeom& g, const TileKeys& k) {
-  return k.hi > k.lo ? (k.hi + g.chunk - 1) / g.chunk - k.lo / g.chunk : 1;
+  return k.hi > k.lo ? (((k.hi - 1) >> g.chunk_shift) - (k.lo >> g.chunk_shift)) + 1 : 1;
 }
 // Units of one head of each lane's request (the whole warp calls; n = 0: none).  A
 // request of many tiles is summed by all lanes.
-__device__ __forceinline__ long long head_units(const PagedAttnArgs& a, const PagedGeom& g, int n, int len) {
-  long long u = 0;
+__device__ __forceinline__ unsigned head_units(const PagedAttnArgs& a, const PagedGeom& g, int n, int len) {
+  unsigned u = 0;
   const bool many = n > 2 * g.tile_tok;
-  if (!many)
-    for (int t0 = 0; t0 < n; t0 += g.tile_tok) u += tile_units(g, tile_keys(a, n, len, t0, min(n, t0 + g.tile_tok)));
+  if (!many && n > 0) {
+    u = tile_units(g, tile_keys(a, n, len, 0, min(n, g.tile_tok)));
+    if (n > g.tile_tok) u += tile_units(g, tile_keys(a, n, len, g.tile_tok, n));
+  }
   for (unsigned rest = __ballot_sync(0xffffffffu, many); rest; rest &= rest - 1) {
     const int src = __ffs(rest) - 1, lane = threadIdx.x & 31;
     const int bn = __shfl_sync(0xffffffffu, n, src), bl = __shfl_sync(0xffffffffu, len, src);
-    long long v = 0;
+    unsigned v = 0;
     for (int t0 = lane * g.tile_tok; t0 < bn; t0 += 32 * g.tile_tok)
       v += tile_units(g, tile_keys(a, bn, bl, t0, min(bn, t0 + g.tile_tok)));
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    v = __reduce_add_sync(0xffffffffu, v);
     if (lane == src) u = v;
   }
   return u;
 }
 
-// x / y of values that almost always have 32 bits
-__device__ __forceinline__ long long div_units(long long x, long long y) {
-  return (x | y) >> 32 ? x / y : static_cast<unsigned>(x) / static_cast<unsigned>(y);
-}
-
 // Where a CTA's run begins (shared memory, made once by all threads).
 struct RunStart {
-  long long u0, u1, per;  // the run, and the units of every run
-  long long begin, head;  // first unit of request b, and the units of one of its heads
+  unsigned u0, u1, per;  // the run, and the units of every run
+  unsigned begin, head;  // first unit of request b, and the units of one of its heads
   int b, row0, n, len;
 };
 
@@ -91,16 +89,16 @@ struct Piece {
   int lo, hi;              // keys of the tile
   int ca, cb;              // this piece's chunks
   int tca, tcb;            // the tile's
-  long long tile_u;        // the tile's first unit
+  unsigned tile_u;         // the tile's first unit
   __device__ bool whole() const { return ca == tca && cb == tcb; }
   __device__ bool empty() const { return tca == tcb; }
 };
 
 // All threads of the block (a multiple of 32, at most 1024): the block's run.
 // `sm` holds 32 values.
-__device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeom& g, RunStart* rs, long long* sm) {
+__device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeom& g, RunStart* rs, unsigned* sm) {
   const int tid = threadIdx.x, nthr = blockDim.x, lane = tid & 31, warp = tid >> 5;
-  long long total = 0, head = 0, units = 0, before = 0;
+  unsigned total = 0, head = 0, units = 0, before = 0;
   Request r{0, 0, 0};
   // a thread per request and round: this round's units, those before the thread's request
   // (up to 32 requests: every warp works it out for itself)
@@ -109,18 +107,20 @@ __device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeo
     r = b < a.batch ? request(a, b) : Request{0, 0, 0};
     head = head_units(a, g, r.n, r.len);
     units = head * a.Hkv;
-    long long v = units;
+    unsigned v = units;
+    if (a.batch > 1) {
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const long long o = __shfl_up_sync(0xffffffffu, v, d);
-      if (lane >= d) v += o;
+      for (int d = 1; d < 32; d <<= 1) {
+        const unsigned o = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += o;
+      }
     }
     before = v - units;
-    if (few) return __shfl_sync(0xffffffffu, v, 31);
+    if (few) return __shfl_sync(0xffffffffu, v, a.batch > 1 ? 31 : 0);
     __syncthreads();
     if (lane == 31) sm[warp] = v;
     __syncthreads();
-    long long sum = 0;
+    unsigned sum = 0;
     for (int w = 0; w < nthr / 32; ++w) {
       if (w < warp) before += sm[w];
       sum += sm[w];
@@ -130,17 +130,16 @@ __device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeo
   if (few) total = round(lane);
   else
     for (int b0 = 0; b0 < a.batch; b0 += nthr) total += round(b0 + tid);
-  long long per = div_units(total + gridDim.x - 1, gridDim.x);
-  if (per < g.min_units) per = g.min_units;
-  const long long u0 = blockIdx.x * per;
+  const unsigned per = max((total + gridDim.x - 1) / gridDim.x, static_cast<unsigned>(g.min_units));
+  const unsigned u0 = min(blockIdx.x * per, total);
   if (tid == 0) {
     rs->u0 = u0;
-    rs->u1 = max(u0, min(u0 + per, total));
+    rs->u1 = min(u0 + per, total);
     rs->per = per;
   }
-  long long base = 0;
+  unsigned base = 0;
   for (int b0 = 0; b0 < a.batch; b0 += nthr) {
-    const long long sum = a.batch <= nthr ? total : round(b0 + tid);
+    const unsigned sum = a.batch <= nthr ? total : round(b0 + tid);
     if ((tid < 32 || !few) && u0 >= base + before && u0 < base + before + units) {  // one thread at most
       rs->b = b0 + tid;
       rs->begin = base + before;
@@ -154,7 +153,7 @@ __device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeo
 
 // The pieces of the block's run, in order (the whole warp calls).
 struct PagedWalk {
-  long long u, u1, per, tu;  // next unit, end of the run, units of a run, first unit of the tile
+  unsigned u, u1, per, tu;  // next unit, end of the run, units of a run, first unit of the tile
   int b, h, t0, n, len, row0;
 
   __device__ void load(const PagedAttnArgs& a) {
@@ -170,7 +169,8 @@ struct PagedWalk {
     if (u >= u1) return;
     b = rs.b, row0 = rs.row0, n = rs.n, len = rs.len;
     t0 = 0;
-    h = static_cast<int>(div_units(u - rs.begin, rs.head));
+    const unsigned in = u - rs.begin;
+    h = in < rs.head ? 0 : in / rs.head;
     tu = rs.begin + h * rs.head;
   }
   __device__ bool next(const PagedAttnArgs& a, const PagedGeom& g, Piece& p) {
@@ -183,10 +183,10 @@ struct PagedWalk {
         p.b = b, p.h = h, p.t0 = t0, p.nt = t1 - t0, p.n = n, p.len = len, p.row0 = row0;
         p.lo = k.lo, p.hi = k.hi;
         p.tile_u = tu;
-        p.tca = k.lo / g.chunk;
+        p.tca = k.lo >> g.chunk_shift;
         p.tcb = k.hi > k.lo ? p.tca + units : p.tca;
         p.ca = p.tca + static_cast<int>(u - tu);
-        const long long e = min(u1, tu + units);
+        const unsigned e = min(u1, tu + units);
         p.cb = min(p.tcb, p.tca + static_cast<int>(e - tu));
         if (p.tcb == p.tca) p.ca = p.tca;
         u = e;
@@ -215,8 +215,8 @@ struct PagedWalk {
   }
   __device__ bool done() const { return u >= u1; }
   // contributors of a cut tile: CTAs [first, last]; CTA c's partial slot
-  __device__ int first_cta(const Piece& p) const { return static_cast<int>(div_units(p.tile_u, per)); }
-  __device__ int last_cta(const Piece& p) const { return static_cast<int>(div_units(p.tile_u + (p.tcb - p.tca) - 1, per)); }
+  __device__ int first_cta(const Piece& p) const { return p.ca == p.tca ? blockIdx.x : p.tile_u / per; }
+  __device__ int last_cta(const Piece& p) const { return p.cb == p.tcb ? blockIdx.x : (p.tile_u + (p.tcb - p.tca) - 1) / per; }
   __device__ int slot(const Piece& p, int c) const { return 2 * c + (c * per < p.tile_u ? 1 : 0); }
 };
 
