@@ -46,7 +46,9 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   pdl_launch_dependents();
   pdl_wait();
-  run_start(a, g, &s.run, s.scan);
+  if (a.batch > kWarpRequests) run_start_block(a, g, &s.run, s.scan);
+  else if (tid < 32) run_start_warp(a, g, &s.run);
+  __syncthreads();
   PagedWalk w;
   w.begin(s.run);
   Piece p;
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
 
 template <int HD, int BM>
 cudaError_t launch(const PagedAttnArgs& a, int grid, cudaStream_t s) {
-  const PagedGeom g{BM / a.group, BM / a.group, 6, 1};
+  const PagedGeom g{BM / a.group, BM / a.group, 6, 1, 2, 2};
   return launch_after(paged_attn_kernel<float, HD, BM>, dim3(grid), kPThreads, sizeof(PagedSmem<HD, BM>), s, a, g);
 }
 

@@ -315,7 +315,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
   }
   pdl_launch_dependents();
   pdl_wait();  // (nothing of the calls before is read above)
-  run_start(a, g, &s.run, reinterpret_cast<unsigned*>(s.ml));
+  if (a.batch > kWarpRequests) run_start_block(a, g, &s.run, reinterpret_cast<unsigned*>(s.ml));
+  __syncthreads();
   if (threadIdx.x >= 32 * kFewWarps) issue_loads<HD>(s, a, g, m, hold);
   else run_few<T, HD>(s, a, g);
   __syncthreads();
@@ -326,7 +327,7 @@ template <class T, int HD>
 cudaError_t launch_few(const PagedMaps& m, const PagedAttnArgs& a, int hold, int sms, cudaStream_t s) {
   const int tt = kFewRows / a.group;
   return launch_after(paged_attn_few_kernel<T, HD>, dim3(2 * sms), kFewThreads, sizeof(FewSmem<HD>), s, m, a,
-                      PagedGeom{tt, tt, FewSmem<HD>::kShift, 2}, hold);
+                      PagedGeom{tt, tt, FewSmem<HD>::kShift, 1, 4, 3}, hold);
 }
 
 template <class T, int HD>

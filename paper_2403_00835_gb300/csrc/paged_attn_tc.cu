@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
   pdl_launch_dependents();
   pdl_wait();  // (nothing of the calls before is read above)
-  run_start(a, g, &s.run, reinterpret_cast<unsigned*>(s.ml));
+  if (a.batch > kWarpRequests) run_start_block(a, g, &s.run, reinterpret_cast<unsigned*>(s.ml));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -515,7 +515,7 @@ cudaError_t launch_tc(const PagedMaps& m, const PagedAttnArgs& a, int hold, int 
   // their keys would have to be cut and their rows merged, so they are halved instead.
   const long long per_request = (static_cast<long long>(a.rows) + a.batch - 1) / a.batch;
   const bool two = per_request > tt && (per_request + 2 * tt - 1) / (2 * tt) * a.batch * a.Hkv >= grid;
-  const PagedGeom g{two ? 2 * tt : tt, tt, kTcShift, 2};
+  const PagedGeom g{two ? 2 * tt : tt, tt, kTcShift, 2, 8, 3};
   return launch_after(paged_attn_tc_kernel<T, HD>, dim3(grid), kTcThreads, sizeof(TcSmem<HD>), s, m, a, g, hold);
 }
 

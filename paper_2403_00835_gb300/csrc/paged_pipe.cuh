@@ -107,6 +107,7 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
     ok = ok && page_wait(bar, parity, &s.abort, &s.busy);
     ok = __all_sync(0xffffffffu, ok);
   };
+  if (a.batch <= kWarpRequests) run_start_warp(a, g, &s.run);
   PagedWalk w;
   w.begin(s.run);
   for (;;) {
@@ -293,58 +294,88 @@ __device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, cons
   }
   all_rows<S>();
   if (!s.last) return;
-  // First the rows' maxima and sums, a thread per row; then 16 columns of a row per
-  // thread, with the loads of several parts in flight (an SM takes them in at 64
-  // bytes a cycle at best).
+  // First the rows' maxima and sums, then their columns, 16 to a thread.  Where there are
+  // fewer rows or columns than threads, `ways` neighbouring lanes share the parts.
+  constexpr int kThreads = 32 * S::kRowWarps;
   const int live = p.nt * a.group, part_rows = rows_of_part<S>(a, p);
   const bool two = p.two;
   auto row_of = [&](int k) { return two && k >= tt * a.group ? 128 + k - tt * a.group : k; };
-  for (int k = tid; k < live; k += 32 * S::kRowWarps) {
-    const int rr = row_of(k);
-    float mm = -INFINITY, ll = 0.f;
+  auto ways_for = [](int items) { return items * 16 <= kThreads ? 16 : items * 4 <= kThreads ? 4 : items * 2 <= kThreads ? 2 : 1; };
+  {
+    const int ways = ways_for(live), sub = tid & (ways - 1);
+    for (int k0 = 0; k0 < live; k0 += kThreads / ways) {
+      const int k = k0 + tid / ways, rr = row_of(min(k, live - 1));
+      float mm = -INFINITY, ll = 0.f;
 #pragma unroll 1
-    for (int c = cta0; c <= cta1; c += 8) {
-      float2 ml[8];
-      float nm = mm;
+      for (int c = cta0 + sub; c <= cta1; c += 4 * ways) {
+        float2 ml[4];
+        float nm = mm;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        ml[u] = c + u <= cta1 ? __ldcg(part_ml_of<S>(a, p.part(c + u)) + rr) : make_float2(-INFINITY, 0.f);
-        nm = fmaxf(nm, ml[u].x);
+        for (int u = 0; u < 4; ++u) {
+          ml[u] = c + u * ways <= cta1 ? __ldcg(part_ml_of<S>(a, p.part(c + u * ways)) + rr) : make_float2(-INFINITY, 0.f);
+          nm = fmaxf(nm, ml[u].x);
+        }
+        ll = mm != -INFINITY ? ll * ex2_ftz(mm - nm) : 0.f;
+        mm = nm;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) ll += ml[u].x != -INFINITY ? ml[u].y * ex2_ftz(ml[u].x - mm) : 0.f;
       }
-      ll = mm != -INFINITY ? ll * ex2_ftz(mm - nm) : 0.f;
-      mm = nm;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) ll += ml[u].x != -INFINITY ? ml[u].y * ex2_ftz(ml[u].x - mm) : 0.f;
+      for (int w = 1; w < ways; w <<= 1) {
+        const float m1 = __shfl_xor_sync(0xffffffffu, mm, w), l1 = __shfl_xor_sync(0xffffffffu, ll, w), nm = fmaxf(mm, m1);
+        // (in the same order on both sides, so that the lanes agree bit for bit)
+        const float a0 = mm != -INFINITY ? ll * ex2_ftz(mm - nm) : 0.f, a1 = m1 != -INFINITY ? l1 * ex2_ftz(m1 - nm) : 0.f;
+        ll = sub & w ? a1 + a0 : a0 + a1;
+        mm = nm;
+      }
+      if (k < live && sub == 0) {
+        (&s.ml[0][0])[k] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
+        const int kt = k * a.group_inv >> 16;
+        store_lse(a, p, p.t0 + kt, p.h * a.group + k - kt * a.group, mm, ll);
+      }
     }
-    (&s.ml[0][0])[k] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
-    store_lse(a, p, p.t0 + k / a.group, p.h * a.group + k % a.group, mm, ll);
   }
   all_rows<S>();
+  const int items = live * (HD / 16), ways = ways_for(items), sub = tid & (ways - 1);
 #pragma unroll 1
-  for (int i = tid; i < live * (HD / 16); i += 32 * S::kRowWarps) {
+  for (int i0 = 0; i0 < items; i0 += kThreads / ways) {
+    const int i = min(i0 + tid / ways, items - 1);
     const int k = i % live, d = i / live * 16, rr = row_of(k);
     const float2 mi = (&s.ml[0][0])[k];
     float o[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[j] = 0.f;
-#pragma unroll 4
-    for (int c = cta0; c <= cta1; ++c) {
-      const float m1 = __ldcg(part_ml_of<S>(a, p.part(c)) + rr).x;
-      const float4* from = part_of<S, HD>(a, p.part(c)) + d / 4 * part_rows + rr;
-      const float u = m1 != -INFINITY ? ex2_ftz(m1 - mi.x) : 0.f;
+#pragma unroll 1
+    for (int c = cta0 + sub; c <= cta1; c += 2 * ways) {
+      float4 y[2][4];
+      float m1[2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float4 y = __ldcg(from + j * part_rows);
-        if (u != 0.f) {
-          o[4 * j] = fmaf(y.x, u, o[4 * j]);
-          o[4 * j + 1] = fmaf(y.y, u, o[4 * j + 1]);
-          o[4 * j + 2] = fmaf(y.z, u, o[4 * j + 2]);
-          o[4 * j + 3] = fmaf(y.w, u, o[4 * j + 3]);
+      for (int u = 0; u < 2; ++u) {  // (the loads of two parts under way)
+        const int part = p.part(min(c + u * ways, cta1));
+        m1[u] = c + u * ways <= cta1 ? __ldcg(part_ml_of<S>(a, part) + rr).x : -INFINITY;
+        const float4* from = part_of<S, HD>(a, part) + d / 4 * part_rows + rr;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[u][j] = __ldcg(from + j * part_rows);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (m1[u] == -INFINITY) continue;  // none of its keys is seen
+        const float f = ex2_ftz(m1[u] - mi.x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          o[4 * j] = fmaf(y[u][j].x, f, o[4 * j]);
+          o[4 * j + 1] = fmaf(y[u][j].y, f, o[4 * j + 1]);
+          o[4 * j + 2] = fmaf(y[u][j].z, f, o[4 * j + 2]);
+          o[4 * j + 3] = fmaf(y[u][j].w, f, o[4 * j + 3]);
         }
       }
     }
-    T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + k / a.group) * a.out_row +
-             static_cast<long long>(p.h * a.group + k % a.group) * a.out_head + d;
+    for (int w = 1; w < ways; w <<= 1)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[j] += __shfl_xor_sync(0xffffffffu, o[j], w);
+    if (sub != 0 || i0 + tid / ways >= items) continue;
+    const int kt = k * a.group_inv >> 16;
+    T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + kt) * a.out_row +
+             static_cast<long long>(p.h * a.group + k - kt * a.group) * a.out_head + d;
     if (write16(out, o, mi.y)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
   }
   all_rows<S>();

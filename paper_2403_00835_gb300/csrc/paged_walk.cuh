@@ -7,7 +7,8 @@
 // the division is made there: all units in order (request, head, tile, chunk)
 // are cut into equal runs, one per CTA.  A run's ends may cut a tile; the pieces
 // leave partial results, and the CTA that finishes a tile last merges them in
-// order of their CTAs, so sums do not depend on who that is.
+// order of their CTAs, so sums do not depend on who that is.  Where the tiles are
+// short, whole tiles are dealt out instead: cutting one costs more than it saves.
 #pragma once
 #include "act.cuh"
 #include "internal.cuh"
@@ -20,6 +21,8 @@ struct PagedGeom {
   int slot_tok;     // tokens of 128 rows (tensor-memory kernel: a tile has one or two times that)
   int chunk_shift;  // log2 of the keys of a unit
   int min_units;    // fewest units of a CTA's run
+  int piece_cost;   // what a piece costs beside its units, and merging a cut tile, in units' time
+  int merge_cost;
 };
 // (A CTA's first loads wait for what follows, in one thread: units are counted in 32
 // bits, which the host sees to, and nothing is divided that a shift or a compare decides.)
@@ -54,32 +57,50 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, int n, int
 __device__ __forceinline__ int tile_units(const PagedGeom& g, const TileKeys& k) {
   return k.hi > k.lo ? (((k.hi - 1) >> g.chunk_shift) - (k.lo >> g.chunk_shift)) + 1 : 1;
 }
-// Units of one head of each lane's request (the whole warp calls; n = 0: none).  A
-// request of many tiles is summed by all lanes.
-__device__ __forceinline__ unsigned head_units(const PagedAttnArgs& a, const PagedGeom& g, int n, int len) {
-  unsigned u = 0;
+// Of one head of each lane's request (the whole warp calls; n = 0: none): all units, tiles, and
+// the units of the longest tile.  A request of many tiles is summed by all lanes.
+struct HeadWork {
+  unsigned units, tiles, longest;
+};
+__device__ __forceinline__ HeadWork head_work(const PagedAttnArgs& a, const PagedGeom& g, int n, int len) {
+  HeadWork w{0, 0, 0};
   const bool many = n > 2 * g.tile_tok;
   if (!many && n > 0) {
-    u = tile_units(g, tile_keys(a, n, len, 0, min(n, g.tile_tok)));
-    if (n > g.tile_tok) u += tile_units(g, tile_keys(a, n, len, g.tile_tok, n));
+    w.units = w.longest = tile_units(g, tile_keys(a, n, len, 0, min(n, g.tile_tok)));
+    w.tiles = 1;
+    if (n > g.tile_tok) {
+      const unsigned u = tile_units(g, tile_keys(a, n, len, g.tile_tok, n));
+      w = {w.units + u, 2, max(w.longest, u)};
+    }
   }
   for (unsigned rest = __ballot_sync(0xffffffffu, many); rest; rest &= rest - 1) {
     const int src = __ffs(rest) - 1, lane = threadIdx.x & 31;
     const int bn = __shfl_sync(0xffffffffu, n, src), bl = __shfl_sync(0xffffffffu, len, src);
-    unsigned v = 0;
-    for (int t0 = lane * g.tile_tok; t0 < bn; t0 += 32 * g.tile_tok)
-      v += tile_units(g, tile_keys(a, bn, bl, t0, min(bn, t0 + g.tile_tok)));
-    v = __reduce_add_sync(0xffffffffu, v);
-    if (lane == src) u = v;
+    HeadWork v{0, 0, 0};
+    for (int t0 = lane * g.tile_tok; t0 < bn; t0 += 32 * g.tile_tok) {
+      const unsigned u = tile_units(g, tile_keys(a, bn, bl, t0, min(bn, t0 + g.tile_tok)));
+      v = {v.units + u, v.tiles + 1, max(v.longest, u)};
+    }
+    v = {__reduce_add_sync(0xffffffffu, v.units), __reduce_add_sync(0xffffffffu, v.tiles), __reduce_max_sync(0xffffffffu, v.longest)};
+    if (lane == src) w = v;
   }
-  return u;
+  return w;
 }
 
-// Where a CTA's run begins (shared memory, made once by all threads).
+// Whether whole tiles are dealt out: rounds of whole tiles against equal runs of units, whose
+// ends are pieces of their own and merged.
+__device__ __forceinline__ bool deal_tiles(const PagedGeom& g, unsigned units, unsigned tiles, unsigned longest) {
+  if (longest > 64) return false;
+  const unsigned per = max((units + gridDim.x - 1) / gridDim.x, static_cast<unsigned>(g.min_units));
+  const unsigned rounds = (tiles + gridDim.x - 1) / gridDim.x;
+  return rounds * (longest + g.piece_cost) <= per + g.piece_cost + g.piece_cost * per * tiles / max(units, 1u) + g.merge_cost;
+}
+
+// Where a CTA's run begins (shared memory).  (`whole`: a unit is a tile.)
 struct RunStart {
   unsigned u0, u1, per;  // the run, and the units of every run
   unsigned begin, head;  // first unit of request b, and the units of one of its heads
-  int b, row0, n, len;
+  int b, row0, n, len, whole;
 };
 
 // A piece: the chunks [ca, cb) of a tile that belong to this CTA's run.
@@ -94,58 +115,91 @@ struct Piece {
   __device__ bool empty() const { return tca == tcb; }
 };
 
-// All threads of the block (a multiple of 32, at most 1024): the block's run.
-// `sm` holds 32 values.
-__device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeom& g, RunStart* rs, unsigned* sm) {
-  const int tid = threadIdx.x, nthr = blockDim.x, lane = tid & 31, warp = tid >> 5;
-  unsigned total = 0, head = 0, units = 0, before = 0;
-  Request r{0, 0, 0};
-  // a thread per request and round: this round's units, those before the thread's request
-  // (up to 32 requests: every warp works it out for itself)
-  const bool few = a.batch <= 32;
-  auto round = [&](int b) {
-    r = b < a.batch ? request(a, b) : Request{0, 0, 0};
-    head = head_units(a, g, r.n, r.len);
-    units = head * a.Hkv;
-    unsigned v = units;
-    if (a.batch > 1) {
+// The run of this CTA among `total` units, and where it begins if that is in one of the
+// lanes' (threads') requests, each with `units` units after `before`.
+__device__ __forceinline__ void set_run(RunStart* rs, unsigned total, int min_units, bool whole, bool writer) {
+  const unsigned per = max((total + gridDim.x - 1) / gridDim.x, static_cast<unsigned>(min_units));
+  const unsigned u0 = min(blockIdx.x * per, total);
+  if (writer) rs->u0 = u0, rs->u1 = min(u0 + per, total), rs->per = per, rs->whole = whole;
+}
+__device__ __forceinline__ void set_begin(RunStart* rs, unsigned u0, unsigned before, unsigned units, unsigned head, int b,
+                                          const Request& r) {
+  if (u0 >= before && u0 < before + units) {  // one thread at most
+    rs->b = b;
+    rs->begin = before;
+    rs->head = head;
+    rs->row0 = r.row0, rs->n = r.n, rs->len = r.len;
+  }
+}
+
+// Up to 32 requests: the block's run, by one warp.
+constexpr int kWarpRequests = 32;
+__device__ __forceinline__ void run_start_warp(const PagedAttnArgs& a, const PagedGeom& g, RunStart* rs) {
+  const int lane = threadIdx.x & 31;
+  const Request r = lane < a.batch ? request(a, lane) : Request{0, 0, 0};
+  const HeadWork w = head_work(a, g, r.n, r.len);
+  const unsigned units = __reduce_add_sync(0xffffffffu, w.units) * a.Hkv, tiles = __reduce_add_sync(0xffffffffu, w.tiles) * a.Hkv;
+  const bool whole = deal_tiles(g, units, tiles, __reduce_max_sync(0xffffffffu, w.longest));
+  const unsigned head = whole ? w.tiles : w.units, mine = head * a.Hkv;
+  unsigned v = mine;
+  if (a.batch > 1) {
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const unsigned o = __shfl_up_sync(0xffffffffu, v, d);
-        if (lane >= d) v += o;
-      }
+    for (int d = 1; d < 32; d <<= 1) {
+      const unsigned o = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) v += o;
     }
-    before = v - units;
-    if (few) return __shfl_sync(0xffffffffu, v, a.batch > 1 ? 31 : 0);
+  }
+  set_run(rs, whole ? tiles : units, whole ? 1 : g.min_units, whole, lane == 0);
+  __syncwarp();
+  set_begin(rs, rs->u0, v - mine, mine, head, lane, r);
+  __syncwarp();
+}
+
+// Any number: all threads of the block (a multiple of 32, at most 1024) call.  `sm` holds 32 values.
+__device__ __forceinline__ void run_start_block(const PagedAttnArgs& a, const PagedGeom& g, RunStart* rs, unsigned* sm) {
+  const int tid = threadIdx.x, nthr = blockDim.x, lane = tid & 31, warp = tid >> 5;
+  HeadWork w{0, 0, 0};
+  Request r{0, 0, 0};
+  // a thread per request and round
+  auto load = [&](int b) {
+    r = b < a.batch ? request(a, b) : Request{0, 0, 0};
+    w = head_work(a, g, r.n, r.len);
+  };
+  auto all = [&](unsigned x, bool largest) {
+    x = largest ? __reduce_max_sync(0xffffffffu, x) : __reduce_add_sync(0xffffffffu, x);
+    __syncthreads();
+    if (lane == 0) sm[warp] = x;
+    __syncthreads();
+    unsigned sum = 0;
+    for (int i = 0; i < nthr / 32; ++i) sum = largest ? max(sum, sm[i]) : sum + sm[i];
+    return sum;
+  };
+  unsigned units = 0, tiles = 0, longest = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += nthr) {
+    load(b0 + tid);
+    units += w.units, tiles += w.tiles, longest = max(longest, w.longest);
+  }
+  units = all(units, false) * a.Hkv, tiles = all(tiles, false) * a.Hkv, longest = all(longest, true);
+  const bool whole = deal_tiles(g, units, tiles, longest);
+  set_run(rs, whole ? tiles : units, whole ? 1 : g.min_units, whole, tid == 0);
+  unsigned base = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += nthr) {
+    if (a.batch > nthr) load(b0 + tid);
+    const unsigned head = whole ? w.tiles : w.units, mine = head * a.Hkv;
+    unsigned v = mine, before = 0, sum = 0;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const unsigned o = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) v += o;
+    }
     __syncthreads();
     if (lane == 31) sm[warp] = v;
     __syncthreads();
-    unsigned sum = 0;
-    for (int w = 0; w < nthr / 32; ++w) {
-      if (w < warp) before += sm[w];
-      sum += sm[w];
+    for (int i = 0; i < nthr / 32; ++i) {
+      if (i < warp) before += sm[i];
+      sum += sm[i];
     }
-    return sum;
-  };
-  if (few) total = round(lane);
-  else
-    for (int b0 = 0; b0 < a.batch; b0 += nthr) total += round(b0 + tid);
-  const unsigned per = max((total + gridDim.x - 1) / gridDim.x, static_cast<unsigned>(g.min_units));
-  const unsigned u0 = min(blockIdx.x * per, total);
-  if (tid == 0) {
-    rs->u0 = u0;
-    rs->u1 = min(u0 + per, total);
-    rs->per = per;
-  }
-  unsigned base = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += nthr) {
-    const unsigned sum = a.batch <= nthr ? total : round(b0 + tid);
-    if ((tid < 32 || !few) && u0 >= base + before && u0 < base + before + units) {  // one thread at most
-      rs->b = b0 + tid;
-      rs->begin = base + before;
-      rs->head = head;
-      rs->row0 = r.row0, rs->n = r.n, rs->len = r.len;
-    }
+    set_begin(rs, rs->u0, base + before + v - mine, mine, head, b0 + tid, r);
     base += sum;
   }
   __syncthreads();
@@ -154,7 +208,7 @@ __device__ __forceinline__ void run_start(const PagedAttnArgs& a, const PagedGeo
 // The pieces of the block's run, in order (the whole warp calls).
 struct PagedWalk {
   unsigned u, u1, per, tu;  // next unit, end of the run, units of a run, first unit of the tile
-  int b, h, t0, n, len, row0;
+  int b, h, t0, n, len, row0, whole;
 
   __device__ void load(const PagedAttnArgs& a) {
     const Request q = request(a, b);
@@ -166,6 +220,7 @@ struct PagedWalk {
     u = rs.u0;
     u1 = rs.u1;
     per = rs.per;
+    whole = rs.whole;
     if (u >= u1) return;
     b = rs.b, row0 = rs.row0, n = rs.n, len = rs.len;
     t0 = 0;
@@ -178,17 +233,16 @@ struct PagedWalk {
     for (;;) {
       const int t1 = min(n, t0 + g.tile_tok);
       const TileKeys k = tile_keys(a, n, len, t0, t1);
-      const int units = tile_units(g, k);
+      const int chunks = tile_units(g, k), units = whole ? 1 : chunks;
       if (u < tu + units) {
         p.b = b, p.h = h, p.t0 = t0, p.nt = t1 - t0, p.n = n, p.len = len, p.row0 = row0;
         p.lo = k.lo, p.hi = k.hi;
         p.tile_u = tu;
         p.tca = k.lo >> g.chunk_shift;
-        p.tcb = k.hi > k.lo ? p.tca + units : p.tca;
-        p.ca = p.tca + static_cast<int>(u - tu);
+        p.tcb = k.hi > k.lo ? p.tca + chunks : p.tca;
         const unsigned e = min(u1, tu + units);
-        p.cb = min(p.tcb, p.tca + static_cast<int>(e - tu));
-        if (p.tcb == p.tca) p.ca = p.tca;
+        p.ca = p.tca, p.cb = p.tcb;
+        if (!whole && p.tcb > p.tca) p.ca += u - tu, p.cb = p.tca + static_cast<int>(e - tu);
         u = e;
         return true;
       }
