@@ -3,8 +3,11 @@
 //   o = sum_k p_k v_k / sum_k p_k,  p_k = 2^(scale log2(e) q.k - m),  m the running maximum
 //
 // in one pass over the keys: fp32 throughout.  A CTA holds a tile of BM rows (tokens
-// times the query heads of one key/value head) and takes its keys 64 at a time.
-// A thread computes BM/16 rows x 4 scores, and of the output BM/16 rows x HD/16 columns.
+// times the query heads of one key/value head) and takes its keys 64 at a time, the
+// next 64 on their way (cp.async) meanwhile.  A thread computes BM/16 rows x 4 scores,
+// and of the output BM/16 rows x HD/16 columns; with BM = 64 a shared-memory load of 16
+// bytes serves 8 to 11 multiply-adds, which bounds it near half the FMA rate, with BM =
+// 16 (few rows) a quarter of that.
 #include "paged.cuh"
 #include "paged_walk.cuh"
 #include "ptx.cuh"
@@ -19,8 +22,8 @@ constexpr int kPChunk = 64;  // 2^6
 template <int HD, int BM>
 struct PagedSmem {
   float q[BM][HD + 4];
-  float k[kPChunk][HD + 4];
-  float v[kPChunk][HD + 4];
+  float k[2][kPChunk][HD + 4];
+  float v[2][kPChunk][HD + 4];
   float p[BM][kPChunk + 4];
   unsigned scan[32];
   RunStart run;
@@ -29,18 +32,15 @@ struct PagedSmem {
 };
 
 __device__ __forceinline__ float4 ld4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <class T>
-__device__ __forceinline__ void st4(T* p, float4 v) {
-  st_act(p, 0, v.x), st_act(p, 1, v.y), st_act(p, 2, v.z), st_act(p, 3, v.w);
-}
 __device__ __forceinline__ void st4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 __device__ __forceinline__ bool finite4(float4 v) {
   return isfinite(v.x) && isfinite(v.y) && isfinite(v.z) && isfinite(v.w);
 }
 
-template <class T, int HD, int BM>
+template <int HD, int BM>
 __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_constant__ PagedAttnArgs a, const PagedGeom g) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
+  using T = float;
   PagedSmem<HD, BM>& s = *reinterpret_cast<PagedSmem<HD, BM>*>(smem_raw);
   constexpr int R = BM / 16, C = HD / 64;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
       const int r = i / (HD / 4), d = i % (HD / 4) * 4;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
       if (r < rows) {
-        const int tok = r / a.group, hh = p.h * a.group + r % a.group;
+        const int tok = (r * a.group_inv >> 16), hh = p.h * a.group + r % a.group;
         x = ld4(static_cast<const T*>(a.q) + static_cast<long long>(p.row0 + p.t0 + tok) * a.q_row + hh * a.q_head + d);
       }
       *reinterpret_cast<float4*>(&s.q[r][d]) = x;
@@ -71,92 +71,112 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int r = ty * R + i;
-      rk[i] = row_keys(a, p.n, p.len, p.row0, p.t0 + min(r, rows - 1) / a.group);
+      rk[i] = row_keys(a, p.n, p.len, p.row0, p.t0 + (min(r, rows - 1) * a.group_inv >> 16));
       m[i] = -INFINITY, l[i] = 0.f;
 #pragma unroll
       for (int c = 0; c < C; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    for (int c = p.ca; c < p.cb; ++c) {
-      const int kb = c * kPChunk;
-      __syncthreads();
-      for (int i = tid; i < kPChunk * (HD / 4); i += kPThreads) {
-        const int key = i / (HD / 4), d = i % (HD / 4) * 4, pos = kb + key;
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-        if (pos >= p.lo && pos < p.hi) {
-          const T* kp = pool_row<T>(a, a.k, p.b, p.h, pos);
-          const T* vp = pool_row<T>(a, a.v, p.b, p.h, pos);
-          if (kp != nullptr) x = ld4(kp + d), y = ld4(vp + d);
-        }
-        *reinterpret_cast<float4*>(&s.k[key][d]) = x;
-        *reinterpret_cast<float4*>(&s.v[key][d]) = y;
-      }
-      __syncthreads();
-      float x[R][4];
+    // 8 lanes to a key; keys that no row of the tile sees become zeros
+    auto load = [&](int c) {
+      const int st = (c - p.ca) & 1;
 #pragma unroll
-      for (int i = 0; i < R; ++i)
+      for (int u = 0; u < 2; ++u) {
+        const int key = (tid >> 3) + 32 * u, pos = c * kPChunk + key;
+        const T *kp = nullptr, *vp = nullptr;
+        if (pos >= p.lo && pos < p.hi) kp = pool_row<T>(a, a.k, p.b, p.h, pos), vp = pool_row<T>(a, a.v, p.b, p.h, pos);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
-#pragma unroll 4
-      for (int d = 0; d < HD; d += 4) {
-        float4 kv[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) kv[j] = ld4(&s.k[tx + 16 * j][d]);
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-          const float4 q = ld4(&s.q[ty * R + i][d]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            x[i][j] = fmaf(q.w, kv[j].w, fmaf(q.z, kv[j].z, fmaf(q.y, kv[j].y, fmaf(q.x, kv[j].x, x[i][j]))));
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const uint32_t b0 = key_bits(rk[i], kb), b1 = key_bits(rk[i], kb + 32);
-        const bool see[4] = {(b0 >> tx & 1) != 0, (b0 >> (tx + 16) & 1) != 0, (b1 >> tx & 1) != 0, (b1 >> (tx + 16) & 1) != 0};
-        float cm = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[i][j] = see[j] ? x[i][j] * a.scale_log2 : -INFINITY;
-          cm = fmaxf(cm, x[i][j]);
-        }
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, d));
-        const float nm = fmaxf(m[i], cm), base = nm == -INFINITY ? 0.f : nm;
-        const float f = exp2f(m[i] - base);
-        m[i] = nm;
-        l[i] *= f;
-#pragma unroll
-        for (int e = 0; e < C; ++e) o[i][e].x *= f, o[i][e].y *= f, o[i][e].z *= f, o[i][e].w *= f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float pr = exp2f(x[i][j] - base);
-          l[i] += pr;
-          s.p[ty * R + i][tx + 16 * j] = pr;
-        }
-      }
-      __syncwarp();  // (a warp's probabilities are its own rows')
-#pragma unroll 2
-      for (int key = 0; key < kPChunk; key += 4) {
-        float pr[R][4];
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-          const float4 t = ld4(&s.p[ty * R + i][key]);
-          pr[i][0] = t.x, pr[i][1] = t.y, pr[i][2] = t.z, pr[i][3] = t.w;
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int e = 0; e < C; ++e) {
-            const float4 v = ld4(&s.v[key + u][tx * 4 + 64 * e]);
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-              o[i][e].x = fmaf(pr[i][u], v.x, o[i][e].x);
-              o[i][e].y = fmaf(pr[i][u], v.y, o[i][e].y);
-              o[i][e].z = fmaf(pr[i][u], v.z, o[i][e].z);
-              o[i][e].w = fmaf(pr[i][u], v.w, o[i][e].w);
-            }
+        for (int d = (tid & 7) * 4; d < HD; d += 32) {
+          if (kp != nullptr) {
+            cp_async16(&s.k[st][key][d], kp + d);
+            cp_async16(&s.v[st][key][d], vp + d);
+          } else {
+            *reinterpret_cast<float4*>(&s.k[st][key][d]) = make_float4(0.f, 0.f, 0.f, 0.f);
+            *reinterpret_cast<float4*>(&s.v[st][key][d]) = make_float4(0.f, 0.f, 0.f, 0.f);
           }
+        }
       }
+      cp_async_commit();
+    };
+    const bool live = (tid >> 5) * 2 * R < rows;  // some row of the warp is
+    if (p.ca < p.cb) load(p.ca);
+    for (int c = p.ca; c < p.cb; ++c) {
+      const int kb = c * kPChunk, st = (c - p.ca) & 1;
+      if (c + 1 < p.cb) {
+        load(c + 1);
+        cp_async_wait_but1();
+      } else {
+        cp_async_wait_all();
+      }
+      __syncthreads();
+      if (live) {
+        float x[R][4];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
+#pragma unroll 4
+        for (int d = 0; d < HD; d += 4) {
+          float4 kv[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) kv[j] = ld4(&s.k[st][tx + 16 * j][d]);
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            const float4 q = ld4(&s.q[ty * R + i][d]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              x[i][j] = fmaf(q.w, kv[j].w, fmaf(q.z, kv[j].z, fmaf(q.y, kv[j].y, fmaf(q.x, kv[j].x, x[i][j]))));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const uint32_t b0 = key_bits(rk[i], kb), b1 = key_bits(rk[i], kb + 32);
+          const bool see[4] = {(b0 >> tx & 1) != 0, (b0 >> (tx + 16) & 1) != 0, (b1 >> tx & 1) != 0, (b1 >> (tx + 16) & 1) != 0};
+          float cm = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[i][j] = see[j] ? x[i][j] * a.scale_log2 : -INFINITY;
+            cm = fmaxf(cm, x[i][j]);
+          }
+#pragma unroll
+          for (int d = 1; d < 16; d <<= 1) cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, d));
+          const float nm = fmaxf(m[i], cm), base = nm == -INFINITY ? 0.f : nm;
+          const float f = exp2f(m[i] - base);
+          m[i] = nm;
+          l[i] *= f;
+#pragma unroll
+          for (int e = 0; e < C; ++e) o[i][e].x *= f, o[i][e].y *= f, o[i][e].z *= f, o[i][e].w *= f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float pr = exp2f(x[i][j] - base);
+            l[i] += pr;
+            s.p[ty * R + i][tx + 16 * j] = pr;
+          }
+        }
+        __syncwarp();  // (a warp's probabilities are its own rows')
+#pragma unroll 2
+        for (int key = 0; key < kPChunk; key += 4) {
+          float pr[R][4];
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            const float4 t = ld4(&s.p[ty * R + i][key]);
+            pr[i][0] = t.x, pr[i][1] = t.y, pr[i][2] = t.z, pr[i][3] = t.w;
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < C; ++e) {
+              const float4 v = ld4(&s.v[st][key + u][tx * 4 + 64 * e]);
+#pragma unroll
+              for (int i = 0; i < R; ++i) {
+                o[i][e].x = fmaf(pr[i][u], v.x, o[i][e].x);
+                o[i][e].y = fmaf(pr[i][u], v.y, o[i][e].y);
+                o[i][e].z = fmaf(pr[i][u], v.z, o[i][e].z);
+                o[i][e].w = fmaf(pr[i][u], v.w, o[i][e].w);
+              }
+            }
+        }
+      }
+      __syncthreads();  // (the buffer is loaded anew by the next turn)
     }
 #pragma unroll
     for (int i = 0; i < R; ++i)
@@ -164,7 +184,7 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
       for (int d = 1; d < 16; d <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
 
     auto store = [&](int r, int d, float4 x, float mm, float ll) {  // a row's 4 columns from d
-      const int tok = r / a.group, hh = p.h * a.group + r % a.group;
+      const int tok = (r * a.group_inv >> 16), hh = p.h * a.group + r % a.group;
       const size_t row = static_cast<size_t>(p.row0 + p.t0 + tok);
       const bool any = ll != 0.f;
       if (any) x = make_float4(x.x / ll, x.y / ll, x.z / ll, x.w / ll);
@@ -224,23 +244,23 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
     __syncthreads();
     if (done)
       for (int r = tid >> 5; r < rows; r += kPThreads / 32)
-        if (s.bad[r >> 5] >> (r & 31) & 1) exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + r / a.group, p.h * a.group + r % a.group);
+        if (s.bad[r >> 5] >> (r & 31) & 1) exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + (r * a.group_inv >> 16), p.h * a.group + r % a.group);
   }
 }
 
 template <int HD, int BM>
 cudaError_t launch(const PagedAttnArgs& a, int grid, cudaStream_t s) {
   const PagedGeom g{BM / a.group, BM / a.group, 6, 1, 2, 2};
-  return launch_after(paged_attn_kernel<float, HD, BM>, dim3(grid), kPThreads, sizeof(PagedSmem<HD, BM>), s, a, g);
+  return launch_after(paged_attn_kernel<HD, BM>, dim3(grid), kPThreads, sizeof(PagedSmem<HD, BM>), s, a, g);
 }
 
 }  // namespace
 
 cudaError_t paged_attention_f32_set_attributes() {
-  cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<float, 64, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 16>));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<float, 128, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 16>));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<float, 64, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 64>));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<float, 128, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 64>));
+  cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<64, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 16>));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<128, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 16>));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<64, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 64>));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<128, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 64>));
   return e;
 }
 
