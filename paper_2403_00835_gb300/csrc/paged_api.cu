@@ -235,7 +235,8 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
   cudaError_t e;
   if (c->es == 4) {
     e = launch_paged_attention_f32(a, d.head_dim, c->sms, st);
-  } else if (rows <= kFewRows && group <= kFewRows) {
+  } else if (group <= kFewRows && (rows <= kFewRows || (rows <= 2 * kFewRows && 2 * p->batch * d.n_kv_heads <= c->sms))) {
+    // (a second tile of 16 rows reads its keys again: worth it while SMs are idle)
     e = launch_paged_attention_few(a, c->mk_few, c->mv_few, d.dtype, d.head_dim, c->hold, c->sms, st);
   } else {
     e = launch_paged_attention_tc(a, c->mk, c->mv, d.dtype, d.head_dim, c->hold, c->sms, st);

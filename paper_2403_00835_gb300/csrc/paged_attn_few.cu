@@ -26,7 +26,7 @@ template <int HD>
 struct FewSmem {
   static constexpr int kShift = 6, kRing = HD == 128 ? 4 : 8;
   static constexpr int kTile = kFewKeys * HD * 2;
-  static constexpr int kRows = kFewRows, kRowWarps = kFewWarps, kPartRows = 32;
+  static constexpr int kRows = kFewRows, kRowWarps = kFewWarps, kPartRows = 32, kMergeBatch = 4;
   static constexpr bool kAhead = false, kIssuer = false;
   alignas(1024) uint8_t q[1][kRows * HD * 2];
   alignas(1024) uint8_t ring[kRing][kTile];
@@ -35,7 +35,7 @@ struct FewSmem {
   float2 ml[1][32];  // also the scratch of run_start
   uint64_t full[kRing], empty[kRing], qfull, qempty;
   uint64_t pfull[kPagePieces], pempty[kPagePieces], pfree[kPagePieces];
-  PagePiece piece[kPagePieces], cut;
+  PagePiece piece[kPagePieces], cut[2];  // (cut: to be merged after the run)
   RunStart run;
   unsigned bad[8];
   int abort, busy, last;
@@ -67,8 +67,7 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
   RingAt<S::kRing> at;
   RingAt<kPagePieces> pat;
   uint32_t nq = 0;       // pieces with keys so far
-  bool cut = false;      // a part is left to be merged
-  int cut_arrivals = 0;  // thread 0: the parts of it that were there before this CTA's
+  int cuts = 0, before0 = 0, before1 = 0;  // parts to be merged; thread 0: the parts of them that were there before
   for (;; ++pat) {
     if (!piece_wait(&s.pfull[pat.i], pat.phase)) break;
     const PagePiece& p = s.piece[pat.i];
@@ -263,22 +262,19 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
         __threadfence();
         before = atomicAdd(a.tickets + p.cta0, 1);
       }
-      if (p.final) {
-        merge_if_last<T, HD>(s, a, p, tt, before);
-      } else {
-        // nothing waits for the counter's answer here: whether this CTA has to merge the
-        // tile is seen to after the run
-        cut = true;
-        cut_arrivals = before;
-        if (tid < sizeof(PagePiece) / 4) reinterpret_cast<int*>(&s.cut)[tid] = reinterpret_cast<const int*>(&p)[tid];
-      }
+      // nothing waits for the counter's answer here: whether this CTA has to merge the
+      // tile is seen to after the run (whose first and last pieces may be parts)
+      (cuts == 0 ? before0 : before1) = before;
+      if (tid < sizeof(PagePiece) / 4) reinterpret_cast<int*>(&s.cut[cuts])[tid] = reinterpret_cast<const int*>(&p)[tid];
+      ++cuts;
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&s.pempty[pat.i]);
   }
-  if (cut) {
+#pragma unroll 1
+  for (int k = cuts - 1; k >= 0; --k) {
     all_rows<S>();
-    merge_if_last<T, HD>(s, a, s.cut, tt, cut_arrivals);
+    merge_if_last<T, HD>(s, a, s.cut[k], tt, k == 0 ? before0 : before1);
   }
 }
 

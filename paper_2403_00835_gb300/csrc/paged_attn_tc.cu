@@ -32,7 +32,7 @@ constexpr int kTcThreads = 320;  // warps 0-3, 4-7: the slots' rows; 8 MMAs; 9 l
 constexpr int kTcRows = 128, kTcShift = 7, kTcChunk = 1 << kTcShift, kTcHalf = 64;
 template <int HD>
 struct TcSmem {
-  static constexpr int kRows = kTcRows, kRowWarps = 8, kShift = kTcShift, kPartRows = 2 * kTcRows;
+  static constexpr int kRows = kTcRows, kRowWarps = 8, kShift = kTcShift, kPartRows = 2 * kTcRows, kMergeBatch = 4;
   static constexpr bool kAhead = true, kIssuer = true;
   static constexpr int kRing = HD == 128 ? 5 : 10;
   static constexpr int kTile = kTcChunk * HD * 2;
@@ -42,7 +42,7 @@ struct TcSmem {
   uint64_t full[kRing], empty[kRing], qfull, qempty, ofree, drain;
   uint64_t sfull[2], pready[2][2], ofull[2];  // of a slot: S is there; P of a half of the keys is; the piece's O is
   uint64_t pfull[kPagePieces], pempty[kPagePieces], pfree[kPagePieces];  // a piece is there; the rows, the issuer are done with it
-  PagePiece piece[kPagePieces], cut;  // (cut: one to be merged after the run)
+  PagePiece piece[kPagePieces], cut[2];  // (cut: to be merged after the run)
   RunStart run;
   unsigned bad[8];  // rows whose result is not finite
   uint32_t tmem;
@@ -206,8 +206,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
     tc_fence_after();
   };
   uint32_t r = 0, ns = 0, no[2] = {0, 0};  // loads of the pieces before, chunks of this slot, pieces of both
-  bool cut = false;        // a part is left to be merged
-  int cut_arrivals = 0;    // thread 0: the parts of it that were there before this CTA's
+  int cuts = 0, before0 = 0, before1 = 0;  // parts to be merged; thread 0: the parts of them that were there before
   RingAt<kPagePieces> pat;
   for (;; ++pat) {
     if (!piece_wait(&s.pfull[pat.i], pat.phase)) break;
@@ -421,15 +420,11 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
         __threadfence();
         before = atomicAdd(a.tickets + p.cta0, 1);
       }
-      if (p.final) {
-        merge_if_last<T, HD>(s, a, p, tt, before);
-      } else {
-        // nothing waits for the counter's answer here: whether this CTA has to merge the
-        // tile is seen to after the run
-        cut = true;
-        cut_arrivals = before;
-        if (tid < sizeof(PagePiece) / 4) reinterpret_cast<int*>(&s.cut)[tid] = reinterpret_cast<const int*>(&p)[tid];
-      }
+      // nothing waits for the counter's answer here: whether this CTA has to merge the
+      // tile is seen to after the run (whose first and last pieces may be parts)
+      (cuts == 0 ? before0 : before1) = before;
+      if (tid < sizeof(PagePiece) / 4) reinterpret_cast<int*>(&s.cut[cuts])[tid] = reinterpret_cast<const int*>(&p)[tid];
+      ++cuts;
     } else if (!two) {
       all_rows<TcSmem<HD>>();  // (s.ml is free again)
       redo_bad<T, HD>(s, a, p, tt);
@@ -437,9 +432,10 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
     __syncwarp();
     if (lane == 0) mbar_arrive(&s.pempty[pat.i]);
   }
-  if (cut) {
+#pragma unroll 1
+  for (int k = cuts - 1; k >= 0; --k) {
     all_rows<TcSmem<HD>>();
-    merge_if_last<T, HD>(s, a, s.cut, tt, cut_arrivals);
+    merge_if_last<T, HD>(s, a, s.cut[k], tt, k == 0 ? before0 : before1);
   }
 }
 

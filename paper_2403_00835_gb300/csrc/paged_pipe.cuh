@@ -30,7 +30,7 @@ struct PagePiece {
   int two, whole;                          // 128 rows in each slot; the whole tile
   int slot, cta0, cta1, first_slot;        // of a cut tile: this part's slot, the CTAs of its parts, the first's slot
   SlotChunks c[2];
-  int final, end;                          // the run's last piece; no piece: the run is over
+  int end;                                 // no piece: the run is over
   __device__ int part(int cta) const { return cta == cta0 ? first_slot : 2 * cta; }
 };
 constexpr int kPagePieces = 4;
@@ -126,7 +126,7 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
         if (more) {
           o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0, o.lo = p.lo, o.hi = p.hi;
           o.ca = p.ca, o.chunks = p.cb - p.ca;
-          o.two = p.nt > tt, o.whole = p.whole(), o.final = w.done();
+          o.two = p.nt > tt, o.whole = p.whole();
           if (!p.whole()) {
             o.slot = w.slot(p, blockIdx.x);
             o.cta0 = w.first_cta(p), o.cta1 = w.last_cta(p);
@@ -296,7 +296,7 @@ __device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, cons
   if (!s.last) return;
   // First the rows' maxima and sums, then their columns, 16 to a thread.  Where there are
   // fewer rows or columns than threads, `ways` neighbouring lanes share the parts.
-  constexpr int kThreads = 32 * S::kRowWarps;
+  constexpr int kThreads = 32 * S::kRowWarps, kBatch = S::kMergeBatch;  // parts whose loads are under way together
   const int live = p.nt * a.group, part_rows = rows_of_part<S>(a, p);
   const bool two = p.two;
   auto row_of = [&](int k) { return two && k >= tt * a.group ? 128 + k - tt * a.group : k; };
@@ -345,20 +345,21 @@ __device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, cons
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[j] = 0.f;
 #pragma unroll 1
-    for (int c = cta0 + sub; c <= cta1; c += 2 * ways) {
-      float4 y[2][4];
-      float m1[2];
+    for (int c = cta0 + sub; c <= cta1; c += kBatch * ways) {
+      float4 y[kBatch][4];
+      float m1[kBatch];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {  // (the loads of two parts under way)
-        const int part = p.part(min(c + u * ways, cta1));
-        m1[u] = c + u * ways <= cta1 ? __ldcg(part_ml_of<S>(a, part) + rr).x : -INFINITY;
+      for (int u = 0; u < kBatch; ++u) {
+        if (u > 0 && c + u * ways > cta1) continue;
+        const int part = p.part(c + u * ways);
+        m1[u] = __ldcg(part_ml_of<S>(a, part) + rr).x;
         const float4* from = part_of<S, HD>(a, part) + d / 4 * part_rows + rr;
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[u][j] = __ldcg(from + j * part_rows);
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if (m1[u] == -INFINITY) continue;  // none of its keys is seen
+      for (int u = 0; u < kBatch; ++u) {
+        if (c + u * ways > cta1 || m1[u] == -INFINITY) continue;  // (none of its keys is seen)
         const float f = ex2_ftz(m1[u] - mi.x);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

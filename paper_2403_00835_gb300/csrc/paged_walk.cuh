@@ -267,7 +267,6 @@ struct PagedWalk {
       load(a);
     }
   }
-  __device__ bool done() const { return u >= u1; }
   // contributors of a cut tile: CTAs [first, last]; CTA c's partial slot
   __device__ int first_cta(const Piece& p) const { return p.ca == p.tca ? blockIdx.x : p.tile_u / per; }
   __device__ int last_cta(const Piece& p) const { return p.cb == p.tcb ? blockIdx.x : (p.tile_u + (p.tcb - p.tca) - 1) / per; }
