@@ -8,6 +8,12 @@
 
 namespace cllm {
 
+// A cut tile's counters: parts written, groups of its rows taken for merging, parts' CTAs
+// that are done with it (the last of them clears the counters).
+struct PageTicket {
+  int arrived, claimed, left, unused;
+};
+
 // Arguments of an attention launch (device pointers; strides in elements).
 struct PagedAttnArgs {
   const void* q;
@@ -29,11 +35,11 @@ struct PagedAttnArgs {
   const void* v;
   long long s_page, s_head, s_pos;
   int layer, n_pages, page_shift;
-  // work that is cut over several CTAs: two partial tiles per CTA and an
-  // arrival counter per CTA (zero between launches)
+  // work that is cut over several CTAs: two partial tiles per CTA, and the
+  // counters of the tile that begins in it and goes on (zero between launches)
   float* part_o;
   float2* part_ml;
-  int* tickets;
+  PageTicket* tickets;
   int* err;
 };
 

@@ -15,8 +15,8 @@ struct cllm_paged {
   int dev = 0, sms = 0, page_shift = 0, es = 0;
   float* part_o = nullptr;
   float2* part_ml = nullptr;
-  int* tickets = nullptr;  // one per CTA, then the status word (all in part_o's allocation)
-  int n_tickets = 0;
+  PageTicket* tickets = nullptr;  // one per CTA, then the status word (all in part_o's allocation)
+  size_t ticket_bytes = 0;        // with the status word
   int* err = nullptr;
   CUtensorMap mk, mv, mk_few, mv_few;  // the pools (16-bit types) in boxes of 128 and 64 positions
   int hold = 0;            // test hook
@@ -122,20 +122,20 @@ extern "C" int cllm_paged_create(const cllm_paged_desc* desc, cllm_paged** out) 
     // (one allocation: it takes as long as the rest of the call)
     const size_t rows = 2 * static_cast<size_t>(sms) * kPagedPartRows;
     const size_t tickets = static_cast<size_t>(sms) * kPagedCtas;
-    const size_t so = rows * d.head_dim * 4, sm = rows * 8;
+    const size_t st = tickets * sizeof(PageTicket) + 4, so = rows * d.head_dim * 4, sm = rows * 8;
     static_assert(kPagedPartRows >= 64 * kPagedCtas, "slots of the kernels with several CTAs per SM");
     void* base = nullptr;
-    if (lib_malloc(&base, so + sm + (tickets + 1) * 4) != cudaSuccess) {
+    if (lib_malloc(&base, so + sm + st) != cudaSuccess) {
       rc = CLLM_ENOMEM;
       break;
     }
     c->part_o = static_cast<float*>(base);
     c->part_ml = reinterpret_cast<float2*>(static_cast<char*>(base) + so);
-    c->tickets = reinterpret_cast<int*>(static_cast<char*>(base) + so + sm);
-    c->n_tickets = static_cast<int>(tickets);
-    c->err = c->tickets + tickets;
+    c->tickets = reinterpret_cast<PageTicket*>(static_cast<char*>(base) + so + sm);
+    c->ticket_bytes = st;
+    c->err = reinterpret_cast<int*>(c->tickets + tickets);
     // (the default stream orders the clearing before any later work)
-    e = cudaMemset(c->tickets, 0, (tickets + 1) * 4);
+    e = cudaMemset(c->tickets, 0, st);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) rc = cuda_fail(e, "paged_create");
   } while (false);
@@ -155,7 +155,7 @@ extern "C" int cllm_paged_status(cllm_paged* c, void* cuda_stream) {
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e == cudaSuccess && err != 0) {
     // (a timed-out launch may leave arrival counters behind)
-    e = cudaMemsetAsync(c->tickets, 0, (c->n_tickets + 1) * 4, s);
+    e = cudaMemsetAsync(c->tickets, 0, c->ticket_bytes, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   }
   if (e != cudaSuccess) return cuda_fail(e, "paged_status");

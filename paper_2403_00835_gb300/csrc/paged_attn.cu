@@ -216,8 +216,8 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
       __threadfence();
       __syncthreads();
       if (tid == 0) {
-        s.last = atomicAdd(a.tickets + c0, 1) == c1 - c0;
-        if (s.last) a.tickets[c0] = 0;
+        s.last = atomicAdd(&a.tickets[c0].arrived, 1) == c1 - c0;
+        if (s.last) a.tickets[c0].arrived = 0;
         __threadfence();
       }
       __syncthreads();

@@ -26,19 +26,19 @@ template <int HD>
 struct FewSmem {
   static constexpr int kShift = 6, kRing = HD == 128 ? 4 : 8;
   static constexpr int kTile = kFewKeys * HD * 2;
-  static constexpr int kRows = kFewRows, kRowWarps = kFewWarps, kPartRows = 32, kMergeBatch = 4;
+  static constexpr int kRows = kFewRows, kRowWarps = kFewWarps, kPartRows = 32;
   static constexpr bool kAhead = false, kIssuer = false;
   alignas(1024) uint8_t q[1][kRows * HD * 2];
   alignas(1024) uint8_t ring[kRing][kTile];
   float o[kFewWarps][kFewRows][HD + 4];  // the warps' outputs at a tile's end
   float2 wml[kFewWarps][kFewRows];
-  float2 ml[1][32];  // also the scratch of run_start
+  unsigned scan[32];                     // of run_start_block
   uint64_t full[kRing], empty[kRing], qfull, qempty;
   uint64_t pfull[kPagePieces], pempty[kPagePieces], pfree[kPagePieces];
   PagePiece piece[kPagePieces], cut[2];  // (cut: to be merged after the run)
   RunStart run;
   unsigned bad[8];
-  int abort, busy, last;
+  int abort, busy, last, claim;
 };
 static_assert(2 * (sizeof(FewSmem<128>) + 1024) <= 228 * 1024, "two CTAs to an SM");
 static_assert(1 << FewSmem<64>::kShift == kFewKeys, "keys of a tile");
@@ -257,11 +257,7 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
     if (whole) {
       redo_bad<T, HD>(s, a, p, tt);
     } else {
-      int before = 0;
-      if (tid == 0) {
-        __threadfence();
-        before = atomicAdd(a.tickets + p.cta0, 1);
-      }
+      const int before = arrive_part<S>(a, p);
       // nothing waits for the counter's answer here: whether this CTA has to merge the
       // tile is seen to after the run (whose first and last pieces may be parts)
       (cuts == 0 ? before0 : before1) = before;
@@ -272,10 +268,7 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
     if (lane == 0) mbar_arrive(&s.pempty[pat.i]);
   }
 #pragma unroll 1
-  for (int k = cuts - 1; k >= 0; --k) {
-    all_rows<S>();
-    merge_if_last<T, HD>(s, a, s.cut[k], tt, k == 0 ? before0 : before1);
-  }
+  for (int k = cuts - 1; k >= 0; --k) finish_cut<T, HD>(s, a, s.cut[k], tt, k == 0 ? before0 : before1);
 }
 
 template <class T, int HD>
@@ -311,7 +304,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
   }
   pdl_launch_dependents();
   pdl_wait();  // (nothing of the calls before is read above)
-  if (a.batch > kWarpRequests) run_start_block(a, g, &s.run, reinterpret_cast<unsigned*>(s.ml));
+  if (a.batch > kWarpRequests) run_start_block(a, g, &s.run, s.scan);
   __syncthreads();
   if (threadIdx.x >= 32 * kFewWarps) issue_loads<HD>(s, a, g, m, hold);
   else run_few<T, HD>(s, a, g);

@@ -32,7 +32,7 @@ constexpr int kTcThreads = 320;  // warps 0-3, 4-7: the slots' rows; 8 MMAs; 9 l
 constexpr int kTcRows = 128, kTcShift = 7, kTcChunk = 1 << kTcShift, kTcHalf = 64;
 template <int HD>
 struct TcSmem {
-  static constexpr int kRows = kTcRows, kRowWarps = 8, kShift = kTcShift, kPartRows = 2 * kTcRows, kMergeBatch = 4;
+  static constexpr int kRows = kTcRows, kRowWarps = 8, kShift = kTcShift, kPartRows = 2 * kTcRows;
   static constexpr bool kAhead = true, kIssuer = true;
   static constexpr int kRing = HD == 128 ? 5 : 10;
   static constexpr int kTile = kTcChunk * HD * 2;
@@ -46,7 +46,7 @@ struct TcSmem {
   RunStart run;
   unsigned bad[8];  // rows whose result is not finite
   uint32_t tmem;
-  int abort, busy, last;
+  int abort, busy, last, claim;
 };
 static_assert(sizeof(TcSmem<128>) <= 227 * 1024 && sizeof(TcSmem<64>) <= 227 * 1024, "shared memory");
 
@@ -414,12 +414,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
       for (int u = 0; u < 2; ++u) no[u] += p.c[u].any();
     }
     if (!whole) {
-      all_rows<TcSmem<HD>>();
-      int before = 0;
-      if (tid == 0) {
-        __threadfence();
-        before = atomicAdd(a.tickets + p.cta0, 1);
-      }
+      const int before = arrive_part<TcSmem<HD>>(a, p);
       // nothing waits for the counter's answer here: whether this CTA has to merge the
       // tile is seen to after the run (whose first and last pieces may be parts)
       (cuts == 0 ? before0 : before1) = before;
@@ -433,10 +428,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD>& s, const PagedAttnArgs& a, 
     if (lane == 0) mbar_arrive(&s.pempty[pat.i]);
   }
 #pragma unroll 1
-  for (int k = cuts - 1; k >= 0; --k) {
-    all_rows<TcSmem<HD>>();
-    merge_if_last<T, HD>(s, a, s.cut[k], tt, k == 0 ? before0 : before1);
-  }
+  for (int k = cuts - 1; k >= 0; --k) finish_cut<T, HD>(s, a, s.cut[k], tt, k == 0 ? before0 : before1);
 }
 
 template <class T, int HD>

@@ -281,106 +281,137 @@ __device__ __forceinline__ float2* part_ml_of(const PagedAttnArgs& a, int slot) 
   return a.part_ml + static_cast<size_t>(slot) * S::kPartRows;
 }
 
-// Merge the parts of a tile, in order, if the others were there before this CTA's
-// (`before`: thread 0 has their number).
+// Merge group `group` of a tile's rows from its parts, in order: 16 columns of a row to a
+// thread, or to `ways` neighbouring lanes that share the parts; the loads of 4 parts are
+// under way together.
+template <class S, int HD>
+__device__ __forceinline__ int merge_ways(int parts) {
+  return parts >= 8 ? 4 : 1;
+}
+template <class S, int HD>
+__device__ __forceinline__ int merge_rows(int ways) {  // rows of a group
+  return 32 * S::kRowWarps / (HD / 16) / ways;
+}
 template <class T, int HD, class S>
-__device__ __forceinline__ void merge_if_last(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt, int before) {
-  const int tid = threadIdx.x;
-  const int cta0 = p.cta0, cta1 = p.cta1;
+__device__ __forceinline__ void merge_group(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt, int group, int ways) {
+  const int rows = merge_rows<S, HD>(ways), tid = threadIdx.x, sub = tid & (ways - 1), it = tid / ways;
+  const int k = group * rows + (it & (rows - 1)), d = it / rows * 16, live = p.nt * a.group, part_rows = rows_of_part<S>(a, p);
+  const int kk = min(k, live - 1), rr = p.two && kk >= tt * a.group ? 128 + kk - tt * a.group : kk;
+  float mm = -INFINITY, ll = 0.f, o[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) o[j] = 0.f;
+#pragma unroll 1
+  for (int c = p.cta0 + sub; c <= p.cta1; c += 4 * ways) {
+    float4 y[4][4];
+    float2 ml[4];
+    float nm = mm;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      ml[u] = make_float2(-INFINITY, 0.f);
+      if (c + u * ways > p.cta1) continue;
+      const int part = p.part(c + u * ways);
+      ml[u] = __ldcg(part_ml_of<S>(a, part) + rr);
+      const float4* from = part_of<S, HD>(a, part) + d / 4 * part_rows + rr;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[u][j] = __ldcg(from + j * part_rows);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) nm = fmaxf(nm, ml[u].x);
+    const float f = mm != -INFINITY ? ex2_ftz(mm - nm) : 0.f;
+    mm = nm;
+    ll *= f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[j] *= f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (ml[u].x == -INFINITY) continue;  // (none of its keys is seen)
+      const float w = ex2_ftz(ml[u].x - mm);
+      ll = fmaf(ml[u].y, w, ll);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o[4 * j] = fmaf(y[u][j].x, w, o[4 * j]);
+        o[4 * j + 1] = fmaf(y[u][j].y, w, o[4 * j + 1]);
+        o[4 * j + 2] = fmaf(y[u][j].z, w, o[4 * j + 2]);
+        o[4 * j + 3] = fmaf(y[u][j].w, w, o[4 * j + 3]);
+      }
+    }
+  }
+  for (int w = 1; w < ways; w <<= 1) {
+    const float m1 = __shfl_xor_sync(0xffffffffu, mm, w), l1 = __shfl_xor_sync(0xffffffffu, ll, w), nm = fmaxf(mm, m1);
+    const float f0 = mm != -INFINITY ? ex2_ftz(mm - nm) : 0.f, f1 = m1 != -INFINITY ? ex2_ftz(m1 - nm) : 0.f;
+    mm = nm;
+    ll = ll * f0 + l1 * f1;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float o1 = __shfl_xor_sync(0xffffffffu, o[j], w);
+      o[j] = (f0 != 0.f ? o[j] * f0 : 0.f) + (f1 != 0.f ? o1 * f1 : 0.f);
+    }
+  }
+  if (sub == 0 && k < live) {
+    const int kt = k * a.group_inv >> 16, head = p.h * a.group + k - kt * a.group;
+    T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + kt) * a.out_row + static_cast<long long>(head) * a.out_head + d;
+    if (write16(out, o, ll != 0.f ? 1.f / ll : 0.f)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
+    if (d == 0) store_lse(a, p, p.t0 + kt, head, mm, ll);
+  }
+}
+
+// A part of a tile has been written (all row warps call; what its counter said goes to
+// thread 0): the parts that were there before.
+template <class S>
+__device__ __forceinline__ int arrive_part(const PagedAttnArgs& a, const PagePiece& p) {
+  all_rows<S>();
+  int before = 0;
+  if (threadIdx.x == 0) {
+    __threadfence();
+    before = atomicAdd(&a.tickets[p.cta0].arrived, 1);
+  }
+  return before;
+}
+
+// See to a cut tile after the run: its last part's CTA merges it.  Where that is much (a
+// block of 64 rows in 19 parts: 0.6 MB, which one SM takes in in 9 us), the
+// CTAs of the other parts stay for a while and take groups of its rows too; none is
+// waited for.
+constexpr uint64_t kMergeLingerNs = 20000;
+template <class T, int HD, class S>
+__device__ __forceinline__ void finish_cut(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt, int before) {
+  // (the piece was copied by other threads, and s.last of the tile before has been read)
+  all_rows<S>();
+  const int tid = threadIdx.x, parts = p.cta1 - p.cta0 + 1, live = p.nt * a.group, ways = merge_ways<S, HD>(parts);
+  const int groups = (live + merge_rows<S, HD>(ways) - 1) / merge_rows<S, HD>(ways);
+  const bool share = ways > 1 && groups > 1;  // (of two or three parts each CTA has one to merge anyway)
+  PageTicket* t = a.tickets + p.cta0;
   if (tid == 0) {
-    s.last = before == cta1 - cta0;
-    if (s.last) a.tickets[cta0] = 0;
+    bool there = before == parts - 1;
+    if (!there && share) {
+      const uint64_t t0 = globaltimer_ns();
+      while (!there && globaltimer_ns() - t0 < kMergeLingerNs) {
+        there = *const_cast<volatile int*>(&t->arrived) == parts;
+        if (!there) __nanosleep(200);
+      }
+    }
+    s.last = there;
     __threadfence();
   }
   all_rows<S>();
-  if (!s.last) return;
-  // First the rows' maxima and sums, then their columns, 16 to a thread.  Where there are
-  // fewer rows or columns than threads, `ways` neighbouring lanes share the parts.
-  constexpr int kThreads = 32 * S::kRowWarps, kBatch = S::kMergeBatch;  // parts whose loads are under way together
-  const int live = p.nt * a.group, part_rows = rows_of_part<S>(a, p);
-  const bool two = p.two;
-  auto row_of = [&](int k) { return two && k >= tt * a.group ? 128 + k - tt * a.group : k; };
-  auto ways_for = [](int items) { return items * 16 <= kThreads ? 16 : items * 4 <= kThreads ? 4 : items * 2 <= kThreads ? 2 : 1; };
-  {
-    const int ways = ways_for(live), sub = tid & (ways - 1);
-    for (int k0 = 0; k0 < live; k0 += kThreads / ways) {
-      const int k = k0 + tid / ways, rr = row_of(min(k, live - 1));
-      float mm = -INFINITY, ll = 0.f;
-#pragma unroll 1
-      for (int c = cta0 + sub; c <= cta1; c += 4 * ways) {
-        float2 ml[4];
-        float nm = mm;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          ml[u] = c + u * ways <= cta1 ? __ldcg(part_ml_of<S>(a, p.part(c + u * ways)) + rr) : make_float2(-INFINITY, 0.f);
-          nm = fmaxf(nm, ml[u].x);
-        }
-        ll = mm != -INFINITY ? ll * ex2_ftz(mm - nm) : 0.f;
-        mm = nm;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) ll += ml[u].x != -INFINITY ? ml[u].y * ex2_ftz(ml[u].x - mm) : 0.f;
+  if (s.last) {
+    int g = 0;
+    for (int k = 0;; ++k) {
+      if (share) {
+        all_rows<S>();
+        if (tid == 0) s.claim = atomicAdd(&t->claimed, 1);
+        all_rows<S>();
+        g = s.claim;
+      } else {
+        g = k;
       }
-      for (int w = 1; w < ways; w <<= 1) {
-        const float m1 = __shfl_xor_sync(0xffffffffu, mm, w), l1 = __shfl_xor_sync(0xffffffffu, ll, w), nm = fmaxf(mm, m1);
-        // (in the same order on both sides, so that the lanes agree bit for bit)
-        const float a0 = mm != -INFINITY ? ll * ex2_ftz(mm - nm) : 0.f, a1 = m1 != -INFINITY ? l1 * ex2_ftz(m1 - nm) : 0.f;
-        ll = sub & w ? a1 + a0 : a0 + a1;
-        mm = nm;
-      }
-      if (k < live && sub == 0) {
-        (&s.ml[0][0])[k] = make_float2(mm, ll != 0.f ? 1.f / ll : 0.f);
-        const int kt = k * a.group_inv >> 16;
-        store_lse(a, p, p.t0 + kt, p.h * a.group + k - kt * a.group, mm, ll);
-      }
+      if (g >= groups) break;
+      merge_group<T, HD>(s, a, p, tt, g, ways);
     }
+    all_rows<S>();
+    redo_bad<T, HD>(s, a, p, tt);
   }
-  all_rows<S>();
-  const int items = live * (HD / 16), ways = ways_for(items), sub = tid & (ways - 1);
-#pragma unroll 1
-  for (int i0 = 0; i0 < items; i0 += kThreads / ways) {
-    const int i = min(i0 + tid / ways, items - 1);
-    const int k = i % live, d = i / live * 16, rr = row_of(k);
-    const float2 mi = (&s.ml[0][0])[k];
-    float o[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) o[j] = 0.f;
-#pragma unroll 1
-    for (int c = cta0 + sub; c <= cta1; c += kBatch * ways) {
-      float4 y[kBatch][4];
-      float m1[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        if (u > 0 && c + u * ways > cta1) continue;
-        const int part = p.part(c + u * ways);
-        m1[u] = __ldcg(part_ml_of<S>(a, part) + rr).x;
-        const float4* from = part_of<S, HD>(a, part) + d / 4 * part_rows + rr;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[u][j] = __ldcg(from + j * part_rows);
-      }
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        if (c + u * ways > cta1 || m1[u] == -INFINITY) continue;  // (none of its keys is seen)
-        const float f = ex2_ftz(m1[u] - mi.x);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          o[4 * j] = fmaf(y[u][j].x, f, o[4 * j]);
-          o[4 * j + 1] = fmaf(y[u][j].y, f, o[4 * j + 1]);
-          o[4 * j + 2] = fmaf(y[u][j].z, f, o[4 * j + 2]);
-          o[4 * j + 3] = fmaf(y[u][j].w, f, o[4 * j + 3]);
-        }
-      }
-    }
-    for (int w = 1; w < ways; w <<= 1)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) o[j] += __shfl_xor_sync(0xffffffffu, o[j], w);
-    if (sub != 0 || i0 + tid / ways >= items) continue;
-    const int kt = k * a.group_inv >> 16;
-    T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + kt) * a.out_row +
-             static_cast<long long>(p.h * a.group + k - kt * a.group) * a.out_head + d;
-    if (write16(out, o, mi.y)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
-  }
-  all_rows<S>();
-  redo_bad<T, HD>(s, a, p, tt);
+  if (tid == 0 && atomicAdd(&t->left, 1) == parts - 1) t->arrived = t->claimed = t->left = 0;
 }
 
 }  // namespace cllm
