@@ -60,6 +60,13 @@ __device__ T block_scan(T v, T* sm, T& total) {
   return plus(before, v);
 }
 
+// Index `k` places after `first` in the ring (both below n, unless the caller's numbers are
+// not a ring's: the result is inside it in any case).
+__device__ __forceinline__ unsigned ring_at(unsigned first, unsigned k, unsigned n) {
+  const unsigned x = first + k;
+  return x < n ? x : x - n < n ? x - n : x % n;
+}
+
 __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs a) {
   extern __shared__ int sm_req[];
   __shared__ long long sm_scan[kPlanThreads / 32];
@@ -79,13 +86,16 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   const int count = min(max(__ldcg(a.in.state + 1), 0), N);
   const int per = (B + kPlanThreads - 1) / kPlanThreads, b0 = min(tid * per, B), b1 = min(b0 + per, B);
 
-  long long rows = 0, total_rows;
-  for (int b = b0; b < b1; ++b) rows += max(__ldcg(a.new_rows + b), 0);
+  // (a thread's first request is loaded at once: most batches have no second)
+  int c0 = 0, n0 = 0, h0 = 0;
+  if (b0 < b1) c0 = __ldcg(a.ctx + b0), n0 = __ldcg(a.new_rows + b0), h0 = __ldcg(a.in.held + b0);
+  long long rows = max(n0, 0), total_rows;
+  for (int b = b0 + 1; b < b1; ++b) rows += max(__ldcg(a.new_rows + b), 0);
   long long end = block_scan(rows, sm_scan, total_rows) - rows;
   int2 pages = make_int2(0, 0), total;  // taken if granted, given back
   for (int b = b0; b < b1; ++b) {
-    const long long c = __ldcg(a.ctx + b), n = __ldcg(a.new_rows + b);
-    const int h = min(max(__ldcg(a.in.held + b), 0), W);
+    const long long c = b == b0 ? c0 : __ldcg(a.ctx + b), n = b == b0 ? n0 : __ldcg(a.new_rows + b);
+    const int h = min(max(b == b0 ? h0 : __ldcg(a.in.held + b), 0), W);
     end += max(n, 0ll);
     const bool valid = c >= 0 && n >= 0 && c + n <= static_cast<long long>(W) * P && end <= a.rows.max_rows;
     const int need = valid ? static_cast<int>((c + n + P - 1) >> a.page_shift) : h;
@@ -111,32 +121,12 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   if (taken > 0) atomicMax(&sm_taken, taken);
   __syncthreads();
 
-  // every input that may be updated in place has been read: the last CTA to get
-  // here writes the requests' results
-  if (tid == 0) {
-    sm_last = 1;
-    if (gridDim.x > 1) {
-      __threadfence();
-      sm_last = atomicAdd(a.out.state + 2, 1) == static_cast<int>(gridDim.x) - 1;
-      __threadfence();
-    }
-  }
-  __syncthreads();
-  if (sm_last) {
-    for (int b = tid; b < B; b += kPlanThreads) {
-      const bool ok = after[b] >= 0;
-      const int len = ok ? start[b] + row_end[b] - (b > 0 ? row_end[b - 1] : 0) : 0;
-      a.out.held[b] = ok ? after[b] : held[b];
-      a.rows.granted[b] = ok;
-      a.rows.seq_len[b] = len;
-      a.rows.row_start[b + 1] = row_end[b];
-    }
-    if (tid == 0) {
-      a.rows.row_start[0] = 0;
-      a.out.state[0] = static_cast<int>((static_cast<long long>(head) + sm_taken) % N);
-      a.out.state[1] = min(count - sm_taken + total.y, N);
-      a.out.state[2] = 0;
-    }
+  // Every input that may be updated in place has been read: the last CTA to get here
+  // writes the requests' results, at its end (the counter's answer takes a while).
+  int arrived = 0;
+  if (tid == 0 && gridDim.x > 1) {
+    __threadfence();
+    arrived = atomicAdd(a.out.state + 2, 1);
   }
 
   // block tables, a warp per request
@@ -145,12 +135,23 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
     const int h = held[b], h2 = after[b] >= 0 ? after[b] : h, keep = min(h, h2);
     const int* in = a.in.table + static_cast<size_t>(b) * W;
     int* out = a.out.table + static_cast<size_t>(b) * W;
-    for (int j = (in == out ? keep : 0) + lane; j < W; j += 32) {
-      int page = -1;
-      if (j < keep) page = in[j];
-      else if (j < h2) page = __ldcg(a.in.ring + (static_cast<unsigned>(first[b]) + (j - h)) % N);
-      else if (j < h) a.in.ring[(static_cast<unsigned>(first[b]) + (j - h2)) % N] = in[j];
-      out[j] = page;
+    // (8 loads under way before the first store)
+    for (int j0 = (in == out ? keep : 0) + lane; j0 < W; j0 += 256) {
+      int page[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int j = j0 + 32 * u;
+        page[u] = -1;
+        if (j < h) page[u] = in[j];
+        else if (j < h2) page[u] = __ldcg(a.in.ring + ring_at(first[b], j - h, N));
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int j = j0 + 32 * u;
+        if (j >= W) break;
+        if (j >= h2 && j < h) a.in.ring[ring_at(first[b], j - h2, N)] = page[u], page[u] = -1;
+        out[j] = page[u];
+      }
     }
   }
 
@@ -169,12 +170,34 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
         pos = start[lo] + t - (lo > 0 ? row_end[lo - 1] : 0);
         const int j = pos >> a.page_shift, h = held[lo];
         const int page = j < h ? a.in.table[static_cast<size_t>(lo) * W + j]
-                               : __ldcg(a.in.ring + (static_cast<unsigned>(first[lo]) + (j - h)) % N);
+                               : __ldcg(a.in.ring + ring_at(first[lo], j - h, N));
         slot = (static_cast<long long>(page) << a.page_shift) + (pos & (P - 1));
       }
     }
     a.rows.slots[t] = slot;
     a.rows.positions[t] = pos;
+  }
+
+  if (tid == 0) {
+    sm_last = arrived == static_cast<int>(gridDim.x) - 1;
+    __threadfence();
+  }
+  __syncthreads();
+  if (sm_last) {
+    for (int b = tid; b < B; b += kPlanThreads) {
+      const bool ok = after[b] >= 0;
+      const int len = ok ? start[b] + row_end[b] - (b > 0 ? row_end[b - 1] : 0) : 0;
+      a.out.held[b] = ok ? after[b] : held[b];
+      a.rows.granted[b] = ok;
+      a.rows.seq_len[b] = len;
+      a.rows.row_start[b + 1] = row_end[b];
+    }
+    if (tid == 0) {
+      a.rows.row_start[0] = 0;
+      a.out.state[0] = static_cast<int>((static_cast<long long>(head) + sm_taken) % N);
+      a.out.state[1] = min(count - sm_taken + total.y, N);
+      a.out.state[2] = 0;
+    }
   }
 }
 
