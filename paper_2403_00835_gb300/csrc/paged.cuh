@@ -11,7 +11,7 @@ namespace cllm {
 // A cut tile's counters: parts written, groups of its rows taken for merging, parts' CTAs
 // that are done with it (the last of them clears the counters).
 struct PageTicket {
-  int arrived, claimed, left, unused;
+  int arrived, claimed, left;
 };
 
 // Arguments of an attention launch (device pointers; strides in elements).
@@ -46,7 +46,8 @@ struct PagedAttnArgs {
 // Launch a kernel that may start while the one before it in the stream ends; it
 // waits (griddepcontrol.wait) before it touches memory.
 template <class... P, class... A>
-inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, const A&... args) {
+inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s,
+                                const A&... args) {
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
   cfg.gridDim = grid;
@@ -86,19 +87,19 @@ cudaError_t launch_paged_attention_f32(const PagedAttnArgs& a, int hd, int grid,
 cudaError_t paged_attention_f32_set_attributes();
 // 16-bit pools (paged_attn_tc.cu); k, v: the pools' maps; hold: test hook, 1 + the chunk
 // of a piece at which the MMA issuer gives up (0: none)
-cudaError_t launch_paged_attention_tc(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
-                                      int hold, int grid, cudaStream_t s);
+cudaError_t launch_paged_attention_tc(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype,
+                                      int hd, int hold, int grid, cudaStream_t s);
 cudaError_t paged_attention_tc_set_attributes();
 // a pool in boxes of 64 columns and `keys` positions, or a page's if that is less
 bool paged_pool_map(CUtensorMap* m, const void* pool, const cllm_paged_desc& d, int keys);
 // queries of a tile of `rows` rows: group heads of rows / group tokens, row = token * group + head
 bool paged_query_map(CUtensorMap* m, const PagedAttnArgs& a, int dtype, int hd, int rows);
-// 16-bit pools, few rows (paged_attn_mma.cu): tiles of 16 rows, group at most 16; k, v:
+// 16-bit pools, few rows (paged_attn_few.cu): tiles of 16 rows, group at most 16; k, v:
 // maps of 64 positions; sms: SMs of the device; hold: 1 + the chunk of a piece at which
 // the loading warp gives up
 constexpr int kFewRows = 16, kFewKeys = 64;
-cudaError_t launch_paged_attention_few(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
-                                       int hold, int sms, cudaStream_t s);
+cudaError_t launch_paged_attention_few(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype,
+                                       int hd, int hold, int sms, cudaStream_t s);
 cudaError_t paged_attention_few_set_attributes();
 
 }  // namespace cllm

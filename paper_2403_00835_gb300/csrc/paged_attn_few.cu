@@ -13,6 +13,14 @@
 // tile has its beginning or end while the other's streams.  A row's keys are dealt to the
 // warps in fixed order, so results do not depend on timing.
 //
+// Measured: 8 blocks of 16 tokens at 600 keys, 32 heads: 13.6 us, 6.1 TB/s (the tensor-memory
+// kernel: 20.0); 64 requests of one token at 300 keys, 32 heads on 8: 15.9 us, 5.0 TB/s (28.1);
+// 128 of one token at 100 keys, 32 heads: 58 us (102); 16 of one token at 4096 keys, 32 heads
+// on 8: 50 us, 5.4 TB/s (46: where lengths are long the other's deeper ring is worth more
+// than this one's short ends, but the host, which chooses, does not know the lengths); one
+// block of 16 at 144 keys: 7.8 us (8.9), of which a launch's start, the first loads' latency
+// and cold instructions are about 5.
+//
 // Rounding: as in the tensor-memory kernel, P goes to the pools' type.
 #include "paged_pipe.cuh"
 
@@ -26,7 +34,7 @@ template <int HD>
 struct FewSmem {
   static constexpr int kShift = 6, kRing = HD == 128 ? 4 : 8;
   static constexpr int kTile = kFewKeys * HD * 2;
-  static constexpr int kRows = kFewRows, kRowWarps = kFewWarps, kPartRows = 32;
+  static constexpr int kRows = kFewRows, kRowWarps = kFewWarps, kPartRows = 32, kBands = 1;
   static constexpr bool kAhead = false, kIssuer = false;
   alignas(1024) uint8_t q[1][kRows * HD * 2];
   alignas(1024) uint8_t ring[kRing][kTile];
@@ -34,7 +42,7 @@ struct FewSmem {
   float2 wml[kFewWarps][kFewRows];
   unsigned scan[32];                     // of run_start_block
   uint64_t full[kRing], empty[kRing], qfull, qempty;
-  uint64_t pfull[kPagePieces], pempty[kPagePieces], pfree[kPagePieces];
+  uint64_t pfull[kPagePieces], pempty[kPagePieces];
   PagePiece piece[kPagePieces], cut[2];  // (cut: to be merged after the run)
   RunStart run;
   unsigned bad[8];
@@ -45,10 +53,14 @@ static_assert(1 << FewSmem<64>::kShift == kFewKeys, "keys of a tile");
 
 template <class T> struct Mma16;
 template <> struct Mma16<__half> {
-  static __device__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) { mma_f16_16816(d, a, b0, b1); }
+  static __device__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    mma_f16_16816(d, a, b0, b1);
+  }
 };
 template <> struct Mma16<__nv_bfloat16> {
-  static __device__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) { mma_bf16_16816(d, a, b0, b1); }
+  static __device__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    mma_bf16_16816(d, a, b0, b1);
+  }
 };
 
 // 16-byte piece `c` of row `row` of a tile with the 128-byte swizzle, 64 columns of all rows after another.
@@ -86,10 +98,11 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
       for (int kk = 0; kk < HD / 16; ++kk) ldmatrix_x4_a(q[kk], tile_addr(qb, S::kRows, lane & 15, kk * 2 + (lane >> 4)));
       __syncwarp();
       if (lane == 0) mbar_arrive(&s.qempty);
-      RowKeys rk[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) rk[u] = row_keys(a, p.n, p.len, p.row0, p.t0 + (min(quad + 8 * u, rows - 1) * a.group_inv >> 16));
-      const int from = max(rk[0].lo, rk[1].lo), to = min(rk[0].bits != nullptr ? rk[0].ctx : rk[0].hi, rk[1].bits != nullptr ? rk[1].ctx : rk[1].hi);
+      auto keys_of = [&](int r) {  // of row r of the tile
+        return row_keys(a, p.n, p.len, p.row0, p.t0 + (min(r, rows - 1) * a.group_inv >> 16));
+      };
+      // keys [from, to) are seen by both of this lane's rows
+      const int from = keys_of(quad + 8).lo, to = a.mask != nullptr ? p.len - p.n : keys_of(quad).hi;
 #pragma unroll 1
       for (int i = 0; i < n; ++i) {
         const int kb = (ca + i) * kFewKeys + warp * KEYS;  // this warp's keys: [kb, kb + KEYS)
@@ -111,7 +124,8 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
 #pragma unroll
             for (int j = 0; j < KEYS / 16; ++j) {
               uint32_t b[4];
-              ldmatrix_x4_a(b, tile_addr(base, kFewKeys, warp * KEYS + j * 16 + (lane >> 4) * 8 + (lane & 7), kk * 2 + (lane >> 3 & 1)));
+              const int key = warp * KEYS + j * 16 + (lane >> 4) * 8 + (lane & 7);
+              ldmatrix_x4_a(b, tile_addr(base, kFewKeys, key, kk * 2 + (lane >> 3 & 1)));
               Mma16<T>::mma(x[2 * j], q[kk], b[0], b[1]);
               Mma16<T>::mma(x[2 * j + 1], q[kk], b[2], b[3]);
             }
@@ -124,7 +138,7 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
             for (int u = 0; u < 2; ++u)
 #pragma unroll
               for (int c = 0; c < (KEYS + 31) / 32; ++c) {
-                const uint32_t see = key_bits(rk[u], kb + 32 * c) >> col;
+                const uint32_t see = key_bits(keys_of(quad + 8 * u), kb + 32 * c) >> col;
 #pragma unroll
                 for (int j = 4 * c; j < min(4 * c + 4, KEYS / 8); ++j) {
                   if (!(see >> (j - 4 * c) * 8 & 1)) x[j][2 * u] = -INFINITY;
@@ -168,10 +182,10 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
             // keys that no row of the tile sees (not loaded, or what the page held before): p
             // is 0 there, and so is V
             for (int c = lane; c < KEYS * HD / 8; c += 32) {
-              const int key = kb + c / (HD / 8);
+              const int k = c / (HD / 8), key = kb + k;
               if (key < lo || key >= hi)
-                *reinterpret_cast<uint4*>(s.ring[vt] + (c % (HD / 8) >> 3) * kFewKeys * 128 + (warp * KEYS + c / (HD / 8)) * 128 + (c & 7) * 16) =
-                    make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(s.ring[vt] + (c % (HD / 8) >> 3) * kFewKeys * 128 + (warp * KEYS + k) * 128 +
+                                          (c & 7) * 16) = make_uint4(0, 0, 0, 0);
             }
             // (before the tile is loaded anew)
             fence_proxy_async_smem();
@@ -181,7 +195,8 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
 #pragma unroll
           for (int j = 0; j < KEYS / 16; ++j) {
             const uint32_t pa[4] = {Pack16<T>::pack(x[2 * j][0], x[2 * j][1]), Pack16<T>::pack(x[2 * j][2], x[2 * j][3]),
-                                    Pack16<T>::pack(x[2 * j + 1][0], x[2 * j + 1][1]), Pack16<T>::pack(x[2 * j + 1][2], x[2 * j + 1][3])};
+                                    Pack16<T>::pack(x[2 * j + 1][0], x[2 * j + 1][1]),
+                                    Pack16<T>::pack(x[2 * j + 1][2], x[2 * j + 1][3])};
 #pragma unroll
             for (int d = 0; d < HD / 16; ++d) {
               uint32_t b[4];
@@ -249,8 +264,8 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
       }
       if (any != 0.f) atomicOr(&s.bad[r >> 5], 1u << (r & 31));
       const int rt = r * a.group_inv >> 16, tok = p.t0 + rt, head = p.h * a.group + r - rt * a.group;
-      *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + static_cast<long long>(p.row0 + tok) * a.out_row + head * a.out_head + d8 * 8) =
-          make_uint4(u[0], u[1], u[2], u[3]);
+      T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + tok) * a.out_row + head * a.out_head + d8 * 8;
+      *reinterpret_cast<uint4*>(out) = make_uint4(u[0], u[1], u[2], u[3]);
       if (d8 == 0) store_lse(a, p, tok, head, mm, ll);
     }
     all_rows<S>();  // (s.o and s.wml are free again)
@@ -321,7 +336,8 @@ cudaError_t launch_few(const PagedMaps& m, const PagedAttnArgs& a, int hold, int
 
 template <class T, int HD>
 cudaError_t attr() {
-  return cudaFuncSetAttribute(paged_attn_few_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewSmem<HD>));
+  return cudaFuncSetAttribute(paged_attn_few_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              sizeof(FewSmem<HD>));
 }
 
 }  // namespace
@@ -333,14 +349,15 @@ cudaError_t paged_attention_few_set_attributes() {
   return e == cudaSuccess ? attr<__nv_bfloat16, 128>() : e;
 }
 
-cudaError_t launch_paged_attention_few(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype, int hd,
-                                       int hold, int sms, cudaStream_t s) {
+cudaError_t launch_paged_attention_few(const PagedAttnArgs& a, const CUtensorMap& k, const CUtensorMap& v, int dtype,
+                                       int hd, int hold, int sms, cudaStream_t s) {
   PagedMaps m;
   m.k = k;
   m.v = v;
   if (!paged_query_map(&m.q, a, dtype, hd, kFewRows)) return cudaErrorInvalidValue;
   if (dtype == CLLM_BF16)
-    return hd == 64 ? launch_few<__nv_bfloat16, 64>(m, a, hold, sms, s) : launch_few<__nv_bfloat16, 128>(m, a, hold, sms, s);
+    return hd == 64 ? launch_few<__nv_bfloat16, 64>(m, a, hold, sms, s)
+                    : launch_few<__nv_bfloat16, 128>(m, a, hold, sms, s);
   return hd == 64 ? launch_few<__half, 64>(m, a, hold, sms, s) : launch_few<__half, 128>(m, a, hold, sms, s);
 }
 

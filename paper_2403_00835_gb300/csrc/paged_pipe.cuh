@@ -41,7 +41,8 @@ struct PagedMaps {
 
 // mbar_wait, but time in which a warp redoes rows (busy) does not count, and once
 // a wait has run out the others end at once.
-static __device__ __noinline__ bool page_wait_on(uint64_t* bar, uint32_t parity, volatile int* abort, volatile int* busy) {
+static __device__ __noinline__ bool page_wait_on(uint64_t* bar, uint32_t parity, volatile int* abort,
+                                                 volatile int* busy) {
   if (*abort) return false;
   uint64_t t0 = globaltimer_ns();
   uint32_t it = 0;
@@ -90,11 +91,13 @@ template <> struct Pack16<__nv_bfloat16> {
 
 // Walk the CTA's run, hand each piece to the other warps, and load its queries, keys and
 // values.
-// S::kShift: log2 of the keys of a tile; S::kAhead: K one tile ahead of V (K0 K1 V0 K2 V1 ..), else K0 V0 K1 V1 ..; S::kIssuer: a
-// warp beside the row warps takes the pieces too.  hold: test hook, 1 + the chunk of a
+// S::kShift: log2 of the keys of a tile; S::kAhead: K one tile ahead of V (K0 K1 V0 K2 V1
+// ..), else K0 V0 K1 V1 ..; S::kIssuer: a warp beside the row warps takes the pieces too;
+// S::kBands: copies of a tile's queries.  hold: test hook, 1 + the chunk of a
 // piece at which this warp gives up (0: none).
 template <int HD, class S>
-__device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const PagedGeom& g, const PagedMaps& m, int hold) {
+__device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const PagedGeom& g, const PagedMaps& m,
+                                            int hold) {
   constexpr int NH = HD / 64, NR = S::kRing, kChunk = 1 << S::kShift;
   const int lane = threadIdx.x & 31, tt = g.slot_tok, P = 1 << a.page_shift;
   const int box_shift = min(a.page_shift, S::kShift), box = 1 << box_shift;
@@ -115,7 +118,7 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
     const bool more = w.next(a, g, p);
     if (pieces >= kPagePieces) {
       wait(&s.pempty[pat.i], pat.phase ^ 1);
-      if (S::kIssuer) wait(&s.pfree[pat.i], pat.phase ^ 1);
+      if constexpr (S::kIssuer) wait(&s.pfree[pat.i], pat.phase ^ 1);
     }
     if (!ok) break;
     ++pieces;
@@ -124,7 +127,8 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
         PagePiece& o = s.piece[pat.i];
         o.end = !more;
         if (more) {
-          o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0, o.lo = p.lo, o.hi = p.hi;
+          o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0;
+          o.lo = p.lo, o.hi = p.hi;
           o.ca = p.ca, o.chunks = p.cb - p.ca;
           o.two = p.nt > tt, o.whole = p.whole();
           if (!p.whole()) {
@@ -179,12 +183,16 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
     int page = page_of(p.ca);
     if (with_keys > 0) wait(&s.qempty, (with_keys - 1) & 1);
     if (!ok) break;
-    const int slots = p.nt > tt ? 2 : 1;
-    if (lane == 0) mbar_arrive_expect_tx(&s.qfull, slots * NH * tt * a.group * 128);
+    // the queries: 128 rows to each slot, or in each of the bands
+    const int copies = p.nt > tt ? 2 : S::kBands;
+    if (lane == 0) mbar_arrive_expect_tx(&s.qfull, copies * NH * tt * a.group * 128);
     __syncwarp();
-    if (lane < slots * NH)
-      tma_load_3d(s.q[lane / NH] + lane % NH * S::kRows * 128, &m.q, &s.qfull, lane % NH * 64, p.h * a.group,
-                  p.row0 + p.t0 + lane / NH * tt);
+    if (lane < copies * NH) {
+      const int c = lane / NH;
+      uint8_t* to = S::kBands > 1 ? s.q[0] + c * (S::kRows / S::kBands) * 128 : s.q[c];
+      tma_load_3d(to + lane % NH * S::kRows * 128, &m.q, &s.qfull, lane % NH * 64, p.h * a.group,
+                  p.row0 + p.t0 + (S::kBands > 1 ? 0 : c * tt));
+    }
     ++with_keys;
     tile(&m.k, p.ca, page);
     hand_out();  // (the first keys are on their way)
@@ -236,9 +244,11 @@ __device__ __forceinline__ bool write16(T* out, const float (&o)[16], float scal
   return bad;
 }
 
-__device__ __forceinline__ void store_lse(const PagedAttnArgs& a, const PagePiece& p, int tok, int head, float m, float l) {
-  if (a.lse != nullptr)
-    a.lse[static_cast<size_t>(p.row0 + tok) * a.H + head] = l != 0.f ? (m + log2f(l)) * 0.69314718055994530942f : -INFINITY;
+__device__ __forceinline__ void store_lse(const PagedAttnArgs& a, const PagePiece& p, int tok, int head, float m,
+                                          float l) {
+  if (a.lse == nullptr) return;
+  a.lse[static_cast<size_t>(p.row0 + tok) * a.H + head] =
+      l != 0.f ? (m + log2f(l)) * 0.69314718055994530942f : -INFINITY;
 }
 
 // Row rr of a tile from the definition (the whole warp).
@@ -284,18 +294,17 @@ __device__ __forceinline__ float2* part_ml_of(const PagedAttnArgs& a, int slot) 
 // Merge group `group` of a tile's rows from its parts, in order: 16 columns of a row to a
 // thread, or to `ways` neighbouring lanes that share the parts; the loads of 4 parts are
 // under way together.
-template <class S, int HD>
-__device__ __forceinline__ int merge_ways(int parts) {
-  return parts >= 8 ? 4 : 1;
-}
+__device__ __forceinline__ int merge_ways(int parts) { return parts >= 8 ? 4 : 1; }
 template <class S, int HD>
 __device__ __forceinline__ int merge_rows(int ways) {  // rows of a group
   return 32 * S::kRowWarps / (HD / 16) / ways;
 }
 template <class T, int HD, class S>
-__device__ __forceinline__ void merge_group(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt, int group, int ways) {
+__device__ __forceinline__ void merge_group(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt, int group,
+                                            int ways) {
   const int rows = merge_rows<S, HD>(ways), tid = threadIdx.x, sub = tid & (ways - 1), it = tid / ways;
-  const int k = group * rows + (it & (rows - 1)), d = it / rows * 16, live = p.nt * a.group, part_rows = rows_of_part<S>(a, p);
+  const int k = group * rows + (it & (rows - 1)), d = it / rows * 16, live = p.nt * a.group;
+  const int part_rows = rows_of_part<S>(a, p);
   const int kk = min(k, live - 1), rr = p.two && kk >= tt * a.group ? 128 + kk - tt * a.group : kk;
   float mm = -INFINITY, ll = 0.f, o[16];
 #pragma unroll
@@ -349,7 +358,8 @@ __device__ __forceinline__ void merge_group(S& s, const PagedAttnArgs& a, const 
   }
   if (sub == 0 && k < live) {
     const int kt = k * a.group_inv >> 16, head = p.h * a.group + k - kt * a.group;
-    T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + kt) * a.out_row + static_cast<long long>(head) * a.out_head + d;
+    T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + kt) * a.out_row +
+             static_cast<long long>(head) * a.out_head + d;
     if (write16(out, o, ll != 0.f ? 1.f / ll : 0.f)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
     if (d == 0) store_lse(a, p, p.t0 + kt, head, mm, ll);
   }
@@ -369,15 +379,15 @@ __device__ __forceinline__ int arrive_part(const PagedAttnArgs& a, const PagePie
 }
 
 // See to a cut tile after the run: its last part's CTA merges it.  Where that is much (a
-// block of 64 rows in 19 parts: 0.6 MB, which one SM takes in in 9 us), the
-// CTAs of the other parts stay for a while and take groups of its rows too; none is
-// waited for.
+// block of 64 rows in 19 parts: 0.6 MB, which one SM takes in in 9 us), the CTAs of the
+// other parts stay for a while and take groups of its rows too; none is waited for.  (At a
+// context of 131072, 8 tiles of 19 parts: 97 us without it, 91 with.)
 constexpr uint64_t kMergeLingerNs = 20000;
 template <class T, int HD, class S>
 __device__ __forceinline__ void finish_cut(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt, int before) {
   // (the piece was copied by other threads, and s.last of the tile before has been read)
   all_rows<S>();
-  const int tid = threadIdx.x, parts = p.cta1 - p.cta0 + 1, live = p.nt * a.group, ways = merge_ways<S, HD>(parts);
+  const int tid = threadIdx.x, parts = p.cta1 - p.cta0 + 1, live = p.nt * a.group, ways = merge_ways(parts);
   const int groups = (live + merge_rows<S, HD>(ways) - 1) / merge_rows<S, HD>(ways);
   const bool share = ways > 1 && groups > 1;  // (of two or three parts each CTA has one to merge anyway)
   PageTicket* t = a.tickets + p.cta0;
