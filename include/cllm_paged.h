@@ -118,7 +118,8 @@ void cllm_paged_destroy(cllm_paged *cache);
 /* Wait for the stream and return (and clear) what the calls before found on the
  * device: CLLM_OK, CLLM_EDEVICE (a page or slot outside the pool, a position
  * outside the rotary table: those rows were skipped or read as zeros) or
- * CLLM_ETIMEOUT (a bounded wait ran out; the attention's outputs are not valid). */
+ * CLLM_ETIMEOUT (a bounded wait ran out; the outputs of that attention call, and of those
+ * after it until this one, are not valid). */
 int cllm_paged_status(cllm_paged *cache, void *cuda_stream);
 
 /*

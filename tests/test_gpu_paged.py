@@ -314,6 +314,43 @@ def test_what_a_row_does_not_see_never_reaches_it(dtype, bad, new):
     assert bool(((seen.double() - o).abs()[clean] <= tol[clean]).all())
 
 
+# 17 to 64 rows a key/value head on average and enough heads, or groups of more than 16: tiles
+# in 4 or 2 bands; among them tiles without tokens or keys, of one row, and cut ones
+BANDS = [(32, 8, 64, 16, *RAGGED), (32, 8, 128, 32, *RAGGED), (20, 1, 128, 8, [0, 5, 200, 3000], [1, 0, 2, 1]),
+         (32, 1, 64, 64, [2900], [1]), (33, 1, 128, 16, [100, 700], [1, 1]), (8, 1, 128, 64, [0, 1000, 63], [8, 5, 11]),
+         (16, 16, 64, 8, [0, 100, 130, 64, 31, 200], [17, 32, 31, 1, 40, 3])]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("heads,kv,hd,page,ctx,new", BANDS)
+@pytest.mark.parametrize("window,masked", [(0, False), (40, False), (0, True), (20, True)])
+def test_attention_bands(dtype, heads, kv, hd, page, ctx, new, window, masked):
+    step = Step(ctx, new, heads, kv, hd, page, dtype, seed=heads + window)
+    mask = None
+    if masked:
+        mask = torch.rand(step.rows, max(new), generator=torch.Generator().manual_seed(2)) < 0.3
+        mask[::3] = False
+    _check(step, mask=mask, window=window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("heads,kv,new", [(40, 40, 20), (24, 1, 2)])
+def test_bands_keep_out_what_is_not_seen(dtype, bad, heads, kv, new):
+    step = Step([90, 0], [new, new], heads, kv, 64, 16, dtype, seed=new)
+    o, _, ab, delta = step.attention()
+    tol, _ = step.bound(ab, delta, o)
+    for b in range(2):
+        for pool in (step.k, step.v):
+            step.token(pool, b, step.ctx[b] + new - 1)[...] = bad
+    cache = paged.PagedCache(step.k, step.v, heads)
+    got = cache.attention(0, step.q, paged.PageRows(step.row_start, step.seq_len), paged.PageTables(step.table, page_size=16))
+    cache.check()
+    clean = [b * new + i for b in range(2) for i in range(new - 1)]
+    assert bool(((got.double() - o).abs()[clean] <= tol[clean]).all())
+    assert bool((~torch.isfinite(got[new - 1])).all())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_refused_requests_are_zeros(dtype):
     """A request that a plan refused has rows and a length of 0."""
@@ -427,6 +464,24 @@ def test_a_wait_that_runs_out_is_reported(chunk, new):
     assert torch.equal(cache.attention(0, step.q, rows, tables), want)
     cache.check()
     assert lib.cllm_test_hold_paged(None, 0) == -1 and lib.cllm_test_hold_paged(cache._h, -2) == -1
+
+
+def test_a_wait_that_runs_out_in_bands_is_reported():
+    lib = cllm.load()
+    step = Step([60000], [1], 24, 1, 128, 256, "bf16", seed=9)
+    cache = paged.PagedCache(step.k, step.v, 24)
+    rows, tables = paged.PageRows(step.row_start, step.seq_len), paged.PageTables(step.table, page_size=256)
+    want = cache.attention(0, step.q, rows, tables)
+    cache.check()
+    lib.cllm_test_hold_paged.argtypes = [ctypes.c_void_p, ctypes.c_int]
+    assert lib.cllm_test_hold_paged(cache._h, 1) == 0
+    cache.attention(0, step.q, rows, tables)
+    with pytest.raises(cllm.CllmError) as e:
+        cache.check()
+    assert e.value.status == -5
+    assert lib.cllm_test_hold_paged(cache._h, -1) == 0
+    assert torch.equal(cache.attention(0, step.q, rows, tables), want)
+    cache.check()
 
 
 # ---- together --------------------------------------------------------------------------
