@@ -632,7 +632,7 @@ cudaError_t launch_tc(const PagedMaps& m, const PagedAttnArgs& a, int hold, int 
   // tokens, 32 heads on 8, 700 to 1100 keys: 17.6 us, 34 with tiles of 256).
   const long long per_request = (static_cast<long long>(a.rows) + a.batch - 1) / a.batch;
   const bool two = NB == 1 && per_request > tt && (per_request + 2 * tt - 1) / (2 * tt) * a.batch * a.Hkv >= grid;
-  const PagedGeom g{two ? 2 * tt : tt, tt, kTcShift, 2, 8, 3};
+  const PagedGeom g{two ? 2 * tt : tt, tt, kTcShift, 2, 8, 8};
   return launch_after(paged_attn_tc_kernel<T, HD, NB>, dim3(grid), kTcThreads, sizeof(TcSmem<HD, NB>), s, m, a, g, hold);
 }
 

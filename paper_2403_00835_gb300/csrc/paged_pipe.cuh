@@ -380,8 +380,9 @@ __device__ __forceinline__ int arrive_part(const PagedAttnArgs& a, const PagePie
 
 // See to a cut tile after the run: its last part's CTA merges it.  Where that is much (a
 // block of 64 rows in 19 parts: 0.6 MB, which one SM takes in in 9 us), the CTAs of the
-// other parts stay for a while and take groups of its rows too; none is waited for.  (At a
-// context of 131072, 8 tiles of 19 parts: 97 us without it, 91 with.)
+// other parts stay for a while and take groups of its rows too; none is waited for.  (Without
+// and with it: 16 tokens at 131072, 8 tiles of 19 parts, 97 and 91 us; 61 tokens at 1000, 32
+// heads on 8, 16 tiles of 5, 31 and 18; 300 tokens at 2000, 8 heads, 26 and 20.)
 constexpr uint64_t kMergeLingerNs = 20000;
 template <class T, int HD, class S>
 __device__ __forceinline__ void finish_cut(S& s, const PagedAttnArgs& a, const PagePiece& p, int tt, int before) {
@@ -389,7 +390,7 @@ __device__ __forceinline__ void finish_cut(S& s, const PagedAttnArgs& a, const P
   all_rows<S>();
   const int tid = threadIdx.x, parts = p.cta1 - p.cta0 + 1, live = p.nt * a.group, ways = merge_ways(parts);
   const int groups = (live + merge_rows<S, HD>(ways) - 1) / merge_rows<S, HD>(ways);
-  const bool share = ways > 1 && groups > 1;  // (of two or three parts each CTA has one to merge anyway)
+  const bool share = parts >= 4 && groups > 1;  // (of two or three parts each CTA has one to merge anyway)
   PageTicket* t = a.tickets + p.cta0;
   if (tid == 0) {
     bool there = before == parts - 1;
