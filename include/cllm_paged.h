@@ -155,7 +155,8 @@ int cllm_paged_append(cllm_paged *cache, const cllm_paged_rows *r, void *cuda_st
  * out = softmax(scale q k) v in the pools' type; a row that sees nothing (its mask
  * is empty, or seq_len[b] < rows, as a plan leaves a refused request) is 0 with lse
  * -inf.  lse[row][head] = log sum exp(scale q k), natural, may be NULL.  What a row
- * does not see never reaches it, infinities and NaN included.  Rows from
+ * does not see never reaches it, infinities and NaN included; a score that it does see and
+ * that is NaN or +inf makes the row and its lse NaN.  Rows from
  * row_start[batch] on are not written.  Pages wholly before the window are not read.
  */
 typedef struct {

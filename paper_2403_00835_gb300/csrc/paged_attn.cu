@@ -188,6 +188,8 @@ __global__ void __launch_bounds__(kPThreads, 1)
     for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int d = 1; d < 16; d <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+#pragma unroll
+    for (int i = 0; i < R; ++i) m[i] = share_max(m[i], l[i]);
 
     auto store = [&](int r, int d, float4 x, float mm, float ll) {  // a row's 4 columns from d
       const int tok = (r * a.group_inv >> 16), hh = p.h * a.group + r % a.group;
@@ -195,7 +197,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
       const bool any = ll != 0.f;
       if (any) x = make_float4(x.x / ll, x.y / ll, x.z / ll, x.w / ll);
       else x = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (!finite4(x)) atomicOr(&s.bad[r >> 5], 1u << (r & 31));
+      if (!finite4(x) && ll == ll) atomicOr(&s.bad[r >> 5], 1u << (r & 31));
       st4(static_cast<T*>(a.out) + row * a.out_row + hh * a.out_head + d, x);
       if (d == 0 && a.lse != nullptr)
         a.lse[row * a.H + hh] = any ? (mm + log2f(ll)) * 0.69314718055994530942f : -INFINITY;

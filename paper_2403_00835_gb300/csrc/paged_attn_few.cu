@@ -215,6 +215,7 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
     for (int u = 0; u < 2; ++u) {
       l[u] += __shfl_xor_sync(0xffffffffu, l[u], 1);
       l[u] += __shfl_xor_sync(0xffffffffu, l[u], 2);
+      m[u] = share_max(m[u], l[u]);
       if ((lane & 3) == 0) s.wml[warp][quad + 8 * u] = make_float2(m[u], l[u]);
 #pragma unroll
       for (int j = 0; j < HD / 8; ++j)
@@ -249,7 +250,7 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
       if (!whole) {
         part[2 * d8 * part_rows + r] = x;
         part[(2 * d8 + 1) * part_rows + r] = y;
-        if (d8 == 0) part_ml[r] = make_float2(mm, ll);
+        if (d8 == 0) part_ml[r] = make_float2(share_max(mm, ll), ll);
         continue;
       }
       const float f = ll != 0.f ? 1.f / ll : 0.f;
@@ -262,7 +263,7 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
         any = fmaf(v0, 0.f, fmaf(v1, 0.f, any));
         u[e] = Pack16<T>::pack(v0, v1);
       }
-      if (any != 0.f) atomicOr(&s.bad[r >> 5], 1u << (r & 31));
+      if (any != 0.f && ll == ll) atomicOr(&s.bad[r >> 5], 1u << (r & 31));
       const int rt = r * a.group_inv >> 16, tok = p.t0 + rt, head = p.h * a.group + r - rt * a.group;
       T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + tok) * a.out_row + head * a.out_head + d8 * 8;
       *reinterpret_cast<uint4*>(out) = make_uint4(u[0], u[1], u[2], u[3]);

@@ -392,6 +392,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD, NB>& s, const PagedAttnArgs&
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
+      m = share_max(m, l);
     }
     const bool whole = p.whole;
     // a part: [HD / 4][rows][4], so that the rows' threads write and read side by side
@@ -496,7 +497,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD, NB>& s, const PagedAttnArgs&
       }
       if (live && tid < BR) {
         if (whole) store_lse(a, p, tok, head, mm, ll);
-        else part_ml[row] = make_float2(mm, ll);
+        else part_ml[row] = make_float2(share_max(mm, ll), ll);
       }
       if (bad) atomicOr(&s.bad[row >> 5], 1u << (row & 31));
     } else {
@@ -529,7 +530,7 @@ __device__ __forceinline__ void run_rows(TcSmem<HD, NB>& s, const PagedAttnArgs&
       }
       if (live && t == 0) {
         if (whole) store_lse(a, p, tok, head, mm, ll);
-        else part_ml[row] = make_float2(mm, ll);
+        else part_ml[row] = make_float2(share_max(mm, ll), ll);
       }
       if (bad) atomicOr(&s.bad[row >> 5], 1u << (row & 31));
     }

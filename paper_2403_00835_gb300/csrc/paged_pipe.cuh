@@ -226,7 +226,7 @@ __device__ __forceinline__ void all_rows() {
   named_bar_sync(1, 32 * S::kRowWarps);
 }
 
-// 16 columns of a result; whether one is not finite.
+// 16 columns of a result (scale: 1 over the row's sum); whether one is not finite though the sum is.
 template <class T>
 __device__ __forceinline__ bool write16(T* out, const float (&o)[16], float scale) {
   bool bad = false;
@@ -241,7 +241,7 @@ __device__ __forceinline__ bool write16(T* out, const float (&o)[16], float scal
     }
     *reinterpret_cast<uint4*>(out + j) = make_uint4(u[0], u[1], u[2], u[3]);
   }
-  return bad;
+  return bad && scale == scale;
 }
 
 __device__ __forceinline__ void store_lse(const PagedAttnArgs& a, const PagePiece& p, int tok, int head, float m,

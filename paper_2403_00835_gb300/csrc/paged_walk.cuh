@@ -318,6 +318,12 @@ __device__ __forceinline__ uint32_t key_bits(const RowKeys& r, int kb) {
   return m;
 }
 
+// A row's maximum m and sum l over some of its keys, for merging: m -inf means that none of
+// them has weight.  Maxima pass NaN over, sums do not, so a sum that is no number takes the
+// maximum with it.  (The sum is NaN only where a score that the row sees is NaN or +inf: all
+// of the row is NaN then, and needs no second look by exact_row.)
+__device__ __forceinline__ float share_max(float m, float l) { return l == l ? m : l; }
+
 // Address of (page of position pos) in a pool; null when the table's entry is
 // outside the pool (noted in the status word).
 template <class T>
