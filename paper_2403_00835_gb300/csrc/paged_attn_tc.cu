@@ -196,9 +196,10 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD, NB>& s, uint32_t tmem, int
       if (!ok) break;
       ++pieces;
     }
-    if (!ok) {
-      *const_cast<volatile int*>(&s.abort) = 1;
-      tc_commit_warp(&s.drain);  // MMAs in flight end before the CTA leaves
+    if (!ok) *const_cast<volatile int*>(&s.abort) = 1;
+    if (!ok || pieces > 0) {
+      // MMAs in flight end before the CTA leaves, also when it is another role that gave up
+      tc_commit_warp(&s.drain);
       mbar_wait(&s.drain, 0, nullptr);
     }
   }

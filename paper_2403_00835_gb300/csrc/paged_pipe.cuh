@@ -206,13 +206,16 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
     }
     if (!ok) break;
   }
-  if (!ok && lane == 0) {
-    // the rows get their end (they go on past every wait now), and loads in flight land
-    // before the CTA leaves
-    *const_cast<volatile int*>(&s.abort) = 1;
-    if (pieces >= kPagePieces) mbar_wait(&s.pempty[pat.i], pat.phase ^ 1, nullptr);
-    s.piece[pat.i].end = 1;
-    mbar_arrive(&s.pfull[pat.i]);
+  if (lane == 0) {
+    if (!ok) {
+      // the rows get their end (they go on past every wait now)
+      *const_cast<volatile int*>(&s.abort) = 1;
+      if (pieces >= kPagePieces) mbar_wait(&s.pempty[pat.i], pat.phase ^ 1, nullptr);
+      s.piece[pat.i].end = 1;
+      mbar_arrive(&s.pfull[pat.i]);
+    }
+    // Loads in flight land before the CTA leaves, also when it is another role that gave up
+    // after the last one was issued here.
     for (uint32_t i = r > NR ? r - NR : 0; i < r; ++i) mbar_wait(&s.full[i % NR], (i / NR) & 1, nullptr);
     if (with_keys > 0) mbar_wait(&s.qfull, (with_keys - 1) & 1, nullptr);
   }
