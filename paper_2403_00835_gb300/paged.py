@@ -21,6 +21,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
+from contextlib import nullcontext
 from typing import Optional
 
 import torch
@@ -252,13 +253,15 @@ class PagedCache:
     def attention(self, layer: int, q, rows: PageRows, tables: PageTables, out=None, lse=None,
                   scale: Optional[float] = None, window: int = 0, block_mask=None, stream=None):
         """Attention of the step's rows q [T][n_heads][hd] (any row and head stride)
-        over their requests' pages; returns out.  lse: float32 [T][n_heads] to fill.
+        over their requests' pages; returns out (None: allocated on the stream of the call).  lse: float32 [T][n_heads] to fill.
         scale: default head_dim ** -0.5.  window: keys nearer than that (0: all).
         block_mask: int32 [T][words], bit j of word w: the row sees new token 32 w + j of
         its request (None: causal)."""
         dev, dtype = self._dev, self.dtype
         if out is None:
-            out = torch.empty(q.shape, dtype=dtype, device=self.device)
+            # (from the memory of the stream that writes it: the current stream's may still be in use there)
+            with nullcontext() if stream is None else torch.cuda.stream(stream):
+                out = torch.empty(q.shape, dtype=dtype, device=self.device)
         t = q.shape[0]
         shape = (t, self.n_heads, self.head_dim)
         qs, qh, q1 = q.stride() if q.shape == shape else (0, 0, 0)
