@@ -44,7 +44,9 @@ struct PagedAttnArgs {
 };
 
 // Launch a kernel that may start while the one before it in the stream ends; it
-// waits (griddepcontrol.wait) before it touches memory.
+// waits (griddepcontrol.wait) before it touches memory.  What it reads may be written by that
+// one, so none of it is read by non-coherent loads, which ask for memory that nobody writes while the
+// kernel lives (and may be moved to before the wait).
 template <class... P, class... A>
 inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s,
                                 const A&... args) {

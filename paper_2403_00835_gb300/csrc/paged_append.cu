@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const Page
     if (rotated) {
 #pragma unroll
       for (int i = 0; i < V::n; i += 2) {
-        const float4 x = __ldg(reinterpret_cast<const float4*>(a.rope + static_cast<size_t>(pos) * (HD / 2) + d + i));
+        const float4 x = *reinterpret_cast<const float4*>(a.rope + static_cast<size_t>(pos) * (HD / 2) + d + i);
         cs[i] = make_float2(x.x, x.y);
         cs[i + 1] = make_float2(x.z, x.w);
       }

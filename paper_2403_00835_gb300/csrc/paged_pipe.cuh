@@ -160,7 +160,7 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
     // this lane's page of a chunk (its box's; the pages that hold keys of the tile are loaded)
     auto page_of = [&](int c) {
       const int pos = c * kChunk + (j << box_shift);
-      return pos < p.hi ? __ldg(a.table + static_cast<size_t>(p.b) * a.table_width + (pos >> a.page_shift)) : 0;
+      return pos < p.hi ? a.table[static_cast<size_t>(p.b) * a.table_width + (pos >> a.page_shift)] : 0;
     };
     auto tile = [&](const CUtensorMap* map, int c, int page) {
       const int kb = c * kChunk;

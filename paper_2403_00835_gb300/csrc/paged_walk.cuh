@@ -33,7 +33,7 @@ struct Request {
   int row0, n, len;
 };
 __device__ __forceinline__ Request request(const PagedAttnArgs& a, int b) {
-  Request r{__ldg(a.row_start + b), __ldg(a.row_start + b + 1), __ldg(a.seq_len + b)};
+  Request r{a.row_start[b], a.row_start[b + 1], a.seq_len[b]};
   r.n -= r.row0;
   const bool rows = r.row0 >= 0 && r.n >= 0 && r.row0 <= a.rows && r.n <= a.rows - r.row0;
   const bool fits = r.len <= static_cast<long long>(a.table_width) << a.page_shift;
@@ -309,10 +309,10 @@ __device__ __forceinline__ uint32_t key_bits(const RowKeys& r, int kb) {
     const int j = kb - r.ctx;  // new token of bit 0
     if (j >= 0) {
       const int w = j >> 5;
-      const uint32_t w0 = w < r.words ? __ldg(r.bits + w) : 0u, w1 = w + 1 < r.words ? __ldg(r.bits + w + 1) : 0u;
+      const uint32_t w0 = w < r.words ? r.bits[w] : 0u, w1 = w + 1 < r.words ? r.bits[w + 1] : 0u;
       m &= __funnelshift_r(w0, w1, j & 31);
     } else if (j > -32) {
-      m &= (__ldg(r.bits) << -j) | ~(~0u << -j);
+      m &= (r.bits[0] << -j) | ~(~0u << -j);
     }
   }
   return m;
@@ -329,7 +329,7 @@ __device__ __forceinline__ float share_max(float m, float l) { return l == l ? m
 template <class T>
 __device__ __forceinline__ const T* pool_row(const PagedAttnArgs& a, const void* pool, int b, int h, int pos) {
   const int j = pos >> a.page_shift;
-  const int page = j < a.table_width ? __ldg(a.table + static_cast<size_t>(b) * a.table_width + j) : -1;
+  const int page = j < a.table_width ? a.table[static_cast<size_t>(b) * a.table_width + j] : -1;
   if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
     atomicOr(a.err, DERR_CAPACITY);
     return nullptr;
