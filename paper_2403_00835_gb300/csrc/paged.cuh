@@ -69,6 +69,7 @@ inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, si
 constexpr int kPagedPartRows = 256;
 constexpr int kPagedCtas = 2;  // CTAs per SM, at most
 
+constexpr int kPlanBatch = 4096;  // requests of a plan, at most
 cudaError_t launch_page_plan(const cllm_page_tables& in, const cllm_page_tables& out, const cllm_page_rows& rows,
                              int B, const int* ctx, const int* new_rows, cudaStream_t s);
 

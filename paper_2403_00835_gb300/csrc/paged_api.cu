@@ -36,7 +36,7 @@ int log2i(int x) {
 
 bool tables_ok(const cllm_page_tables* t) {
   return t && t->table && t->held && t->ring && t->state && aligned(t->table, 4) && aligned(t->held, 4) &&
-         aligned(t->ring, 4) && aligned(t->state, 4) && t->max_batch >= 1 && t->max_batch <= 4096 && t->width >= 1 &&
+         aligned(t->ring, 4) && aligned(t->state, 4) && t->max_batch >= 1 && t->max_batch <= kPlanBatch && t->width >= 1 &&
          t->n_pages >= 1 && pow2(t->page_size) &&
          static_cast<int64_t>(t->width) * t->page_size <= 0x7fffffff &&
          static_cast<int64_t>(t->max_batch) * t->width <= 0x7fffffff;

@@ -24,6 +24,8 @@ namespace cllm {
 namespace {
 
 constexpr int kPlanThreads = 512;
+constexpr int kPlanWords = 5;       // shared memory of a request, in words
+constexpr int kPlanStatic = 1024;   // at least the kernel's other shared memory
 
 struct PlanArgs {
   cllm_page_tables in, out;
@@ -34,7 +36,7 @@ struct PlanArgs {
 };
 
 // Inclusive sum over the block's threads (T: long long or int2); every thread
-// gets its own, `total` the whole.  `sm` holds 17 values.
+// gets its own, `total` the whole.  `sm` holds a value per warp.
 __device__ __forceinline__ long long plus(long long a, long long b) { return a + b; }
 __device__ __forceinline__ int2 plus(int2 a, int2 b) { return make_int2(a.x + b.x, a.y + b.y); }
 __device__ __forceinline__ long long shfl_up(long long v, int d) { return __shfl_up_sync(~0u, v, d); }
@@ -72,6 +74,7 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   extern __shared__ int sm_req[];
   __shared__ long long sm_scan[kPlanThreads / 32];
   __shared__ int sm_taken, sm_last;
+  static_assert(sizeof(sm_scan) + sizeof(sm_taken) + sizeof(sm_last) <= kPlanStatic, "shared memory without asking");
   const int tid = threadIdx.x, B = a.B, W = a.in.width, N = a.in.n_pages, P = a.in.page_size;
   int* row_end = sm_req;       // rows of the requests up to this one
   int* held = sm_req + B;      // pages before
@@ -208,9 +211,13 @@ cudaError_t launch_page_plan(const cllm_page_tables& in, const cllm_page_tables&
                              int B, const int* ctx, const int* new_rows, cudaStream_t s) {
   PlanArgs a{in, out, rows, ctx, new_rows, B, 0};
   while ((1 << a.page_shift) < in.page_size) ++a.page_shift;
-  const int smem = 5 * B * 4;
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(page_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int smem = kPlanWords * 4 * B;
+  // 48 KB without asking, of which the kernel's own variables are a part.  The limit is raised to
+  // the largest batch's need, and never lowered: calls of several threads do not take it
+  // from each other.
+  if (smem > 48 * 1024 - kPlanStatic) {
+    const cudaError_t e = cudaFuncSetAttribute(page_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               kPlanWords * 4 * kPlanBatch);
     if (e != cudaSuccess) return e;
   }
   const int want = max((rows.max_rows + kPlanThreads - 1) / kPlanThreads,
