@@ -18,6 +18,8 @@
  *   - Arrays are DEVICE memory owned by the caller.  Each call queues its work on
  *     cuda_stream (a cudaStream_t, NULL = the legacy default stream) and returns
  *     without waiting; nothing is allocated, so calls can be captured in a graph.
+ *   - Calls on a cache use the device that it was created on, whichever is current (NULL is that
+ *     device's default stream); cllm_page_plan uses the current device.
  *   - Return value: CLLM_OK or a negative CLLM_E* code for what the host can see;
  *     then nothing is queued and the outputs are left untouched.  What only the
  *     device can see (a page number outside the pool) is kept in the cache's

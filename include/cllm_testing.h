@@ -116,6 +116,13 @@ int cllm_test_hold_gemm(cllm_ctx *ctx, int chunk);
 int cllm_test_hold_paged(cllm_paged *cache, int chunk);
 
 /*
+ * Let the cache take `dev` >= 0 for its device (of which nothing is checked or moved), and
+ * return the number it had: a call on a device that does not exist has to fail and
+ * queue nothing.  Put back what was returned before the cache is destroyed.  EINVAL on a null cache.
+ */
+int cllm_test_paged_device(cllm_paged *cache, int dev);
+
+/*
  * The same for the split-K waits of launches of up to 256 rows: every weight
  * tile's arrival count is set to `count`.  With -1 the first contributor of a
  * tile that is cut over several ranges waits for one arrival more than there

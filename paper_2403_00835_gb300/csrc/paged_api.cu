@@ -26,6 +26,28 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// The cache's device for a call (its memory, its tensor maps and the default stream are that
+// device's), then the caller's again.
+class OnDevice {
+ public:
+  explicit OnDevice(int dev) {
+    error = cudaGetDevice(&before_);
+    if (error != cudaSuccess || before_ == dev) return;
+    error = cudaSetDevice(dev);
+    back_ = error == cudaSuccess;
+  }
+  ~OnDevice() {
+    if (back_) cudaSetDevice(before_);
+  }
+  OnDevice(const OnDevice&) = delete;
+  OnDevice& operator=(const OnDevice&) = delete;
+  cudaError_t error;
+
+ private:
+  int before_ = 0;
+  bool back_ = false;
+};
+
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 int log2i(int x) {
@@ -60,12 +82,11 @@ extern "C" int cllm_page_plan(const cllm_page_tables* in, const cllm_page_tables
 
 extern "C" void cllm_paged_destroy(cllm_paged* c) {
   if (!c) return;
-  int dev = 0;
-  const bool back = cudaGetDevice(&dev) == cudaSuccess && dev != c->dev;
-  cudaSetDevice(c->dev);
-  cudaDeviceSynchronize();
-  cudaFree(c->part_o);
-  if (back) cudaSetDevice(dev);
+  {
+    const OnDevice on(c->dev);
+    cudaDeviceSynchronize();
+    cudaFree(c->part_o);
+  }
   delete c;
 }
 
@@ -152,7 +173,9 @@ extern "C" int cllm_paged_status(cllm_paged* c, void* cuda_stream) {
   if (!c) return CLLM_EINVAL;
   const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   int err = 0;
-  cudaError_t e = cudaMemcpyAsync(&err, c->err, 4, cudaMemcpyDeviceToHost, s);
+  const OnDevice on(c->dev);
+  cudaError_t e = on.error;
+  if (e == cudaSuccess) e = cudaMemcpyAsync(&err, c->err, 4, cudaMemcpyDeviceToHost, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e == cudaSuccess && err != 0) {
     // (a timed-out launch may leave arrival counters behind)
@@ -190,7 +213,9 @@ extern "C" int cllm_paged_append(cllm_paged* c, const cllm_paged_rows* r, void* 
   a.max_pos = r->max_pos, a.T = r->rows, a.H = r->q ? d.n_heads : 0, a.Hkv = d.n_kv_heads, a.hd = d.head_dim;
   a.n_pages = d.n_pages, a.page_shift = c->page_shift;
   a.err = c->err;
-  const cudaError_t e = launch_paged_append(a, d.dtype, static_cast<cudaStream_t>(cuda_stream));
+  const OnDevice on(c->dev);
+  cudaError_t e = on.error;
+  if (e == cudaSuccess) e = launch_paged_append(a, d.dtype, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? CLLM_OK : cuda_fail(e, "paged_append");
 }
 
@@ -233,6 +258,8 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
   a.layer = p->layer, a.n_pages = d.n_pages, a.page_shift = c->page_shift;
   a.part_o = c->part_o, a.part_ml = c->part_ml, a.tickets = c->tickets, a.err = c->err;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const OnDevice on(c->dev);
+  if (on.error != cudaSuccess) return cuda_fail(on.error, "paged_attention");
   // rows of one key/value head in an average request
   const int64_t rows = (static_cast<int64_t>(p->rows) + p->batch - 1) / p->batch * a.group;
   cudaError_t e;
@@ -247,6 +274,13 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
     e = launch_paged_attention_tc(a, c->mk, c->mv, d.dtype, d.head_dim, c->hold, c->sms, st);
   }
   return e == cudaSuccess ? CLLM_OK : cuda_fail(e, "paged_attention");
+}
+
+extern "C" int cllm_test_paged_device(cllm_paged* c, int dev) {
+  if (!c || dev < 0) return CLLM_EINVAL;
+  const int before = c->dev;
+  c->dev = dev;
+  return before;
 }
 
 extern "C" int cllm_test_hold_paged(cllm_paged* c, int chunk) {

@@ -97,8 +97,15 @@ def _tensor(t, what: str, dtype, shape=None, index=None):
 _current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _stream(stream, index: int) -> int:
-    return _current(index) if stream is None else stream.cuda_stream
+    if stream is None:
+        return _current(index)
+    if stream.device_index != index:
+        raise ValueError(f"stream: on cuda:{stream.device_index}, the tensors on cuda:{index}")
+    return stream.cuda_stream
 
 
 class PageTables:
@@ -169,9 +176,14 @@ def plan(tables: PageTables, rows: PageRows, ctx, new_rows, out: Optional[PageTa
     dev, b = tables._dev, ctx.numel()
     c = _tensor(ctx, "ctx", torch.int32, None, dev)
     n = _tensor(new_rows, "new_rows", torch.int32, ctx.shape, dev)
-    if rows._dev != dev or rows._max < b:
-        raise ValueError("rows: on another device, or too small for the batch")
-    rc = load().cllm_page_plan(tables._p, out._p, rows._p, b, c, n, _stream(stream, dev))
+    if rows._dev != dev or out._dev != dev or rows._max < b:
+        raise ValueError("rows or out: on another device, or too small for the batch")
+    args = tables._p, out._p, rows._p, b, c, n, _stream(stream, dev)
+    if _device() == dev:
+        rc = load().cllm_page_plan(*args)
+    else:
+        with torch.cuda.device(dev):
+            rc = load().cllm_page_plan(*args)
     if rc:
         _c._check(rc, "cllm_page_plan")
     rows.batch = b
