@@ -73,7 +73,7 @@ typedef struct {
  * gives all its pages back.  Requests are served in order: one is refused, and
  * keeps what it holds, when the pages it and the requests before it ask for
  * exceed the free ones; when its length is negative or more than width pages; or
- * when its rows would pass max_rows.  Pages given back (in order of request, then of
+ * when its rows would pass max_rows (row_start counts them all the same, past max_rows too).  Pages given back (in order of request, then of
  * position) can be handed out from the next call on.
  * in, out: the tables before and after; the same tables for an update in place,
  * or another table/held/state over the same ring to see what a step would get
@@ -162,7 +162,8 @@ int cllm_paged_append(cllm_paged *cache, const cllm_paged_rows *r, void *cuda_st
  * row_start[batch] on are not written.  Pages wholly before the window are not read.
  */
 typedef struct {
-  int layer, batch, rows; /* rows: of q and out, at least row_start[batch] */
+  int layer, batch, rows; /* rows: of q and out, at least row_start[batch]; only requests of
+                           * seq_len 0 may have rows past them, which are not written */
   const void *q;
   void *out;
   float *lse;

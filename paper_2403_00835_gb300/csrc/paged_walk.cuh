@@ -28,13 +28,19 @@ struct PagedGeom {
 // bits, which the host sees to, and nothing is divided that a shift or a compare decides.)
 
 // Request b's rows and length as the device has them.  Rows outside the arrays
-// or a length past the block table make it a request without rows, or without keys.
+// or a length past the block table make it a request without rows, or without keys.  Of a
+// request without tokens, as a plan leaves one that it refuses, the rows past the arrays are
+// left out without a word: want of rows may be why it was refused.
 struct Request {
   int row0, n, len;
 };
 __device__ __forceinline__ Request request(const PagedAttnArgs& a, int b) {
   Request r{a.row_start[b], a.row_start[b + 1], a.seq_len[b]};
   r.n -= r.row0;
+  if (r.len == 0 && r.row0 >= 0 && r.n >= 0) {
+    r.row0 = min(r.row0, a.rows);
+    r.n = min(r.n, a.rows - r.row0);
+  }
   const bool rows = r.row0 >= 0 && r.n >= 0 && r.row0 <= a.rows && r.n <= a.rows - r.row0;
   const bool fits = r.len <= static_cast<long long>(a.table_width) << a.page_shift;
   if (!rows) r.n = 0;
