@@ -167,7 +167,7 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
           }
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const float nm = m[u] == -INFINITY ? 0.f : -m[u];
+            const float nm = m[u] == -INFINITY ? 0.f : Pack16<T>::kTop - m[u];
 #pragma unroll
             for (int j = 0; j < KEYS / 8; ++j) {
               x[j][2 * u] = ex2_ftz(fmaf(x[j][2 * u], a.scale_log2, nm));
@@ -267,7 +267,7 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
       const int rt = r * a.group_inv >> 16, tok = p.t0 + rt, head = p.h * a.group + r - rt * a.group;
       T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + tok) * a.out_row + head * a.out_head + d8 * 8;
       *reinterpret_cast<uint4*>(out) = make_uint4(u[0], u[1], u[2], u[3]);
-      if (d8 == 0) store_lse(a, p, tok, head, mm, ll);
+      if (d8 == 0) store_lse<T>(a, p, tok, head, mm, ll);
     }
     all_rows<S>();  // (s.o and s.wml are free again)
     if (whole) {

@@ -81,11 +81,18 @@ struct RingAt {
   }
 };
 
-template <class T> struct Pack16;  // two fp32 values to 16 bits each
+// Two fp32 values to 16 bits each.  kTop: log2 of P at its row's running maximum.  A row's l
+// and O hold 2^kTop times their values, in every share of its keys, and the quotient does not.
+// fp16 has room above (P reaches 2^(7 + 8) at most) and little below: P is a normal number from
+// 2^-21 of the largest on, and lost below 2^-32 of it, which a context of 2^17 equally small
+// probabilities feels as 2^-15 of V's size (with kTop 0: 2^-8).
+template <class T> struct Pack16;
 template <> struct Pack16<__half> {
+  static constexpr float kTop = 7.f;
   static __device__ uint32_t pack(float a, float b) { return pack_f16x2(a, b); }
 };
 template <> struct Pack16<__nv_bfloat16> {
+  static constexpr float kTop = 0.f;
   static __device__ uint32_t pack(float a, float b) { return pack_bf16x2(a, b); }
 };
 
@@ -247,11 +254,12 @@ __device__ __forceinline__ bool write16(T* out, const float (&o)[16], float scal
   return bad && scale == scale;
 }
 
+template <class T>
 __device__ __forceinline__ void store_lse(const PagedAttnArgs& a, const PagePiece& p, int tok, int head, float m,
                                           float l) {
   if (a.lse == nullptr) return;
   a.lse[static_cast<size_t>(p.row0 + tok) * a.H + head] =
-      l != 0.f ? (m + log2f(l)) * 0.69314718055994530942f : -INFINITY;
+      l != 0.f ? (m + log2f(l * (1.f / (1 << static_cast<int>(Pack16<T>::kTop))))) * 0.69314718055994530942f : -INFINITY;
 }
 
 // Row rr of a tile from the definition (the whole warp).
@@ -364,7 +372,7 @@ __device__ __forceinline__ void merge_group(S& s, const PagedAttnArgs& a, const 
     T* out = static_cast<T*>(a.out) + static_cast<long long>(p.row0 + p.t0 + kt) * a.out_row +
              static_cast<long long>(head) * a.out_head + d;
     if (write16(out, o, ll != 0.f ? 1.f / ll : 0.f)) atomicOr(&s.bad[rr >> 5], 1u << (rr & 31));
-    if (d == 0) store_lse(a, p, p.t0 + kt, head, mm, ll);
+    if (d == 0) store_lse<T>(a, p, p.t0 + kt, head, mm, ll);
   }
 }
 
