@@ -268,7 +268,7 @@ class PagedCache:
         over their requests' pages; returns out (None: allocated on the stream of the call).  lse: float32 [T][n_heads] to fill.
         scale: default head_dim ** -0.5.  window: keys nearer than that (0: all).
         block_mask: int32 [T][words], bit j of word w: the row sees new token 32 w + j of
-        its request (None: causal)."""
+        its request (None: causal), at least one word."""
         dev, dtype = self._dev, self.dtype
         if out is None:
             # (from the memory of the stream that writes it: the current stream's may still be in use there)
@@ -286,7 +286,9 @@ class PagedCache:
         lp = 0 if lse is None else _tensor(lse, "lse", torch.float32, (t, self.n_heads), dev)
         mp = words = 0
         if block_mask is not None:
-            words = block_mask.shape[1]
+            words = block_mask.shape[1] if isinstance(block_mask, torch.Tensor) and block_mask.dim() == 2 else 0
+            if words == 0:  # (its address would be that of no mask)
+                raise ValueError("block_mask: need [rows][words], one word at least")
             mp = _tensor(block_mask, "block_mask", torch.int32, (t, words), dev)
         _ATTN.pack_into(self._args, 0, layer, rows.batch, t, q.data_ptr(), out.data_ptr(), lp, qs, qh, os, oh, rows._start,
                         rows._len, tables._table, tables._width, self._scale if scale is None else scale, window, mp, words)
