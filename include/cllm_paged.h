@@ -165,7 +165,7 @@ typedef struct {
   int layer, batch, rows; /* rows: of q and out, at least row_start[batch]; only requests of
                            * seq_len 0 may have rows past them, which are not written */
   const void *q;
-  void *out;
+  void *out; /* no element of q or of the pools (a row may be read again after others are written) */
   float *lse;
   int64_t q_stride, q_head_stride, out_stride, out_head_stride; /* elements */
   const int32_t *row_start; /* [batch + 1] */
@@ -178,7 +178,7 @@ typedef struct {
   int mask_words;
 } cllm_paged_attn;
 
-/* Errors: EINVAL (null or misaligned pointers, strides not multiples of 16 bytes,
+/* Errors: EINVAL (null or misaligned pointers, out the same as q, strides not multiples of 16 bytes,
  * sizes outside their ranges, scale not positive and finite), EUNSUPPORTED (rows x
  * table_width so large that the work may exceed 2^31 - 1 units of a few rows and 64
  * keys: cut the step), ECUDA. */

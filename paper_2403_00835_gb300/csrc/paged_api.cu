@@ -230,7 +230,7 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
     return x && aligned(x, 16) && (p->rows == 1 || ok(row)) && (d.n_heads == 1 || ok(head));
   };
   if (!strides_ok(p->q, p->q_stride, p->q_head_stride) || !strides_ok(p->out, p->out_stride, p->out_head_stride) ||
-      !p->row_start || !p->seq_len || !p->table || !aligned(p->row_start, 4) || !aligned(p->seq_len, 4) ||
+      p->q == p->out || !p->row_start || !p->seq_len || !p->table || !aligned(p->row_start, 4) || !aligned(p->seq_len, 4) ||
       !aligned(p->table, 4) || !aligned(p->lse, 4) || p->table_width < 1 || p->window < 0 ||
       !(p->scale > 0.f) || !isfinite(p->scale * kLog2e) ||
       static_cast<int64_t>(p->table_width) * d.page_size > 0x7fffffff ||

@@ -265,7 +265,8 @@ class PagedCache:
     def attention(self, layer: int, q, rows: PageRows, tables: PageTables, out=None, lse=None,
                   scale: Optional[float] = None, window: int = 0, block_mask=None, stream=None):
         """Attention of the step's rows q [T][n_heads][hd] (any row and head stride)
-        over their requests' pages; returns out (None: allocated on the stream of the call).  lse: float32 [T][n_heads] to fill.
+        over their requests' pages; returns out (None: allocated on the stream of the call;
+        else no part of q).  lse: float32 [T][n_heads] to fill.
         scale: default head_dim ** -0.5.  window: keys nearer than that (0: all).
         block_mask: int32 [T][words], bit j of word w: the row sees new token 32 w + j of
         its request (None: causal), at least one word."""

@@ -4,7 +4,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from paper_2403_00835_gb300 import paged
+from paper_2403_00835_gb300 import cllm, paged
 from tests.paged_util import Step
 
 pytestmark = pytest.mark.gpu
@@ -23,3 +23,13 @@ def test_a_mask_without_words_is_refused(shape):
     with pytest.raises(ValueError, match="block_mask"):
         cache.attention(0, step.q, rows, tables, out=out, block_mask=torch.zeros(shape, device="cuda", dtype=torch.int32))
     assert bool((out == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_output_over_the_queries_is_refused(dtype):
+    """A row that is done again from the definition would read its own result."""
+    step, cache, rows, tables = _step(dtype)
+    before = step.q.clone()
+    with pytest.raises(cllm.CllmError):
+        cache.attention(0, step.q, rows, tables, out=step.q)
+    assert torch.equal(step.q, before)
