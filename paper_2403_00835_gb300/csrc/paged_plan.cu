@@ -136,23 +136,23 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   // block tables, a warp per request
   const int lane = tid & 31, warps = gridDim.x * (kPlanThreads / 32);
   for (int b = blockIdx.x * (kPlanThreads / 32) + (tid >> 5); b < B; b += warps) {
-    const int h = held[b], h2 = after[b] >= 0 ? after[b] : h, keep = min(h, h2);
+    const unsigned h = held[b], h2 = after[b] >= 0 ? after[b] : h, keep = min(h, h2);
     const int* in = a.in.table + static_cast<size_t>(b) * W;
     int* out = a.out.table + static_cast<size_t>(b) * W;
-    // (8 loads under way before the first store)
-    for (int j0 = (in == out ? keep : 0) + lane; j0 < W; j0 += 256) {
+    // (8 loads under way before the first store; a table may be 2^31 - 1 wide: steps pass that)
+    for (unsigned j0 = (in == out ? keep : 0) + lane; j0 < static_cast<unsigned>(W); j0 += 256) {
       int page[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int j = j0 + 32 * u;
+        const unsigned j = j0 + 32 * u;
         page[u] = -1;
         if (j < h) page[u] = in[j];
         else if (j < h2) page[u] = __ldcg(a.in.ring + ring_at(first[b], j - h, N));
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int j = j0 + 32 * u;
-        if (j >= W) break;
+        const unsigned j = j0 + 32 * u;
+        if (j >= static_cast<unsigned>(W)) break;
         if (j >= h2 && j < h) a.in.ring[ring_at(first[b], j - h2, N)] = page[u], page[u] = -1;
         out[j] = page[u];
       }
@@ -160,18 +160,19 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   }
 
   // slots, a thread per row
-  for (int t = blockIdx.x * kPlanThreads + tid; t < a.rows.max_rows; t += gridDim.x * kPlanThreads) {
+  for (unsigned t = blockIdx.x * kPlanThreads + tid; t < static_cast<unsigned>(a.rows.max_rows);
+       t += gridDim.x * kPlanThreads) {
     long long slot = -1;
     int pos = 0;
     if (t < total_rows) {
       int lo = 0, hi = B - 1;  // the request: the first whose rows end past t
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (row_end[mid] > t) hi = mid;
+        if (static_cast<unsigned>(row_end[mid]) > t) hi = mid;
         else lo = mid + 1;
       }
       if (after[lo] >= 0) {
-        pos = start[lo] + t - (lo > 0 ? row_end[lo - 1] : 0);
+        pos = start[lo] + static_cast<int>(t - (lo > 0 ? row_end[lo - 1] : 0));
         const int j = pos >> a.page_shift, h = held[lo];
         const int page = j < h ? a.in.table[static_cast<size_t>(lo) * W + j]
                                : __ldcg(a.in.ring + ring_at(first[lo], j - h, N));
