@@ -169,7 +169,7 @@ typedef struct {
   float *lse;
   int64_t q_stride, q_head_stride, out_stride, out_head_stride; /* elements */
   const int32_t *row_start; /* [batch + 1] */
-  const int32_t *seq_len;   /* [batch] */
+  const int32_t *seq_len;   /* [batch] at most table_width pages, and at most 2^31 - 8192 */
   const int32_t *table;     /* [batch][table_width] */
   int table_width;
   float scale;

@@ -34,6 +34,8 @@ struct PagedGeom {
 struct Request {
   int row0, n, len;
 };
+// Positions are held in 32 bits, a loading lane's too (32 boxes of up to 128 keys from a chunk's first).
+constexpr int kLongest = 0x7fffffff - 8191;
 __device__ __forceinline__ Request request(const PagedAttnArgs& a, int b) {
   Request r{a.row_start[b], a.row_start[b + 1], a.seq_len[b]};
   r.n -= r.row0;
@@ -42,7 +44,7 @@ __device__ __forceinline__ Request request(const PagedAttnArgs& a, int b) {
     r.n = min(r.n, a.rows - r.row0);
   }
   const bool rows = r.row0 >= 0 && r.n >= 0 && r.row0 <= a.rows && r.n <= a.rows - r.row0;
-  const bool fits = r.len <= static_cast<long long>(a.table_width) << a.page_shift;
+  const bool fits = r.len <= kLongest && r.len <= static_cast<long long>(a.table_width) << a.page_shift;
   if (!rows) r.n = 0;
   if (!fits) r.len = 0;
   if (!rows || !fits) atomicOr(a.err, DERR_CAPACITY);

@@ -3,7 +3,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from paper_2403_00835_gb300 import paged
+from paper_2403_00835_gb300 import cllm, paged
 from tests.test_gpu_paged import _i32
 
 pytestmark = pytest.mark.gpu
@@ -42,3 +42,25 @@ def test_plan_of_the_widest_table(in_place):
     assert out.held.tolist() == [3] and out.state.tolist() == [3, 5, 0, 0]
     assert rows.slots.tolist() == [1, 2, -1, -1] and out.table[0, :4].tolist() == [0, 1, 2, -1]
     assert _none(out.table[0, 3:], -1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("heads", [1, 24, 40])
+@pytest.mark.parametrize("length", [2 ** 31 - 8, 2 ** 31 - 8191])
+def test_a_length_whose_chunks_pass_32_bits_is_reported(dtype, hd, heads, length):
+    """The longest table, every entry the same page: nothing is read of a request that long."""
+    page = 8
+    k = torch.randn(1, 1, 1, page, hd, device="cuda").to(dtype)
+    cache = paged.PagedCache(k, k.clone(), heads)
+    table = torch.zeros(2, (2 ** 31 - 8) // page, dtype=torch.int32, device="cuda")
+    q = torch.randn(2, heads, hd, device="cuda").to(dtype)
+    out = torch.full_like(q, 5.0)
+    cache.attention(0, q, paged.PageRows(_i32([0, 1, 2]), _i32([8, length])), paged.PageTables(table, page_size=page), out=out)
+    with pytest.raises(cllm.CllmError) as e:
+        cache.check()
+    assert e.value.status == -6
+    assert bool((out[1] == 0).all())
+    want = torch.softmax(q[0].double() @ k[0, 0, 0].double().T * hd ** -0.5, -1) @ k[0, 0, 0].double()
+    # (V is K: a probability's and the result's rounding, each of at most max |V|)
+    assert bool(((out[0].double() - want).abs() <= 4 * torch.finfo(dtype).eps * k.abs().max().double() + 1e-5).all())
