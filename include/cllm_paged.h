@@ -109,7 +109,7 @@ typedef struct cllm_paged cllm_paged;
 
 /* Create a cache over the pools: checks the shape, builds their tensor maps and
  * allocates (owns) the scratch of the attention's split work on the current
- * device.  The pools stay the caller's and must outlive the cache.
+ * device: 512 rows of head_dim + 2 floats per SM (40 MB at head_dim 128).  The pools stay the caller's and must outlive the cache.
  * Errors: EINVAL, EUNSUPPORTED (shape outside the constraints, not an sm_103
  * device), ENOMEM, ECUDA. */
 int cllm_paged_create(const cllm_paged_desc *desc, cllm_paged **out);
@@ -126,7 +126,8 @@ int cllm_paged_status(cllm_paged *cache, void *cuda_stream);
 
 /*
  * Write rows of keys and values into their slots (cllm_page_plan's, or any
- * others; -1 skips a row's K and V, two rows with one slot leave either).
+ * others; -1 skips a row's K and V; two rows with one slot may leave a mix of both, in pieces
+ * of 16 bytes).
  * rope: K as it is when NULL (q unused).  With it K and, when q is not NULL, q are
  * rotated (pairs i, i + head_dim/2: the engine's convention) by row positions[t] in
  * fp32 and rounded once; q goes to q_out (which may be q).
@@ -153,7 +154,9 @@ int cllm_paged_append(cllm_paged *cache, const cllm_paged_rows *r, void *cuda_st
  * and values are in the cache already).  It sees key k when
  *   k < ctx, or among the new tokens k <= ctx + i (mask NULL), or bit k - ctx of
  *   the row's mask words (mask: verification of several candidates at once);
- *   and, with window > 0, (ctx + i) - k < window.
+ *   and, with window > 0, (ctx + i) - k < window.  (With a mask too the window goes by the
+ *   row's place i in the block, not by its depth in a candidate: a row of the second candidate
+ *   sees fewer cached keys than its position's window has.)
  * out = softmax(scale q k) v in the pools' type; a row that sees nothing (its mask
  * is empty, or seq_len[b] < rows, as a plan leaves a refused request) is 0 with lse
  * -inf.  lse[row][head] = log sum exp(scale q k), natural, may be NULL.  What a row

@@ -16,12 +16,13 @@
 // Measured: 8 blocks of 16 tokens at 600 keys, 32 heads: 13.6 us, 6.1 TB/s (the tensor-memory
 // kernel: 20.0); 64 requests of one token at 300 keys, 32 heads on 8: 15.9 us, 5.0 TB/s (28.1);
 // 128 of one token at 100 keys, 32 heads: 58 us (102); 16 of one token at 4096 keys, 32 heads
-// on 8: 50 us, 5.4 TB/s (46: where lengths are long the other's deeper ring is worth more
-// than this one's short ends, but the host, which chooses, does not know the lengths); one
+// on 8: 51 us, 5.3 TB/s (46: where lengths are long the other's deeper ring is worth more
+// than this one's short ends; the host, which chooses, knows the tables' width, a bound on the lengths,
+// and does not use it); one
 // block of 16 at 144 keys: 7.8 us (8.9), of which a launch's start, the first loads' latency
 // and cold instructions are about 5.
 //
-// Rounding: as in the tensor-memory kernel, P goes to the pools' type.
+// Rounding: as in the tensor-memory kernel, P goes to the pools' type, in fp16 at 2^7 times its value.
 #include "paged_pipe.cuh"
 
 namespace cllm {

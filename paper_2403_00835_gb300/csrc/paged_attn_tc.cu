@@ -19,10 +19,11 @@
 // 0 for the others, and the bands' O are summed with the slots'.  Rows are tokens times
 // the query heads of a key/value head, so grouped heads read K and V once.
 //
-// Bound: the exponentials and the alternation of MMAs and rows for long tiles (2048 tokens
-// after 4096, 32 heads: 164 us, 1.05 PFLOP/s; a chunk of 2 x 128 rows x 128 keys takes 3850
-// cycles, 2048 of MMAs and as many of exponentials), HBM for long contexts (16 tokens, 32
-// heads on 8, over 131072: 91 us, 5.9 TB/s), what a piece costs beside its keys (2 to 3 us:
+// Bound: for long tiles no unit by itself (2048 tokens after 4096, 32 heads: 164 us, 1.05
+// PFLOP/s; a chunk of 2 x 128 rows x 128 keys takes 3850 cycles, 2048 of them the MMAs' at their
+// full rate; counters: tensor pipe 41 % of the cycles, the exponentials' pipe 21 %, issue slots 35 %)
+// but the row warps' dependent steps from S to P, which the other slot's MMAs hide in part; HBM for
+// long contexts (16 tokens, 32 heads on 8, over 131072: 91 us, 5.9 TB/s); what a piece costs beside its keys (2 to 3 us:
 // its first loads, S and O one after another) for short ones (8 requests of 32 tokens, 256
 // to 1024 keys, 32 heads: 26.5 us, 3.5 TB/s).
 //
@@ -30,7 +31,7 @@
 // wider one beside 16-bit values (S, m, l and O stay fp32).  A p is off by at most 2^-8 of itself
 // in bf16, 2^-11 in fp16 down to 2^-21 of the row's largest, errors that average over the
 // keys, and below that in fp16 by 2^-32 of the largest; l sums the unrounded p.  Against 64
-// bits results are off by 0.0021-0.0023 (bf16) and 0.00026-0.00028 (fp16) relative, rounding alone
+// bits results are off by 0.0020-0.0023 (bf16) and 0.00026-0.00028 (fp16) relative, rounding alone
 // by 0.0017 and 0.00021.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
