@@ -10,8 +10,11 @@
  * new ones (a Jacobi block of n, a chunk of a prompt, or 1 for greedy decoding):
  *
  *   cllm_page_plan         pages for every request, and where each new row goes
- *   per layer: cllm_paged_append     K, V of the new rows into their slots
+ *   per layer: cllm_paged_append     K, V of the new rows into their slots (cllm_paged_append_heads: with
+ *                                    norms per head and partial or interleaved rotation)
  *              cllm_paged_attention  the new rows over all pages of their request
+ *
+ * cllm_rope_table makes the rotation's table.
  *
  * Conventions for the calls of this header (they differ from the engine's, since
  * they are parts of a caller's own step):
@@ -19,7 +22,7 @@
  *     cuda_stream (a cudaStream_t, NULL = the legacy default stream) and returns
  *     without waiting; nothing is allocated, so calls can be captured in a graph.
  *   - Calls on a cache use the device that it was created on, whichever is current (NULL is that
- *     device's default stream); cllm_page_plan uses the current device.
+ *     device's default stream); cllm_page_plan and cllm_rope_table use the current device.
  *   - Return value: CLLM_OK or a negative CLLM_E* code for what the host can see;
  *     then nothing is queued and the outputs are left untouched.  What only the
  *     device can see (a page number outside the pool) is kept in the cache's
@@ -147,6 +150,42 @@ typedef struct {
 /* Errors: EINVAL (null or misaligned pointers, strides too small or not multiples of 16
  * bytes, layer outside the pools, rows < 0, q without rope), ECUDA. */
 int cllm_paged_append(cllm_paged *cache, const cllm_paged_rows *r, void *cuda_stream);
+
+/*
+ * The same for decoders that normalise queries and keys per head, rotate a part of
+ * each head, or rotate neighbours in pairs.  Of every head of K (and of q, if given):
+ *   norm    x <- x / sqrt(mean(x^2) + eps) * gain, over the head_dim values, where k_norm (q_norm) is given;
+ *   rotate  the first rotary_dims values, with rope rows of rotary_dims / 2 pairs [max_pos][rotary_dims / 2][2]:
+ *           values i and i + rotary_dims / 2, or (interleaved) 2 i and 2 i + 1; the rest stay as they are.
+ * In fp32, rounded once.  V is written as it is.  q may be given without rope too (to be
+ * normalised, or passed on to q_out).
+ */
+typedef struct {
+  const void *q_norm, *k_norm; /* [head_dim] gains in the pools' type, or NULL */
+  float eps;                   /* >= 0 */
+  int rotary_dims;             /* a multiple of 16, at most head_dim (unused without rope) */
+  int interleaved;             /* 0: halves */
+} cllm_paged_heads;
+
+/* Errors: as cllm_paged_append, and EINVAL (heads NULL, gains not multiples of 16 bytes, q_norm without
+ * q, eps negative or not finite, rotary_dims outside [1, head_dim], neither rope nor a norm), EUNSUPPORTED
+ * (rotary_dims not a multiple of 16). */
+int cllm_paged_append_heads(cllm_paged *cache, const cllm_paged_rows *r, const cllm_paged_heads *heads,
+                            void *cuda_stream);
+
+/* ---- rotary tables ----------------------------------------------------------------- */
+
+/*
+ * Rows of a rotary table for cllm_paged_append: table[p][i] = amplitude * (cos, sin)((first + p) * f_i),
+ * p < positions, i < dims / 2, f_i = frequencies[i] radians a position (HOST memory, read before the
+ * call returns).  Frequencies scaled for long contexts and an amplitude come from the
+ * caller.  The angle is reduced exactly, in 64-bit fractions of a turn: each value is within
+ * 2^-22 |amplitude| of its true one at every position.
+ * Runs on the current device.  Errors: EINVAL (null or misaligned pointers (table: 16 bytes), first or positions < 0, their sum
+ * past 2^31 - 1, dims not an even number in [2, 256], frequencies outside [-2^20, 2^20], amplitude not finite), ECUDA.
+ */
+int cllm_rope_table(float *table, int first, int positions, int dims, const double *frequencies, float amplitude,
+                    void *cuda_stream);
 
 /*
  * Attention of a step.  Request b's rows are row_start[b] .. row_start[b+1]-1 of

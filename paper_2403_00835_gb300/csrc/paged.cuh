@@ -80,10 +80,18 @@ struct PagedAppendArgs {
   const long long* slots;
   const float2* rope;
   const int* positions;
+  const void *q_gain, *k_gain;  // of the heads' norms, or null
+  float eps;
+  int dims, interleaved;        // rotated values of a head; neighbours in pairs
   int max_pos, T, H, Hkv, hd, n_pages, page_shift;  // H = 0: no queries
   int* err;
 };
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int dtype, cudaStream_t s);
+
+constexpr int kRopeDims = 256;  // rotated values of a head, at most
+// turns: a position's fraction of a turn, in 2^-64
+cudaError_t launch_rope_table(float* table, int first, int positions, int dims, const unsigned long long* turns,
+                              float amplitude, cudaStream_t s);
 
 // fp32 pools (paged_attn.cu)
 cudaError_t launch_paged_attention_f32(const PagedAttnArgs& a, int hd, int grid, cudaStream_t s);

@@ -6,6 +6,7 @@
 
 #include "../../include/cllm_testing.h"
 #include "internal.cuh"
+#include "on_device.cuh"
 #include "paged.cuh"
 
 using namespace cllm;
@@ -25,28 +26,6 @@ struct cllm_paged {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-
-// The cache's device for a call (its memory, its tensor maps and the default stream are that
-// device's), then the caller's again.
-class OnDevice {
- public:
-  explicit OnDevice(int dev) {
-    error = cudaGetDevice(&before_);
-    if (error != cudaSuccess || before_ == dev) return;
-    error = cudaSetDevice(dev);
-    back_ = error == cudaSuccess;
-  }
-  ~OnDevice() {
-    if (back_) cudaSetDevice(before_);
-  }
-  OnDevice(const OnDevice&) = delete;
-  OnDevice& operator=(const OnDevice&) = delete;
-  cudaError_t error;
-
- private:
-  int before_ = 0;
-  bool back_ = false;
-};
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
@@ -186,7 +165,8 @@ extern "C" int cllm_paged_status(cllm_paged* c, void* cuda_stream) {
   return err == 0 ? CLLM_OK : err & DERR_TIMEOUT ? CLLM_ETIMEOUT : CLLM_EDEVICE;
 }
 
-extern "C" int cllm_paged_append(cllm_paged* c, const cllm_paged_rows* r, void* cuda_stream) {
+// heads: null for a rotation of whole heads in halves, no norms.
+static int append(cllm_paged* c, const cllm_paged_rows* r, const cllm_paged_heads* heads, void* cuda_stream) {
   if (!c || !r || r->layer < 0 || r->layer >= c->d.layers || r->rows < 0) return CLLM_EINVAL;
   if (r->rows == 0) return CLLM_OK;
   const cllm_paged_desc& d = c->d;
@@ -199,9 +179,24 @@ extern "C" int cllm_paged_append(cllm_paged* c, const cllm_paged_rows* r, void* 
     return CLLM_EINVAL;
   if (r->rope && (!aligned(r->rope, 16) || r->max_pos < 1 || !r->positions || !aligned(r->positions, 4)))
     return CLLM_EINVAL;
-  if (r->q && (!r->rope || !rows_ok(r->q, r->q_stride, d.n_heads) || !rows_ok(r->q_out, r->q_out_stride, d.n_heads)))
+  if (r->q && ((!r->rope && !heads) || !rows_ok(r->q, r->q_stride, d.n_heads) ||
+               !rows_ok(r->q_out, r->q_out_stride, d.n_heads)))
     return CLLM_EINVAL;
   PagedAppendArgs a{};
+  a.dims = r->rope ? d.head_dim : 0;
+  if (heads) {
+    if (!aligned(heads->q_norm, 16) || !aligned(heads->k_norm, 16) || (heads->q_norm && !r->q) ||
+        ((heads->q_norm || heads->k_norm) && !(heads->eps >= 0.f && isfinite(heads->eps))) ||
+        (!r->rope && !heads->q_norm && !heads->k_norm))
+      return CLLM_EINVAL;
+    if (r->rope) {
+      if (heads->rotary_dims < 1 || heads->rotary_dims > d.head_dim) return CLLM_EINVAL;
+      if (heads->rotary_dims % 16) return CLLM_EUNSUPPORTED;
+      a.dims = heads->rotary_dims;
+      a.interleaved = heads->interleaved != 0;
+    }
+    a.q_gain = heads->q_norm, a.k_gain = heads->k_norm, a.eps = heads->eps;
+  }
   const int64_t at = r->layer * d.stride_layer * c->es;
   a.k = r->k, a.v = r->v, a.q = r->q, a.q_out = r->q_out;
   a.kp = static_cast<char*>(d.k) + at, a.vp = static_cast<char*>(d.v) + at;
@@ -217,6 +212,43 @@ extern "C" int cllm_paged_append(cllm_paged* c, const cllm_paged_rows* r, void* 
   cudaError_t e = on.error;
   if (e == cudaSuccess) e = launch_paged_append(a, d.dtype, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? CLLM_OK : cuda_fail(e, "paged_append");
+}
+
+extern "C" int cllm_paged_append(cllm_paged* c, const cllm_paged_rows* r, void* cuda_stream) {
+  return append(c, r, nullptr, cuda_stream);
+}
+
+extern "C" int cllm_paged_append_heads(cllm_paged* c, const cllm_paged_rows* r, const cllm_paged_heads* heads,
+                                       void* cuda_stream) {
+  return heads ? append(c, r, heads, cuda_stream) : CLLM_EINVAL;
+}
+
+// f / 2 pi modulo 1, in 2^-64: the quotient in two doubles (1 / 2 pi to 2^-109), whole turns taken off
+// the first exactly.
+static unsigned long long turns_of(double f) {
+  constexpr double hi = 0.15915494309189534561, lo = -9.839338337591243e-18;  // 1 / 2 pi
+  double t = f * hi;
+  const double rest = fma(f, hi, -t) + f * lo;
+  t -= nearbyint(t);
+  if (t >= 0.5) t -= 1.0;
+  return static_cast<unsigned long long>(static_cast<long long>(ldexp(t, 64))) +
+         static_cast<unsigned long long>(llrint(ldexp(rest, 64)));
+}
+
+extern "C" int cllm_rope_table(float* table, int first, int positions, int dims, const double* frequencies,
+                               float amplitude, void* cuda_stream) {
+  if ((positions != 0 && !table) || !aligned(table, 16) || first < 0 || positions < 0 || first > 0x7fffffff - positions || dims < 2 ||
+      dims > kRopeDims || dims % 2 || !frequencies || !isfinite(amplitude))
+    return CLLM_EINVAL;
+  unsigned long long turns[kRopeDims / 2];
+  for (int i = 0; i < dims / 2; ++i) {
+    if (!(fabs(frequencies[i]) <= 1048576.0)) return CLLM_EINVAL;
+    turns[i] = turns_of(frequencies[i]);
+  }
+  if (positions == 0) return CLLM_OK;
+  const cudaError_t e =
+      launch_rope_table(table, first, positions, dims, turns, amplitude, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? CLLM_OK : cuda_fail(e, "rope_table");
 }
 
 extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, void* cuda_stream) {

@@ -77,71 +77,136 @@ template <> struct Vec16<__nv_bfloat16> {
   }
 };
 
-// grid: (rows, parts); the heads of a row, queries first, are dealt to the parts.
+// Head h of row t, queries first, then keys, then values: where it comes from and goes to.
+template <class T>
+struct HeadAt {
+  const T* src = nullptr;  // null: nothing to do
+  T* dst = nullptr;
+};
 template <class T, int HD>
+__device__ __forceinline__ HeadAt<T> head_at(const PagedAppendArgs& a, int t, int h, size_t at, bool stored) {
+  HeadAt<T> r;
+  if (h < a.H) {
+    r.src = static_cast<const T*>(a.q) + t * a.q_row + static_cast<size_t>(h) * HD;
+    r.dst = static_cast<T*>(a.q_out) + t * a.qo_row + static_cast<size_t>(h) * HD;
+  } else if (stored && h < a.H + 2 * a.Hkv) {
+    const int g = h - a.H;
+    if (g < a.Hkv) {
+      r.src = static_cast<const T*>(a.k) + t * a.k_row + static_cast<size_t>(g) * HD;
+      r.dst = static_cast<T*>(a.kp) + at + g * a.s_head;
+    } else {
+      r.src = static_cast<const T*>(a.v) + t * a.v_row + static_cast<size_t>(g - a.Hkv) * HD;
+      r.dst = static_cast<T*>(a.vp) + at + (g - a.Hkv) * a.s_head;
+    }
+  }
+  return r;
+}
+
+// grid: (rows, parts); the heads of a row, queries first, are dealt to the parts.  A thread's
+// two pieces of 16 bytes: pairs of halves are element by element of two pieces, r/2 apart; what is
+// not rotated comes in neighbouring pieces after them.  Neighbours in pairs lie in one piece.
+template <class T, int HD, bool NORM>
 __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const PagedAppendArgs a) {
   using V = Vec16<T>;
   constexpr int kLanes = HD / 2 / V::n;             // threads of one head
   constexpr int kHeads = kAppendThreads / kLanes;   // heads at a time
-  const int t = blockIdx.x, d = (threadIdx.x % kLanes) * V::n;
+  const int t = blockIdx.x, lane = threadIdx.x % kLanes;
   const int all = a.H + 2 * a.Hkv, step = kHeads * gridDim.y;
+  const int half = a.interleaved ? kLanes : a.dims / 2 / V::n;  // pieces between the two of a thread that is rotated
+  const int p0 = lane < half ? lane : 2 * lane, p1 = lane < half ? lane + half : 2 * lane + 1;
+  const bool turn0 = p0 * V::n < a.dims, turn1 = p1 * V::n < a.dims;
   pdl_launch_dependents();
   pdl_wait();
   const long long slot = a.slots[t];
   const bool stored = slot >= 0 && (slot >> a.page_shift) < a.n_pages;
-  bool rotated = a.rope != nullptr;
+  bool skip = false;  // a position outside the table: the row is left out
   float2 cs[V::n];
-  if (rotated) {
+  if (a.rope != nullptr) {
     const int pos = a.positions[t];
-    rotated = static_cast<unsigned>(pos) < static_cast<unsigned>(a.max_pos);
-    if (rotated) {
+    skip = static_cast<unsigned>(pos) >= static_cast<unsigned>(a.max_pos);
+    if (!skip) {
+      const float2* row = a.rope + static_cast<size_t>(pos) * (a.dims / 2);
 #pragma unroll
       for (int i = 0; i < V::n; i += 2) {
-        const float4 x = *reinterpret_cast<const float4*>(a.rope + static_cast<size_t>(pos) * (HD / 2) + d + i);
-        cs[i] = make_float2(x.x, x.y);
-        cs[i + 1] = make_float2(x.z, x.w);
+        // half: the n pairs of this thread; interleaved: n / 2 of either piece
+        const int at = !a.interleaved ? p0 * V::n + i : (i < V::n / 2 ? p0 : p1 - 1) * (V::n / 2) + i;
+        if (i < V::n / 2 || !a.interleaved ? turn0 : turn1) {
+          const float4 x = *reinterpret_cast<const float4*>(row + at);
+          cs[i] = make_float2(x.x, x.y);
+          cs[i + 1] = make_float2(x.z, x.w);
+        }
       }
     }
   }
-  const bool skip = a.rope != nullptr && !rotated;  // a position outside the table: the row is left out
   if (threadIdx.x == 0 && blockIdx.y == 0 && (skip || (slot != -1 && !stored))) atomicOr(a.err, DERR_CAPACITY);
   if (skip) return;
   const long long page = slot >> a.page_shift, off = slot & ((1 << a.page_shift) - 1);
   const size_t at = static_cast<size_t>(page * a.s_page + off * a.s_pos);
-  for (int h = blockIdx.y * kHeads + threadIdx.x / kLanes; h < all; h += step) {
-    const T* src;
-    T* dst;
-    if (h < a.H) {
-      src = static_cast<const T*>(a.q) + t * a.q_row + static_cast<size_t>(h) * HD;
-      dst = static_cast<T*>(a.q_out) + t * a.qo_row + static_cast<size_t>(h) * HD;
-    } else {
-      if (!stored) break;
-      const int g = h - a.H;
-      if (g < a.Hkv) {
-        src = static_cast<const T*>(a.k) + t * a.k_row + static_cast<size_t>(g) * HD;
-        dst = static_cast<T*>(a.kp) + at + g * a.s_head;
-      } else {
-        src = static_cast<const T*>(a.v) + t * a.v_row + static_cast<size_t>(g - a.Hkv) * HD;
-        dst = static_cast<T*>(a.vp) + at + (g - a.Hkv) * a.s_head;
+  // (all lanes of a warp go round together: they exchange sums)
+  for (int h0 = blockIdx.y * kHeads + threadIdx.x / 32 * (32 / kLanes); h0 < all; h0 += step) {
+    const int h = h0 + threadIdx.x % 32 / kLanes;
+    const HeadAt<T> w = head_at<T, HD>(a, t, h, at, stored);
+    const bool key = h >= a.H;
+    const T* gain = NORM && h < a.H + a.Hkv ? static_cast<const T*>(key ? a.k_gain : a.q_gain) : nullptr;
+    const bool turned = h < a.H + a.Hkv && a.rope != nullptr;
+    if constexpr (!NORM) {
+      if (w.src == nullptr) continue;
+      if (!turned) {
+        const uint4 x = *reinterpret_cast<const uint4*>(w.src + p0 * V::n), y = *reinterpret_cast<const uint4*>(w.src + p1 * V::n);
+        *reinterpret_cast<uint4*>(w.dst + p0 * V::n) = x;
+        *reinterpret_cast<uint4*>(w.dst + p1 * V::n) = y;
+        continue;
       }
     }
-    if (rotated && h < a.H + a.Hkv) {
-      float x[V::n], y[V::n];
-      V::load(src + d, x);
-      V::load(src + d + HD / 2, y);
+    float x[V::n], y[V::n];
+    if (w.src != nullptr) {
+      V::load(w.src + p0 * V::n, x);
+      V::load(w.src + p1 * V::n, y);
+    } else {
 #pragma unroll
-      for (int i = 0; i < V::n; ++i) {
-        const float u = x[i], w = y[i];
-        x[i] = u * cs[i].x - w * cs[i].y;
-        y[i] = w * cs[i].x + u * cs[i].y;
-      }
-      V::store(dst + d, x);
-      V::store(dst + d + HD / 2, y);
-    } else {
-      const uint4 x = *reinterpret_cast<const uint4*>(src + d), y = *reinterpret_cast<const uint4*>(src + d + HD / 2);
-      *reinterpret_cast<uint4*>(dst + d) = x;
-      *reinterpret_cast<uint4*>(dst + d + HD / 2) = y;
+      for (int i = 0; i < V::n; ++i) x[i] = y[i] = 0.f;
     }
+    if constexpr (NORM) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < V::n; ++i) sum = fmaf(x[i], x[i], fmaf(y[i], y[i], sum));
+#pragma unroll
+      for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      if (w.src == nullptr) continue;
+      if (gain != nullptr) {
+        const float r = rsqrtf(sum * (1.f / HD) + a.eps);
+        float g[V::n];
+        V::load(gain + p0 * V::n, g);
+#pragma unroll
+        for (int i = 0; i < V::n; ++i) x[i] *= r * g[i];
+        V::load(gain + p1 * V::n, g);
+#pragma unroll
+        for (int i = 0; i < V::n; ++i) y[i] *= r * g[i];
+      }
+    }
+    if (turned) {
+      if (a.interleaved) {
+#pragma unroll
+        for (int i = 0; i < V::n; i += 2) {
+          const float u = x[i], v = x[i + 1], c = cs[i / 2].x, s = cs[i / 2].y;
+          if (turn0) x[i] = u * c - v * s, x[i + 1] = v * c + u * s;
+        }
+#pragma unroll
+        for (int i = 0; i < V::n; i += 2) {
+          const float u = y[i], v = y[i + 1], c = cs[(V::n + i) / 2].x, s = cs[(V::n + i) / 2].y;
+          if (turn1) y[i] = u * c - v * s, y[i + 1] = v * c + u * s;
+        }
+      } else if (turn0) {
+#pragma unroll
+        for (int i = 0; i < V::n; ++i) {
+          const float u = x[i], v = y[i];
+          x[i] = u * cs[i].x - v * cs[i].y;
+          y[i] = v * cs[i].x + u * cs[i].y;
+        }
+      }
+    }
+    V::store(w.dst + p0 * V::n, x);
+    V::store(w.dst + p1 * V::n, y);
   }
 }
 
@@ -151,8 +216,10 @@ cudaError_t launch_append(const PagedAppendArgs& a, cudaStream_t s) {
   // few rows: a row's heads are spread over as many CTAs as there are groups of heads
   const int groups = (a.H + 2 * a.Hkv + kHeads - 1) / kHeads;
   const dim3 grid(a.T, a.T < 2 * 152 ? groups : 1);
-  return launch_after(a.hd == 128 ? paged_append_kernel<T, 128> : paged_append_kernel<T, 64>, grid, kAppendThreads, 0, s,
-                      a);
+  auto launch = [&](auto kernel) { return launch_after(kernel, grid, kAppendThreads, 0, s, a); };
+  if (a.q_gain != nullptr || a.k_gain != nullptr)
+    return a.hd == 128 ? launch(paged_append_kernel<T, 128, true>) : launch(paged_append_kernel<T, 64, true>);
+  return a.hd == 128 ? launch(paged_append_kernel<T, 128, false>) : launch(paged_append_kernel<T, 64, false>);
 }
 
 }  // namespace

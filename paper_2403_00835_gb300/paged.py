@@ -20,7 +20,9 @@ type, device or shape raise ValueError, what the library refuses CllmError;
 from __future__ import annotations
 
 import ctypes
+import math
 import struct
+from array import array
 from contextlib import nullcontext
 from typing import Optional
 
@@ -33,7 +35,7 @@ DTYPES = {torch.float32: _c.CLLM_F32, torch.bfloat16: _c.CLLM_BF16, torch.float1
 
 # Every function declared in include/cllm_paged.h.
 EXPORTS = ("cllm_page_plan", "cllm_paged_create", "cllm_paged_destroy", "cllm_paged_status", "cllm_paged_append",
-           "cllm_paged_attention")
+           "cllm_paged_append_heads", "cllm_rope_table", "cllm_paged_attention")
 
 
 class _Tables(ctypes.Structure):
@@ -54,9 +56,11 @@ class _Desc(ctypes.Structure):
                 ("stride_page", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_pos", ctypes.c_int64)]
 
 
-# cllm_paged_rows and cllm_paged_attn as they lie in memory (native alignment): one call
+# cllm_paged_rows, cllm_paged_heads and cllm_paged_attn as they lie in memory (native alignment): one call
 # fills them, which is a third of what a ctypes structure's fields take.
 _ROWS_IN = struct.Struct("@2i4P4q3Pi")
+_HEADS = struct.Struct("@2Pf2i")
+_HEADS_AT = -(-_ROWS_IN.size // 8) * 8  # behind the rows, on a pointer's boundary
 _ATTN = struct.Struct("@3i3P4q3PifiPi")
 
 _lib = None
@@ -74,6 +78,8 @@ def load():
         lib.cllm_paged_destroy.restype = None
         lib.cllm_paged_status.argtypes = [vp, vp]
         lib.cllm_paged_append.argtypes = [vp, vp, vp]
+        lib.cllm_paged_append_heads.argtypes = [vp, vp, vp, vp]
+        lib.cllm_rope_table.argtypes = [vp, i, i, i, vp, ctypes.c_float, vp]
         lib.cllm_paged_attention.argtypes = [vp, vp, vp]
         for name in EXPORTS:
             if name != "cllm_paged_destroy":
@@ -189,6 +195,62 @@ def plan(tables: PageTables, rows: PageRows, ctx, new_rows, out: Optional[PageTa
     rows.batch = b
 
 
+def rope_frequencies(dims: int, theta: float = 1e4, scaling: Optional[str] = None, factor: float = 1.0,
+                     trained: int = 0, fast: float = 32.0, slow: float = 1.0) -> array:
+    """Radians a position of the dims / 2 pairs of a rotary embedding: theta ** (-2 i / dims), or
+    scaled for contexts ``factor`` times as long as a decoder was trained on:
+
+    "linear"  all divided by factor (position interpolation, arXiv 2306.15595)
+    "base"    of a larger theta, theta * factor ** (dims / (dims - 2)): the slowest pair is divided by factor,
+              the fastest one kept
+    "ramp"    by the turns that a pair makes over the ``trained`` positions (arXiv 2309.00071): kept from
+              ``fast`` turns on, divided by factor up to ``slow``, and a mix of both between; that
+              paper's tables have the amplitude 0.1 ln(factor) + 1
+    """
+    if dims < 2 or dims % 2 or not theta > 0.0 or not (factor > 0.0 and math.isfinite(factor)):
+        raise ValueError("rope_frequencies: need an even dims, theta > 0 and a finite factor > 0")
+    if scaling == "base":
+        if dims == 2:
+            raise ValueError("rope_frequencies: one pair has no base")
+        theta = theta * factor ** (dims / (dims - 2))
+    f = array("d", (theta ** (-2.0 * i / dims) for i in range(dims // 2)))
+    if scaling == "linear":
+        return array("d", (x / factor for x in f))
+    if scaling == "ramp":
+        if trained < 1 or not fast > slow:
+            raise ValueError("rope_frequencies: a ramp needs the trained positions and fast > slow")
+        out = array("d")
+        for x in f:
+            keep = min(1.0, max(0.0, (trained * x / (2.0 * math.pi) - slow) / (fast - slow)))
+            out.append(x * keep + x / factor * (1.0 - keep))
+        return out
+    if scaling not in (None, "base"):
+        raise ValueError("rope_frequencies: scaling is None, 'linear', 'base' or 'ramp'")
+    return f
+
+
+def rope_table(positions: int, frequencies, amplitude: float = 1.0, first: int = 0, out=None, device="cuda", stream=None):
+    """Rows first .. first + positions - 1 of a rotary table: amplitude * (cos, sin)(position * frequency), float32
+    [positions][pairs][2] as ``PagedCache.append`` takes it (``cllm_rope_table``).  frequencies: radians
+    a position (``rope_frequencies``, or any numbers).  out: the rows to fill (None: allocated on the stream of the call)."""
+    f = frequencies if isinstance(frequencies, array) and frequencies.typecode == "d" else array("d", frequencies)
+    pairs = len(f)
+    if out is None:
+        with nullcontext() if stream is None else torch.cuda.stream(stream):
+            out = torch.empty(positions, pairs, 2, device=device if stream is None else stream.device)
+    ptr = _tensor(out, "out", torch.float32, (positions, pairs, 2))
+    dev = out.get_device()
+    args = ptr, first, positions, 2 * pairs, f.buffer_info()[0], amplitude, _stream(stream, dev)
+    if _device() == dev:
+        rc = load().cllm_rope_table(*args)
+    else:
+        with torch.cuda.device(dev):
+            rc = load().cllm_rope_table(*args)
+    if rc:
+        _c._check(rc, "cllm_rope_table")
+    return out
+
+
 class PagedCache:
     """K and V pools [layer][page][kv_head][position][head_dim] of one dtype and
     equal strides, the innermost contiguous (a permuted view gives pages that
@@ -211,7 +273,7 @@ class PagedCache:
         with torch.cuda.device(self.device):
             _c._check(lib.cllm_paged_create(ctypes.byref(d), ctypes.byref(h)), "cllm_paged_create")
         self._h, self._lib, self._dev = h, lib, k.get_device()
-        self._args = ctypes.create_string_buffer(max(_ROWS_IN.size, _ATTN.size))
+        self._args = ctypes.create_string_buffer(max(_HEADS_AT + _HEADS.size, _ATTN.size))
         self._argp = ctypes.addressof(self._args)
         self._scale = self.head_dim ** -0.5
 
@@ -235,30 +297,58 @@ class PagedCache:
                 return t.data_ptr(), row
         raise ValueError(f"{what}: need [{rows}][{heads}][{hd}] {self.dtype} on {self.device}, heads side by side")
 
-    def append(self, layer: int, k, v, slots, q=None, q_out=None, rope=None, positions=None, stream=None):
+    def _gain(self, t, what: str) -> int:
+        if not (isinstance(t, torch.Tensor) and t.dtype is self.dtype and t.shape == (self.head_dim,) and t.is_contiguous()
+                and t.get_device() == self._dev):
+            raise ValueError(f"{what}: need a contiguous [{self.head_dim}] {self.dtype} tensor on {self.device}")
+        return t.data_ptr()
+
+    def append(self, layer: int, k, v, slots, q=None, q_out=None, rope=None, positions=None, stream=None, *,
+               q_norm=None, k_norm=None, eps: float = 1e-6, interleaved: bool = False):
         """Write rows k, v [T][kv_heads][hd] into slots (int64 [T] or more; -1: none).
-        With rope (float32 [max_pos][hd/2][2]: cos, sin) K is rotated by positions
-        (int32 [T] or more), and q [T][n_heads][hd] into q_out (None: in place)."""
+        With rope (float32 [max_pos][r/2][2]: cos, sin) the first r values of each head of K are rotated
+        by positions (int32 [T] or more), in halves (i and i + r/2) or interleaved (2 i and 2 i + 1),
+        and so is q [T][n_heads][hd], into q_out (None: in place).  r: hd, or a smaller multiple of 16.
+        q_norm, k_norm ([hd], of the cache's type): before that every head of q, of k is divided by the
+        root of its mean square (+ eps) and multiplied by these gains."""
         t = k.shape[0]
         kp, ks = self._heads(k, "k", t, self.n_kv_heads)
         vp, vs = self._heads(v, "v", t, self.n_kv_heads)
         sp = _tensor(slots, "slots", torch.int64, None, self._dev)
         if slots.numel() < t:
             raise ValueError("slots: fewer than rows")
-        qp = qs = op = os = rp = pp = max_pos = 0
+        qp = qs = op = os = rp = pp = max_pos = dims = qg = kg = 0
         if rope is not None:
-            max_pos = rope.shape[0]
-            rp = _tensor(rope, "rope", torch.float32, (max_pos, self.head_dim // 2, 2), self._dev)
+            if not (isinstance(rope, torch.Tensor) and rope.dim() == 3):
+                raise ValueError("rope: need [max_pos][pairs][2]")
+            max_pos, pairs, _ = rope.shape
+            dims = 2 * pairs
+            if not 0 < dims <= self.head_dim:
+                raise ValueError(f"rope: rows of 1 to {self.head_dim // 2} pairs, got {pairs}")
+            rp = _tensor(rope, "rope", torch.float32, (max_pos, pairs, 2), self._dev)
             pp = _tensor(positions, "positions", torch.int32, None, self._dev)
             if positions.numel() < t:
                 raise ValueError("positions: fewer than rows")
-            if q is not None:
-                qp, qs = self._heads(q, "q", t, self.n_heads)
-                op, os = (qp, qs) if q_out is None else self._heads(q_out, "q_out", t, self.n_heads)
-        elif q is not None:
-            raise ValueError("q is only rotated: pass rope")
+        elif interleaved:
+            raise ValueError("interleaved pairs of what: pass rope")
+        if q_norm is not None:
+            if q is None:
+                raise ValueError("q_norm without q")
+            qg = self._gain(q_norm, "q_norm")
+        if k_norm is not None:
+            kg = self._gain(k_norm, "k_norm")
+        whole = dims == self.head_dim and not interleaved and q_norm is None and k_norm is None
+        if q is not None:
+            if rope is None and q_norm is None and k_norm is None:
+                raise ValueError("q is only rotated or normalised: pass rope or norms")
+            qp, qs = self._heads(q, "q", t, self.n_heads)
+            op, os = (qp, qs) if q_out is None else self._heads(q_out, "q_out", t, self.n_heads)
         _ROWS_IN.pack_into(self._args, 0, layer, t, kp, vp, qp, op, ks, vs, qs, os, sp, rp, pp, max_pos)
-        rc = self._lib.cllm_paged_append(self._h, self._argp, _stream(stream, self._dev))
+        if whole or (rope is None and q_norm is None and k_norm is None):
+            rc = self._lib.cllm_paged_append(self._h, self._argp, _stream(stream, self._dev))
+        else:
+            _HEADS.pack_into(self._args, _HEADS_AT, qg, kg, eps, dims, interleaved)
+            rc = self._lib.cllm_paged_append_heads(self._h, self._argp, self._argp + _HEADS_AT, _stream(stream, self._dev))
         if rc:
             _c._check(rc, "cllm_paged_append")
 
