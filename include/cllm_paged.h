@@ -226,6 +226,15 @@ typedef struct {
  * keys: cut the step), ECUDA. */
 int cllm_paged_attention(cllm_paged *cache, const cllm_paged_attn *a, void *cuda_stream);
 
+/*
+ * The same with a window beside which the first `sinks` tokens of a request stay visible: of the keys
+ * that the order or the mask lets a row see, it sees those with (ctx + i) - k < window or k < sinks
+ * (without a window, all).  Pages that hold none of the first `sinks` tokens and lie wholly before
+ * the windows of the request's new rows are not read: their table entries may be anything.
+ * Errors: as cllm_paged_attention, and EINVAL (sinks negative).
+ */
+int cllm_paged_attention_sinks(cllm_paged *cache, const cllm_paged_attn *a, int sinks, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,7 @@ struct PagedAttnArgs {
   int H, Hkv, group;       // group = H / Hkv query heads share a key/value head
   int group_inv;           // x / group = x * group_inv >> 16 for x < 256 (ceil(2^16 / group), group <= 64)
   float scale_log2;        // scale * log2(e)
-  int window;
+  int window, sinks;       // sinks: first keys seen beside the window (0 without one)
   const uint32_t* mask;
   int mask_words;
   // this layer's pools

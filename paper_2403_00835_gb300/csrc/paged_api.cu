@@ -252,7 +252,11 @@ extern "C" int cllm_rope_table(float* table, int first, int positions, int dims,
 }
 
 extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, void* cuda_stream) {
-  if (!c || !p || p->layer < 0 || p->layer >= c->d.layers || p->batch < 0 || p->rows < 0) return CLLM_EINVAL;
+  return cllm_paged_attention_sinks(c, p, 0, cuda_stream);
+}
+
+extern "C" int cllm_paged_attention_sinks(cllm_paged* c, const cllm_paged_attn* p, int sinks, void* cuda_stream) {
+  if (!c || !p || sinks < 0 || p->layer < 0 || p->layer >= c->d.layers || p->batch < 0 || p->rows < 0) return CLLM_EINVAL;
   if (p->batch == 0 || p->rows == 0) return CLLM_OK;
   const cllm_paged_desc& d = c->d;
   auto strides_ok = [&](const void* x, int64_t row, int64_t head) {
@@ -284,7 +288,7 @@ extern "C" int cllm_paged_attention(cllm_paged* c, const cllm_paged_attn* p, voi
   a.H = d.n_heads, a.Hkv = d.n_kv_heads, a.group = group;
   a.scale_log2 = p->scale * kLog2e;
   a.group_inv = (65536 + group - 1) / group;
-  a.window = p->window, a.mask = p->mask, a.mask_words = p->mask_words;
+  a.window = p->window, a.sinks = p->window > 0 ? sinks : 0, a.mask = p->mask, a.mask_words = p->mask_words;
   a.k = static_cast<const char*>(d.k) + at, a.v = static_cast<const char*>(d.v) + at;
   a.s_page = d.stride_page, a.s_head = d.stride_head, a.s_pos = d.stride_pos;
   a.layer = p->layer, a.n_pages = d.n_pages, a.page_shift = c->page_shift;

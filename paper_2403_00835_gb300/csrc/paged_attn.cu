@@ -86,9 +86,9 @@ __global__ void __launch_bounds__(kPThreads, 1)
       const int st = (c - p.ca) & 1;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int key = (tid >> 3) + 32 * u, pos = c * kPChunk + key;
+        const int key = (tid >> 3) + 32 * u, pos = p.chunk(c) * kPChunk + key;
         const T *kp = nullptr, *vp = nullptr;
-        if (pos >= p.lo && pos < p.hi) kp = pool_row<T>(a, a.k, p.b, p.h, pos), vp = pool_row<T>(a, a.v, p.b, p.h, pos);
+        if (p.keys.has(pos)) kp = pool_row<T>(a, a.k, p.b, p.h, pos), vp = pool_row<T>(a, a.v, p.b, p.h, pos);
 #pragma unroll
         for (int d = (tid & 7) * 4; d < HD; d += 32) {
           if (kp != nullptr) {
@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
     const bool live = (tid >> 5) * 2 * R < rows;  // some row of the warp is
     if (p.ca < p.cb) load(p.ca);
     for (int c = p.ca; c < p.cb; ++c) {
-      const int kb = c * kPChunk, st = (c - p.ca) & 1;
+      const int kb = p.chunk(c) * kPChunk, st = (c - p.ca) & 1;
       if (c + 1 < p.cb) {
         load(c + 1);
         cp_async_wait_but1();

@@ -85,7 +85,8 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
     if (!piece_wait(&s.pfull[pat.i], pat.phase)) break;
     const PagePiece& p = s.piece[pat.i];
     if (p.end) break;
-    const int n = p.chunks, rows = p.nt * a.group, lo = p.lo, hi = p.hi, ca = p.ca;
+    const int n = p.chunks, rows = p.nt * a.group;
+    const TileKeys keys = p.keys;
     float o[HD / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < HD / 8; ++j)
@@ -106,8 +107,8 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
       const int from = keys_of(quad + 8).lo, to = a.mask != nullptr ? p.len - p.n : keys_of(quad).hi;
 #pragma unroll 1
       for (int i = 0; i < n; ++i) {
-        const int kb = (ca + i) * kFewKeys + warp * KEYS;  // this warp's keys: [kb, kb + KEYS)
-        const bool some = kb < hi && kb + KEYS > lo;
+        const int kb = p.chunk(i) * kFewKeys + warp * KEYS;  // this warp's keys: [kb, kb + KEYS)
+        const bool some = keys.some(kb, kb + KEYS);
         const uint32_t kt = at.i, k_phase = at.phase;
         ++at;
         const uint32_t vt = at.i, v_phase = at.phase;
@@ -179,12 +180,12 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
         }
         warp_wait(&s.full[vt], v_phase);
         if (some) {
-          if (lo > kb || hi < kb + KEYS) {
+          if (!keys.all(kb, kb + KEYS)) {
             // keys that no row of the tile sees (not loaded, or what the page held before): p
             // is 0 there, and so is V
             for (int c = lane; c < KEYS * HD / 8; c += 32) {
-              const int k = c / (HD / 8), key = kb + k;
-              if (key < lo || key >= hi)
+              const int k = c / (HD / 8);
+              if (!keys.has(kb + k))
                 *reinterpret_cast<uint4*>(s.ring[vt] + (c % (HD / 8) >> 3) * kFewKeys * 128 + (warp * KEYS + k) * 128 +
                                           (c & 7) * 16) = make_uint4(0, 0, 0, 0);
             }

@@ -241,22 +241,22 @@ __device__ __forceinline__ void run_rows(TcSmem<HD, NB>& s, const PagedAttnArgs&
     const bool band = row - lane < rows;  // some row of the warp is live
     float m = -INFINITY, l = 0.f;
     if (n > 0) {
-      const int first = p.c[t].first, end = p.c[t].end, step = p.c[t].step, lo = p.lo, hi = p.hi;
+      const int first = p.c[t].first, end = p.c[t].end, step = p.c[t].step;
+      const TileKeys keys = p.keys;
       RowKeys rk = row_keys(a, p.n, p.len, p.row0, tok);
       const int all_to = rk.bits != nullptr ? rk.ctx : rk.hi;  // every key from rk.lo to here is seen
       for (int i = first; i < end; i += step) {
-        const int kb = (p.ca + i) * kTcChunk;
+        const int kb = p.chunk(i) * kTcChunk;
         warp_wait(&s.sfull[t], ns++ & 1);
-        if (lo > kb || hi < kb + kTcChunk) {
+        if (!keys.all(kb, kb + kTcChunk)) {
           // keys of the chunk that no row of the tile sees (not loaded, or what the
           // page held before): p is 0 there, and so is V
           const int v = r + ring_v(i, n);
           warp_wait(&s.full[v % NR], (v / NR) & 1);
-          const int z0 = max(lo - kb, 0), z1 = min(hi - kb, kTcChunk);  // keys seen: [z0, z1)
           // (16 bytes each, 64 columns of the keys after another)
           for (int c = at; c < kTcChunk * HD / 8; c += kTcRows) {
             const int key = c >> 3 & (kTcChunk - 1);
-            if (key < z0 || key >= z1) *reinterpret_cast<uint4*>(s.ring[v % NR] + c * 16) = make_uint4(0, 0, 0, 0);
+            if (!keys.has(kb + key)) *reinterpret_cast<uint4*>(s.ring[v % NR] + c * 16) = make_uint4(0, 0, 0, 0);
           }
           fence_proxy_async_smem();
         }

@@ -25,12 +25,15 @@ struct SlotChunks {
 
 // A piece as the loading warp hands it to the others.
 struct PagePiece {
-  int b, h, t0, nt, n, len, row0, lo, hi;  // as in Piece
+  int b, h, t0, nt, n, len, row0;          // as in Piece
+  TileKeys keys;
+  int near, gap;
   int ca, chunks;                          // first chunk and number of chunks (0: no keys)
   int two, whole;                          // 128 rows in each slot; the whole tile
   int slot, cta0, cta1, first_slot;        // of a cut tile: this part's slot, the CTAs of its parts, the first's slot
   SlotChunks c[2];
   int end;                                 // no piece: the run is over
+  __device__ int chunk(int i) const { return ca + i - (ca + i < near ? gap : 0); }  // where in the request its i-th is
   __device__ int part(int cta) const { return cta == cta0 ? first_slot : 2 * cta; }
 };
 constexpr int kPagePieces = 4;
@@ -135,7 +138,8 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
         o.end = !more;
         if (more) {
           o.b = p.b, o.h = p.h, o.t0 = p.t0, o.nt = p.nt, o.n = p.n, o.len = p.len, o.row0 = p.row0;
-          o.lo = p.lo, o.hi = p.hi;
+          o.keys = p.keys;
+          o.near = p.near, o.gap = p.gap;
           o.ca = p.ca, o.chunks = p.cb - p.ca;
           o.two = p.nt > tt, o.whole = p.whole();
           if (!p.whole()) {
@@ -149,7 +153,9 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
             } else {
               const int t0 = p.t0 + t * tt;
               const TileKeys k = tile_keys(a, p.n, p.len, t0, min(p.t0 + p.nt, t0 + tt));
-              o.c[t] = {max(0, k.lo / kChunk - p.ca), min(o.chunks, (k.hi + kChunk - 1) / kChunk - p.ca), 1};
+              // (a slot's chunks are a run: with first keys in the piece it begins there)
+              const bool sinks = p.chunk(p.ca) * kChunk < k.sink;
+              o.c[t] = {sinks ? 0 : max(0, k.lo / kChunk - p.ca), min(o.chunks, (k.hi + kChunk - 1) / kChunk - p.ca), 1};
             }
           }
         }
@@ -166,23 +172,24 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
     const int n = p.cb - p.ca;
     // this lane's page of a chunk (its box's; the pages that hold keys of the tile are loaded)
     auto page_of = [&](int c) {
-      const int pos = c * kChunk + (j << box_shift);
-      return pos < p.hi ? a.table[static_cast<size_t>(p.b) * a.table_width + (pos >> a.page_shift)] : 0;
+      const int pos = p.chunk(c) * kChunk + (j << box_shift);
+      return pos < p.keys.hi ? a.table[static_cast<size_t>(p.b) * a.table_width + (pos >> a.page_shift)] : 0;
     };
     auto tile = [&](const CUtensorMap* map, int c, int page) {
-      const int kb = c * kChunk;
+      const int kb = p.chunk(c) * kChunk, pos = kb + (j << box_shift);
       if (r >= NR) wait(&s.empty[at.i], at.phase ^ 1);
       if (!ok) return;
-      const int b0 = max(p.lo - kb, 0) >> box_shift, b1 = (min(p.hi - kb, kChunk) + box - 1) >> box_shift;
-      if (lane == 0) mbar_arrive_expect_tx(&s.full[at.i], (b1 - b0) * box * HD * 2);
+      const bool mine = pos < kb + kChunk && p.keys.some(pos, pos + box);
+      const int boxes = __popc(__ballot_sync(0xffffffffu, mine));  // (of 64 columns)
+      if (lane == 0) mbar_arrive_expect_tx(&s.full[at.i], boxes * box * 128);
       __syncwarp();
-      if (j >= b0 && j < b1) {
+      if (mine) {
         if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
           atomicOr(a.err, DERR_CAPACITY);
           page = a.n_pages;  // outside the map: reads as zeros
         }
         tma_load_5d(s.ring[at.i] + half * kChunk * 128 + (j << box_shift) * 128, map, &s.full[at.i], half * 64,
-                    (kb + (j << box_shift)) & (P - 1), p.h, page, a.layer);
+                    pos & (P - 1), p.h, page, a.layer);
       }
       ++r;
       ++at;

@@ -52,7 +52,11 @@ __device__ __forceinline__ Request request(const PagedAttnArgs& a, int b) {
 }
 
 struct TileKeys {
-  int lo, hi;  // keys [lo, hi) that some row sees (hi <= lo: none)
+  int lo, hi, sink;  // keys [0, sink) and [lo, hi) that some row may see (hi <= lo: none; sink < lo, or 0)
+  __device__ bool has(int key) const { return (key >= lo && key < hi) || key < sink; }
+  // of keys [a, b): whether one is such a key, and whether all are
+  __device__ bool some(int a, int b) const { return (a < hi && b > lo) || a < sink; }
+  __device__ bool all(int a, int b) const { return (a >= lo && b <= hi) || b <= sink; }
 };
 // Keys seen by tokens [t0, t1) of a request of n new tokens and `len` in all.
 __device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, int n, int len, int t0, int t1) {
@@ -60,11 +64,23 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, int n, int
   const int ctx = len - n;
   k.hi = ctx < 0 ? 0 : (a.mask != nullptr ? len : ctx + t1);
   k.lo = a.window > 0 ? max(0, ctx + t0 - a.window + 1) : 0;
+  k.sink = a.sinks < k.lo ? min(a.sinks, k.hi) : 0;
+  if (a.sinks >= k.lo) k.lo = 0;
   return k;
 }
-__device__ __forceinline__ int tile_units(const PagedGeom& g, const TileKeys& k) {
-  return k.hi > k.lo ? (((k.hi - 1) >> g.chunk_shift) - (k.lo >> g.chunk_shift)) + 1 : 1;
+// The chunks of a tile: those of its first keys and those from `near` on, which come after them
+// in the order of the work; a tile's chunks are counted so that the near ones have
+// their own numbers, and the others the `gap` numbers before.
+struct TileChunks {
+  int near, gap, units;
+};
+__device__ __forceinline__ TileChunks tile_chunks(const PagedGeom& g, const TileKeys& k) {
+  const int first = k.sink > 0 ? ((k.sink - 1) >> g.chunk_shift) + 1 : 0, near = max(k.lo >> g.chunk_shift, first);
+  TileChunks c{near, near - first, 1};
+  if (k.hi > k.lo) c.units = ((k.hi - 1) >> g.chunk_shift) + 1 - c.gap;
+  return c;
 }
+__device__ __forceinline__ int tile_units(const PagedGeom& g, const TileKeys& k) { return tile_chunks(g, k).units; }
 // Of one head of each lane's request (the whole warp calls; n = 0: none): all units, tiles, and
 // the units of the longest tile.  A request of many tiles is summed by all lanes.
 struct HeadWork {
@@ -120,12 +136,14 @@ struct RunStart {
 struct Piece {
   int b, h, t0, nt;        // request, key/value head, first token and tokens of the tile
   int n, len, row0;        // the request's new tokens, all tokens, first row
-  int lo, hi;              // keys of the tile
+  TileKeys keys;           // of the tile
+  int near, gap;           // as in TileChunks
   int ca, cb;              // this piece's chunks
   int tca, tcb;            // the tile's
   unsigned tile_u;         // the tile's first unit
   __device__ bool whole() const { return ca == tca && cb == tcb; }
   __device__ bool empty() const { return tca == tcb; }
+  __device__ int chunk(int c) const { return c < near ? c - gap : c; }  // where in the request chunk c is
 };
 
 // The run of this CTA among `total` units, and where it begins if that is in one of the
@@ -247,12 +265,14 @@ struct PagedWalk {
     for (;;) {
       const int t1 = min(n, t0 + g.tile_tok);
       const TileKeys k = tile_keys(a, n, len, t0, t1);
-      const int chunks = tile_units(g, k), units = whole ? 1 : chunks;
+      const TileChunks ch = tile_chunks(g, k);
+      const int chunks = ch.units, units = whole ? 1 : chunks;
       if (u < tu + units) {
         p.b = b, p.h = h, p.t0 = t0, p.nt = t1 - t0, p.n = n, p.len = len, p.row0 = row0;
-        p.lo = k.lo, p.hi = k.hi;
+        p.keys = k;
+        p.near = ch.near, p.gap = ch.gap;
         p.tile_u = tu;
-        p.tca = k.lo >> g.chunk_shift;
+        p.tca = ch.gap;
         p.tcb = k.hi > k.lo ? p.tca + chunks : p.tca;
         const unsigned e = min(u1, tu + units);
         p.ca = p.tca, p.cb = p.tcb;
@@ -291,10 +311,10 @@ struct PagedWalk {
 
 // ---- a row's keys ------------------------------------------------------------------
 
-// Keys [lo, hi) that token i of a request may see; with a mask, those from ctx on
-// only where their bit is set.
+// Keys [lo, hi), and of those before lo the first `sink`, that token i of a request may see; with a
+// mask, those from ctx on only where their bit is set.
 struct RowKeys {
-  int lo, hi, ctx;
+  int lo, hi, sink, ctx;
   const uint32_t* bits;  // the row's mask words, or null
   int words;
 };
@@ -304,14 +324,16 @@ __device__ __forceinline__ RowKeys row_keys(const PagedAttnArgs& a, int n, int l
   const int idx = r.ctx + i;
   r.hi = r.ctx < 0 ? 0 : (a.mask != nullptr ? len : idx + 1);
   r.lo = a.window > 0 ? max(0, idx - a.window + 1) : 0;
+  r.sink = a.sinks;
   r.bits = a.mask != nullptr ? a.mask + static_cast<size_t>(row0 + i) * a.mask_words : nullptr;
   r.words = a.mask_words;
   return r;
 }
 // Bit j: whether the row sees key kb + j, j < 32.
 __device__ __forceinline__ uint32_t key_bits(const RowKeys& r, int kb) {
-  const int below = r.lo - kb, above = r.hi - kb;
+  const int below = r.lo - kb, above = r.hi - kb, first = r.sink - kb;
   uint32_t m = below <= 0 ? ~0u : below >= 32 ? 0u : ~0u << below;
+  if (first > 0) m |= first >= 32 ? ~0u : ~(~0u << first);
   m &= above >= 32 ? ~0u : above <= 0 ? 0u : ~(~0u << above);
   if (r.bits != nullptr && m != 0) {
     const int j = kb - r.ctx;  // new token of bit 0
@@ -360,7 +382,8 @@ __device__ __noinline__ void exact_row(const PagedAttnArgs& a, int b, int h, int
 #pragma unroll
   for (int e = 0; e < E; ++e) qv[e] = ld_act(q, lane * E + e), o[e] = 0.f;
   float m = -INFINITY, l = 0.f;
-  for (int kb = r.lo & ~31; kb < r.hi; kb += 32) {
+  const int from = r.lo & ~31;
+  for (int kb = r.sink > 0 ? 0 : from; kb < r.hi; kb = kb + 32 >= r.sink ? max(kb + 32, from) : kb + 32) {
     for (uint32_t bits = key_bits(r, kb); bits; bits &= bits - 1) {
       const int k = kb + __ffs(bits) - 1;
       const T* kp = pool_row<T>(a, a.k, b, h, k);

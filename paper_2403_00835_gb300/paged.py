@@ -35,7 +35,7 @@ DTYPES = {torch.float32: _c.CLLM_F32, torch.bfloat16: _c.CLLM_BF16, torch.float1
 
 # Every function declared in include/cllm_paged.h.
 EXPORTS = ("cllm_page_plan", "cllm_paged_create", "cllm_paged_destroy", "cllm_paged_status", "cllm_paged_append",
-           "cllm_paged_append_heads", "cllm_rope_table", "cllm_paged_attention")
+           "cllm_paged_append_heads", "cllm_rope_table", "cllm_paged_attention", "cllm_paged_attention_sinks")
 
 
 class _Tables(ctypes.Structure):
@@ -81,6 +81,7 @@ def load():
         lib.cllm_paged_append_heads.argtypes = [vp, vp, vp, vp]
         lib.cllm_rope_table.argtypes = [vp, i, i, i, vp, ctypes.c_float, vp]
         lib.cllm_paged_attention.argtypes = [vp, vp, vp]
+        lib.cllm_paged_attention_sinks.argtypes = [vp, vp, i, vp]
         for name in EXPORTS:
             if name != "cllm_paged_destroy":
                 getattr(lib, name).restype = ctypes.c_int
@@ -353,11 +354,13 @@ class PagedCache:
             _c._check(rc, "cllm_paged_append")
 
     def attention(self, layer: int, q, rows: PageRows, tables: PageTables, out=None, lse=None,
-                  scale: Optional[float] = None, window: int = 0, block_mask=None, stream=None):
+                  scale: Optional[float] = None, window: int = 0, block_mask=None, stream=None, *,
+                  sinks: int = 0):
         """Attention of the step's rows q [T][n_heads][hd] (any row and head stride)
         over their requests' pages; returns out (None: allocated on the stream of the call;
         else no part of q).  lse: float32 [T][n_heads] to fill.
-        scale: default head_dim ** -0.5.  window: keys nearer than that (0: all).
+        scale: default head_dim ** -0.5.  window: keys nearer than that (0: all), and the
+        request's first ``sinks`` beside them.
         block_mask: int32 [T][words], bit j of word w: the row sees new token 32 w + j of
         its request (None: causal), at least one word."""
         dev, dtype = self._dev, self.dtype
@@ -383,7 +386,7 @@ class PagedCache:
             mp = _tensor(block_mask, "block_mask", torch.int32, (t, words), dev)
         _ATTN.pack_into(self._args, 0, layer, rows.batch, t, q.data_ptr(), out.data_ptr(), lp, qs, qh, os, oh, rows._start,
                         rows._len, tables._table, tables._width, self._scale if scale is None else scale, window, mp, words)
-        rc = self._lib.cllm_paged_attention(self._h, self._argp, _stream(stream, dev))
+        rc = self._lib.cllm_paged_attention_sinks(self._h, self._argp, sinks, _stream(stream, dev))
         if rc:
             _c._check(rc, "cllm_paged_attention")
         return out

@@ -84,3 +84,8 @@ def test_the_packed_arguments_are_where_the_library_reads_them():
     h = Heads.from_buffer(buf, paged._HEADS_AT)
     assert (h.q, h.k, h.eps, h.dims, h.interleaved) == (5, 6, 0.5, 32, 1)
     assert cllm.STATUS[EUNSUPPORTED] == "CLLM_EUNSUPPORTED"
+
+
+def test_a_null_cache_with_first_tokens(lib):
+    zeros = ctypes.create_string_buffer(256)
+    assert lib.cllm_paged_attention_sinks(None, ctypes.addressof(zeros), 4, None) == EINVAL
