@@ -1,0 +1,127 @@
+"""Python binding of draft verification in include/cllm_verify.h (argument marshalling only).
+
+After the target's logits of a step over blocks of drafted tokens::
+
+    verifier = DraftVerifier(max_rows, max_batch)
+    accepted, following = verifier.verify(logits, tokens, rows, uniforms=u, race=e, temperature=t)
+
+``rows`` is the step's ``paged.PageRows``; what stands is committed (``paged.plan`` with
+ctx + accepted gives the other tokens' pages back), and ``following`` begins the next block.
+Conventions are those of ``paged``.
+"""
+from __future__ import annotations
+
+import ctypes
+import struct
+from contextlib import nullcontext
+
+import torch
+
+from . import cllm as _c
+from . import paged as _paged
+from .paged import DTYPES, _stream, _tensor
+
+# Every function declared in include/cllm_verify.h.
+EXPORTS = ("cllm_verifier_create", "cllm_verifier_destroy", "cllm_verify")
+
+# cllm_verify_args as it lies in memory (native alignment).
+_ARGS = struct.Struct("@4iPq6PqPq3P")
+
+_lib = None
+
+
+def load():
+    """The library with this header's signatures."""
+    global _lib
+    if _lib is None:
+        lib = _paged.load()
+        vp, i = ctypes.c_void_p, ctypes.c_int
+        lib.cllm_verifier_create.argtypes = [i, i, ctypes.POINTER(vp)]
+        lib.cllm_verifier_destroy.argtypes = [vp]
+        lib.cllm_verifier_destroy.restype = None
+        lib.cllm_verify.argtypes = [vp, vp, vp]
+        lib.cllm_verifier_create.restype = lib.cllm_verify.restype = i
+        _lib = lib
+    return _lib
+
+
+class DraftVerifier:
+    """Scratch of verifications of up to max_rows rows and max_batch requests on a device."""
+
+    def __init__(self, max_rows: int, max_batch: int, device="cuda"):
+        lib = load()
+        self.max_rows, self.max_batch = max_rows, max_batch
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError("device: need a CUDA device")
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            self._dev = torch.cuda.current_device()
+            _c._check(lib.cllm_verifier_create(max_rows, max_batch, ctypes.byref(h)), "cllm_verifier_create")
+        self.device = torch.device("cuda", self._dev)
+        self._h, self._lib = h, lib
+        self._args = ctypes.create_string_buffer(_ARGS.size)
+        self._argp = ctypes.addressof(self._args)
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            self._lib.cllm_verifier_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _rows(self, t, what: str, dtype, rows: int, vocab: int):
+        """Rows of a vocabulary's values: (address, row stride)."""
+        if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == self._dev and t.dim() == 2:
+            n, width = t.shape
+            row, one = t.stride()
+            if n >= rows and width == vocab and (one == 1 or vocab == 1):
+                return t.data_ptr(), row
+        raise ValueError(f"{what}: need [{rows}][{vocab}] {dtype} on {self.device}, rows contiguous")
+
+    def _vector(self, t, what: str, dtype, n: int) -> int:
+        p = _tensor(t, what, dtype, None, self._dev)
+        if t.numel() < n:
+            raise ValueError(f"{what}: fewer than {n}")
+        return p
+
+    def verify(self, logits, tokens, rows, uniforms=None, race=None, temperature=None, draft_probs=None, accepted=None,
+               next_tokens=None, target_probs=None, stream=None):
+        """Judge the drafts of a step: tokens (int32 [T]) of the requests of ``rows`` against logits
+        [T][vocab] (float32, bfloat16 or float16, any row stride).  Returns int32 [batch] tensors
+        (accepted, next): how many tokens of each request stand, its first among them, and
+        the token that follows them (0 and -1 for a request without rows, or refused by its plan).
+        uniforms (float32 [T], in [0, 1)) and race (float32 [batch][vocab], exponentially distributed):
+        the random numbers; without both all requests are greedy.  temperature: float32 [batch] (None: 1; 0:
+        greedy).  draft_probs: float32 [T][vocab], row i the distribution that token i + 1 was
+        drawn from (None: the drafts are certain).  accepted, next_tokens: outputs to fill (None: allocated on
+        the stream of the call); target_probs: float32 [T] to fill with the target's probability of each row's draft."""
+        if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in DTYPES:
+            raise ValueError("logits: need a [rows][vocab] tensor of float32, bfloat16 or float16")
+        t, vocab = logits.shape
+        b, dev = rows.batch, self._dev
+        if rows._dev != dev:
+            raise ValueError("rows: on another device than the verifier")
+        lp, ls = self._rows(logits, "logits", logits.dtype, t, vocab)
+        tp = self._vector(tokens, "tokens", torch.int32, t)
+        up = 0 if uniforms is None else self._vector(uniforms, "uniforms", torch.float32, t)
+        rp, rs = (0, 0) if race is None else self._rows(race, "race", torch.float32, b, vocab)
+        hp = 0 if temperature is None else self._vector(temperature, "temperature", torch.float32, b)
+        qp, qs = (0, 0) if draft_probs is None else self._rows(draft_probs, "draft_probs", torch.float32, t, vocab)
+        if accepted is None or next_tokens is None:
+            with nullcontext() if stream is None else torch.cuda.stream(stream):
+                accepted = torch.empty(b, dtype=torch.int32, device=self.device) if accepted is None else accepted
+                next_tokens = torch.empty(b, dtype=torch.int32, device=self.device) if next_tokens is None else next_tokens
+        ap = self._vector(accepted, "accepted", torch.int32, b)
+        np = self._vector(next_tokens, "next_tokens", torch.int32, b)
+        pp = 0 if target_probs is None else self._vector(target_probs, "target_probs", torch.float32, t)
+        _ARGS.pack_into(self._args, 0, b, t, vocab, DTYPES[logits.dtype], lp, ls, tp, rows._start, rows._len, hp, up, rp, rs, qp,
+                        qs, ap, np, pp)
+        rc = self._lib.cllm_verify(self._h, self._argp, _stream(stream, dev))
+        if rc:
+            _c._check(rc, "cllm_verify")
+        return accepted, next_tokens
