@@ -1,13 +1,19 @@
-// The write of a step's keys and values into their pages (cllm_paged_append),
-// with the rotary embedding of K and Q:
+// The write of a step's keys and values into their pages (cllm_paged_append,
+// cllm_paged_append_heads), with norms of K and Q per head and their rotary embedding:
 //
-//   rope(x)_i = x_i cos - x_{i+h/2} sin,  rope(x)_{i+h/2} = x_{i+h/2} cos + x_i sin
+//   norm(x) = x / sqrt(sum x^2 / hd + eps) * gain
+//   rope(x)_i = x_i cos - x_j sin,  rope(x)_j = x_j cos + x_i sin,  j = i + r/2, or i even and j = i + 1
 //
 // in fp32, rounded once.  Bound: HBM, every value read once and written once.
-// A thread holds 16 bytes of each half of a head and their cosines and sines,
-// which serve all of its heads of that row; a row's threads cover 32 (16 in
-// fp32) heads at a time, so loads and stores are whole 128-byte lines.  Measured: 8192
-// rows, 32 + 2 x 32 heads of 128 in bf16: 64.7 us, 6.3 TB/s; 256 rows 3.6 us, 16 rows 1.9 us (an
+// A thread holds two pieces of 16 bytes of a head and their cosines and sines, which serve all
+// of its heads of that row; the threads of a head are neighbours, which add up its squares.
+// The loads of two heads are under way before the row's slot and position are known.
+//
+// Small CTAs (2 warps) of a row each: a CTA's heads are a loop of several turns after one wait for
+// slot, position and table, and 14 to 16 of them on an SM keep its loads apart in time.  Measured, 8192
+// rows of 32 + 2 x 32 heads of 128 in bf16: rotated 62.5 us, 6.5 TB/s; normalised too 66.8, 6.1
+// (CTAs of 4 warps 61.4 and 67.3 to 71, of 8 warps 70.9 and 94.5; one head's loads at a time 63.2
+// and 76, three 62.4 and 65 to 69, four 62.0 and 72); 256 rows of 32 + 2 x 8 heads 3.2 us, 16 rows 2.2 us (an
 // empty launch of the kind takes 1.9).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -21,23 +27,22 @@ namespace cllm {
 
 namespace {
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 64;
+constexpr int kAppendAhead = 2;  // heads of a thread on their way
 
 template <class T> struct Vec16;  // 16 bytes of T as floats
 template <> struct Vec16<float> {
   static constexpr int n = 4;
-  static __device__ void load(const float* p, float (&v)[4]) {
-    const float4 x = *reinterpret_cast<const float4*>(p);
-    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+  static __device__ void unpack(const uint4& x, float (&v)[4]) {
+    v[0] = __uint_as_float(x.x), v[1] = __uint_as_float(x.y), v[2] = __uint_as_float(x.z), v[3] = __uint_as_float(x.w);
   }
-  static __device__ void store(float* p, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  static __device__ uint4 pack(const float (&v)[4]) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
   }
 };
 template <> struct Vec16<__half> {
   static constexpr int n = 8;
-  static __device__ void load(const __half* p, float (&v)[8]) {
-    const uint4 x = *reinterpret_cast<const uint4*>(p);
+  static __device__ void unpack(const uint4& x, float (&v)[8]) {
     const uint32_t u[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -45,20 +50,19 @@ template <> struct Vec16<__half> {
       v[2 * i] = f.x, v[2 * i + 1] = f.y;
     }
   }
-  static __device__ void store(__half* p, const float (&v)[8]) {
+  static __device__ uint4 pack(const float (&v)[8]) {
     uint32_t u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
       u[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
-    *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+    return make_uint4(u[0], u[1], u[2], u[3]);
   }
 };
 template <> struct Vec16<__nv_bfloat16> {
   static constexpr int n = 8;
-  static __device__ void load(const __nv_bfloat16* p, float (&v)[8]) {
-    const uint4 x = *reinterpret_cast<const uint4*>(p);
+  static __device__ void unpack(const uint4& x, float (&v)[8]) {
     const uint32_t u[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -66,57 +70,71 @@ template <> struct Vec16<__nv_bfloat16> {
       v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
     }
   }
-  static __device__ void store(__nv_bfloat16* p, const float (&v)[8]) {
+  static __device__ uint4 pack(const float (&v)[8]) {
     uint32_t u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
       u[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
-    *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+    return make_uint4(u[0], u[1], u[2], u[3]);
   }
 };
 
-// Head h of row t, queries first, then keys, then values: where it comes from and goes to.
-template <class T>
-struct HeadAt {
-  const T* src = nullptr;  // null: nothing to do
-  T* dst = nullptr;
-};
+// Head h of a row, queries first, then keys, then values: where it comes from, and goes to.
 template <class T, int HD>
-__device__ __forceinline__ HeadAt<T> head_at(const PagedAppendArgs& a, int t, int h, size_t at, bool stored) {
-  HeadAt<T> r;
-  if (h < a.H) {
-    r.src = static_cast<const T*>(a.q) + t * a.q_row + static_cast<size_t>(h) * HD;
-    r.dst = static_cast<T*>(a.q_out) + t * a.qo_row + static_cast<size_t>(h) * HD;
-  } else if (stored && h < a.H + 2 * a.Hkv) {
-    const int g = h - a.H;
-    if (g < a.Hkv) {
-      r.src = static_cast<const T*>(a.k) + t * a.k_row + static_cast<size_t>(g) * HD;
-      r.dst = static_cast<T*>(a.kp) + at + g * a.s_head;
-    } else {
-      r.src = static_cast<const T*>(a.v) + t * a.v_row + static_cast<size_t>(g - a.Hkv) * HD;
-      r.dst = static_cast<T*>(a.vp) + at + (g - a.Hkv) * a.s_head;
-    }
-  }
-  return r;
+__device__ __forceinline__ const T* head_from(const PagedAppendArgs& a, int t, int h) {
+  if (h < a.H) return static_cast<const T*>(a.q) + t * a.q_row + static_cast<size_t>(h) * HD;
+  const int g = h - a.H;
+  return g < a.Hkv ? static_cast<const T*>(a.k) + t * a.k_row + static_cast<size_t>(g) * HD
+                   : static_cast<const T*>(a.v) + t * a.v_row + static_cast<size_t>(g - a.Hkv) * HD;
 }
+template <class T, int HD>
+__device__ __forceinline__ T* head_to(const PagedAppendArgs& a, int t, int h, size_t at) {
+  if (h < a.H) return static_cast<T*>(a.q_out) + t * a.qo_row + static_cast<size_t>(h) * HD;
+  const int g = h - a.H;
+  return (g < a.Hkv ? static_cast<T*>(a.kp) + g * a.s_head : static_cast<T*>(a.vp) + (g - a.Hkv) * a.s_head) + at;
+}
+
+// What a launch's heads need: a rotation of whole heads in halves (or none), any rotation, norms too.
+enum AppendKind { kWhole, kTurned, kNormed };
 
 // grid: (rows, parts); the heads of a row, queries first, are dealt to the parts.  A thread's
 // two pieces of 16 bytes: pairs of halves are element by element of two pieces, r/2 apart; what is
 // not rotated comes in neighbouring pieces after them.  Neighbours in pairs lie in one piece.
-template <class T, int HD, bool NORM>
-__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const PagedAppendArgs a) {
+template <class T, int HD, AppendKind KIND>
+__global__ void __launch_bounds__(kAppendThreads, KIND == kNormed ? 14 : 16) paged_append_kernel(const PagedAppendArgs a) {
   using V = Vec16<T>;
   constexpr int kLanes = HD / 2 / V::n;             // threads of one head
   constexpr int kHeads = kAppendThreads / kLanes;   // heads at a time
+  constexpr int U = kAppendAhead;
   const int t = blockIdx.x, lane = threadIdx.x % kLanes;
-  const int all = a.H + 2 * a.Hkv, step = kHeads * gridDim.y;
-  const int half = a.interleaved ? kLanes : a.dims / 2 / V::n;  // pieces between the two of a thread that is rotated
+  const int all = a.H + 2 * a.Hkv, step = kHeads * gridDim.y, turned_heads = a.rope != nullptr ? a.H + a.Hkv : 0;
+  // pieces between the two of a thread that is rotated
+  const int half = KIND == kWhole || a.interleaved ? kLanes : a.dims / 2 / V::n;
   const int p0 = lane < half ? lane : 2 * lane, p1 = lane < half ? lane + half : 2 * lane + 1;
-  const bool turn0 = p0 * V::n < a.dims, turn1 = p1 * V::n < a.dims;
+  const bool turn0 = KIND == kWhole || p0 * V::n < a.dims, turn1 = KIND == kWhole || p1 * V::n < a.dims;
+  const bool inter = KIND != kWhole && a.interleaved;
   pdl_launch_dependents();
   pdl_wait();
+  // (all lanes of a warp go round together: with norms they exchange sums)
+  int h0 = blockIdx.y * kHeads + threadIdx.x / kLanes;
+  const int end = all + (threadIdx.x % 32) / kLanes;
+  uint4 x[U], y[U];
+  auto load = [&] {  // the next heads, U at a time
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * step;
+      if (h < all) {
+        const T* from = head_from<T, HD>(a, t, h);
+        x[u] = *reinterpret_cast<const uint4*>(from + p0 * V::n);
+        y[u] = *reinterpret_cast<const uint4*>(from + p1 * V::n);
+      } else {
+        x[u] = y[u] = make_uint4(0, 0, 0, 0);
+      }
+    }
+  };
+  load();
   const long long slot = a.slots[t];
   const bool stored = slot >= 0 && (slot >> a.page_shift) < a.n_pages;
   bool skip = false;  // a position outside the table: the row is left out
@@ -125,15 +143,15 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const Page
     const int pos = a.positions[t];
     skip = static_cast<unsigned>(pos) >= static_cast<unsigned>(a.max_pos);
     if (!skip) {
-      const float2* row = a.rope + static_cast<size_t>(pos) * (a.dims / 2);
+      const float2* row = a.rope + static_cast<size_t>(pos) * ((KIND == kWhole ? HD : a.dims) / 2);
 #pragma unroll
       for (int i = 0; i < V::n; i += 2) {
         // half: the n pairs of this thread; interleaved: n / 2 of either piece
-        const int at = !a.interleaved ? p0 * V::n + i : (i < V::n / 2 ? p0 : p1 - 1) * (V::n / 2) + i;
-        if (i < V::n / 2 || !a.interleaved ? turn0 : turn1) {
-          const float4 x = *reinterpret_cast<const float4*>(row + at);
-          cs[i] = make_float2(x.x, x.y);
-          cs[i + 1] = make_float2(x.z, x.w);
+        const int at = !inter ? p0 * V::n + i : (i < V::n / 2 ? p0 : p1 - 1) * (V::n / 2) + i;
+        if (i < V::n / 2 || !inter ? turn0 : turn1) {
+          const float4 c = *reinterpret_cast<const float4*>(row + at);
+          cs[i] = make_float2(c.x, c.y);
+          cs[i + 1] = make_float2(c.z, c.w);
         }
       }
     }
@@ -142,71 +160,63 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const Page
   if (skip) return;
   const long long page = slot >> a.page_shift, off = slot & ((1 << a.page_shift) - 1);
   const size_t at = static_cast<size_t>(page * a.s_page + off * a.s_pos);
-  // (all lanes of a warp go round together: they exchange sums)
-  for (int h0 = blockIdx.y * kHeads + threadIdx.x / 32 * (32 / kLanes); h0 < all; h0 += step) {
-    const int h = h0 + threadIdx.x % 32 / kLanes;
-    const HeadAt<T> w = head_at<T, HD>(a, t, h, at, stored);
-    const bool key = h >= a.H;
-    const T* gain = NORM && h < a.H + a.Hkv ? static_cast<const T*>(key ? a.k_gain : a.q_gain) : nullptr;
-    const bool turned = h < a.H + a.Hkv && a.rope != nullptr;
-    if constexpr (!NORM) {
-      if (w.src == nullptr) continue;
-      if (!turned) {
-        const uint4 x = *reinterpret_cast<const uint4*>(w.src + p0 * V::n), y = *reinterpret_cast<const uint4*>(w.src + p1 * V::n);
-        *reinterpret_cast<uint4*>(w.dst + p0 * V::n) = x;
-        *reinterpret_cast<uint4*>(w.dst + p1 * V::n) = y;
-        continue;
-      }
-    }
-    float x[V::n], y[V::n];
-    if (w.src != nullptr) {
-      V::load(w.src + p0 * V::n, x);
-      V::load(w.src + p1 * V::n, y);
-    } else {
+  for (; h0 < end; h0 += U * step, load()) {
 #pragma unroll
-      for (int i = 0; i < V::n; ++i) x[i] = y[i] = 0.f;
-    }
-    if constexpr (NORM) {
-      float sum = 0.f;
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * step;
+      const bool live = h < all && (stored || h < a.H);
+      const T* gain = nullptr;
+      if constexpr (KIND == kNormed) gain = h < a.H ? static_cast<const T*>(a.q_gain) : h < a.H + a.Hkv ? static_cast<const T*>(a.k_gain) : nullptr;
+      if (KIND != kNormed && !live) continue;
+      if (KIND == kNormed || h < turned_heads) {
+        float v[V::n], w[V::n];
+        V::unpack(x[u], v);
+        V::unpack(y[u], w);
+        if constexpr (KIND == kNormed) {
+          float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < V::n; ++i) sum = fmaf(x[i], x[i], fmaf(y[i], y[i], sum));
+          for (int i = 0; i < V::n; ++i) sum = fmaf(v[i], v[i], fmaf(w[i], w[i], sum));
 #pragma unroll
-      for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      if (w.src == nullptr) continue;
-      if (gain != nullptr) {
-        const float r = rsqrtf(sum * (1.f / HD) + a.eps);
-        float g[V::n];
-        V::load(gain + p0 * V::n, g);
+          for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+          if (!live) continue;
+          if (gain != nullptr) {
+            const float r = rsqrtf(sum * (1.f / HD) + a.eps);
+            float g[V::n];
+            V::unpack(*reinterpret_cast<const uint4*>(gain + p0 * V::n), g);
 #pragma unroll
-        for (int i = 0; i < V::n; ++i) x[i] *= r * g[i];
-        V::load(gain + p1 * V::n, g);
+            for (int i = 0; i < V::n; ++i) v[i] *= r * g[i];
+            V::unpack(*reinterpret_cast<const uint4*>(gain + p1 * V::n), g);
 #pragma unroll
-        for (int i = 0; i < V::n; ++i) y[i] *= r * g[i];
-      }
-    }
-    if (turned) {
-      if (a.interleaved) {
-#pragma unroll
-        for (int i = 0; i < V::n; i += 2) {
-          const float u = x[i], v = x[i + 1], c = cs[i / 2].x, s = cs[i / 2].y;
-          if (turn0) x[i] = u * c - v * s, x[i + 1] = v * c + u * s;
+            for (int i = 0; i < V::n; ++i) w[i] *= r * g[i];
+          }
         }
+        if (h < turned_heads) {
+          if (inter) {
 #pragma unroll
-        for (int i = 0; i < V::n; i += 2) {
-          const float u = y[i], v = y[i + 1], c = cs[(V::n + i) / 2].x, s = cs[(V::n + i) / 2].y;
-          if (turn1) y[i] = u * c - v * s, y[i + 1] = v * c + u * s;
-        }
-      } else if (turn0) {
+            for (int i = 0; i < V::n; i += 2) {
+              const float e = v[i], f = v[i + 1], c = cs[i / 2].x, s = cs[i / 2].y;
+              if (turn0) v[i] = e * c - f * s, v[i + 1] = f * c + e * s;
+            }
 #pragma unroll
-        for (int i = 0; i < V::n; ++i) {
-          const float u = x[i], v = y[i];
-          x[i] = u * cs[i].x - v * cs[i].y;
-          y[i] = v * cs[i].x + u * cs[i].y;
+            for (int i = 0; i < V::n; i += 2) {
+              const float e = w[i], f = w[i + 1], c = cs[(V::n + i) / 2].x, s = cs[(V::n + i) / 2].y;
+              if (turn1) w[i] = e * c - f * s, w[i + 1] = f * c + e * s;
+            }
+          } else if (turn0) {
+#pragma unroll
+            for (int i = 0; i < V::n; ++i) {
+              const float e = v[i], f = w[i];
+              v[i] = e * cs[i].x - f * cs[i].y;
+              w[i] = f * cs[i].x + e * cs[i].y;
+            }
+          }
         }
+        if (KIND != kNormed || gain != nullptr || h < turned_heads) x[u] = V::pack(v), y[u] = V::pack(w);
       }
+      T* to = head_to<T, HD>(a, t, h, at);
+      *reinterpret_cast<uint4*>(to + p0 * V::n) = x[u];
+      *reinterpret_cast<uint4*>(to + p1 * V::n) = y[u];
     }
-    V::store(w.dst + p0 * V::n, x);
-    V::store(w.dst + p1 * V::n, y);
   }
 }
 
@@ -217,9 +227,13 @@ cudaError_t launch_append(const PagedAppendArgs& a, cudaStream_t s) {
   const int groups = (a.H + 2 * a.Hkv + kHeads - 1) / kHeads;
   const dim3 grid(a.T, a.T < 2 * 152 ? groups : 1);
   auto launch = [&](auto kernel) { return launch_after(kernel, grid, kAppendThreads, 0, s, a); };
-  if (a.q_gain != nullptr || a.k_gain != nullptr)
-    return a.hd == 128 ? launch(paged_append_kernel<T, 128, true>) : launch(paged_append_kernel<T, 64, true>);
-  return a.hd == 128 ? launch(paged_append_kernel<T, 128, false>) : launch(paged_append_kernel<T, 64, false>);
+  auto kind = [&](auto whole, auto turned, auto normed) {
+    if (a.q_gain != nullptr || a.k_gain != nullptr) return launch(normed);
+    return a.interleaved || (a.rope != nullptr && a.dims != a.hd) ? launch(turned) : launch(whole);
+  };
+  if (a.hd == 128)
+    return kind(paged_append_kernel<T, 128, kWhole>, paged_append_kernel<T, 128, kTurned>, paged_append_kernel<T, 128, kNormed>);
+  return kind(paged_append_kernel<T, 64, kWhole>, paged_append_kernel<T, 64, kTurned>, paged_append_kernel<T, 64, kNormed>);
 }
 
 }  // namespace

@@ -15,13 +15,14 @@ namespace cllm {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopePairs = 16;  // pairs of a thread, two to a store
+constexpr int kRopeTurns = 16;  // stores of a thread, at most
 
 struct RopeArgs {
-  float4* table;
-  long long pairs;  // all of the table's
-  unsigned first;
-  int per;          // pairs of a position
+  float2* table;
+  unsigned first, positions;
+  int per;               // pairs of a position
+  int unit, lanes, side; // positions of a unit (an even number of pairs), its threads, units side by side in a CTA
+  int turns;             // stores of a thread
   float amplitude;
   unsigned long long g[kRopeDims / 2];
 };
@@ -44,35 +45,29 @@ __device__ __forceinline__ float2 cos_sin(unsigned long long turn) {
                      __uint_as_float(__float_as_uint(v) ^ (quarter << 30 & 0x80000000u)));
 }
 
+// A thread keeps its two pairs of a unit and goes from unit to unit: a step adds to its fractions.
 __global__ void __launch_bounds__(kRopeThreads) paged_rope_kernel(const __grid_constant__ RopeArgs a) {
-  __shared__ unsigned long long g[kRopeDims / 2];
-  if (threadIdx.x < static_cast<unsigned>(a.per)) g[threadIdx.x] = a.g[threadIdx.x];
-  __syncthreads();
+  const int at = threadIdx.x / a.lanes, e = (threadIdx.x - at * a.lanes) * 2;
   pdl_launch_dependents();
-  const long long base = static_cast<long long>(blockIdx.x) * (kRopeThreads * kRopePairs);
-  const long long p0 = base / a.per;
-  const int left = static_cast<int>(base - p0 * a.per);
-  auto value = [&](unsigned pos, int i) {
-    const float2 x = cos_sin(pos * g[i]);
-    return make_float2(a.amplitude * x.x, a.amplitude * x.y);
-  };
+  if (at >= a.side) return;
+  const int o0 = e >= a.per, o1 = e + 1 >= a.per;  // position in the unit
+  const unsigned long long g0 = a.g[e - o0 * a.per], g1 = a.g[e + 1 - o1 * a.per];
+  unsigned pos = (blockIdx.x * (a.side * a.turns) + at) * static_cast<unsigned>(a.unit);
+  const unsigned step = a.side * a.unit;
+  unsigned long long x = (a.first + pos + o0) * g0, y = (a.first + pos + o1) * g1;
+  float2* to = a.table + static_cast<size_t>(pos) * a.per + e;
   pdl_wait();
-#pragma unroll 4
-  for (int u = 0; u < kRopePairs / 2; ++u) {
-    const int e = (u * kRopeThreads + static_cast<int>(threadIdx.x)) * 2;  // this thread's pair of the block
-    if (base + e >= a.pairs) break;
-    unsigned pos = (left + e) / a.per;
-    int i = left + e - pos * a.per;
-    pos += a.first + static_cast<unsigned>(p0);
-    const float2 x = value(pos, i);
-    if (++i == a.per) i = 0, ++pos;
-    float4* to = a.table + ((base + e) >> 1);
-    if (base + e + 1 < a.pairs) {
-      const float2 y = value(pos, i);
-      *to = make_float4(x.x, x.y, y.x, y.y);
+#pragma unroll 2
+  for (int k = 0; k < a.turns; ++k) {
+    if (pos + o0 >= a.positions) break;
+    const float2 u = cos_sin(x), v = cos_sin(y);
+    if (pos + o1 < a.positions) {
+      *reinterpret_cast<float4*>(to) = make_float4(a.amplitude * u.x, a.amplitude * u.y, a.amplitude * v.x, a.amplitude * v.y);
     } else {
-      *reinterpret_cast<float2*>(to) = x;
+      *to = make_float2(a.amplitude * u.x, a.amplitude * u.y);
     }
+    x += step * g0, y += step * g1;
+    pos += step, to += static_cast<size_t>(step) * a.per;
   }
 }
 
@@ -81,12 +76,15 @@ __global__ void __launch_bounds__(kRopeThreads) paged_rope_kernel(const __grid_c
 cudaError_t launch_rope_table(float* table, int first, int positions, int dims, const unsigned long long* turns,
                               float amplitude, cudaStream_t s) {
   RopeArgs a;
-  a.table = reinterpret_cast<float4*>(table);
-  a.first = first, a.per = dims / 2, a.amplitude = amplitude;
-  a.pairs = static_cast<long long>(positions) * a.per;
+  a.table = reinterpret_cast<float2*>(table);
+  a.first = first, a.positions = positions, a.per = dims / 2, a.amplitude = amplitude;
+  a.unit = a.per % 2 ? 2 : 1;  // (a store takes two pairs)
+  a.lanes = a.per * a.unit / 2;
+  a.side = kRopeThreads / a.lanes;
+  const int units = (positions - 1) / a.unit + 1;
+  a.turns = min(max(units / (a.side * 152 * 8), 1), kRopeTurns);
   for (int i = 0; i < kRopeDims / 2; ++i) a.g[i] = i < a.per ? turns[i] : 0;
-  constexpr long long block = kRopeThreads * kRopePairs;
-  return launch_after(paged_rope_kernel, dim3(static_cast<unsigned>((a.pairs + block - 1) / block)), kRopeThreads, 0, s, a);
+  return launch_after(paged_rope_kernel, dim3((units - 1) / (a.side * a.turns) + 1), kRopeThreads, 0, s, a);
 }
 
 }  // namespace cllm
