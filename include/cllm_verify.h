@@ -30,7 +30,7 @@ extern "C" {
 typedef struct cllm_verifier cllm_verifier;
 
 /* A verifier owns the scratch of calls of up to max_rows rows and max_batch requests on the current
- * device (28 bytes a row, 12 a request and 16 KB).  Calls on one verifier must not overlap in time.
+ * device (28 bytes a row, 12 a request and 40 KB).  Calls on one verifier must not overlap in time.
  * Errors: EINVAL (sizes < 1, null), EUNSUPPORTED (not an sm_103 device), ENOMEM, ECUDA. */
 int cllm_verifier_create(int max_rows, int max_batch, cllm_verifier **out);
 
@@ -51,7 +51,7 @@ void cllm_verifier_destroy(cllm_verifier *v);
  * unless greedy, +inf; none above -inf; a temperature that is negative, NaN or above 2^40) ends its
  * request: no draft stands against it, and next is -1 if it decides.
  * Logits of -inf are tokens that are never drawn.
- * In fp32, probabilities to about 2^-20 of themselves (their sum's terms to 2^-21), a draft's own in fp64.
+ * In fp32: probabilities to about 2^-20 of themselves.
  */
 typedef struct {
   int batch, rows, vocab, dtype;        /* rows: of the logits; dtype: CLLM_F32 | CLLM_BF16 | CLLM_F16, of the logits */

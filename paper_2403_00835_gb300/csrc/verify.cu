@@ -3,17 +3,22 @@
 //   p(x) = 2^(c (z_x - m)) / S,  S = sum_v 2^(c (z_v - m)),  c = log2(e) / temperature,  m = max z
 //   a draft stands:  u q(x) < p(x);   next = argmax_v max(p - q, 0)_v / e_v
 //
-// The first kernel reads all logits once, a row in as many shares as fill the GPU: a thread
-// keeps its running maximum and sum; the CTA that brings a row's last share adds them up in order and
-// judges its draft.  The second finds each request's first row whose draft falls, and runs
-// the race over that row, its vocabulary in parts; results meet in one atomicMax on (ratio, lowest
+// The first kernel reads all logits once, a row in as many shares as there are warps on the GPU: a
+// lane keeps its running maximum and sum; the warp that brings a row's last share adds them up in
+// order and judges its draft.  The second finds each request's first row whose draft falls, and
+// runs the race over that row, its vocabulary in parts; results meet in one atomicMax on (ratio, lowest
 // index), whose order does not matter.
 //
 // c is held in two floats, the first rounded down, so that both products of an infinite
-// difference have its sign.  Sums and probabilities are in fp32; a draft's own probability is
-// taken in fp64 (its border decides), one a row.
+// difference have its sign.  Sums and probabilities are in fp32.
 //
-// Bound: HBM, the logits.
+// Bound: HBM, the logits, then the race and the deciding rows (which are in L2 where all logits
+// are).  Measured: 768 rows of 131072 in bf16 (201 MB) 37 us, 5.4 TB/s, as long as a bare reduction of these bytes
+// takes (39); 3072 rows 125 us, 6.45 TB/s.  The race of 102 requests over them (81 MB) 16 us.
+// 16 rows of 32000 in fp32: 8.6 us for both, two launches and their trips to L2.
+// Next vectors are loaded while these are summed: 36.9 us against 42 without.  More warps with fewer registers
+// 42, CTAs of 8 warps that reduce a share together 40 to 44, shares a half or a quarter as long 41
+// and 45; requests to L2 ahead of the race's loads change nothing.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -26,38 +31,78 @@ namespace cllm {
 
 namespace {
 
-constexpr int kVThreads = 256, kVWarps = kVThreads / 32;
+// CTAs of two warps: the warps have nothing to do with one another, and a CTA's place is free when both have ended.
+constexpr int kVThreads = 64, kVWarps = kVThreads / 32;
+constexpr int kDrawWarps = 24;  // of the second kernel on an SM
 constexpr float kLog2eHi = 1.44269502162933349609f, kLog2eLo = 1.9259629911e-8f;
 
-template <class T> struct Logits;  // 16 bytes of logits
+// 16 bytes of logits.  kNone: four bytes of -inf.
+template <class T> struct Logits;
 template <> struct Logits<float> {
   static constexpr int n = 4;
-  static __device__ void unpack(const uint4& x, float (&v)[4]) {
-    v[0] = __uint_as_float(x.x), v[1] = __uint_as_float(x.y), v[2] = __uint_as_float(x.z), v[3] = __uint_as_float(x.w);
+  static constexpr uint32_t kNone = 0xff800000u;
+  static __device__ float2 pair(const uint4& x, int i) {
+    return i == 0 ? make_float2(__uint_as_float(x.x), __uint_as_float(x.y)) : make_float2(__uint_as_float(x.z), __uint_as_float(x.w));
   }
   static __device__ float one(const float* p) { return *p; }
-};
-template <> struct Logits<__half> {
-  static constexpr int n = 8;
-  static __device__ void unpack(const uint4& x, float (&v)[8]) {
-    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+  static __device__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+  }
+  // the largest of some vectors; NaN if one is (else without notice)
+  template <bool NAN_TOO, int U>
+  static __device__ float top(const uint4 (&x)[U]) {
+    float m = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
-      v[2 * i] = f.x, v[2 * i + 1] = f.y;
-    }
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 v = pair(x[u], i);
+        m = NAN_TOO ? max_nan(m, max_nan(v.x, v.y)) : fmaxf(m, fmaxf(v.x, v.y));
+      }
+    return m;
+  }
+};
+template <class T, class T2>
+struct Logits16 {
+  static constexpr int n = 8;
+  template <bool NAN_TOO, int U>
+  static __device__ float top(const uint4 (&x)[U]) {
+    auto two = [](uint32_t w) { return *reinterpret_cast<const T2*>(&w); };
+    auto larger = [](T2 a, T2 b) { return NAN_TOO ? __hmax2_nan(a, b) : __hmax2(a, b); };
+    T2 m = two(x[0].x);
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = larger(m, larger(larger(two(x[u].x), two(x[u].y)), larger(two(x[u].z), two(x[u].w))));
+    const float lo = Logits<T>::wide(m.x), hi = Logits<T>::wide(m.y);
+    return NAN_TOO ? Logits<float>::max_nan(lo, hi) : fmaxf(lo, hi);
+  }
+  static __device__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
+};
+template <> struct Logits<__half> : Logits16<__half, __half2> {
+  static constexpr uint32_t kNone = 0xfc00fc00u;
+  static __device__ float wide(__half x) { return __half2float(x); }
+  static __device__ float2 pair(const uint4& x, int i) {
+    const uint32_t w = word(x, i);
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
   }
   static __device__ float one(const __half* p) { return __half2float(*p); }
 };
-template <> struct Logits<__nv_bfloat16> {
-  static constexpr int n = 8;
-  static __device__ void unpack(const uint4& x, float (&v)[8]) {
-    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(u[i] << 16), v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+template <> struct Logits<__nv_bfloat16> : Logits16<__nv_bfloat16, __nv_bfloat162> {
+  static constexpr uint32_t kNone = 0xff80ff80u;
+  static __device__ float wide(__nv_bfloat16 x) { return __bfloat162float(x); }
+  static __device__ float2 pair(const uint4& x, int i) {
+    const uint32_t w = word(x, i);
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   }
   static __device__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 };
+
+__device__ __forceinline__ float rcp_ftz(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // c = log2(e) / t in two floats, hi < c.
 struct Heat {
@@ -80,6 +125,10 @@ __device__ __forceinline__ Heat heat_of(const VerifyArgs& a, int b) {
 __device__ __forceinline__ float exponent(const Heat& c, float z, float m) {
   const float d = z - m;
   return fmaf(d, c.hi, d * c.lo);
+}
+__device__ __forceinline__ float2 exponents(const Heat& c, float2 z, float m) {
+  const float2 d = add2(z, make_float2(-m, -m));
+  return fma2(d, make_float2(c.hi, c.hi), mul2(d, make_float2(c.lo, c.lo)));
 }
 // The sum of 2^(c (z - max)) over some values; max -inf: none of them is above that.
 struct Share {
@@ -143,66 +192,92 @@ __device__ __forceinline__ Rows rows_of(const VerifyArgs& a, int b) {
   return r;
 }
 
-// Vectors of 16 bytes from the first boundary on, single values before and after.
-template <class T, class Vec, class One>
-__device__ __forceinline__ void for_logits(const T* z, int from, int to, Vec vec, One one) {
-  constexpr int n = Logits<T>::n, U = 4;
-  const int tid = threadIdx.x, off = static_cast<int>(reinterpret_cast<uintptr_t>(z + from) & 15) / static_cast<int>(sizeof(T));
-  const int head = min((n - off) % n, to - from), vecs = (to - from - head) / n, tail = from + head + vecs * n;
-  const uint4* p = reinterpret_cast<const uint4*>(z + from + head);
-  for (int i = tid; i < vecs; i += U * kVThreads) {
-    uint4 x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * kVThreads < vecs) x[u] = p[i + u * kVThreads];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * kVThreads < vecs) vec(x[u], from + head + (i + u * kVThreads) * n);
+// Values [from, to) of a row for a warp: vectors of 16 bytes from the first boundary on, U of a lane
+// at a time, and up to n - 1 single ones before and after.
+template <class T, int U>
+struct Span {
+  static constexpr int n = Logits<T>::n;
+  const uint4* p;
+  const T* z;
+  int from, to, head, vecs;
+  __device__ Span(const T* row, int from, int to) : z(row), from(from), to(to) {
+    const int past = static_cast<int>(reinterpret_cast<uintptr_t>(row + from) & 15) / static_cast<int>(sizeof(T));
+    head = min((n - past) % n, to - from);
+    vecs = (to - from - head) / n;
+    p = reinterpret_cast<const uint4*>(row + from + head);
   }
-  if (tid < head) one(Logits<T>::one(z + from + tid), from + tid);
-  if (tid < to - tail) one(Logits<T>::one(z + tail + tid), tail + tid);
-}
+  __device__ void load(uint4 (&x)[U], int i) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      constexpr uint32_t none = Logits<T>::kNone;
+      x[u] = make_uint4(none, none, none, none);
+      if (i + u * 32 < vecs) x[u] = p[i + u * 32];
+    }
+  }
+  __device__ int index(int i, int u) const { return from + head + (i + u * 32) * n; }  // of a vector's first value
+  template <class One>
+  __device__ void single(One one) const {
+    const int tail = from + head + vecs * n, i = threadIdx.x & 31;
+    if (i < head) one(Logits<T>::one(z + from + i), from + i);
+    if (i < to - tail) one(Logits<T>::one(z + tail + i), tail + i);
+  }
+};
 
+// A warp takes a share of a row.
 template <class T>
-__global__ void __launch_bounds__(kVThreads) verify_rows_kernel(const __grid_constant__ VerifyArgs a) {
-  __shared__ unsigned long long sm[kVWarps];
-  __shared__ int sm_request;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+__global__ void __launch_bounds__(kVThreads, kVerifyWarps / kVWarps) verify_rows_kernel(const __grid_constant__ VerifyArgs a) {
+  const int lane = threadIdx.x & 31, unit = blockIdx.x * kVWarps + (threadIdx.x >> 5);
+  const int row = unit / a.splits, split = unit - row * a.splits;
   pdl_launch_dependents();
   pdl_wait();
-  if (warp == 0) {
-    const int b = request_of(a, row);
-    if (lane == 0) sm_request = b;
-  }
-  __syncthreads();
-  const int b = sm_request;
+  if (row >= a.rows) return;
+  const T* z = static_cast<const T*>(a.logits) + row * a.logits_row;
+  const int v0 = split * a.split_len, v1 = min(v0 + a.split_len, a.vocab);
+  constexpr int U = 4;
+  const Span<T, U> span(z, v0, v1);
+  // (vectors, the draft, its logit and its numbers are on their way while the row's request is looked for)
+  uint4 x[U];
+  int i = lane;
+  const int draft = row + 1 < a.rows ? a.tokens[row + 1] : -1;
+  const float u = a.race != nullptr ? a.uniforms[row] : 0.f;
+  span.load(x, i);
+  const bool known = static_cast<unsigned>(draft) < static_cast<unsigned>(a.vocab);
+  const float zx = known ? Logits<T>::one(z + draft) : 0.f;
+  const float qx = known && a.draft_probs != nullptr ? a.draft_probs[row * a.probs_row + draft] : 1.f;
+  const int b = request_of(a, row);
+  const Heat c = b >= 0 ? heat_of(a, b) : Heat{0.f, 0.f, kNothing};
   const Rows r = b >= 0 ? rows_of(a, b) : Rows{0, 0, false};
   if (!r.live) {
-    if (b >= 0 && row < r.end && split == 0 && tid == 0 && a.target_probs != nullptr) a.target_probs[row] = 0.f;
+    if (b >= 0 && row < r.end && split == 0 && lane == 0 && a.target_probs != nullptr) a.target_probs[row] = 0.f;
     return;
   }
   if (row >= r.end) return;  // behind the last request
-  const Heat c = heat_of(a, b);
-  const T* z = static_cast<const T*>(a.logits) + row * a.logits_row;
-  const int v0 = split * a.split_len, v1 = min(v0 + a.split_len, a.vocab);
-  constexpr int n = Logits<T>::n;
-  const bool greedy = c.kind == kGreedy;
+  const bool greedy = c.kind == kGreedy, drafted = known && row + 1 < r.end;
   unsigned long long mine;
   if (greedy) {
     float top = -INFINITY;
     int at = a.vocab;
     bool bad = false;
-    auto take = [&](float x, int i) {
-      bad |= x != x;
-      if (x > top || (x == top && i < at)) top = x, at = i;
-    };
-    for_logits<T>(z, v0, v1, [&](const uint4& raw, int i) {
-      float x[n];
-      Logits<T>::unpack(raw, x);
+    for (; i - lane < span.vecs; i += U * 32, span.load(x, i)) {
+      const float m = Logits<T>::template top<true>(x);
+      bad |= m != m;
+      if (m > top) {
+        top = m;
+        at = a.vocab;
 #pragma unroll
-      for (int j = 0; j < n; ++j) take(x[j], i + j);
-    }, take);
+        for (int u = U - 1; u >= 0; --u)
+#pragma unroll
+          for (int j = Logits<T>::n / 2 - 1; j >= 0; --j) {
+            const float2 v = Logits<T>::pair(x[u], j);
+            if (v.y == m) at = span.index(i, u) + 2 * j + 1;
+            if (v.x == m) at = span.index(i, u) + 2 * j;
+          }
+      }
+    }
+    span.single([&](float v, int k) {
+      bad |= v != v;
+      if (v > top || (v == top && k < at)) top = v, at = k;
+    });
     mine = warp_largest(bad ? kBadKey : key_of(top, at));
   } else {
     Share s{-INFINITY, 0.f};
@@ -212,31 +287,37 @@ __global__ void __launch_bounds__(kVThreads) verify_rows_kernel(const __grid_con
       s.max = top;
     };
     auto base = [&] { return s.max == -INFINITY ? 0.f : s.max; };
-    if (c.kind == 0)
-      for_logits<T>(z, v0, v1, [&](const uint4& raw, int) {
-        float x[n];
-        Logits<T>::unpack(raw, x);
-        float top = x[0];
-#pragma unroll
-        for (int j = 1; j < n; ++j) top = fmaxf(top, x[j]);
-        raise(top);
+    if (c.kind == 0) {
+      auto add = [&](const uint4 (&x)[U]) {
+        raise(Logits<T>::template top<false>(x));
         const float m = base();
-        float t[2] = {0.f, 0.f};
+        float2 t[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int j = 0; j < n; ++j) t[j & 1] += ex2_ftz(exponent(c, x[j], m));
-        s.sum += t[0] + t[1];
-      }, [&](float x, int) {
-        raise(x);
-        s.sum += ex2_ftz(exponent(c, x, base()));
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int j = 0; j < Logits<T>::n / 2; ++j) {
+            const float2 e = exponents(c, Logits<T>::pair(x[u], j), m);
+            t[j & 1] = add2(t[j & 1], make_float2(ex2_ftz(e.x), ex2_ftz(e.y)));
+          }
+        s.sum += (t[0].x + t[0].y) + (t[1].x + t[1].y);
+      };
+      // (the next vectors are on their way meanwhile)
+      uint4 y[U];
+      for (; i - lane < span.vecs; i += 2 * U * 32) {
+        span.load(y, i + U * 32);
+        add(x);
+        span.load(x, i + 2 * U * 32);
+        add(y);
+      }
+      span.single([&](float v, int) {
+        raise(v);
+        s.sum += ex2_ftz(exponent(c, v, base()));
       });
+    }
     mine = pack(warp_plus(c, s));
   }
-  if (lane == 0) sm[warp] = mine;
-  __syncthreads();
-  if (warp != 0) return;
   auto join = [&](unsigned long long x) { return greedy ? warp_largest(x) : pack(warp_plus(c, unpack(x))); };
   const unsigned long long none = greedy ? 0ull : pack(Share{-INFINITY, 0.f});
-  mine = join(lane < kVWarps ? sm[lane] : none);
   if (a.splits > 1) {
     int last = 0;
     if (lane == 0) {
@@ -257,9 +338,7 @@ __global__ void __launch_bounds__(kVThreads) verify_rows_kernel(const __grid_con
   }
   if (lane != 0) return;
   // the row's verdict
-  VerifyRow f{0.f, 0.f, c.kind, -1};
-  const int draft = row + 1 < r.end ? a.tokens[row + 1] : -1;
-  const bool drafted = static_cast<unsigned>(draft) < static_cast<unsigned>(a.vocab);
+  VerifyRow f{0.f, 0.f, c.kind, drafted ? draft : -1};
   float p = 0.f;
   if (greedy) {
     f.top = index_of(mine);
@@ -271,58 +350,142 @@ __global__ void __launch_bounds__(kVThreads) verify_rows_kernel(const __grid_con
     if (!(s.sum > 0.f && s.sum < INFINITY)) {
       f.verdict = kNothing;
     } else if (drafted) {
-      const double d = static_cast<double>(Logits<T>::one(z + draft)) - s.max;
-      const double px = exp2(d * c.hi + d * c.lo) / s.sum;
-      const float q = a.draft_probs != nullptr ? a.draft_probs[row * a.probs_row + draft] : 1.f;
-      if (static_cast<double>(a.uniforms[row]) * q < px) f.verdict |= kStands;
-      p = static_cast<float>(px);
+      // (difference and exponent in two floats, so that their rounding does not count)
+      const float d = zx - s.max, back = d - zx, rest = (zx - (d - back)) - (s.max + back), hi = d * c.hi;
+      const float lo = hi > -INFINITY ? fmaf(d, c.hi, -hi) + fmaf(rest, c.hi, d * c.lo) : 0.f;
+      p = exp2f(hi) * fmaf(lo, 0.693147180559945f, 1.f) / s.sum;
+      if (u * qx < p) f.verdict |= kStands;
     }
   }
   a.found[row] = f;
   if (a.target_probs != nullptr) a.target_probs[row] = p;
 }
 
-// The race over values [from, to) of a row: the largest w / e and its index.
-template <class T>
-__device__ __forceinline__ unsigned long long race(const Heat& c, const VerifyRow& f, const T* z, const float* e, const float* q,
-                                                   int skip, int from, int to) {
-  const float inv = 1.f / f.sum;
-  float best = 0.f;
-  int at = 0;
-  auto take = [&](float x, float ev, float qv, int v) {
-    const float w = fmaf(ex2_ftz(exponent(c, x, f.max)), inv, -qv), ratio = __fdividef(w, ev);
-    if (ratio > best && v != skip) best = ratio, at = v;
+// The race over values [from, to) of a row, by a warp: the largest w / e and its index.  Where rows
+// begin on boundaries of 16 bytes, in vectors, of which a lane keeps the largest ratio and the
+// vector's place; which of the vector's values it was is found at the end.  (A branch for every
+// value that is larger than those before took half the time: a warp has a hundred of them.)
+template <class T, bool PROBS>
+struct Race {
+  static constexpr int n = Logits<T>::n;
+  const Heat& c;
+  const VerifyRow& f;
+  const T* z;
+  const float *e, *q;
+  int skip;
+  float inv;
+  __device__ Race(const Heat& c, const VerifyRow& f, const T* z, const float* e, const float* q, int skip)
+      : c(c), f(f), z(z), e(e), q(q), skip(skip), inv(PROBS ? 1.f / f.sum : 1.f) {}  // (a common factor does not matter)
+  struct Piece {
+    uint4 x;
+    float4 e[n / 4], q[PROBS ? n / 4 : 1];
   };
-  constexpr int U = 8;
-  for (int v = from + static_cast<int>(threadIdx.x); v < to; v += U * kVThreads) {
-    float x[U], ev[U], qv[U];
+  __device__ float ratio(float power, float ev, float qv) const {
+    return (PROBS ? fmaf(power, inv, -qv) : power) * rcp_ftz(ev);
+  }
+  __device__ void load(Piece& p, int v, int end) const {
+    if (v >= end) return;
+    p.x = *reinterpret_cast<const uint4*>(z + v);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = v + u * kVThreads;
-      x[u] = -INFINITY, ev[u] = 1.f, qv[u] = 0.f;
-      if (i < to) {
-        x[u] = Logits<T>::one(z + i), ev[u] = e[i];
-        if (q != nullptr) qv[u] = q[i];
+    for (int k = 0; k < n / 4; ++k) {
+      p.e[k] = *reinterpret_cast<const float4*>(e + v + 4 * k);
+      if (PROBS) p.q[k] = *reinterpret_cast<const float4*>(q + v + 4 * k);
+    }
+  }
+  __device__ void ratios(const Piece& p, int v, float (&r)[n]) const {
+#pragma unroll
+    for (int k = 0; k < n / 4; ++k) {
+      const float2 a = exponents(c, Logits<T>::pair(p.x, 2 * k), f.max), b = exponents(c, Logits<T>::pair(p.x, 2 * k + 1), f.max);
+      const float4 qv = PROBS ? p.q[k] : make_float4(0.f, 0.f, 0.f, 0.f);
+      r[4 * k] = ratio(ex2_ftz(a.x), p.e[k].x, qv.x);
+      r[4 * k + 1] = ratio(ex2_ftz(a.y), p.e[k].y, qv.y);
+      r[4 * k + 2] = ratio(ex2_ftz(b.x), p.e[k].z, qv.z);
+      r[4 * k + 3] = ratio(ex2_ftz(b.y), p.e[k].w, qv.w);
+    }
+    if (static_cast<unsigned>(skip - v) < static_cast<unsigned>(n)) {
+#pragma unroll
+      for (int j = 0; j < n; ++j)
+        if (j == skip - v) r[j] = 0.f;
+    }
+  }
+  __device__ unsigned long long run(int from, int to) const {
+    const int lane = threadIdx.x & 31;
+    float best = 0.f;
+    int at = 0, v = from;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(z + from) | reinterpret_cast<uintptr_t>(e + from) |
+                           (PROBS ? reinterpret_cast<uintptr_t>(q + from) : 0);
+    if ((bits & 15) == 0) {
+      const int whole = from + (to - from) / n * n;
+      auto take = [&](const Piece& p, int v) {
+        if (v >= whole) return;
+        float r[n];
+        ratios(p, v, r);
+        float m = fmaxf(r[0], r[1]);
+#pragma unroll
+        for (int j = 2; j < n; j += 2) m = fmaxf(m, fmaxf(r[j], r[j + 1]));
+        if (m > best) best = m, at = v;
+      };
+      // (the next piece is on its way meanwhile)
+      Piece p0, p1;
+      v = from + lane * n;
+      load(p0, v, whole);
+      for (; v < whole; v += 64 * n) {
+        load(p1, v + 32 * n, whole);
+        take(p0, v);
+        load(p0, v + 64 * n, whole);
+        take(p1, v + 32 * n);
+      }
+      if (best > 0.f) {
+        float r[n];
+        load(p0, at, whole);
+        ratios(p0, at, r);
+        int j = 0;
+#pragma unroll
+        for (int k = n - 1; k >= 0; --k)
+          if (r[k] == best) j = k;
+        at += j;
+      }
+      v = whole;
+    }
+    constexpr int S = 8;
+    for (v += lane; v < to; v += S * 32) {
+      float x[S], ev[S], qv[S];
+#pragma unroll
+      for (int u = 0; u < S; ++u) {
+        const int i = v + u * 32;
+        x[u] = -INFINITY, ev[u] = 1.f, qv[u] = 0.f;
+        if (i < to) {
+          x[u] = Logits<T>::one(z + i), ev[u] = e[i];
+          if (PROBS) qv[u] = q[i];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < S; ++u) {
+        const float r = ratio(ex2_ftz(exponent(c, x[u], f.max)), ev[u], qv[u]);
+        if (r > best && v + u * 32 != skip) best = r, at = v + u * 32;
       }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) take(x[u], ev[u], qv[u], v + u * kVThreads);
+    return warp_largest(best > 0.f ? key_of(best, at) : 0ull);
   }
-  return warp_largest(best > 0.f ? key_of(best, at) : 0ull);
-}
+};
 
+// A warp takes a part of a request's deciding row.
 template <class T>
-__global__ void __launch_bounds__(kVThreads) verify_draw_kernel(const __grid_constant__ VerifyArgs a) {
-  __shared__ unsigned long long sm[kVWarps];
-  __shared__ int sm_last, sm_none;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, b = blockIdx.y, part = blockIdx.x;
+__global__ void __launch_bounds__(kVThreads, kDrawWarps / kVWarps) verify_draw_kernel(const __grid_constant__ VerifyArgs a) {
+  const int lane = threadIdx.x & 31, unit = blockIdx.x * kVWarps + (threadIdx.x >> 5);
+  const int b = unit / a.parts, part = unit - b * a.parts;
+  const bool first = part == 0 && lane == 0;
   pdl_launch_dependents();
   pdl_wait();
+  if (b >= a.batch) return;
+  const Heat c = heat_of(a, b);
   const Rows r = rows_of(a, b);
   if (!r.live) {
-    if (part == 0 && tid == 0) a.accepted[b] = 0, a.next[b] = -1;
+    if (first) a.accepted[b] = 0, a.next[b] = -1;
     return;
   }
+  const int v0 = part * a.part_len, v1 = min(v0 + a.part_len, a.vocab);
+  const float* e = a.race + b * a.race_row;
   // the first row whose draft does not stand (the last row has none)
   int row = r.first;
   VerifyRow f;
@@ -339,65 +502,56 @@ __global__ void __launch_bounds__(kVThreads) verify_draw_kernel(const __grid_con
     break;
   }
   if (f.verdict & (kNothing | kGreedy)) {
-    if (part == 0 && tid == 0) a.accepted[b] = row - r.first + 1, a.next[b] = f.verdict & kNothing ? -1 : f.top;
+    if (first) a.accepted[b] = row - r.first + 1, a.next[b] = f.verdict & kNothing ? -1 : f.top;
     return;
   }
-  const Heat c = heat_of(a, b);
-  const int draft = row + 1 < r.end ? a.tokens[row + 1] : -1;
-  const bool drafted = static_cast<unsigned>(draft) < static_cast<unsigned>(a.vocab);
   const T* z = static_cast<const T*>(a.logits) + row * a.logits_row;
-  const float* e = a.race + b * a.race_row;
-  const float* q = drafted && a.draft_probs != nullptr ? a.draft_probs + row * a.probs_row : nullptr;
-  const int skip = drafted && a.draft_probs == nullptr ? draft : -1;
-  const int v0 = part * a.part_len, v1 = min(v0 + a.part_len, a.vocab);
-  auto whole = [&](unsigned long long k) {  // of all warps, in warp 0
-    __syncthreads();
-    if (lane == 0) sm[warp] = k;
-    __syncthreads();
-    return warp == 0 ? warp_largest(lane < kVWarps ? sm[lane] : 0ull) : 0ull;
-  };
-  unsigned long long best = whole(race<T>(c, f, z, e, q, skip, v0, v1));
+  // (f.top: the draft that fell, -1: none)
+  unsigned long long best =
+      f.top >= 0 && a.draft_probs != nullptr
+          ? Race<T, true>(c, f, z, e, a.draft_probs + row * a.probs_row, -1).run(v0, v1)
+          : Race<T, false>(c, f, z, e, nullptr, f.top).run(v0, v1);
   if (a.parts > 1) {
-    if (tid == 0) {
+    int last = 0;
+    if (lane == 0) {
       if (best != 0) atomicMax(a.best + b, best);
       __threadfence();
-      sm_last = atomicAdd(a.request_tickets + b, 1) == a.parts - 1;
-      __threadfence();
-      if (sm_last) {
+      last = atomicAdd(a.request_tickets + b, 1) == a.parts - 1;
+      if (last) {
+        __threadfence();
         best = atomicExch(a.best + b, 0ull);
         a.request_tickets[b] = 0;
       }
     }
-    __syncthreads();
-    if (!sm_last) return;
+    if (!__shfl_sync(~0u, last, 0)) return;
+    best = __shfl_sync(~0u, best, 0);
   }
-  if (tid == 0) sm_none = best == 0;
-  __syncthreads();
-  if (sm_none) best = whole(race<T>(c, f, z, e, nullptr, -1, 0, a.vocab));  // nothing is left beside q: from p itself
-  if (tid == 0) a.accepted[b] = row - r.first + 1, a.next[b] = best != 0 ? index_of(best) : -1;
+  if (best == 0) best = Race<T, false>(c, f, z, e, nullptr, -1).run(0, a.vocab);  // nothing is left beside q: from p itself
+  if (lane == 0) a.accepted[b] = row - r.first + 1, a.next[b] = best != 0 ? index_of(best) : -1;
 }
 
 template <class T>
 cudaError_t launch(const VerifyArgs& a, cudaStream_t s) {
+  auto ctas = [](int rows, int pieces) { return dim3((static_cast<long long>(rows) * pieces + kVWarps - 1) / kVWarps); };
   if (a.rows > 0) {
-    const cudaError_t e = launch_after(verify_rows_kernel<T>, dim3(a.rows * a.splits), kVThreads, 0, s, a);
+    const cudaError_t e = launch_after(verify_rows_kernel<T>, ctas(a.rows, a.splits), kVThreads, 0, s, a);
     if (e != cudaSuccess) return e;
   }
-  return launch_after(verify_draw_kernel<T>, dim3(a.parts, a.batch), kVThreads, 0, s, a);
+  return launch_after(verify_draw_kernel<T>, ctas(a.batch, a.parts), kVThreads, 0, s, a);
 }
 
 }  // namespace
 
 cudaError_t launch_verify(VerifyArgs a, int dtype, int sms, cudaStream_t s) {
-  // shares of a row (parts of a vocabulary): as many as give each SM 8 CTAs (4), of 2048 values at least
-  auto cut = [&](int rows, int per_sm, int& pieces, int& len) {
-    const int want = (per_sm * sms + rows - 1) / rows, most = (a.vocab + 2047) / 2048;
+  // shares of a row, parts of a vocabulary: as many as the warps that the GPU holds, of 1024 (512) values at least
+  auto cut = [&](int rows, int warps, int least, int& pieces, int& len) {
+    const int want = max(warps / rows, 1), most = (a.vocab + least - 1) / least;
     pieces = want < most ? want : most;
     len = ((a.vocab + pieces - 1) / pieces + 7) & ~7;
     pieces = (a.vocab + len - 1) / len;
   };
-  cut(max(a.rows, 1), 8, a.splits, a.split_len);
-  cut(a.batch, 4, a.parts, a.part_len);
+  cut(max(a.rows, 1), kVerifyWarps * sms, 1024, a.splits, a.split_len);
+  cut(a.batch, kDrawWarps * sms, 512, a.parts, a.part_len);
   if (dtype == CLLM_F32) return launch<float>(a, s);
   if (dtype == CLLM_BF16) return launch<__nv_bfloat16>(a, s);
   return launch<__half>(a, s);

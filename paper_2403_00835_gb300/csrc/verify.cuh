@@ -10,7 +10,7 @@ namespace cllm {
 // What the first kernel finds of a row: its largest logit and sum; of a greedy row the token.
 struct alignas(16) VerifyRow {
   float max, sum;
-  int verdict, top;  // kStands | kNothing | kGreedy
+  int verdict, top;  // kStands | kNothing | kGreedy; else top is the draft, -1: none
 };
 constexpr int kStands = 1, kNothing = 2, kGreedy = 4;
 
@@ -33,7 +33,7 @@ struct VerifyArgs {
   int* request_tickets;
 };
 
-constexpr int kVerifyShares = 2048;  // shares beyond one a row
+constexpr int kVerifyWarps = 32;  // of the first kernel on an SM: shares of rows, beyond one a row
 cudaError_t launch_verify(VerifyArgs a, int dtype, int sms, cudaStream_t s);
 
 }  // namespace cllm

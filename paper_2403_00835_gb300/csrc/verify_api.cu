@@ -43,12 +43,12 @@ extern "C" int cllm_verifier_create(int max_rows, int max_batch, cllm_verifier**
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return cuda_fail(e, "verifier_create");
-  if (major != 10 || minor != 3 || 8 * sms > kVerifyShares) return CLLM_EUNSUPPORTED;
+  if (major != 10 || minor != 3) return CLLM_EUNSUPPORTED;
   cllm_verifier* v = new (std::nothrow) cllm_verifier;
   if (!v) return CLLM_ENOMEM;
   v->max_rows = max_rows, v->max_batch = max_batch, v->dev = dev, v->sms = sms;
   const size_t rows = max_rows, batch = max_batch;
-  const size_t found = rows * sizeof(VerifyRow), shares = (rows + kVerifyShares) * 8, best = batch * 8;
+  const size_t found = rows * sizeof(VerifyRow), shares = (rows + static_cast<size_t>(kVerifyWarps) * sms) * 8, best = batch * 8;
   const size_t counters = (rows + batch) * 4;
   if (lib_malloc(&v->scratch, found + shares + best + counters) != cudaSuccess) {
     v->scratch = nullptr;
