@@ -180,12 +180,11 @@ __device__ __forceinline__ void run_few(FewSmem<HD>& s, const PagedAttnArgs& a, 
         }
         warp_wait(&s.full[vt], v_phase);
         if (some) {
-          if (!keys.all(kb, kb + KEYS)) {
-            // keys that no row of the tile sees (not loaded, or what the page held before): p
-            // is 0 there, and so is V
+          if (kb + KEYS > keys.hi) {
+            // keys behind the tile's last (what the page held before): p is 0 there, and so is V
             for (int c = lane; c < KEYS * HD / 8; c += 32) {
               const int k = c / (HD / 8);
-              if (!keys.has(kb + k))
+              if (kb + k >= keys.hi)
                 *reinterpret_cast<uint4*>(s.ring[vt] + (c % (HD / 8) >> 3) * kFewKeys * 128 + (warp * KEYS + k) * 128 +
                                           (c & 7) * 16) = make_uint4(0, 0, 0, 0);
             }

@@ -19,7 +19,7 @@
 // 0 for the others, and the bands' O are summed with the slots'.  Rows are tokens times
 // the query heads of a key/value head, so grouped heads read K and V once.
 //
-// Bound: for long tiles no unit by itself (2048 tokens after 4096, 32 heads: 164 us, 1.05
+// Bound: for long tiles no unit by itself (2048 tokens after 4096, 32 heads: 159 us, 1.08
 // PFLOP/s; a chunk of 2 x 128 rows x 128 keys takes 3850 cycles, 2048 of them the MMAs' at their
 // full rate; counters: tensor pipe 41 % of the cycles, the exponentials' pipe 21 %, issue slots 35 %)
 // but the row warps' dependent steps from S to P, which the other slot's MMAs hide in part; HBM for
@@ -113,8 +113,10 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD, NB>& s, uint32_t tmem, int
       if (same(p.end)) break;
       const int n = same(p.chunks);
       const bool two = same(p.two);
-      const SlotChunks c0{same(p.c[0].first), same(p.c[0].end), two ? 1 : 2},
-          c1{same(p.c[1].first), same(p.c[1].end), two ? 1 : 2};
+      auto chunks_of = [&](const SlotChunks& c) {
+        return SlotChunks{same(c.first), same(c.end), two ? same(c.hole) : -1, same(c.resume)};
+      };
+      const SlotChunks c0 = chunks_of(p.c[0]), c1 = chunks_of(p.c[1]);
       __syncwarp();
       if (lane == 0) mbar_arrive(&s.pfree[pat.i]);
       if (n == 0) continue;
@@ -150,7 +152,7 @@ __device__ __forceinline__ void issue_mmas(TcSmem<HD, NB>& s, uint32_t tmem, int
             tc_mma_f16_ts_warp(tmem + t * 256 + 128, tmem + t * 256 + kk * 8, desc(va + (kk * 16 * 128 >> 4), v_hi), id_o,
                                kk > 0 ? 1u : first);
         }
-        if (i + c.step >= c.end) tc_commit_warp(&s.ofull[t]);
+        if (c.next(i) >= c.end) tc_commit_warp(&s.ofull[t]);
       };
       wait(&s.qfull, pieces & 1);
       const uint32_t k0 = next_tile();
@@ -241,22 +243,21 @@ __device__ __forceinline__ void run_rows(TcSmem<HD, NB>& s, const PagedAttnArgs&
     const bool band = row - lane < rows;  // some row of the warp is live
     float m = -INFINITY, l = 0.f;
     if (n > 0) {
-      const int first = p.c[t].first, end = p.c[t].end, step = p.c[t].step;
-      const TileKeys keys = p.keys;
+      const SlotChunks todo = p.c[t];
+      const int first = todo.first, end = todo.end, hi = p.keys.hi;
       RowKeys rk = row_keys(a, p.n, p.len, p.row0, tok);
       const int all_to = rk.bits != nullptr ? rk.ctx : rk.hi;  // every key from rk.lo to here is seen
-      for (int i = first; i < end; i += step) {
+      for (int i = first; i < end; i = todo.next(i)) {
         const int kb = p.chunk(i) * kTcChunk;
         warp_wait(&s.sfull[t], ns++ & 1);
-        if (!keys.all(kb, kb + kTcChunk)) {
-          // keys of the chunk that no row of the tile sees (not loaded, or what the
-          // page held before): p is 0 there, and so is V
+        if (kb + kTcChunk > hi) {
+          // keys behind the tile's last (what the page held before): p is 0 there, and so is V
           const int v = r + ring_v(i, n);
           warp_wait(&s.full[v % NR], (v / NR) & 1);
           // (16 bytes each, 64 columns of the keys after another)
           for (int c = at; c < kTcChunk * HD / 8; c += kTcRows) {
             const int key = c >> 3 & (kTcChunk - 1);
-            if (!keys.has(kb + key)) *reinterpret_cast<uint4*>(s.ring[v % NR] + c * 16) = make_uint4(0, 0, 0, 0);
+            if (kb + key >= hi) *reinterpret_cast<uint4*>(s.ring[v % NR] + c * 16) = make_uint4(0, 0, 0, 0);
           }
           fence_proxy_async_smem();
         }
@@ -296,39 +297,40 @@ __device__ __forceinline__ void run_rows(TcSmem<HD, NB>& s, const PagedAttnArgs&
           cm = fmaxf(m2[0], m2[1]) * a.scale_log2;
         }
         if (NB == 1 && band) {
+          float m2[2] = {-INFINITY, -INFINITY};
+          auto largest = [&](const uint32_t (&v)[32]) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+#pragma unroll
+              for (int u = 0; u < 2; ++u)
+                m2[u] = fmaxf(m2[u], fmaxf(__uint_as_float(v[j + 2 * u]), __uint_as_float(v[j + 2 * u + 1])));
+          };
+          tmem_ld32_start(mine, x[0]);
           if (__any_sync(0xffffffffu, rk.lo > kb || kb + kTcChunk > all_to)) {
             // some row does not see every key: what it does not see becomes -inf
             rk = row_keys(a, p.n, p.len, p.row0, tok);
 #pragma unroll 1
             for (int c = 0; c < kTcChunk; c += 32) {
-              tmem_ld32_start(mine + c, x[0]);
               const uint32_t see = key_bits(rk, kb + c);
               tmem_wait32(x[0]);
 #pragma unroll
               for (int j = 0; j < 32; ++j)
                 if (!(see >> j & 1)) x[0][j] = 0xff800000u;
               tmem_st32(mine + c, x[0]);
+              largest(x[0]);
+              if (c + 32 == kTcChunk) tmem_st_wait();
+              tmem_ld32_start(mine + (c + 32 & 127), x[0]);
             }
-            tmem_st_wait();
-          }
-          float m2[2] = {-INFINITY, -INFINITY};
-          tmem_ld32_start(mine, x[0]);
+          } else {
 #pragma unroll 1
-          for (int c = 0; c < kTcChunk; c += 64) {
-            tmem_wait32(x[0]);
-            tmem_ld32_start(mine + c + 32, x[1]);
-#pragma unroll
-            for (int j = 0; j < 32; j += 4)
-#pragma unroll
-              for (int u = 0; u < 2; ++u)
-                m2[u] = fmaxf(m2[u], fmaxf(__uint_as_float(x[0][j + 2 * u]), __uint_as_float(x[0][j + 2 * u + 1])));
-            tmem_wait32(x[1]);
-            tmem_ld32_start(mine + (c + 64 & 127), x[0]);  // (at the end: the first columns again, for the next loop)
-#pragma unroll
-            for (int j = 0; j < 32; j += 4)
-#pragma unroll
-              for (int u = 0; u < 2; ++u)
-                m2[u] = fmaxf(m2[u], fmaxf(__uint_as_float(x[1][j + 2 * u]), __uint_as_float(x[1][j + 2 * u + 1])));
+            for (int c = 0; c < kTcChunk; c += 64) {
+              tmem_wait32(x[0]);
+              tmem_ld32_start(mine + c + 32, x[1]);
+              largest(x[0]);
+              tmem_wait32(x[1]);
+              tmem_ld32_start(mine + (c + 64 & 127), x[0]);  // (at the end: the first columns again, for the next loop)
+              largest(x[1]);
+            }
           }
           cm = fmaxf(m2[0], m2[1]) * a.scale_log2;
         }
@@ -633,7 +635,7 @@ template <class T, int HD, int NB>
 cudaError_t launch_tc(const PagedMaps& m, const PagedAttnArgs& a, int hold, int grid, cudaStream_t s) {
   const int tt = kTcRows / NB / a.group;
   // Tiles of 256 rows read K and V once for twice the rows (2048 tokens after 4096, 32
-  // heads: 165 us, 170 with tiles of 128); with fewer of them than CTAs their keys
+  // heads: 159 us, 162 with tiles of 128; with a window of 1024 57.7 and 63); with fewer of them than CTAs their keys
   // would have to be cut and their rows merged, so they are halved instead (4 requests of 61
   // tokens, 32 heads on 8, 700 to 1100 keys: 17.6 us, 34 with tiles of 256).
   const long long per_request = (static_cast<long long>(a.rows) + a.batch - 1) / a.batch;

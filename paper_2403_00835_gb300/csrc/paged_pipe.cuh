@@ -15,24 +15,26 @@ namespace cllm {
 // then reach 2^8, and O is rarely rescaled.
 constexpr float kPageSlack = 8.f;
 
-// The chunks of a piece that a slot works on: first, first + step, .. < end
-// (relative to the piece).
+// The chunks of a piece that a slot works on (relative to the piece): first .. end - 1 without [hole,
+// resume), which first keys have before them (hole 0: none left out), or every other one (hole -1).
 struct SlotChunks {
-  int first, end, step;
+  int first, end, hole, resume;
   __device__ bool any() const { return first < end; }
-  __device__ bool has(int i) const { return i >= first && i < end && (step == 1 || ((i - first) & 1) == 0); }
+  __device__ bool has(int i) const {
+    return i >= first && i < end && (hole < 0 ? ((i - first) & 1) == 0 : i < hole || i >= resume);
+  }
+  __device__ int next(int i) const { return hole < 0 ? i + 2 : i + 1 == hole ? resume : i + 1; }
 };
 
 // A piece as the loading warp hands it to the others.
 struct PagePiece {
-  int b, h, t0, nt, n, len, row0;          // as in Piece
+  int b, h, t0, n, len, row0;              // as in Piece
   TileKeys keys;
   int near, gap;
   int ca, chunks;                          // first chunk and number of chunks (0: no keys)
-  int two, whole;                          // 128 rows in each slot; the whole tile
+  short nt, two, whole, end;               // tokens; 128 rows in each slot; the whole tile; no piece: the run is over
   int slot, cta0, cta1, first_slot;        // of a cut tile: this part's slot, the CTAs of its parts, the first's slot
   SlotChunks c[2];
-  int end;                                 // no piece: the run is over
   __device__ int chunk(int i) const { return ca + i - (ca + i < near ? gap : 0); }  // where in the request its i-th is
   __device__ int part(int cta) const { return cta == cta0 ? first_slot : 2 * cta; }
 };
@@ -103,7 +105,10 @@ template <> struct Pack16<__nv_bfloat16> {
 // values.
 // S::kShift: log2 of the keys of a tile; S::kAhead: K one tile ahead of V (K0 K1 V0 K2 V1
 // ..), else K0 V0 K1 V1 ..; S::kIssuer: a warp beside the row warps takes the pieces too;
-// S::kBands: copies of a tile's queries.  hold: test hook, 1 + the chunk of a
+// S::kBands: copies of a tile's queries.  Of K the pages that hold keys of the tile are loaded; V's other
+// places get zeros (a page outside the map), since p = 0 times what was there may not be 0.  Keys
+// in the loaded pages that no row sees, before hi, are the request's own: where one of them is not
+// finite, the row is done again.  hold: test hook, 1 + the chunk of a
 // piece at which this warp gives up (0: none).
 template <int HD, class S>
 __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const PagedGeom& g, const PagedMaps& m,
@@ -149,14 +154,18 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
           }
           for (int t = 0; t < 2; ++t) {
             if (!o.two) {
-              o.c[t] = {t, o.chunks, 2};
-            } else {
-              const int t0 = p.t0 + t * tt;
-              const TileKeys k = tile_keys(a, p.n, p.len, t0, min(p.t0 + p.nt, t0 + tt));
-              // (a slot's chunks are a run: with first keys in the piece it begins there)
-              const bool sinks = p.chunk(p.ca) * kChunk < k.sink;
-              o.c[t] = {sinks ? 0 : max(0, k.lo / kChunk - p.ca), min(o.chunks, (k.hi + kChunk - 1) / kChunk - p.ca), 1};
+              o.c[t] = {t, o.chunks, -1, 0};
+              continue;
             }
+            const int t0 = p.t0 + t * tt;
+            const TileKeys k = tile_keys(a, p.n, p.len, t0, min(p.t0 + p.nt, t0 + tt));
+            // the piece's chunks of first keys, and where the slot's window begins after them
+            const int sinks = min(max(p.tca + (k.sink + kChunk - 1) / kChunk - p.ca, 0), o.chunks);
+            const int from = max(k.lo / kChunk - p.ca, sinks);
+            int end = min(o.chunks, (k.hi + kChunk - 1) / kChunk - p.ca);
+            const bool hole = sinks > 0 && from > sinks && from < end;
+            if (sinks > 0 && from >= end) end = min(end, sinks);
+            o.c[t] = {sinks > 0 ? 0 : from, end, hole ? sinks : 0, hole ? from : 0};
           }
         }
         mbar_arrive(&s.pfull[pat.i]);
@@ -179,12 +188,13 @@ __device__ __forceinline__ void issue_loads(S& s, const PagedAttnArgs& a, const 
       const int kb = p.chunk(c) * kChunk, pos = kb + (j << box_shift);
       if (r >= NR) wait(&s.empty[at.i], at.phase ^ 1);
       if (!ok) return;
-      const bool mine = pos < kb + kChunk && p.keys.some(pos, pos + box);
+      const bool seen = p.keys.some(pos, pos + box), mine = pos < kb + kChunk && (seen || map == &m.v);
       const int boxes = __popc(__ballot_sync(0xffffffffu, mine));  // (of 64 columns)
       if (lane == 0) mbar_arrive_expect_tx(&s.full[at.i], boxes * box * 128);
       __syncwarp();
       if (mine) {
-        if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
+        if (!seen) page = a.n_pages;
+        else if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
           atomicOr(a.err, DERR_CAPACITY);
           page = a.n_pages;  // outside the map: reads as zeros
         }

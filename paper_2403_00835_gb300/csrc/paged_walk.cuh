@@ -54,9 +54,7 @@ __device__ __forceinline__ Request request(const PagedAttnArgs& a, int b) {
 struct TileKeys {
   int lo, hi, sink;  // keys [0, sink) and [lo, hi) that some row may see (hi <= lo: none; sink < lo, or 0)
   __device__ bool has(int key) const { return (key >= lo && key < hi) || key < sink; }
-  // of keys [a, b): whether one is such a key, and whether all are
-  __device__ bool some(int a, int b) const { return (a < hi && b > lo) || a < sink; }
-  __device__ bool all(int a, int b) const { return (a >= lo && b <= hi) || b <= sink; }
+  __device__ bool some(int a, int b) const { return (a < hi && b > lo) || a < sink; }  // of keys [a, b)
 };
 // Keys seen by tokens [t0, t1) of a request of n new tokens and `len` in all.
 __device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, int n, int len, int t0, int t1) {
