@@ -89,6 +89,19 @@ def load():
     return _lib
 
 
+_Tensor = torch.Tensor
+_INT_MAX = 2 ** 31 - 1
+
+
+def _vector(t, what: str, dtype, index: int, n: int) -> int:
+    """The address of n contiguous values or more on device `index`."""
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == index and t.is_contiguous():
+        if t.numel() >= n:
+            return t.data_ptr()
+        raise ValueError(f"{what}: fewer than {n}")
+    raise ValueError(f"{what}: need a contiguous {dtype} tensor on cuda:{index}")
+
+
 def _tensor(t, what: str, dtype, shape=None, index=None):
     """A contiguous CUDA tensor's address."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()):
@@ -234,6 +247,8 @@ def rope_table(positions: int, frequencies, amplitude: float = 1.0, first: int =
     """Rows first .. first + positions - 1 of a rotary table: amplitude * (cos, sin)(position * frequency), float32
     [positions][pairs][2] as ``PagedCache.append`` takes it (``cllm_rope_table``).  frequencies: radians
     a position (``rope_frequencies``, or any numbers).  out: the rows to fill (None: allocated on the stream of the call)."""
+    if not 0 <= first <= first + positions <= _INT_MAX:  # (ctypes would cut them to 32 bits)
+        raise ValueError("rope_table: need positions >= 0 and first >= 0, 2^31 - 1 at most together")
     f = frequencies if isinstance(frequencies, array) and frequencies.typecode == "d" else array("d", frequencies)
     pairs = len(f)
     if out is None:
@@ -289,20 +304,18 @@ class PagedCache:
         except Exception:
             pass
 
-    def _heads(self, t, what: str, rows: int, heads: int):
+    def _heads(self, t, what: str, shape):
         """Rows of heads side by side: (address, row stride)."""
-        hd = self.head_dim
-        if isinstance(t, torch.Tensor) and t.dtype is self.dtype and t.get_device() == self._dev and t.shape == (rows, heads, hd):
+        if isinstance(t, _Tensor) and t.dtype is self.dtype and t.get_device() == self._dev and t.shape == shape:
             row, head, one = t.stride()
-            if one == 1 and (head == hd or heads == 1):
+            if one == 1 and (head == shape[2] or shape[1] == 1):
                 return t.data_ptr(), row
-        raise ValueError(f"{what}: need [{rows}][{heads}][{hd}] {self.dtype} on {self.device}, heads side by side")
+        raise ValueError(f"{what}: need {list(shape)} {self.dtype} on {self.device}, heads side by side")
 
     def _gain(self, t, what: str) -> int:
-        if not (isinstance(t, torch.Tensor) and t.dtype is self.dtype and t.shape == (self.head_dim,) and t.is_contiguous()
-                and t.get_device() == self._dev):
-            raise ValueError(f"{what}: need a contiguous [{self.head_dim}] {self.dtype} tensor on {self.device}")
-        return t.data_ptr()
+        if isinstance(t, _Tensor) and t.shape == (self.head_dim,):
+            return _vector(t, what, self.dtype, self._dev, self.head_dim)
+        raise ValueError(f"{what}: need [{self.head_dim}]")
 
     def append(self, layer: int, k, v, slots, q=None, q_out=None, rope=None, positions=None, stream=None, *,
                q_norm=None, k_norm=None, eps: float = 1e-6, interleaved: bool = False):
@@ -312,24 +325,23 @@ class PagedCache:
         and so is q [T][n_heads][hd], into q_out (None: in place).  r: hd, or a smaller multiple of 16.
         q_norm, k_norm ([hd], of the cache's type): before that every head of q, of k is divided by the
         root of its mean square (+ eps) and multiplied by these gains."""
-        t = k.shape[0]
-        kp, ks = self._heads(k, "k", t, self.n_kv_heads)
-        vp, vs = self._heads(v, "v", t, self.n_kv_heads)
-        sp = _tensor(slots, "slots", torch.int64, None, self._dev)
-        if slots.numel() < t:
-            raise ValueError("slots: fewer than rows")
+        if not isinstance(k, _Tensor) or k.dim() != 3:
+            raise ValueError("k: need [rows][kv_heads][head_dim]")
+        t, dev, hd = k.shape[0], self._dev, self.head_dim
+        shape = t, self.n_kv_heads, hd
+        kp, ks = self._heads(k, "k", shape)
+        vp, vs = self._heads(v, "v", shape)
+        sp = _vector(slots, "slots", torch.int64, dev, t)
         qp = qs = op = os = rp = pp = max_pos = dims = qg = kg = 0
         if rope is not None:
-            if not (isinstance(rope, torch.Tensor) and rope.dim() == 3):
+            if not (isinstance(rope, _Tensor) and rope.dim() == 3):
                 raise ValueError("rope: need [max_pos][pairs][2]")
-            max_pos, pairs, _ = rope.shape
+            max_pos, pairs, two = rope.shape
             dims = 2 * pairs
-            if not 0 < dims <= self.head_dim:
-                raise ValueError(f"rope: rows of 1 to {self.head_dim // 2} pairs, got {pairs}")
-            rp = _tensor(rope, "rope", torch.float32, (max_pos, pairs, 2), self._dev)
-            pp = _tensor(positions, "positions", torch.int32, None, self._dev)
-            if positions.numel() < t:
-                raise ValueError("positions: fewer than rows")
+            if two != 2 or not 0 < dims <= hd:
+                raise ValueError(f"rope: need rows of 1 to {hd // 2} pairs, got {list(rope.shape)}")
+            rp = _vector(rope, "rope", torch.float32, dev, 0)
+            pp = _vector(positions, "positions", torch.int32, dev, t)
         elif interleaved:
             raise ValueError("interleaved pairs of what: pass rope")
         if q_norm is not None:
@@ -338,18 +350,19 @@ class PagedCache:
             qg = self._gain(q_norm, "q_norm")
         if k_norm is not None:
             kg = self._gain(k_norm, "k_norm")
-        whole = dims == self.head_dim and not interleaved and q_norm is None and k_norm is None
+        plain = not (qg or kg)
         if q is not None:
-            if rope is None and q_norm is None and k_norm is None:
+            if plain and rope is None:
                 raise ValueError("q is only rotated or normalised: pass rope or norms")
-            qp, qs = self._heads(q, "q", t, self.n_heads)
-            op, os = (qp, qs) if q_out is None else self._heads(q_out, "q_out", t, self.n_heads)
+            shape = t, self.n_heads, hd
+            qp, qs = self._heads(q, "q", shape)
+            op, os = (qp, qs) if q_out is None else self._heads(q_out, "q_out", shape)
         _ROWS_IN.pack_into(self._args, 0, layer, t, kp, vp, qp, op, ks, vs, qs, os, sp, rp, pp, max_pos)
-        if whole or (rope is None and q_norm is None and k_norm is None):
-            rc = self._lib.cllm_paged_append(self._h, self._argp, _stream(stream, self._dev))
+        if plain and (rope is None or (dims == hd and not interleaved)):
+            rc = self._lib.cllm_paged_append(self._h, self._argp, _stream(stream, dev))
         else:
             _HEADS.pack_into(self._args, _HEADS_AT, qg, kg, eps, dims, interleaved)
-            rc = self._lib.cllm_paged_append_heads(self._h, self._argp, self._argp + _HEADS_AT, _stream(stream, self._dev))
+            rc = self._lib.cllm_paged_append_heads(self._h, self._argp, self._argp + _HEADS_AT, _stream(stream, dev))
         if rc:
             _c._check(rc, "cllm_paged_append")
 
@@ -364,6 +377,8 @@ class PagedCache:
         block_mask: int32 [T][words], bit j of word w: the row sees new token 32 w + j of
         its request (None: causal), at least one word."""
         dev, dtype = self._dev, self.dtype
+        if sinks > _INT_MAX:  # (ctypes would cut it to 32 bits)
+            raise ValueError("sinks: at most 2^31 - 1")
         if out is None:
             # (from the memory of the stream that writes it: the current stream's may still be in use there)
             with nullcontext() if stream is None else torch.cuda.stream(stream):

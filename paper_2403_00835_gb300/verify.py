@@ -19,7 +19,7 @@ import torch
 
 from . import cllm as _c
 from . import paged as _paged
-from .paged import DTYPES, _stream, _tensor
+from .paged import _INT_MAX, DTYPES, _stream, _Tensor, _vector
 
 # Every function declared in include/cllm_verify.h.
 EXPORTS = ("cllm_verifier_create", "cllm_verifier_destroy", "cllm_verify")
@@ -54,6 +54,8 @@ class DraftVerifier:
         self.device = torch.device(device)
         if self.device.type != "cuda":
             raise ValueError("device: need a CUDA device")
+        if max(max_rows, max_batch) > _INT_MAX:  # (ctypes would cut them to 32 bits)
+            raise ValueError("max_rows, max_batch: at most 2^31 - 1")
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             self._dev = torch.cuda.current_device()
@@ -76,18 +78,12 @@ class DraftVerifier:
 
     def _rows(self, t, what: str, dtype, rows: int, vocab: int):
         """Rows of a vocabulary's values: (address, row stride)."""
-        if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == self._dev and t.dim() == 2:
+        if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == self._dev and t.dim() == 2:
             n, width = t.shape
             row, one = t.stride()
             if n >= rows and width == vocab and (one == 1 or vocab == 1):
                 return t.data_ptr(), row
         raise ValueError(f"{what}: need [{rows}][{vocab}] {dtype} on {self.device}, rows contiguous")
-
-    def _vector(self, t, what: str, dtype, n: int) -> int:
-        p = _tensor(t, what, dtype, None, self._dev)
-        if t.numel() < n:
-            raise ValueError(f"{what}: fewer than {n}")
-        return p
 
     def verify(self, logits, tokens, rows, uniforms=None, race=None, temperature=None, draft_probs=None, accepted=None,
                next_tokens=None, target_probs=None, stream=None):
@@ -100,25 +96,31 @@ class DraftVerifier:
         greedy).  draft_probs: float32 [T][vocab], row i the distribution that token i + 1 was
         drawn from (None: the drafts are certain).  accepted, next_tokens: outputs to fill (None: allocated on
         the stream of the call); target_probs: float32 [T] to fill with the target's probability of each row's draft."""
-        if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in DTYPES:
+        if not isinstance(logits, _Tensor) or logits.dim() != 2 or logits.dtype not in DTYPES:
             raise ValueError("logits: need a [rows][vocab] tensor of float32, bfloat16 or float16")
         t, vocab = logits.shape
-        b, dev = rows.batch, self._dev
+        b, dev, f32, i32 = rows.batch, self._dev, torch.float32, torch.int32
         if rows._dev != dev:
             raise ValueError("rows: on another device than the verifier")
         lp, ls = self._rows(logits, "logits", logits.dtype, t, vocab)
-        tp = self._vector(tokens, "tokens", torch.int32, t)
-        up = 0 if uniforms is None else self._vector(uniforms, "uniforms", torch.float32, t)
-        rp, rs = (0, 0) if race is None else self._rows(race, "race", torch.float32, b, vocab)
-        hp = 0 if temperature is None else self._vector(temperature, "temperature", torch.float32, b)
-        qp, qs = (0, 0) if draft_probs is None else self._rows(draft_probs, "draft_probs", torch.float32, t, vocab)
+        tp = _vector(tokens, "tokens", i32, dev, t)
+        up = rp = rs = hp = qp = qs = pp = 0
+        if uniforms is not None:
+            up = _vector(uniforms, "uniforms", f32, dev, t)
+        if race is not None:
+            rp, rs = self._rows(race, "race", f32, b, vocab)
+        if temperature is not None:
+            hp = _vector(temperature, "temperature", f32, dev, b)
+        if draft_probs is not None:
+            qp, qs = self._rows(draft_probs, "draft_probs", f32, t, vocab)
         if accepted is None or next_tokens is None:
             with nullcontext() if stream is None else torch.cuda.stream(stream):
-                accepted = torch.empty(b, dtype=torch.int32, device=self.device) if accepted is None else accepted
-                next_tokens = torch.empty(b, dtype=torch.int32, device=self.device) if next_tokens is None else next_tokens
-        ap = self._vector(accepted, "accepted", torch.int32, b)
-        np = self._vector(next_tokens, "next_tokens", torch.int32, b)
-        pp = 0 if target_probs is None else self._vector(target_probs, "target_probs", torch.float32, t)
+                accepted = torch.empty(b, dtype=i32, device=self.device) if accepted is None else accepted
+                next_tokens = torch.empty(b, dtype=i32, device=self.device) if next_tokens is None else next_tokens
+        ap = _vector(accepted, "accepted", i32, dev, b)
+        np = _vector(next_tokens, "next_tokens", i32, dev, b)
+        if target_probs is not None:
+            pp = _vector(target_probs, "target_probs", f32, dev, t)
         _ARGS.pack_into(self._args, 0, b, t, vocab, DTYPES[logits.dtype], lp, ls, tp, rows._start, rows._len, hp, up, rp, rs, qp,
                         qs, ap, np, pp)
         rc = self._lib.cllm_verify(self._h, self._argp, _stream(stream, dev))

@@ -93,8 +93,6 @@ def test_table_refusals():
     for a in ((4, [1.0, math.nan]), (4, [0.5] * 129), (4, [0.5, 2.0 ** 21])):
         with pytest.raises(cllm.CllmError):
             paged.rope_table(*a)
-    with pytest.raises(cllm.CllmError):
-        paged.rope_table(4, [1.0, 0.5], first=2 ** 31 - 3, out=out)
 
 
 # ---- writes ---------------------------------------------------------------------------------

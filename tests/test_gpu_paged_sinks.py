@@ -247,6 +247,8 @@ def test_refusals():
     for kw in (dict(sinks=-1, window=4), dict(sinks=-1), dict(sinks=4, window=-1)):
         with pytest.raises(cllm.CllmError):
             cache.attention(0, step.q, rows, tables, out=out, **kw)
+    with pytest.raises(ValueError, match="sinks"):
+        cache.attention(0, step.q, rows, tables, out=out, window=4, sinks=2 ** 32 + 4)
     assert bool((out == 5.0).all())
 
 

@@ -61,6 +61,13 @@ def test_a_host_table_is_refused():
         paged.rope_table(4, [1.0], out=torch.zeros(4, 1, 2))
 
 
+@pytest.mark.parametrize("positions,first", [(-1, 0), (2 ** 32 + 4, 0), (4, 2 ** 32), (4, -2), (4, 2 ** 31 - 3), (2 ** 31, 0)])
+def test_positions_past_31_bits_are_refused(positions, first):
+    """(Not cut to the bits that the library takes.)"""
+    with pytest.raises(ValueError, match="positions"):
+        paged.rope_table(positions, [1.0], first=first)
+
+
 def test_null_handles(lib):
     zeros = ctypes.create_string_buffer(256)
     at = ctypes.addressof(zeros)

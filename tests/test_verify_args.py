@@ -1,5 +1,7 @@
 """Draft verification's refusals that need no GPU, and the tests' own model of it on hand-worked steps."""
 import ctypes
+import os
+import re
 
 import numpy as np
 import pytest
@@ -9,6 +11,7 @@ from tests.test_abi import declared_functions
 from tests.verify_util import Model
 
 EINVAL = -1
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2403_00835_gb300", "csrc")
 
 
 @pytest.fixture(scope="module")
@@ -35,6 +38,21 @@ def test_null_verifiers(lib):
     assert lib.cllm_verify(None, ctypes.addressof(zeros), None) == EINVAL
     with pytest.raises(ValueError, match="device"):
         verify.DraftVerifier(4, 4, device="cpu")
+
+
+@pytest.mark.parametrize("rows,batch", [(2 ** 32 + 1, 1), (1, 2 ** 32 + 1)])
+def test_sizes_past_31_bits_are_refused(rows, batch):
+    with pytest.raises(ValueError, match="at most"):
+        verify.DraftVerifier(rows, batch)
+
+
+def test_kernels_wait_before_they_read_with_coherent_loads():
+    """They may start while the kernel before them is still writing what they read."""
+    with open(os.path.join(CSRC, "verify.cu")) as f:
+        code = re.sub(r"//[^\n]*", "", f.read())
+    assert not re.search(r"__ldg\b|__restrict|ld\.global\.(\w+\.)*nc\b", code)
+    kernels = code.split("__global__")[1:]
+    assert len(kernels) == 2 and all("pdl_wait();" in k for k in kernels)
 
 
 def test_the_packed_arguments_are_where_the_library_reads_them():
