@@ -8,10 +8,13 @@ from __future__ import annotations
 
 import concurrent.futures as cf
 import hashlib
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -19,6 +22,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libcllm.so")
+MARSHAL = os.path.join(OUT_DIR, "_marshal.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
@@ -46,7 +50,46 @@ def _fingerprint() -> str:
                 with open(p, "rb") as fh:
                     h.update(fh.read())
     h.update(" ".join(ARCH + NVCC_FLAGS).encode())
+    try:
+        h.update(importlib.metadata.version("torch").encode())
+    except importlib.metadata.PackageNotFoundError:
+        pass
     return h.hexdigest()
+
+
+def _build_marshal() -> None:
+    """csrc/marshal.cpp against this interpreter's Python and torch; a note and no file if that fails."""
+    if os.path.exists(MARSHAL):
+        os.remove(MARSHAL)
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        return
+    torch = spec.submodule_search_locations[0]
+    lib = os.path.join(torch, "lib")
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-isystem", os.path.join(torch, "include"),
+           "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.cpp"), "-o", tmp,
+           "-L" + lib, "-Wl,-rpath," + lib, "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        error = r.stderr[-500:] if r.returncode else ""
+    except OSError as e:
+        error = str(e)
+    if error:
+        print(f"_marshal.so not built, calls take their arguments in Python: {error}", file=sys.stderr)
+    else:
+        os.replace(tmp, MARSHAL)
+
+
+def load_marshal():
+    """The module in _build/_marshal.so, or None."""
+    if not os.path.exists(MARSHAL):
+        return None
+    spec = importlib.util.spec_from_file_location("_marshal", MARSHAL)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=None) -> str:
@@ -72,8 +115,10 @@ def build(force: bool = False, verbose: bool = False, extra_flags=None) -> str:
         return obj
 
     srcs = _sources()
-    with cf.ThreadPoolExecutor(max_workers=min(len(srcs), os.cpu_count() or 4)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(len(srcs) + 1, os.cpu_count() or 4)) as ex:
+        marshal = ex.submit(_build_marshal)
         objs = list(ex.map(compile_one, srcs))
+        marshal.result()
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc] + ARCH + ["-shared", "-o", tmp] + objs + ["-cudart", "static"]
     r = subprocess.run(cmd, capture_output=True, text=True)

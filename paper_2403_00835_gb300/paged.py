@@ -63,12 +63,17 @@ _HEADS = struct.Struct("@2Pf2i")
 _HEADS_AT = -(-_ROWS_IN.size // 8) * 8  # behind the rows, on a pointer's boundary
 _ATTN = struct.Struct("@3i3P4q3PifiPi")
 
+# What marshal.cpp keeps of a cache: the two calls, the handle, its type, device and heads.
+_CACHE = struct.Struct("@3P6i")
+
 _lib = None
+_marshal = None  # marshal.cpp's module, and the address of the call it makes
+_rope_call = 0
 
 
 def load():
     """The library with this header's signatures."""
-    global _lib
+    global _lib, _marshal, _rope_call
     if _lib is None:
         lib = _c.load()
         vp, i = ctypes.c_void_p, ctypes.c_int
@@ -85,6 +90,8 @@ def load():
         for name in EXPORTS:
             if name != "cllm_paged_destroy":
                 getattr(lib, name).restype = ctypes.c_int
+        _marshal = _c._build.load_marshal()
+        _rope_call = ctypes.cast(lib.cllm_rope_table, ctypes.c_void_p).value
         _lib = lib
     return _lib
 
@@ -247,6 +254,17 @@ def rope_table(positions: int, frequencies, amplitude: float = 1.0, first: int =
     """Rows first .. first + positions - 1 of a rotary table: amplitude * (cos, sin)(position * frequency), float32
     [positions][pairs][2] as ``PagedCache.append`` takes it (``cllm_rope_table``).  frequencies: radians
     a position (``rope_frequencies``, or any numbers).  out: the rows to fill (None: allocated on the stream of the call)."""
+    lib = _lib or load()
+    if _marshal is not None and isinstance(out, _Tensor) and out.is_cuda:
+        dev = _device()
+        # (another device's stream, like what else it does not take, is seen to below)
+        if stream is None or stream.device_index == dev:
+            rc = _marshal.rope_table(_rope_call, positions, frequencies, amplitude, first, out, dev,
+                                     _current(dev) if stream is None else stream.cuda_stream)
+            if rc is not None:
+                if rc:
+                    _c._check(rc, "cllm_rope_table")
+                return out
     if not 0 <= first <= first + positions <= _INT_MAX:  # (ctypes would cut them to 32 bits)
         raise ValueError("rope_table: need positions >= 0 and first >= 0, 2^31 - 1 at most together")
     f = frequencies if isinstance(frequencies, array) and frequencies.typecode == "d" else array("d", frequencies)
@@ -258,10 +276,10 @@ def rope_table(positions: int, frequencies, amplitude: float = 1.0, first: int =
     dev = out.get_device()
     args = ptr, first, positions, 2 * pairs, f.buffer_info()[0], amplitude, _stream(stream, dev)
     if _device() == dev:
-        rc = load().cllm_rope_table(*args)
+        rc = lib.cllm_rope_table(*args)
     else:
         with torch.cuda.device(dev):
-            rc = load().cllm_rope_table(*args)
+            rc = lib.cllm_rope_table(*args)
     if rc:
         _c._check(rc, "cllm_rope_table")
     return out
@@ -292,11 +310,14 @@ class PagedCache:
         self._args = ctypes.create_string_buffer(max(_HEADS_AT + _HEADS.size, _ATTN.size))
         self._argp = ctypes.addressof(self._args)
         self._scale = self.head_dim ** -0.5
+        calls = (ctypes.cast(f, ctypes.c_void_p).value for f in (lib.cllm_paged_append, lib.cllm_paged_append_heads))
+        self._packed = _CACHE.pack(*calls, h.value, DTYPES[k.dtype], self._dev, self.head_dim, self.n_kv_heads, n_heads, 0)
+        self._append = None if _marshal is None else _marshal.append
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
             self._lib.cllm_paged_destroy(self._h)
-            self._h = None
+            self._h = self._append = None
 
     def __del__(self):
         try:
@@ -325,6 +346,14 @@ class PagedCache:
         and so is q [T][n_heads][hd], into q_out (None: in place).  r: hd, or a smaller multiple of 16.
         q_norm, k_norm ([hd], of the cache's type): before that every head of q, of k is divided by the
         root of its mean square (+ eps) and multiplied by these gains."""
+        st = _stream(stream, self._dev)
+        if self._append is not None:
+            rc = self._append(self._packed, layer, k, v, slots, q, q_out, rope, positions, q_norm, k_norm, eps, interleaved, st)
+            if rc is not None:
+                if rc:
+                    _c._check(rc, "cllm_paged_append")
+                return
+        # (arguments that it does not take: looked at one by one)
         if not isinstance(k, _Tensor) or k.dim() != 3:
             raise ValueError("k: need [rows][kv_heads][head_dim]")
         t, dev, hd = k.shape[0], self._dev, self.head_dim
@@ -359,10 +388,10 @@ class PagedCache:
             op, os = (qp, qs) if q_out is None else self._heads(q_out, "q_out", shape)
         _ROWS_IN.pack_into(self._args, 0, layer, t, kp, vp, qp, op, ks, vs, qs, os, sp, rp, pp, max_pos)
         if plain and (rope is None or (dims == hd and not interleaved)):
-            rc = self._lib.cllm_paged_append(self._h, self._argp, _stream(stream, dev))
+            rc = self._lib.cllm_paged_append(self._h, self._argp, st)
         else:
             _HEADS.pack_into(self._args, _HEADS_AT, qg, kg, eps, dims, interleaved)
-            rc = self._lib.cllm_paged_append_heads(self._h, self._argp, self._argp + _HEADS_AT, _stream(stream, dev))
+            rc = self._lib.cllm_paged_append_heads(self._h, self._argp, self._argp + _HEADS_AT, st)
         if rc:
             _c._check(rc, "cllm_paged_append")
 

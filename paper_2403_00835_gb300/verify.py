@@ -26,6 +26,8 @@ EXPORTS = ("cllm_verifier_create", "cllm_verifier_destroy", "cllm_verify")
 
 # cllm_verify_args as it lies in memory (native alignment).
 _ARGS = struct.Struct("@4iPq6PqPq3P")
+# What marshal.cpp keeps of a verifier: the call, the handle and the device.
+_VERIFIER = struct.Struct("@2P2i")
 
 _lib = None
 
@@ -62,13 +64,15 @@ class DraftVerifier:
             _c._check(lib.cllm_verifier_create(max_rows, max_batch, ctypes.byref(h)), "cllm_verifier_create")
         self.device = torch.device("cuda", self._dev)
         self._h, self._lib = h, lib
+        self._packed = _VERIFIER.pack(ctypes.cast(lib.cllm_verify, ctypes.c_void_p).value, h.value, self._dev, 0)
+        self._verify = None if _paged._marshal is None else _paged._marshal.verify
         self._args = ctypes.create_string_buffer(_ARGS.size)
         self._argp = ctypes.addressof(self._args)
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
             self._lib.cllm_verifier_destroy(self._h)
-            self._h = None
+            self._h = self._verify = None
 
     def __del__(self):
         try:
@@ -96,12 +100,25 @@ class DraftVerifier:
         greedy).  draft_probs: float32 [T][vocab], row i the distribution that token i + 1 was
         drawn from (None: the drafts are certain).  accepted, next_tokens: outputs to fill (None: allocated on
         the stream of the call); target_probs: float32 [T] to fill with the target's probability of each row's draft."""
-        if not isinstance(logits, _Tensor) or logits.dim() != 2 or logits.dtype not in DTYPES:
-            raise ValueError("logits: need a [rows][vocab] tensor of float32, bfloat16 or float16")
-        t, vocab = logits.shape
         b, dev, f32, i32 = rows.batch, self._dev, torch.float32, torch.int32
         if rows._dev != dev:
             raise ValueError("rows: on another device than the verifier")
+        st = _stream(stream, dev)
+        if accepted is None or next_tokens is None:
+            with nullcontext() if stream is None else torch.cuda.stream(stream):
+                accepted = torch.empty(b, dtype=i32, device=self.device) if accepted is None else accepted
+                next_tokens = torch.empty(b, dtype=i32, device=self.device) if next_tokens is None else next_tokens
+        if self._verify is not None:
+            rc = self._verify(self._packed, b, rows._start, rows._len, logits, tokens, uniforms, race, temperature, draft_probs,
+                              accepted, next_tokens, target_probs, st)
+            if rc is not None:
+                if rc:
+                    _c._check(rc, "cllm_verify")
+                return accepted, next_tokens
+        # (arguments that it does not take: looked at one by one)
+        if not isinstance(logits, _Tensor) or logits.dim() != 2 or logits.dtype not in DTYPES:
+            raise ValueError("logits: need a [rows][vocab] tensor of float32, bfloat16 or float16")
+        t, vocab = logits.shape
         lp, ls = self._rows(logits, "logits", logits.dtype, t, vocab)
         tp = _vector(tokens, "tokens", i32, dev, t)
         up = rp = rs = hp = qp = qs = pp = 0
@@ -113,17 +130,13 @@ class DraftVerifier:
             hp = _vector(temperature, "temperature", f32, dev, b)
         if draft_probs is not None:
             qp, qs = self._rows(draft_probs, "draft_probs", f32, t, vocab)
-        if accepted is None or next_tokens is None:
-            with nullcontext() if stream is None else torch.cuda.stream(stream):
-                accepted = torch.empty(b, dtype=i32, device=self.device) if accepted is None else accepted
-                next_tokens = torch.empty(b, dtype=i32, device=self.device) if next_tokens is None else next_tokens
         ap = _vector(accepted, "accepted", i32, dev, b)
         np = _vector(next_tokens, "next_tokens", i32, dev, b)
         if target_probs is not None:
             pp = _vector(target_probs, "target_probs", f32, dev, t)
         _ARGS.pack_into(self._args, 0, b, t, vocab, DTYPES[logits.dtype], lp, ls, tp, rows._start, rows._len, hp, up, rp, rs, qp,
                         qs, ap, np, pp)
-        rc = self._lib.cllm_verify(self._h, self._argp, _stream(stream, dev))
+        rc = self._lib.cllm_verify(self._h, self._argp, st)
         if rc:
             _c._check(rc, "cllm_verify")
         return accepted, next_tokens

@@ -265,3 +265,38 @@ def test_append_heads_replays_with_other_rows():
     cache.append(0, k, k, slots, **kw)
     assert torch.equal(kp, got) and torch.equal(out, got_q)
     assert int(kp[0].transpose(1, 2).reshape(48, -1).abs().sum(1).count_nonzero()) == 4
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_arguments_are_taken_alike_in_c_and_in_python(dtype, monkeypatch):
+    """The native look at a call's tensors and the one in Python: the same calls, bit for bit."""
+    dt = DTYPES[dtype]
+    assert paged.load() is not None
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    qkv = torch.randn(6, 8 * 64, device="cuda", generator=gen).to(dt)
+    q, k, v = (x.unflatten(1, (-1, 64)) for x in qkv.split([4 * 64, 2 * 64, 2 * 64], 1))
+    gain, slots, pos = torch.randn(64, device="cuda", generator=gen).to(dt), torch.tensor([3, 9, -1, 0, 15, 7, 99], device="cuda"), _i32(list(range(7)))
+    f = paged.rope_frequencies(32)
+    rope, whole = paged.rope_table(9, f), paged.rope_table(9, paged.rope_frequencies(64))
+    calls = [dict(), dict(rope=whole, positions=pos), dict(rope=whole, positions=pos, q=q), dict(rope=rope, positions=pos, q=q, interleaved=True),
+             dict(k_norm=gain), dict(q=q, k_norm=gain), dict(q=q, q_norm=gain, k_norm=gain, eps=0.25, rope=rope, positions=pos)]
+    for kw in calls:
+        got = []
+        for native in (True, False):
+            pools = [torch.zeros(1, 2, 2, 8, 64, device="cuda", dtype=dt) for _ in range(2)]
+            cache = paged.PagedCache(*pools, 4)
+            if not native:
+                monkeypatch.setattr(cache, "_append", None)
+            out = torch.zeros(6, 4, 64, device="cuda", dtype=dt)
+            cache.append(0, k, v, slots, **kw, **({"q_out": out} if "q" in kw else {}))
+            cache.check()
+            got.append([*pools, out])
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+    if paged._marshal is not None:  # what is not taken there is refused in Python, as without it
+        cache.close()
+        with pytest.raises(cllm.CllmError):
+            cache.append(0, k, v, slots)
+        table = torch.zeros(9, 16, 2, device="cuda")
+        assert paged.rope_table(9, list(f), out=table) is table and torch.equal(table, rope)
+        monkeypatch.setattr(paged, "_marshal", None)
+        assert torch.equal(paged.rope_table(9, f, out=torch.zeros_like(table)), rope)

@@ -294,9 +294,29 @@ def test_streams_graphs_and_two_verifiers():
         assert [t.tolist() for t in out] == list(other.check())
 
 
-def test_refusals():
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_arguments_are_taken_alike_in_c_and_in_python(dtype, monkeypatch):
+    b = Batch([4, 2], 300, dtype, True, [0.5, 1.0], seed=15, pad=3)
+    want = [b.call(), b.call(draft_probs=None), b.call(temperature=None, uniforms=None, race=None, draft_probs=None)]
+    for native in (True, False):
+        v = verify.DraftVerifier(6, 2)
+        if not native:
+            monkeypatch.setattr(v, "_verify", None)
+        got = [b.call(v), b.call(v, draft_probs=None), b.call(v, temperature=None, uniforms=None, race=None, draft_probs=None)]
+        for x, y in zip(got, want):
+            assert x[:2] == y[:2] and bool((x[2] == y[2]).all())
+    v = verify.DraftVerifier(6, 2)
+    v.close()
+    with pytest.raises(cllm.CllmError):
+        b.call(v)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_refusals(native, monkeypatch):
     b = Batch([4, 2], 100, seed=14)
     v = verify.DraftVerifier(6, 2)
+    if not native:
+        monkeypatch.setattr(v, "_verify", None)
     ok = dict(logits=b.z, tokens=b.tokens, rows=b.rows, uniforms=b.u, race=b.race)
     out = torch.full((2,), 5, dtype=torch.int32, device="cuda")
     for bad in (dict(logits=b.z.double()), dict(logits=b.z[0]), dict(logits=b.z.cpu()), dict(logits=b.z.T), dict(tokens=b.tokens.long()),
