@@ -109,9 +109,8 @@ struct Heat {
   float hi, lo;
   int kind;  // 0, kNothing or kGreedy
 };
-__device__ __forceinline__ Heat heat_of(const VerifyArgs& a, int b) {
+__device__ __forceinline__ Heat heat_of(const VerifyArgs& a, float t) {
   if (a.race == nullptr) return {0.f, 0.f, kGreedy};
-  const float t = a.temperature != nullptr ? a.temperature[b] : 1.f;
   if (!(t >= 0.f) || t > 0x1p40f) return {0.f, 0.f, kNothing};
   if (t < 0x1p-60f) return {0.f, 0.f, kGreedy};
   float hi = __fdiv_rn(kLog2eHi, t), rest = fmaf(-hi, t, kLog2eHi) + kLog2eLo;
@@ -168,28 +167,33 @@ __device__ __forceinline__ Share unpack(unsigned long long x) {
   return {__uint_as_float(static_cast<uint32_t>(x >> 32)), __uint_as_float(static_cast<uint32_t>(x))};
 }
 
-// The request that row `row` belongs to, by a warp: the last one that begins at or before it (-1: none).
-__device__ __forceinline__ int request_of(const VerifyArgs& a, int row) {
+// A request's rows and temperature: loads of one trip.
+struct Request {
+  int first, end, len;
+  float heat;
+  __device__ bool live(const VerifyArgs& a) const {
+    return first >= 0 && end > first && end <= a.rows && end - first <= len;
+  }
+};
+__device__ __forceinline__ Request request(const VerifyArgs& a, int b) {
+  return {a.row_start[b], a.row_start[b + 1], a.seq_len[b], a.temperature != nullptr ? a.temperature[b] : 1.f};
+}
+// The one that row `row` belongs to, by a warp: the last that begins at or before it (end -1: none).
+__device__ __forceinline__ Request request_of(const VerifyArgs& a, int row) {
   const int lane = threadIdx.x & 31;
   int lo = 0, n = a.batch;  // among requests [lo, lo + n)
-  for (;;) {
-    const int step = (n + 31) / 32, at = lo + lane * step;
-    const unsigned before = __ballot_sync(~0u, lane * step < n && a.row_start[at] <= row);
-    if (before == 0) return -1;
-    const int k = 31 - __clz(before);
+  while (n > 32) {
+    const int step = (n + 31) / 32;
+    const unsigned before = __ballot_sync(~0u, lane * step < n && a.row_start[lo + lane * step] <= row);
+    const int k = before != 0 ? 31 - __clz(before) : 0;
     lo += k * step;
-    if (step == 1) return lo;
     n = min(step, n - k * step);
   }
-}
-struct Rows {
-  int first, end;
-  bool live;
-};
-__device__ __forceinline__ Rows rows_of(const VerifyArgs& a, int b) {
-  Rows r{a.row_start[b], a.row_start[b + 1], false};
-  r.live = r.first >= 0 && r.end > r.first && r.end <= a.rows && r.end - r.first <= a.seq_len[b];
-  return r;
+  const Request r = lane < n ? request(a, lo + lane) : Request{0, -1, 0, 0.f};
+  const unsigned before = __ballot_sync(~0u, lane < n && r.first <= row);
+  if (before == 0) return {0, -1, 0, 0.f};
+  const int k = 31 - __clz(before);
+  return {__shfl_sync(~0u, r.first, k), __shfl_sync(~0u, r.end, k), __shfl_sync(~0u, r.len, k), __shfl_sync(~0u, r.heat, k)};
 }
 
 // Values [from, to) of a row for a warp: vectors of 16 bytes from the first boundary on, U of a lane
@@ -244,14 +248,13 @@ __global__ void __launch_bounds__(kVThreads, kVerifyWarps / kVWarps) verify_rows
   const bool known = static_cast<unsigned>(draft) < static_cast<unsigned>(a.vocab);
   const float zx = known ? Logits<T>::one(z + draft) : 0.f;
   const float qx = known && a.draft_probs != nullptr ? a.draft_probs[row * a.probs_row + draft] : 1.f;
-  const int b = request_of(a, row);
-  const Heat c = b >= 0 ? heat_of(a, b) : Heat{0.f, 0.f, kNothing};
-  const Rows r = b >= 0 ? rows_of(a, b) : Rows{0, 0, false};
-  if (!r.live) {
-    if (b >= 0 && row < r.end && split == 0 && lane == 0 && a.target_probs != nullptr) a.target_probs[row] = 0.f;
+  const Request r = request_of(a, row);
+  if (row >= r.end) return;  // behind the last request
+  if (!r.live(a)) {
+    if (split == 0 && lane == 0 && a.target_probs != nullptr) a.target_probs[row] = 0.f;
     return;
   }
-  if (row >= r.end) return;  // behind the last request
+  const Heat c = heat_of(a, r.heat);
   const bool greedy = c.kind == kGreedy, drafted = known && row + 1 < r.end;
   unsigned long long mine;
   if (greedy) {
@@ -361,6 +364,14 @@ __global__ void __launch_bounds__(kVThreads, kVerifyWarps / kVWarps) verify_rows
   if (a.target_probs != nullptr) a.target_probs[row] = p;
 }
 
+// A lane's race values from v on, as far as they are there (aligned).
+template <class T>
+__device__ __forceinline__ void race_values(float4 (&e0)[Logits<T>::n / 4], const float* e, int v, int to) {
+#pragma unroll
+  for (int k = 0; k < Logits<T>::n / 4; ++k)
+    if (v + 4 * k + 4 <= to) e0[k] = *reinterpret_cast<const float4*>(e + v + 4 * k);
+}
+
 // The race over values [from, to) of a row, by a warp: the largest w / e and its index.  Where rows
 // begin on boundaries of 16 bytes, in vectors, of which a lane keeps the largest ratio and the
 // vector's place; which of the vector's values it was is found at the end.  (A branch for every
@@ -383,12 +394,12 @@ struct Race {
   __device__ float ratio(float power, float ev, float qv) const {
     return (PROBS ? fmaf(power, inv, -qv) : power) * rcp_ftz(ev);
   }
-  __device__ void load(Piece& p, int v, int end) const {
+  __device__ void load(Piece& p, int v, int end, const float4* e0 = nullptr) const {
     if (v >= end) return;
     p.x = *reinterpret_cast<const uint4*>(z + v);
 #pragma unroll
     for (int k = 0; k < n / 4; ++k) {
-      p.e[k] = *reinterpret_cast<const float4*>(e + v + 4 * k);
+      p.e[k] = e0 != nullptr ? e0[k] : *reinterpret_cast<const float4*>(e + v + 4 * k);
       if (PROBS) p.q[k] = *reinterpret_cast<const float4*>(q + v + 4 * k);
     }
   }
@@ -408,7 +419,7 @@ struct Race {
         if (j == skip - v) r[j] = 0.f;
     }
   }
-  __device__ unsigned long long run(int from, int to) const {
+  __device__ unsigned long long run(int from, int to, const float4* e0) const {  // e0: the lane's first race values, if aligned
     const int lane = threadIdx.x & 31;
     float best = 0.f;
     int at = 0, v = from;
@@ -428,7 +439,7 @@ struct Race {
       // (the next piece is on its way meanwhile)
       Piece p0, p1;
       v = from + lane * n;
-      load(p0, v, whole);
+      load(p0, v, whole, e0);
       for (; v < whole; v += 64 * n) {
         load(p1, v + 32 * n, whole);
         take(p0, v);
@@ -478,14 +489,18 @@ __global__ void __launch_bounds__(kVThreads, kDrawWarps / kVWarps) verify_draw_k
   pdl_launch_dependents();
   pdl_wait();
   if (b >= a.batch) return;
-  const Heat c = heat_of(a, b);
-  const Rows r = rows_of(a, b);
-  if (!r.live) {
+  const Request r = request(a, b);
+  const int v0 = part * a.part_len, v1 = min(v0 + a.part_len, a.vocab);
+  const float* e = a.race + b * a.race_row;
+  // (the race's first values are on their way while the deciding row is looked for)
+  float4 e0[Logits<T>::n / 4];
+  const bool ahead = a.race != nullptr && (reinterpret_cast<uintptr_t>(e + v0) & 15) == 0;
+  if (ahead) race_values<T>(e0, e, v0 + lane * Logits<T>::n, v1);
+  const Heat c = heat_of(a, r.heat);
+  if (!r.live(a)) {
     if (first) a.accepted[b] = 0, a.next[b] = -1;
     return;
   }
-  const int v0 = part * a.part_len, v1 = min(v0 + a.part_len, a.vocab);
-  const float* e = a.race + b * a.race_row;
   // the first row whose draft does not stand (the last row has none)
   int row = r.first;
   VerifyRow f;
@@ -509,8 +524,8 @@ __global__ void __launch_bounds__(kVThreads, kDrawWarps / kVWarps) verify_draw_k
   // (f.top: the draft that fell, -1: none)
   unsigned long long best =
       f.top >= 0 && a.draft_probs != nullptr
-          ? Race<T, true>(c, f, z, e, a.draft_probs + row * a.probs_row, -1).run(v0, v1)
-          : Race<T, false>(c, f, z, e, nullptr, f.top).run(v0, v1);
+          ? Race<T, true>(c, f, z, e, a.draft_probs + row * a.probs_row, -1).run(v0, v1, e0)
+          : Race<T, false>(c, f, z, e, nullptr, f.top).run(v0, v1, e0);
   if (a.parts > 1) {
     int last = 0;
     if (lane == 0) {
@@ -526,7 +541,7 @@ __global__ void __launch_bounds__(kVThreads, kDrawWarps / kVWarps) verify_draw_k
     if (!__shfl_sync(~0u, last, 0)) return;
     best = __shfl_sync(~0u, best, 0);
   }
-  if (best == 0) best = Race<T, false>(c, f, z, e, nullptr, -1).run(0, a.vocab);  // nothing is left beside q: from p itself
+  if (best == 0) best = Race<T, false>(c, f, z, e, nullptr, -1).run(0, a.vocab, nullptr);  // nothing is left beside q: from p itself
   if (lane == 0) a.accepted[b] = row - r.first + 1, a.next[b] = best != 0 ? index_of(best) : -1;
 }
 
