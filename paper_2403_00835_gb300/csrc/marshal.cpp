@@ -47,6 +47,16 @@ bool gain(PyObject* o, const Cache& c, at::ScalarType type, const void** p) {
          (vector(o, type, c.device, c.head_dim, p) && THPVariable_Unpack(o).dim() == 1 && THPVariable_Unpack(o).size(0) == c.head_dim);
 }
 
+// The library's call, without the interpreter's lock (a launch may wait for room in the stream).
+template <class F>
+PyObject* called(F call) {
+  int rc;
+  Py_BEGIN_ALLOW_THREADS;
+  rc = call();
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong(rc);
+}
+
 // append(cache, layer, k, v, slots, q, q_out, rope, positions, q_norm, k_norm, eps, interleaved, stream)
 PyObject* append_checked(PyObject* const* a) {
   if (!PyBytes_CheckExact(a[0]) || PyBytes_GET_SIZE(a[0]) != sizeof(Cache)) Py_RETURN_NONE;
@@ -98,7 +108,7 @@ PyObject* append_checked(PyObject* const* a) {
     Py_RETURN_NONE;
   }
   const bool whole = !rotated || (h.rotary_dims == c.head_dim && !h.interleaved);
-  return PyLong_FromLong(!normed && whole ? c.plain(c.handle, &r, stream) : c.with_heads(c.handle, &r, &h, stream));
+  return called([&] { return !normed && whole ? c.plain(c.handle, &r, stream) : c.with_heads(c.handle, &r, &h, stream); });
 }
 
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -146,8 +156,11 @@ PyObject* rope_checked(PyObject* const* a) {
     PyBuffer_Release(&b);
     if (!ok) Py_RETURN_NONE;
   }
-  return PyLong_FromLong(call(static_cast<float*>(out->data_ptr()), static_cast<int>(first), static_cast<int>(positions),
-                              static_cast<int>(2 * pairs), f, static_cast<float>(PyFloat_AS_DOUBLE(a[3])), stream));
+  float* to = static_cast<float*>(out->data_ptr());
+  const float amplitude = static_cast<float>(PyFloat_AS_DOUBLE(a[3]));
+  return called([&] {
+    return call(to, static_cast<int>(first), static_cast<int>(positions), static_cast<int>(2 * pairs), f, amplitude, stream);
+  });
 }
 
 PyObject* rope_table(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -216,7 +229,7 @@ PyObject* verify_checked(PyObject* const* a) {
       (given(a[12]) && !values(a[12], at::kFloat, v.device, t, &p.target_probs)))
     Py_RETURN_NONE;
   p.race = static_cast<const float*>(race), p.draft_probs = static_cast<const float*>(probs);
-  return PyLong_FromLong(v.call(v.handle, &p, stream));
+  return called([&] { return v.call(v.handle, &p, stream); });
 }
 
 PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {

@@ -93,15 +93,24 @@ def test_ragged(dtype, heads, kv, hd, page, order, window, sinks):
     _check(Step(*RAGGED, heads, kv, hd, page, dtype, order, seed=heads + sinks, layers=2), window, sinks)
 
 
+CHUNKS = [([0], [300]), ([257, 5], [128, 129]), ([700, 40], [290, 257])]
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("heads,kv,hd,page", [(4, 4, 128, 16), (6, 2, 64, 64), (7, 1, 128, 8), (80, 80, 64, 32)])
-@pytest.mark.parametrize("ctx,new", [([0], [300]), ([257, 5], [128, 129]), ([700, 40], [290, 257])])
+@pytest.mark.parametrize("heads,kv,hd,page", [(4, 4, 128, 16), (6, 2, 64, 64), (7, 1, 128, 8)])
+@pytest.mark.parametrize("ctx,new", CHUNKS)
 @pytest.mark.parametrize("window,sinks", [(30, 4), (129, 70), (64, 260), (500, 130)])
 def test_chunks(dtype, heads, kv, hd, page, ctx, new, window, sinks):
-    """Tiles of 64, 128 and (80 heads: as many tiles as SMs) 256 rows, whose rows' windows begin in other chunks."""
-    if heads == 80 and (dtype == "bf16" or len(ctx) > 1 and window != 129):
-        pytest.skip("the others show it")
+    """Tiles of 64 and 128 rows, whose rows' windows begin in other chunks."""
     _check(Step(ctx, new, heads, kv, hd, page, dtype, seed=sum(new) + sinks), window, sinks)
+
+
+@pytest.mark.parametrize("ctx,new,window,sinks", [(*CHUNKS[0], 30, 4), (*CHUNKS[0], 129, 70), (*CHUNKS[0], 64, 260), (*CHUNKS[0], 500, 130),
+                                                  (*CHUNKS[1], 129, 70), (*CHUNKS[2], 129, 70), (*CHUNKS[2], 30, 4)])
+def test_tiles_of_256_rows(ctx, new, window, sinks):
+    """(80 heads: as many tiles as SMs.)  The second half's window begins after the first's, behind first tokens
+    that both see."""
+    _check(Step(ctx, new, 80, 80, 64, 32, "f16", seed=sum(new) + sinks), window, sinks)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
