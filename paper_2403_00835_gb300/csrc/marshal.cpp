@@ -1,5 +1,5 @@
-// Arguments of PagedCache.append, rope_table and DraftVerifier.verify from torch tensors to
-// include/cllm_paged.h and cllm_verify.h, for calls whose GPU time is shorter than Python's look at nine
+// Arguments of PagedCache.append and attention, rope_table and DraftVerifier.verify from torch tensors
+// to include/cllm_paged.h and cllm_verify.h, for calls whose GPU time is shorter than Python's look at nine
 // tensors (append of 16 rows: 2.2 us on the GPU, a call 8.2 us in Python, 2.6 here; verify of 4 rows 8.2 and 4).
 //
 // The functions answer with the library's status, or with None where an argument is not what the
@@ -13,12 +13,16 @@
 
 namespace {
 
-struct Cache {  // as the caller packs it: "@3P6i"
+struct Cache {  // as the caller packs it: "@4P6i"
   int (*plain)(cllm_paged*, const cllm_paged_rows*, void*);
   int (*with_heads)(cllm_paged*, const cllm_paged_rows*, const cllm_paged_heads*, void*);
+  int (*attention)(cllm_paged*, const cllm_paged_attn*, int, void*);
   cllm_paged* handle;
   int dtype, device, head_dim, n_kv_heads, n_heads, unused;
 };
+at::ScalarType type_of(const Cache& c) {
+  return c.dtype == CLLM_F32 ? at::kFloat : c.dtype == CLLM_BF16 ? at::kBFloat16 : at::kHalf;
+}
 
 const at::Tensor* tensor(PyObject* o, at::ScalarType type, int device) {
   if (!THPVariable_Check(o)) return nullptr;
@@ -62,7 +66,7 @@ PyObject* append_checked(PyObject* const* a) {
   if (!PyBytes_CheckExact(a[0]) || PyBytes_GET_SIZE(a[0]) != sizeof(Cache)) Py_RETURN_NONE;
   Cache c;
   memcpy(&c, PyBytes_AS_STRING(a[0]), sizeof c);
-  const at::ScalarType type = c.dtype == CLLM_F32 ? at::kFloat : c.dtype == CLLM_BF16 ? at::kBFloat16 : at::kHalf;
+  const at::ScalarType type = type_of(c);
   if (!PyLong_CheckExact(a[1]) || !PyFloat_CheckExact(a[11]) || !PyBool_Check(a[12]) || !PyLong_CheckExact(a[13])) Py_RETURN_NONE;
   int far = 0;
   const long layer = PyLong_AsLongAndOverflow(a[1], &far);
@@ -172,6 +176,63 @@ PyObject* rope_table(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// attention(cache, layer, q, out, lse, row_start, seq_len, batch, table, width, scale, window, sinks, mask, stream)
+PyObject* attention_checked(PyObject* const* a) {
+  if (!PyBytes_CheckExact(a[0]) || PyBytes_GET_SIZE(a[0]) != sizeof(Cache) || !PyFloat_CheckExact(a[10])) Py_RETURN_NONE;
+  Cache c;
+  memcpy(&c, PyBytes_AS_STRING(a[0]), sizeof c);
+  long n[15] = {};
+  for (int i : {1, 7, 9, 11, 12}) {
+    int far = 0;
+    if (!PyLong_CheckExact(a[i])) Py_RETURN_NONE;
+    n[i] = PyLong_AsLongAndOverflow(a[i], &far);
+    if (far || n[i] < 0 || n[i] > 0x7fffffff) Py_RETURN_NONE;
+  }
+  for (int i : {5, 6, 8, 14})
+    if (!PyLong_CheckExact(a[i])) Py_RETURN_NONE;
+  cllm_paged_attn p{};
+  p.row_start = static_cast<const int32_t*>(PyLong_AsVoidPtr(a[5]));
+  p.seq_len = static_cast<const int32_t*>(PyLong_AsVoidPtr(a[6]));
+  p.table = static_cast<const int32_t*>(PyLong_AsVoidPtr(a[8]));
+  void* stream = PyLong_AsVoidPtr(a[14]);
+  if (PyErr_Occurred()) return nullptr;
+  const at::ScalarType type = type_of(c);
+  const at::Tensor *q = tensor(a[2], type, c.device), *out = tensor(a[3], type, c.device);
+  if (!q || !out || q->dim() != 3 || q->size(0) > 0x7fffffff || q->size(1) != c.n_heads || q->size(2) != c.head_dim ||
+      q->stride(2) != 1 || out->sizes() != q->sizes() || out->stride(2) != 1)
+    Py_RETURN_NONE;
+  const int64_t t = q->size(0);
+  p.layer = static_cast<int>(n[1]), p.batch = static_cast<int>(n[7]), p.rows = static_cast<int>(t);
+  p.q = q->data_ptr(), p.out = out->data_ptr();
+  p.q_stride = q->stride(0), p.q_head_stride = q->stride(1), p.out_stride = out->stride(0), p.out_head_stride = out->stride(1);
+  if (a[4] != Py_None) {
+    const at::Tensor* lse = tensor(a[4], at::kFloat, c.device);
+    if (!lse || lse->dim() != 2 || lse->size(0) != t || lse->size(1) != c.n_heads || !lse->is_contiguous()) Py_RETURN_NONE;
+    p.lse = static_cast<float*>(lse->data_ptr());
+  }
+  if (a[13] != Py_None) {
+    const at::Tensor* mask = tensor(a[13], at::kInt, c.device);
+    if (!mask || mask->dim() != 2 || mask->size(0) != t || mask->size(1) < 1 || mask->size(1) > 0x7fffffff || !mask->is_contiguous())
+      Py_RETURN_NONE;
+    p.mask = static_cast<const uint32_t*>(mask->data_ptr());
+    p.mask_words = static_cast<int>(mask->size(1));
+  }
+  p.table_width = static_cast<int>(n[9]);
+  p.scale = static_cast<float>(PyFloat_AS_DOUBLE(a[10]));
+  p.window = static_cast<int>(n[11]);
+  const int sinks = static_cast<int>(n[12]);
+  return called([&] { return c.attention(c.handle, &p, sinks, stream); });
+}
+
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 15) Py_RETURN_NONE;
+  try {
+    return attention_checked(a);
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
+
 struct Verifier {  // as the caller packs it: "@2P2i"
   int (*call)(cllm_verifier*, const cllm_verify_args*, void*);
   cllm_verifier* handle;
@@ -241,7 +302,8 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
-PyMethodDef methods[] = {{"verify", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(verify)), METH_FASTCALL, nullptr},
+PyMethodDef methods[] = {{"attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attention)), METH_FASTCALL, nullptr},
+                         {"verify", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(verify)), METH_FASTCALL, nullptr},
                          {"rope_table", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rope_table)), METH_FASTCALL, nullptr},
                          {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append)), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

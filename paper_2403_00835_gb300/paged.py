@@ -63,8 +63,8 @@ _HEADS = struct.Struct("@2Pf2i")
 _HEADS_AT = -(-_ROWS_IN.size // 8) * 8  # behind the rows, on a pointer's boundary
 _ATTN = struct.Struct("@3i3P4q3PifiPi")
 
-# What marshal.cpp keeps of a cache: the two calls, the handle, its type, device and heads.
-_CACHE = struct.Struct("@3P6i")
+# What marshal.cpp keeps of a cache: the three calls, the handle, its type, device and heads.
+_CACHE = struct.Struct("@4P6i")
 
 _lib = None
 _marshal = None  # marshal.cpp's module, and the address of the call it makes
@@ -310,14 +310,15 @@ class PagedCache:
         self._args = ctypes.create_string_buffer(max(_HEADS_AT + _HEADS.size, _ATTN.size))
         self._argp = ctypes.addressof(self._args)
         self._scale = self.head_dim ** -0.5
-        calls = (ctypes.cast(f, ctypes.c_void_p).value for f in (lib.cllm_paged_append, lib.cllm_paged_append_heads))
+        calls = (ctypes.cast(f, ctypes.c_void_p).value
+                 for f in (lib.cllm_paged_append, lib.cllm_paged_append_heads, lib.cllm_paged_attention_sinks))
         self._packed = _CACHE.pack(*calls, h.value, DTYPES[k.dtype], self._dev, self.head_dim, self.n_kv_heads, n_heads, 0)
-        self._append = None if _marshal is None else _marshal.append
+        self._append, self._attention = (None, None) if _marshal is None else (_marshal.append, _marshal.attention)
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
             self._lib.cllm_paged_destroy(self._h)
-            self._h = self._append = None
+            self._h = self._append = self._attention = None
 
     def __del__(self):
         try:
@@ -412,6 +413,19 @@ class PagedCache:
             # (from the memory of the stream that writes it: the current stream's may still be in use there)
             with nullcontext() if stream is None else torch.cuda.stream(stream):
                 out = torch.empty(q.shape, dtype=dtype, device=self.device)
+        if tables.page_size != self.page_size or rows.batch > tables._batch or tables._dev != dev or rows._dev != dev:
+            raise ValueError("rows and tables: another page size or device, or more requests than tables")
+        st = _stream(stream, dev)
+        if scale is None:
+            scale = self._scale
+        if self._attention is not None:
+            rc = self._attention(self._packed, layer, q, out, lse, rows._start, rows._len, rows.batch, tables._table, tables._width,
+                                 scale, window, sinks, block_mask, st)
+            if rc is not None:
+                if rc:
+                    _c._check(rc, "cllm_paged_attention")
+                return out
+        # (arguments that it does not take: looked at one by one)
         t = q.shape[0]
         shape = (t, self.n_heads, self.head_dim)
         qs, qh, q1 = q.stride() if q.shape == shape else (0, 0, 0)
@@ -419,8 +433,6 @@ class PagedCache:
         if not (q1 == 1 and o1 == 1 and q.dtype is dtype and out.dtype is dtype and q.get_device() == dev
                 and out.get_device() == dev):
             raise ValueError(f"q and out: need [rows][{self.n_heads}][{self.head_dim}] {dtype} on {self.device}")
-        if tables.page_size != self.page_size or rows.batch > tables._batch or tables._dev != dev or rows._dev != dev:
-            raise ValueError("rows and tables: another page size or device, or more requests than tables")
         lp = 0 if lse is None else _tensor(lse, "lse", torch.float32, (t, self.n_heads), dev)
         mp = words = 0
         if block_mask is not None:
@@ -429,8 +441,8 @@ class PagedCache:
                 raise ValueError("block_mask: need [rows][words], one word at least")
             mp = _tensor(block_mask, "block_mask", torch.int32, (t, words), dev)
         _ATTN.pack_into(self._args, 0, layer, rows.batch, t, q.data_ptr(), out.data_ptr(), lp, qs, qh, os, oh, rows._start,
-                        rows._len, tables._table, tables._width, self._scale if scale is None else scale, window, mp, words)
-        rc = self._lib.cllm_paged_attention_sinks(self._h, self._argp, sinks, _stream(stream, dev))
+                        rows._len, tables._table, tables._width, scale, window, mp, words)
+        rc = self._lib.cllm_paged_attention_sinks(self._h, self._argp, sinks, st)
         if rc:
             _c._check(rc, "cllm_paged_attention")
         return out

@@ -281,3 +281,37 @@ def test_a_captured_step_replays_with_other_lengths(dtype):
         o, _, ab, delta = _definition(step, 50, 9, lens=lens)
         assert bool(((got.double() - o).abs() <= step.bound(ab, delta, o)[0]).all())
     cache.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_arguments_are_taken_alike_in_c_and_in_python(dtype, monkeypatch):
+    """The native look at a call's tensors and the one in Python: the same results and refusals."""
+    step = Step([300, 20], [5, 7], 4, 2, 64, 16, dtype, seed=8)
+    wide = torch.zeros(12, 4, 96, device="cuda", dtype=step.q.dtype)
+    wide[..., :64] = step.q
+    rows, tables = paged.PageRows(step.row_start, step.seq_len), paged.PageTables(step.table, page_size=16)
+    mask = pack_mask(torch.rand(12, 7, generator=torch.Generator().manual_seed(3)) < 0.6)
+    got = []
+    for native in (True, False):
+        cache = paged.PagedCache(step.k, step.v, 4)
+        if not native:
+            monkeypatch.setattr(cache, "_attention", None)
+        results = []
+        for kw in (dict(), dict(window=30, sinks=4), dict(window=30, sinks=4, block_mask=mask), dict(scale=0.3), dict(out=wide[..., 32:])):
+            lse = torch.zeros(12, 4, device="cuda")
+            q = step.q if "out" in kw else wide[..., :64]
+            results += [cache.attention(0, q, rows, tables, lse=lse, **kw).clone(), lse]
+        cache.check()
+        got.append(results)
+        wide[..., :64] = step.q
+        for bad in (dict(lse=lse[:5]), dict(lse=lse.double()), dict(q=step.q[:, :3]), dict(q=step.q.cpu()), dict(out=step.q.double()),
+                    dict(block_mask=mask[:5]), dict(block_mask=mask.long()), dict(tables=paged.PageTables(step.table, page_size=32))):
+            with pytest.raises(ValueError):
+                cache.attention(**{**dict(layer=0, q=step.q, rows=rows, tables=tables), **bad})
+        for bad in (dict(layer=1), dict(window=-1), dict(scale=-1.0), dict(scale=math.nan), dict(out=step.q)):
+            with pytest.raises(cllm.CllmError):
+                cache.attention(**{**dict(layer=0, q=step.q, rows=rows, tables=tables), **bad})
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    cache.close()
+    with pytest.raises(cllm.CllmError):
+        cache.attention(0, step.q, rows, tables)
