@@ -164,7 +164,7 @@ typedef struct {
   const void *q_norm, *k_norm; /* [head_dim] gains in the pools' type, or NULL */
   float eps;                   /* >= 0 */
   int rotary_dims;             /* a multiple of 16, at most head_dim (unused without rope) */
-  int interleaved;             /* 0: halves */
+  int interleaved;             /* 0: halves (unused without rope) */
 } cllm_paged_heads;
 
 /* Errors: as cllm_paged_append, and EINVAL (heads NULL, gains not multiples of 16 bytes, q_norm without

@@ -99,8 +99,6 @@ PyObject* append_checked(PyObject* const* a) {
     r.positions = static_cast<const int32_t*>(p);
     r.max_pos = static_cast<int>(table->size(0));
     h.rotary_dims = static_cast<int>(2 * table->size(1));
-  } else if (h.interleaved) {
-    Py_RETURN_NONE;
   }
   if (a[5] != Py_None) {
     if ((!normed && !rotated) || !heads(a[5], c, type, t, c.n_heads, &r.q, &r.q_stride)) Py_RETURN_NONE;

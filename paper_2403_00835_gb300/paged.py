@@ -343,7 +343,7 @@ class PagedCache:
                q_norm=None, k_norm=None, eps: float = 1e-6, interleaved: bool = False):
         """Write rows k, v [T][kv_heads][hd] into slots (int64 [T] or more; -1: none).
         With rope (float32 [max_pos][r/2][2]: cos, sin) the first r values of each head of K are rotated
-        by positions (int32 [T] or more), in halves (i and i + r/2) or interleaved (2 i and 2 i + 1),
+        by positions (int32 [T] or more), in halves (i and i + r/2) or, ``interleaved``, neighbours (2 i and 2 i + 1),
         and so is q [T][n_heads][hd], into q_out (None: in place).  r: hd, or a smaller multiple of 16.
         q_norm, k_norm ([hd], of the cache's type): before that every head of q, of k is divided by the
         root of its mean square (+ eps) and multiplied by these gains."""
@@ -372,8 +372,6 @@ class PagedCache:
                 raise ValueError(f"rope: need rows of 1 to {hd // 2} pairs, got {list(rope.shape)}")
             rp = _vector(rope, "rope", torch.float32, dev, 0)
             pp = _vector(positions, "positions", torch.int32, dev, t)
-        elif interleaved:
-            raise ValueError("interleaved pairs of what: pass rope")
         if q_norm is not None:
             if q is None:
                 raise ValueError("q_norm without q")

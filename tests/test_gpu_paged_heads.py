@@ -228,7 +228,7 @@ def test_append_heads_refusals():
         return torch.zeros(4, pairs, 2, device="cuda")
 
     for bad in (dict(q_norm=gain), dict(q=q, q_norm=gain.float()), dict(q=q, q_norm=gain[:32]), dict(k_norm=gain.cpu()),
-                dict(k_norm=torch.ones(128, **bf)[::2]), dict(interleaved=True), dict(k_norm=gain, interleaved=True),
+                dict(k_norm=torch.ones(128, **bf)[::2]),
                 dict(rope=table(0), positions=pos), dict(rope=table(40), positions=pos), dict(rope=table(32)[..., 0], positions=pos),
                 dict(rope=table(8)), dict(k_norm=gain, q=q[:2])):
         with pytest.raises(ValueError):
@@ -279,7 +279,7 @@ def test_arguments_are_taken_alike_in_c_and_in_python(dtype, monkeypatch):
     f = paged.rope_frequencies(32)
     rope, whole = paged.rope_table(9, f), paged.rope_table(9, paged.rope_frequencies(64))
     calls = [dict(), dict(rope=whole, positions=pos), dict(rope=whole, positions=pos, q=q), dict(rope=rope, positions=pos, q=q, interleaved=True),
-             dict(k_norm=gain), dict(q=q, k_norm=gain), dict(q=q, q_norm=gain, k_norm=gain, eps=0.25, rope=rope, positions=pos)]
+             dict(k_norm=gain), dict(interleaved=True), dict(k_norm=gain, interleaved=True), dict(q=q, k_norm=gain), dict(q=q, q_norm=gain, k_norm=gain, eps=0.25, rope=rope, positions=pos)]
     for kw in calls:
         got = []
         for native in (True, False):
