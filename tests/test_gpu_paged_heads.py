@@ -300,3 +300,38 @@ def test_arguments_are_taken_alike_in_c_and_in_python(dtype, monkeypatch):
         assert paged.rope_table(9, list(f), out=table) is table and torch.equal(table, rope)
         monkeypatch.setattr(paged, "_marshal", None)
         assert torch.equal(paged.rope_table(9, f, out=torch.zeros_like(table)), rope)
+
+
+def test_a_table_past_31_bits():
+    """2^25 + 3 positions of 64 pairs: 2^31 pairs and more."""
+    n, f = 2 ** 25 + 3, paged.rope_frequencies(128, 1e6)
+    got = paged.rope_table(n, f)
+    for first in (0, 2 ** 24 - 2, n - 5):
+        part = got[first:first + 5].cpu().numpy().astype(np.longdouble)
+        assert float(np.abs(part - _true_table(5, f, 1.0, first)).max()) <= 2.0 ** -22
+        assert torch.equal(got[first:first + 5], paged.rope_table(5, f, first=first))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_append_heads_past_31_bits(dtype):
+    """Rows and pages whose values begin past 2^31."""
+    dt, rows = DTYPES[dtype], 2 ** 22 + 3
+    pools = [torch.zeros(1, 2 ** 13 + 2, 8, 256, 128, device="cuda", dtype=dt) for _ in range(2)]
+    cache = paged.PagedCache(*pools, 8)
+    slots = torch.full((rows,), -1, device="cuda")
+    last = (2 ** 13 + 1) * 256 + 255
+    slots[-2:] = torch.tensor([last, last - 300], device="cuda")
+    pos, rope, gain = torch.zeros(rows, dtype=torch.int32, device="cuda"), paged.rope_table(9, paged.rope_frequencies(64)), torch.ones(128, device="cuda", dtype=dt)
+    pos[-2:] = _i32([8, 3])
+    q = torch.empty(rows, 8, 128, device="cuda", dtype=dt)
+    q.normal_()
+    before, out = q[-2:].clone(), torch.empty_like(q)
+    cache.append(0, q, q, slots, q=q, q_out=out, rope=rope, positions=pos, q_norm=gain, k_norm=gain)  # (not in place: q is k)
+    cache.check()
+    small = [torch.zeros(1, 2, 8, 256, 128, device="cuda", dtype=dt) for _ in range(2)]
+    other = paged.PagedCache(*small, 8)
+    want = before.clone()
+    other.append(0, before, before, torch.tensor([3, 4], device="cuda"), q=before, q_out=want, rope=rope, positions=_i32([8, 3]), q_norm=gain, k_norm=gain)
+    assert torch.equal(out[-2:], want)
+    for row, s in ((0, last), (1, last - 300)):
+        assert torch.equal(pools[0][0, s // 256, :, s % 256], small[0][0, 0, :, 3 + row])

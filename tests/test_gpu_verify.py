@@ -338,3 +338,43 @@ def test_refusals(native, monkeypatch):
     assert out.tolist() == [5, 5]
     v.close()
     v.close()
+
+
+def test_offsets_past_31_bits():
+    """17000 rows of 131072 logits: the last request begins past 2^31 values."""
+    vocab, n = 131072, [16990, 6, 4]
+    g = torch.Generator(device="cuda").manual_seed(16)
+    z = torch.zeros(sum(n), vocab, device="cuda", dtype=torch.bfloat16)
+    first = [0, 16990, 16996]
+    for r in [0, 1, *range(16990, 17000)]:
+        z[r] = torch.randn(vocab, device="cuda", generator=g)
+    tokens = torch.randint(0, vocab, (sum(n),), device="cuda", generator=g).int()
+    for r in (16990, 16991, 16996):
+        z[r, int(tokens[r + 1])] = 60.0
+    u = torch.rand(sum(n), device="cuda", generator=g)
+    race = torch.empty(3, vocab, device="cuda").exponential_(generator=g)
+    rows = paged.PageRows(_i32([0, 16990, 16996, 17000]), _i32([20000] * 3))
+    v = verify.DraftVerifier(17000, 3)
+    for greedy in (False, True):
+        p = torch.full((17000,), 7.0, device="cuda")
+        a, x = v.verify(z, tokens, rows, target_probs=p, **({} if greedy else dict(uniforms=u, race=race)))
+        for b, r in enumerate(first):
+            m = Model(z[r:r + 6].double().cpu().numpy(), tokens[r:r + 6].tolist(), None if greedy else race[b].cpu().numpy(), u[r:r + 6].tolist())
+            assert m.allows(int(a[b]), int(x[b]))
+        assert a.tolist()[1:] == [3, 2] and not bool((p == 7.0).any())
+
+
+def test_a_vocabulary_of_2_to_the_26():
+    vocab = 2 ** 26 + 3
+    g = torch.Generator(device="cuda").manual_seed(17)
+    z = torch.randn(2, vocab, device="cuda", generator=g).half()
+    z[0, vocab - 1] = 30.0
+    race = torch.empty(1, vocab, device="cuda").exponential_(generator=g)
+    rows, v, p = paged.PageRows(_i32([0, 2]), _i32([2])), verify.DraftVerifier(2, 1), torch.zeros(2, device="cuda")
+    tokens = _i32([5, vocab - 1])
+    a, x = v.verify(z, tokens, rows, uniforms=torch.tensor([0.5, 0.5], device="cuda"), race=race, target_probs=p)
+    true = torch.softmax(z[0].double(), -1)[-1]
+    assert abs(float(p[0]) - float(true)) <= 2 * TOL * float(true)
+    ratio = z[1].double() - race[0].double().log()
+    assert a.tolist() == [2] and float(ratio[x[0]]) >= float(ratio.max()) - 1e-5
+    assert v.verify(z, tokens, rows)[0].tolist() == [2]

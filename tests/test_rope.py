@@ -96,3 +96,34 @@ def test_the_packed_arguments_are_where_the_library_reads_them():
 def test_a_null_cache_with_first_tokens(lib):
     zeros = ctypes.create_string_buffer(256)
     assert lib.cllm_paged_attention_sinks(None, ctypes.addressof(zeros), 4, None) == EINVAL
+
+
+@pytest.mark.parametrize("dev", [0, 1])
+def test_a_table_is_filled_on_its_device(dev, monkeypatch):
+    """With a stand-in for the library, which notes the device that is current."""
+    import contextlib
+    import types
+    torch = pytest.importorskip("torch")
+    current, calls = [0], []
+
+    @contextlib.contextmanager
+    def device(index):
+        before, current[0] = current[0], index
+        yield
+        current[0] = before
+
+    def call(*args):
+        calls.append((current[0], args))
+        return 0
+
+    monkeypatch.setattr(paged, "_lib", types.SimpleNamespace(cllm_rope_table=call))
+    monkeypatch.setattr(paged, "_device", lambda: current[0])
+    monkeypatch.setattr(paged, "_current", lambda index: 1000 + index)
+    monkeypatch.setattr(paged, "_tensor", lambda t, *a: 64)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    out = types.SimpleNamespace(get_device=lambda: dev)
+    assert paged.rope_table(4, [1.0, 0.5], out=out) is out
+    assert [(c, a[0], a[1:4], a[-1]) for c, a in calls] == [(dev, 64, (0, 4, 4), 1000 + dev)] and current == [0]
+    with pytest.raises(ValueError, match="stream"):
+        paged.rope_table(4, [1.0, 0.5], out=out, stream=types.SimpleNamespace(cuda_stream=5, device_index=1 - dev))
+    assert len(calls) == 1
