@@ -3,8 +3,8 @@
 //   p(x) = 2^(c (z_x - m)) / S,  S = sum_v 2^(c (z_v - m)),  c = log2(e) / temperature,  m = max z
 //   a draft stands:  u q(x) < p(x);   next = argmax_v max(p - q, 0)_v / e_v
 //
-// The first kernel reads all logits once, a row in as many shares as there are warps on the GPU: a
-// lane keeps its running maximum and sum; the warp that brings a row's last share adds them up in
+// The first kernel reads all logits once, a row in as many shares as there are warps on the GPU, or in one CTA's: a
+// lane keeps its running maximum and sum; the warp that brings a row's last share (a CTA's first warp) adds them up in
 // order and judges its draft.  The second finds each request's first row whose draft falls, and
 // runs the race over that row, its vocabulary in parts; results meet in one atomicMax on (ratio, lowest
 // index), whose order does not matter.
@@ -227,16 +227,19 @@ struct Span {
   }
 };
 
-// A warp takes a share of a row.
-template <class T>
-__global__ void __launch_bounds__(kVThreads, kVerifyWarps / kVWarps) verify_rows_kernel(const __grid_constant__ VerifyArgs a) {
-  const int lane = threadIdx.x & 31, unit = blockIdx.x * kVWarps + (threadIdx.x >> 5);
-  const int row = unit / a.splits, split = unit - row * a.splits;
+// A warp takes a share of a row.  W warps of a CTA: all of a row's shares, which meet in shared memory; W = 1:
+// any shares, which meet in memory, counted by the row's ticket.
+template <class T, int W>
+__global__ void __launch_bounds__(W == 1 ? kVThreads : 32 * W, W == 1 ? kVerifyWarps / kVWarps : kVerifyWarps / W)
+    verify_rows_kernel(const __grid_constant__ VerifyArgs a) {
+  __shared__ unsigned long long sm[W];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, unit = blockIdx.x * kVWarps + warp;
+  const int row = W > 1 ? blockIdx.x : unit / a.splits, split = W > 1 ? warp : unit - row * a.splits;
   pdl_launch_dependents();
   pdl_wait();
   if (row >= a.rows) return;
   const T* z = static_cast<const T*>(a.logits) + row * a.logits_row;
-  const int v0 = split * a.split_len, v1 = min(v0 + a.split_len, a.vocab);
+  const int v0 = min(split * a.split_len, a.vocab), v1 = min(v0 + a.split_len, a.vocab);
   constexpr int U = 4;
   const Span<T, U> span(z, v0, v1);
   // (vectors, the draft, its logit and its numbers are on their way while the row's request is looked for)
@@ -321,7 +324,12 @@ __global__ void __launch_bounds__(kVThreads, kVerifyWarps / kVWarps) verify_rows
   }
   auto join = [&](unsigned long long x) { return greedy ? warp_largest(x) : pack(warp_plus(c, unpack(x))); };
   const unsigned long long none = greedy ? 0ull : pack(Share{-INFINITY, 0.f});
-  if (a.splits > 1) {
+  if constexpr (W > 1) {
+    if (lane == 0) sm[warp] = mine;
+    __syncthreads();
+    if (warp != 0) return;
+    mine = join(lane < W ? sm[lane] : none);
+  } else if (a.splits > 1) {
     int last = 0;
     if (lane == 0) {
       a.shares[static_cast<size_t>(row) * a.splits + split] = mine;
@@ -480,17 +488,19 @@ struct Race {
   }
 };
 
-// A warp takes a part of a request's deciding row.
-template <class T>
-__global__ void __launch_bounds__(kVThreads, kDrawWarps / kVWarps) verify_draw_kernel(const __grid_constant__ VerifyArgs a) {
-  const int lane = threadIdx.x & 31, unit = blockIdx.x * kVWarps + (threadIdx.x >> 5);
-  const int b = unit / a.parts, part = unit - b * a.parts;
+// A warp takes a part of a request's deciding row; W as in the first kernel.
+template <class T, int W>
+__global__ void __launch_bounds__(W == 1 ? kVThreads : 32 * W, W == 1 ? kDrawWarps / kVWarps : W == 4 ? 6 : 1)
+    verify_draw_kernel(const __grid_constant__ VerifyArgs a) {
+  __shared__ unsigned long long sm[W];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, unit = blockIdx.x * kVWarps + warp;
+  const int b = W > 1 ? blockIdx.x : unit / a.parts, part = W > 1 ? warp : unit - b * a.parts;
   const bool first = part == 0 && lane == 0;
   pdl_launch_dependents();
   pdl_wait();
   if (b >= a.batch) return;
   const Request r = request(a, b);
-  const int v0 = part * a.part_len, v1 = min(v0 + a.part_len, a.vocab);
+  const int v0 = min(part * a.part_len, a.vocab), v1 = min(v0 + a.part_len, a.vocab);
   const float* e = a.race + b * a.race_row;
   // (the race's first values are on their way while the deciding row is looked for)
   float4 e0[Logits<T>::n / 4];
@@ -526,7 +536,12 @@ __global__ void __launch_bounds__(kVThreads, kDrawWarps / kVWarps) verify_draw_k
       f.top >= 0 && a.draft_probs != nullptr
           ? Race<T, true>(c, f, z, e, a.draft_probs + row * a.probs_row, -1).run(v0, v1, e0)
           : Race<T, false>(c, f, z, e, nullptr, f.top).run(v0, v1, e0);
-  if (a.parts > 1) {
+  if constexpr (W > 1) {
+    if (lane == 0) sm[warp] = best;
+    __syncthreads();
+    if (warp != 0) return;
+    best = warp_largest(lane < W ? sm[lane] : 0ull);
+  } else if (a.parts > 1) {
     int last = 0;
     if (lane == 0) {
       if (best != 0) atomicMax(a.best + b, best);
@@ -545,31 +560,51 @@ __global__ void __launch_bounds__(kVThreads, kDrawWarps / kVWarps) verify_draw_k
   if (lane == 0) a.accepted[b] = row - r.first + 1, a.next[b] = best != 0 ? index_of(best) : -1;
 }
 
+template <class T, int W>
+cudaError_t launch_rows(const VerifyArgs& a, cudaStream_t s) {
+  if (W > 1) return launch_after(verify_rows_kernel<T, W>, dim3(a.rows), 32 * W, 0, s, a);
+  const long long units = static_cast<long long>(a.rows) * a.splits;
+  return launch_after(verify_rows_kernel<T, W>, dim3((units + kVWarps - 1) / kVWarps), kVThreads, 0, s, a);
+}
+template <class T, int W>
+cudaError_t launch_draw(const VerifyArgs& a, cudaStream_t s) {
+  if (W > 1) return launch_after(verify_draw_kernel<T, W>, dim3(a.batch), 32 * W, 0, s, a);
+  const long long units = static_cast<long long>(a.batch) * a.parts;
+  return launch_after(verify_draw_kernel<T, W>, dim3((units + kVWarps - 1) / kVWarps), kVThreads, 0, s, a);
+}
+
 template <class T>
-cudaError_t launch(const VerifyArgs& a, cudaStream_t s) {
-  auto ctas = [](int rows, int pieces) { return dim3((static_cast<long long>(rows) * pieces + kVWarps - 1) / kVWarps); };
+cudaError_t launch(VerifyArgs a, int sms, cudaStream_t s) {
+  auto cut = [&](int pieces, int& n, int& len, bool all) {  // the vocabulary in pieces (`all`: of which some may be empty)
+    len = ((a.vocab + pieces - 1) / pieces + 7) & ~7;
+    n = all ? pieces : (a.vocab + len - 1) / len;
+  };
+  // as many pieces as warps that the GPU holds, of `least` values at least
+  auto spread = [&](int rows, int warps, int least) { return min(max(warps / rows, 1), (a.vocab + least - 1) / least); };
+  // CTAs of W warps where the vocabulary is short and all of them are on the GPU at once: their shares meet in
+  // shared memory, where others' meet through a fence and two atomics.  (With CTAs of 4, of 16 warps, and without: 4 x 4
+  // rows of 1000 4.6, -, 6.1 us; 30 x 5 of 5000 6.5, 7.6, 9.1; 8 x 8 of 12000 -, 6.8, 9.1; 60 x 5 of 32000 -, 10.2, 13.6;
+  // 10 x 8 of 64000 -, 12.7, 12.9; 4 x 6 of 131072 in fp32 -, 21.5, 11.0.)
+  auto group = [&](int rows, int warps) {
+    return a.vocab <= 8192 && 4ll * rows <= warps ? 4 : a.vocab <= 32768 && 16ll * rows <= warps ? 16 : 1;
+  };
   if (a.rows > 0) {
-    const cudaError_t e = launch_after(verify_rows_kernel<T>, ctas(a.rows, a.splits), kVThreads, 0, s, a);
+    const int w = group(a.rows, kVerifyWarps * sms);
+    cut(w > 1 ? w : spread(a.rows, kVerifyWarps * sms, 1024), a.splits, a.split_len, w > 1);
+    const cudaError_t e = w == 4 ? launch_rows<T, 4>(a, s) : w == 16 ? launch_rows<T, 16>(a, s) : launch_rows<T, 1>(a, s);
     if (e != cudaSuccess) return e;
   }
-  return launch_after(verify_draw_kernel<T>, ctas(a.batch, a.parts), kVThreads, 0, s, a);
+  const int w = group(a.batch, 16 * sms);
+  cut(w > 1 ? w : spread(a.batch, kDrawWarps * sms, 512), a.parts, a.part_len, w > 1);
+  return w == 4 ? launch_draw<T, 4>(a, s) : w == 16 ? launch_draw<T, 16>(a, s) : launch_draw<T, 1>(a, s);
 }
 
 }  // namespace
 
-cudaError_t launch_verify(VerifyArgs a, int dtype, int sms, cudaStream_t s) {
-  // shares of a row, parts of a vocabulary: as many as the warps that the GPU holds, of 1024 (512) values at least
-  auto cut = [&](int rows, int warps, int least, int& pieces, int& len) {
-    const int want = max(warps / rows, 1), most = (a.vocab + least - 1) / least;
-    pieces = want < most ? want : most;
-    len = ((a.vocab + pieces - 1) / pieces + 7) & ~7;
-    pieces = (a.vocab + len - 1) / len;
-  };
-  cut(max(a.rows, 1), kVerifyWarps * sms, 1024, a.splits, a.split_len);
-  cut(a.batch, kDrawWarps * sms, 512, a.parts, a.part_len);
-  if (dtype == CLLM_F32) return launch<float>(a, s);
-  if (dtype == CLLM_BF16) return launch<__nv_bfloat16>(a, s);
-  return launch<__half>(a, s);
+cudaError_t launch_verify(const VerifyArgs& a, int dtype, int sms, cudaStream_t s) {
+  if (dtype == CLLM_F32) return launch<float>(a, sms, s);
+  if (dtype == CLLM_BF16) return launch<__nv_bfloat16>(a, sms, s);
+  return launch<__half>(a, sms, s);
 }
 
 }  // namespace cllm

@@ -34,6 +34,6 @@ struct VerifyArgs {
 };
 
 constexpr int kVerifyWarps = 32;  // of the first kernel on an SM: shares of rows, beyond one a row
-cudaError_t launch_verify(VerifyArgs a, int dtype, int sms, cudaStream_t s);
+cudaError_t launch_verify(const VerifyArgs& a, int dtype, int sms, cudaStream_t s);
 
 }  // namespace cllm
