@@ -14,7 +14,7 @@
 //
 // Bound: HBM, the logits, then the race and the deciding rows (which are in L2 where all logits
 // are).  Measured: 768 rows of 131072 in bf16 (201 MB) 37 us, 5.4 TB/s, as long as a bare reduction of these bytes
-// takes (39); 3072 rows 125 us, 6.45 TB/s.  The race of 102 requests over them (81 MB) 16 us.
+// takes (39); 1536 rows 65 us, 6.2 TB/s.  The race of 102 requests over them (81 MB) 16 us.
 // 16 rows of 32000 in fp32: 8.6 us for both, two launches and their trips to L2.
 // Next vectors are loaded while these are summed: 36.9 us against 42 without.  More warps with fewer registers
 // 42, CTAs of 8 warps that reduce a share together 40 to 44, shares a half or a quarter as long 41
