@@ -260,6 +260,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
 
 template <int HD, int BM>
 cudaError_t launch(const PagedAttnArgs& a, int grid, cudaStream_t s) {
+  // (whole and cut: 4 tiles of 2 chunks 6.9 and 7.2 us, of 3 chunks 8.9 and 7.1)
   const PagedGeom g{BM / a.group, BM / a.group, 6, 1, 2, 1};
   return launch_after(paged_attn_kernel<HD, BM>, dim3(grid), kPThreads, sizeof(PagedSmem<HD, BM>), s, a, g);
 }

@@ -5,7 +5,9 @@
 // a turn in one integer multiplication, whatever the position (the product p f_i itself would need 24
 // bits beside those of the turns).
 //
-// Bound: the bytes written, 8 to a pair.
+// Bound: the bytes written, 8 to a pair; the arithmetic (25 instructions a pair) is close behind.  Measured: 2^20
+// positions of 64 pairs 73.9 us, 7.3 TB/s (110 with a product, a division and the library's functions for
+// every pair); 8192 of 32 2.4 us, of which a launch is 1.9.
 #include "internal.cuh"
 #include "paged.cuh"
 #include "ptx.cuh"
