@@ -22,7 +22,19 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libcllm.so")
-MARSHAL = os.path.join(OUT_DIR, "_marshal.so")
+
+
+def _marshal_name() -> str:
+    """Of the module built from csrc/marshal.cpp: it reads torch's and Python's objects as they lie in memory, so it
+    serves the versions that it was built against, which its name tells."""
+    try:
+        torch = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        torch = "none"
+    return f"_marshal-torch{torch}{sysconfig.get_config_var('EXT_SUFFIX') or '.so'}"
+
+
+MARSHAL = os.path.join(OUT_DIR, _marshal_name())
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
@@ -50,17 +62,12 @@ def _fingerprint() -> str:
                 with open(p, "rb") as fh:
                     h.update(fh.read())
     h.update(" ".join(ARCH + NVCC_FLAGS).encode())
-    try:
-        h.update(importlib.metadata.version("torch").encode())
-    except importlib.metadata.PackageNotFoundError:
-        pass
     return h.hexdigest()
 
 
 def _build_marshal() -> None:
-    """csrc/marshal.cpp against this interpreter's Python and torch; a note and no file if that fails."""
-    if os.path.exists(MARSHAL):
-        os.remove(MARSHAL)
+    """csrc/marshal.cpp against this interpreter's Python and torch; a note and no file if that fails (the
+    next build tries again)."""
     spec = importlib.util.find_spec("torch")
     if spec is None:
         return
@@ -77,18 +84,22 @@ def _build_marshal() -> None:
     except OSError as e:
         error = str(e)
     if error:
-        print(f"_marshal.so not built, calls take their arguments in Python: {error}", file=sys.stderr)
+        print(f"{os.path.basename(MARSHAL)} not built, calls take their arguments in Python: {error}", file=sys.stderr)
     else:
         os.replace(tmp, MARSHAL)
 
 
 def load_marshal():
-    """The module in _build/_marshal.so, or None."""
+    """The module built from csrc/marshal.cpp, or None: not built, or, with a note, not one that this interpreter loads."""
     if not os.path.exists(MARSHAL):
         return None
-    spec = importlib.util.spec_from_file_location("_marshal", MARSHAL)
-    module = importlib.util.module_from_spec(spec)
-    spec.loader.exec_module(module)
+    try:
+        spec = importlib.util.spec_from_file_location("_marshal", MARSHAL)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except Exception as e:  # (a damaged file, a symbol that torch lacks)
+        print(f"{os.path.basename(MARSHAL)} not loaded, calls take their arguments in Python: {e}", file=sys.stderr)
+        return None
     return module
 
 
@@ -100,9 +111,14 @@ def build(force: bool = False, verbose: bool = False, extra_flags=None) -> str:
     if not force and os.path.exists(LIB) and os.path.exists(stamp):
         with open(stamp) as fh:
             if fh.read() == fp:
+                if not os.path.exists(MARSHAL):  # (another interpreter or torch, or it failed)
+                    _build_marshal()
                 return LIB
     nvcc = _nvcc()
     flags = NVCC_FLAGS + list(extra_flags or [])
+    for f in os.listdir(OUT_DIR):
+        if f.startswith("_marshal"):  # (of the sources before, whoever they were built for)
+            os.remove(os.path.join(OUT_DIR, f))
 
     def compile_one(src):
         obj = os.path.join(OUT_DIR, os.path.basename(src)[:-3] + ".o")
