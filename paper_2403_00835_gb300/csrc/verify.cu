@@ -340,6 +340,7 @@ __global__ void __launch_bounds__(W == 1 ? kVThreads : 32 * W, W == 1 ? kVerifyW
     }
     last = __shfl_sync(~0u, last, 0);
     if (!last) return;
+    __syncwarp();  // (orders the lanes' reads behind the first lane's fence, which a shuffle does not)
     unsigned long long all = none;
     for (int k = lane; k < a.splits; k += 32) {
       const unsigned long long x = __ldcg(a.shares + static_cast<size_t>(row) * a.splits + k);
