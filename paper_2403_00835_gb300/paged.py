@@ -405,7 +405,7 @@ class PagedCache:
         block_mask: int32 [T][words], bit j of word w: the row sees new token 32 w + j of
         its request (None: causal), at least one word."""
         dev, dtype = self._dev, self.dtype
-        if sinks > _INT_MAX:  # (ctypes would cut it to 32 bits)
+        if not -_INT_MAX <= sinks <= _INT_MAX:  # (ctypes would cut it to 32 bits)
             raise ValueError("sinks: at most 2^31 - 1")
         if out is None:
             # (from the memory of the stream that writes it: the current stream's may still be in use there)

@@ -56,7 +56,7 @@ class DraftVerifier:
         self.device = torch.device(device)
         if self.device.type != "cuda":
             raise ValueError("device: need a CUDA device")
-        if max(max_rows, max_batch) > _INT_MAX:  # (ctypes would cut them to 32 bits)
+        if not all(-_INT_MAX <= x <= _INT_MAX for x in (max_rows, max_batch)):  # (ctypes would cut them to 32 bits)
             raise ValueError("max_rows, max_batch: at most 2^31 - 1")
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
