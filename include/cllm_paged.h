@@ -51,7 +51,8 @@ extern "C" {
 /* The pages of up to max_batch requests, and the free ones.  Free pages wait in
  * a ring: state[0] is the index in ring[] of the next page to hand out, state[1]
  * how many there are.  table[b][j], j < held[b], is the page of request b's
- * positions j*page_size ..; other entries are -1. */
+ * positions j*page_size ..; other entries are -1.  The entries below held are the plan's: it gives
+ * back what they say, so they stay pages also where a window no longer reads them. */
 typedef struct {
   int32_t *table; /* [max_batch][width] */
   int32_t *held;  /* [max_batch] */
@@ -230,7 +231,8 @@ int cllm_paged_attention(cllm_paged *cache, const cllm_paged_attn *a, void *cuda
  * The same with a window beside which the first `sinks` tokens of a request stay visible: of the keys
  * that the order or the mask lets a row see, it sees those with (ctx + i) - k < window or k < sinks
  * (without a window, all).  Pages that hold none of the first `sinks` tokens and lie wholly before
- * the windows of the request's new rows are not read: their table entries may be anything.
+ * the windows of the request's new rows are not read: in a table that no plan keeps their entries may be
+ * anything (cllm_page_plan gives such pages back with the others, when the request shrinks or ends, and none before).
  * Errors: as cllm_paged_attention, and EINVAL (sinks negative).
  */
 int cllm_paged_attention_sinks(cllm_paged *cache, const cllm_paged_attn *a, int sinks, void *cuda_stream);

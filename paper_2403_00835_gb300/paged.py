@@ -401,7 +401,8 @@ class PagedCache:
         over their requests' pages; returns out (None: allocated on the stream of the call;
         else no part of q).  lse: float32 [T][n_heads] to fill.
         scale: default head_dim ** -0.5.  window: keys nearer than that (0: all), and the
-        request's first ``sinks`` beside them.
+        request's first ``sinks`` beside them.  Pages between are not read; in tables that ``plan`` keeps
+        they stay the request's all the same (it gives back what the tables say).
         block_mask: int32 [T][words], bit j of word w: the row sees new token 32 w + j of
         its request (None: causal), at least one word."""
         dev, dtype = self._dev, self.dtype
