@@ -134,7 +134,9 @@ PyObject* rope_checked(PyObject* const* a) {
   const long device = PyLong_AsLongAndOverflow(a[6], &far3);
   void* stream = PyLong_AsVoidPtr(a[7]);
   if ((call == nullptr || stream == nullptr) && PyErr_Occurred()) return nullptr;
-  if (far1 || far2 || far3 || positions < 0 || first < 0 || positions > 0x7fffffff || first > 0x7fffffff - positions) Py_RETURN_NONE;
+  if (far1 || far2 || far3 || positions < 0 || first < 0 || positions > 0x7fffffff || first > 0x7fffffff - positions || device < 0 ||
+      device > 0x7fffffff)
+    Py_RETURN_NONE;
   const at::Tensor* out = tensor(a[5], at::kFloat, static_cast<int>(device));
   if (!out || out->dim() != 3 || !out->is_contiguous() || out->size(0) != positions || out->size(2) != 2) Py_RETURN_NONE;
   double f[128];
