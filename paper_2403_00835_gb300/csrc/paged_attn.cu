@@ -9,9 +9,10 @@
 // bytes serves 8 to 11 multiply-adds, which bounds it near half the FMA rate, with BM =
 // 16 (few rows) a quarter of that.
 //
-// Measured: a chunk of 1024 tokens, 32 heads of 128: 312 us, 27.5 TFLOP/s; 16 requests of one
+// Measured: a chunk of 1024 tokens, 32 heads of 128: 308 us, 27.9 TFLOP/s, after 4096 and within a window of 1024 and
+// 4 first tokens 566 us, 30.5 TFLOP/s; 16 requests of one
 // token, 32 heads on 8, at 2000 keys: 90 us, 2.9 TB/s; a block of 8 tokens, 4 heads of 64, at
-// 32 to 96 keys: 6.8 us, a launch's start and round trips to tables and pages.
+// 32 to 96 keys: 7.0 us, a launch's start and round trips to tables and pages.
 #include "paged.cuh"
 #include "paged_walk.cuh"
 #include "ptx.cuh"
@@ -103,6 +104,9 @@ __global__ void __launch_bounds__(kPThreads, 1)
       cp_async_commit();
     };
     const bool live = (tid >> 5) * 2 * R < rows;  // some row of the warp is
+    // keys [from, to) are seen by all of this thread's rows: of several, whose masks are then left out (1000 tokens at
+    // 8000 keys, 4 heads of 64: 305 us, 324 with them; of one row the test costs what it saves)
+    const int from = rk[R - 1].lo, to = rk[0].bits != nullptr ? rk[0].ctx : rk[0].hi;
     if (p.ca < p.cb) load(p.ca);
     for (int c = p.ca; c < p.cb; ++c) {
       const int kb = p.chunk(c) * kPChunk, st = (c - p.ca) & 1;
@@ -134,7 +138,8 @@ __global__ void __launch_bounds__(kPThreads, 1)
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-          const uint32_t b0 = key_bits(rk[i], kb), b1 = key_bits(rk[i], kb + 32);
+          uint32_t b0 = ~0u, b1 = ~0u;
+          if (R == 1 || from > kb || kb + kPChunk > to) b0 = key_bits(rk[i], kb), b1 = key_bits(rk[i], kb + 32);
           const bool see[4] = {(b0 >> tx & 1) != 0, (b0 >> (tx + 16) & 1) != 0, (b1 >> tx & 1) != 0,
                                (b1 >> (tx + 16) & 1) != 0};
           float cm = -INFINITY;
@@ -260,7 +265,8 @@ __global__ void __launch_bounds__(kPThreads, 1)
 
 template <int HD, int BM>
 cudaError_t launch(const PagedAttnArgs& a, int grid, cudaStream_t s) {
-  // (whole and cut: 4 tiles of 2 chunks 6.9 and 7.2 us, of 3 chunks 8.9 and 7.1)
+  // (whole and cut: 4 tiles of 2 chunks 6.9 and 7.2 us, of 3 chunks 8.9 and 7.1.  A merge's cost of 1 against 2 over 314
+  // sizes, 4 to 2048 tiles of either head_dim: 24 of them, of 3 chunks, 5 to 31 % faster, none slower.)
   const PagedGeom g{BM / a.group, BM / a.group, 6, 1, 2, 1};
   return launch_after(paged_attn_kernel<HD, BM>, dim3(grid), kPThreads, sizeof(PagedSmem<HD, BM>), s, a, g);
 }
