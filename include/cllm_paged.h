@@ -158,7 +158,8 @@ int cllm_paged_append(cllm_paged *cache, const cllm_paged_rows *r, void *cuda_st
  *   norm    x <- x / sqrt(mean(x^2) + eps) * gain, over the head_dim values, where k_norm (q_norm) is given;
  *   rotate  the first rotary_dims values, with rope rows of rotary_dims / 2 pairs [max_pos][rotary_dims / 2][2]:
  *           values i and i + rotary_dims / 2, or (interleaved) 2 i and 2 i + 1; the rest stay as they are.
- * In fp32, rounded once.  V is written as it is.  q may be given without rope too (to be
+ * In fp32, rounded once (a sum of squares past its range, of values of 10^18 and more, is infinite, and the
+ * head's finite values become zeros).  V is written as it is.  q may be given without rope too (to be
  * normalised, or passed on to q_out).
  */
 typedef struct {

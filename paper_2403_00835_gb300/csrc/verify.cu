@@ -385,6 +385,8 @@ __device__ __forceinline__ void race_values(float4 (&e0)[Logits<T>::n / 4], cons
 // begin on boundaries of 16 bytes, in vectors, of which a lane keeps the largest ratio and the
 // vector's place; which of the vector's values it was is found at the end.  (A branch for every
 // value that is larger than those before took half the time: a warp has a hundred of them.)
+// Other rows go one value at a time: 128 requests of 4 to 8 rows in bf16 28.6 us at 50257 tokens, 25.7 at 50256 (in
+// fp32 37.7 both).
 template <class T, bool PROBS>
 struct Race {
   static constexpr int n = Logits<T>::n;
@@ -583,9 +585,10 @@ cudaError_t launch(VerifyArgs a, int sms, cudaStream_t s) {
   // as many pieces as warps that the GPU holds, of `least` values at least
   auto spread = [&](int rows, int warps, int least) { return min(max(warps / rows, 1), (a.vocab + least - 1) / least); };
   // CTAs of W warps where the vocabulary is short and all of them are on the GPU at once: their shares meet in
-  // shared memory, where others' meet through a fence and two atomics.  (With CTAs of 4, of 16 warps, and without: 4 x 4
+  // shared memory, where others' meet through a fence and two atomics.  (With CTAs of 4, of 16 warps, and without, bf16: 4 x 4
   // rows of 1000 4.6, -, 6.1 us; 30 x 5 of 5000 6.5, 7.6, 9.1; 8 x 8 of 12000 -, 6.8, 9.1; 60 x 5 of 32000 -, 10.2, 13.6;
-  // 10 x 8 of 64000 -, 12.7, 12.9; 4 x 6 of 131072 in fp32 -, 21.5, 11.0.)
+  // 10 x 8 of 64000 -, 12.7, 12.9; 4 x 6 of 131072 in fp32 -, 21.5, 11.0.  Rows of fp32 are twice the bytes to the same SM,
+  // and still as fast or faster up to here: 16 rows of 32768 8.8 and 8.9 us, 8 x 8 of 32000 9.3 and 10.2, 60 x 5 12.6 and 13.6.)
   auto group = [&](int rows, int warps) {
     return a.vocab <= 8192 && 4ll * rows <= warps ? 4 : a.vocab <= 32768 && 16ll * rows <= warps ? 16 : 1;
   };
