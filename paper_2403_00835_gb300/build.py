@@ -7,6 +7,7 @@ linked statically, so the library loads on a machine without a GPU driver).
 from __future__ import annotations
 
 import concurrent.futures as cf
+import contextlib
 import hashlib
 import importlib.metadata
 import importlib.util
@@ -117,8 +118,10 @@ def build(force: bool = False, verbose: bool = False, extra_flags=None) -> str:
     nvcc = _nvcc()
     flags = NVCC_FLAGS + list(extra_flags or [])
     for f in os.listdir(OUT_DIR):
-        if f.startswith("_marshal"):  # (of the sources before, whoever they were built for)
-            os.remove(os.path.join(OUT_DIR, f))
+        # of the sources before, whoever they were built for (.tmp: another process is at it)
+        if f.startswith("_marshal") and ".tmp" not in f:
+            with contextlib.suppress(FileNotFoundError):
+                os.remove(os.path.join(OUT_DIR, f))
 
     def compile_one(src):
         obj = os.path.join(OUT_DIR, os.path.basename(src)[:-3] + ".o")

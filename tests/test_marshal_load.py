@@ -72,14 +72,14 @@ def test_a_build_makes_up_for_a_missing_one(tmp_path, monkeypatch):
 
 
 def test_one_of_the_sources_before_does_not_stay(tmp_path, monkeypatch):
-    """Another interpreter's too: it would read arguments of another layout."""
+    """Another interpreter's too: it would read arguments of another layout.  One that another process is building does."""
     monkeypatch.setattr(build, "OUT_DIR", str(tmp_path))
     monkeypatch.setattr(build, "LIB", str(tmp_path / "libcllm.so"))
     monkeypatch.setattr(build, "_build_marshal", lambda: None)
     monkeypatch.setattr(build, "_sources", lambda: [str(tmp_path / "none.cu")])
-    for f in ("libcllm.so", "_marshal.so", "_marshal-torch0.cpython-30.so"):
+    for f in ("libcllm.so", "_marshal.so", "_marshal-torch0.cpython-30.so", "_marshal.so.tmp1"):
         (tmp_path / f).write_bytes(b"")
     (tmp_path / "stamp").write_text("another")
     with pytest.raises(RuntimeError, match="none.cu"):
         build.build()
-    assert sorted(f for f in os.listdir(tmp_path) if f.startswith("_marshal")) == []
+    assert sorted(f for f in os.listdir(tmp_path) if f.startswith("_marshal")) == ["_marshal.so.tmp1"]
